@@ -42,7 +42,9 @@ enum {
   BITNET_ERR_WORKSPACE = 3,         /* workspace missing or smaller than *_workspace_bytes reports   */
   BITNET_ERR_BAD_WEIGHT = 4,        /* reserved: packers report bad weights through dev_status       */
   BITNET_ERR_CUDA = 5,              /* a CUDA call failed; see bitnet_last_cuda_error()              */
-  BITNET_ERR_TIMEOUT = 6            /* a bounded device-side wait gave up (reported via dev_status)  */
+  BITNET_ERR_TIMEOUT = 6,           /* a bounded device-side wait gave up (reported via dev_status)  */
+  BITNET_ERR_BAD_PAGE = 7,          /* reported through dev_status: a page, sequence or position out of range */
+  BITNET_ERR_NO_PAGE = 8            /* reported through dev_status: the pool has too few free pages   */
 };
 
 /* Text for a status code (static storage). */
@@ -399,6 +401,116 @@ int bitnet_unpack_tl(bitnet_fmt_t fmt, const void* packed, int64_t M, int64_t K,
 int64_t bitnet_tl_num_groups(bitnet_fmt_t fmt, int64_t K, int bk3);
 int bitnet_tl_build_lut_debug(bitnet_fmt_t fmt, const int8_t* q_row, int64_t K, int bk3, int16_t* lut,
                               void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------------
+ * Paged key-value cache and the attention over it: what lies between the Q/K/V linear and the O linear of a decoder layer.
+ *
+ * A cache is two pools K and V [layers][num_pages][kv_heads][page_size][head_dim] of 16-bit values (any order of the outer
+ * dimensions: the strides say where things are) and its books, which are plain device arrays of the caller:
+ *   table[seqs][table_width] int32   row s holds the pages of sequence s: its token at position p is row p % page_size of page
+ *                                    table[s][p / page_size]; -1 = no page;
+ *   kv_len[seqs] int32               tokens of each sequence;
+ *   refs[num_pages] int32            how many table entries hold each page; 0 = free.
+ * New tokens of several sequences are passed one after the other; q_start[seqs + 1] (int32, ascending, q_start[0] = 0,
+ * q_start[seqs] = tokens) says which are whose, and NULL that sequence i has exactly token i.  kv_len counts the new tokens: token j
+ * of the n new ones of sequence s is at position kv_len[s] - n + j.
+ *
+ * Values that only the device sees are checked there: a page outside the pool, a position outside the table or a sequence out of
+ * range is skipped (attention reads zeros) and reported in *dev_status (nullable device int) as BITNET_ERR_BAD_PAGE; nothing
+ * outside the arrays is read or written.
+ */
+enum { BITNET_KV_BF16 = 0, BITNET_KV_F16 = 1, BITNET_KV_F32 = 2 };
+
+typedef struct bitnet_kv_cache {
+  /* filled in by the caller */
+  int32_t dtype;                 /* BITNET_KV_BF16 or BITNET_KV_F16                                             */
+  int32_t kv_heads;
+  int32_t page_size;             /* tokens: a power of two, 8 to 2^20                                            */
+  int32_t head_dim;              /* 4 to 128, a multiple of 4                                                     */
+  int64_t layers, num_pages;
+  void* k;                       /* 16-byte aligned                                                              */
+  void* v;
+  int64_t stride_layer, stride_page, stride_head, stride_row;   /* elements, multiples of 8; of both pools         */
+  /* filled in by bitnet_kv_cache_init */
+  uint64_t ready;
+  uint64_t maps[2][16];          /* how the tensor copies address the pools                                      */
+} bitnet_kv_cache_t;
+
+/* Checks the description and completes it (host only; nothing is launched).  The handle stays valid while the pools stay
+ * where they are; it may be copied, and shared by streams and threads. */
+int bitnet_kv_cache_init(bitnet_kv_cache_t* cache);
+
+/*
+ * Writes the K and V rows of new tokens into their pages: pool[layer][table[s][p / page_size]][h][p % page_size] = k[t][h], rounded to
+ * nearest even.  k, v: [tokens][kv_heads][head_dim] of `in_dtype` (fp32 -- slices of the Q/K/V linear's output, say -- or the
+ * cache's own type), head_dim contiguous, strides in elements (multiples of 4), 16-byte (16-bit types: 8-byte) aligned.
+ */
+int bitnet_kv_append(const bitnet_kv_cache_t* cache, int64_t layer, const void* k, const void* v, int in_dtype, int64_t stride_token,
+                     int64_t stride_head, int64_t tokens, const int32_t* table, int64_t table_width, const int32_t* kv_len,
+                     const int32_t* q_start, int64_t seqs, int* dev_status, void* stream);
+
+/*
+ * Gives rows of the table the pages that growing from from_len[s] to to_len[s] tokens takes: entries ceil(from / page_size) up to
+ * ceil(to / page_size), which must hold none, get the lowest free pages in the order of the rows, with refs = 1.
+ * BITNET_ERR_NO_PAGE in *dev_status: the pool (or the table's width) did not suffice; entries that got no page are -1.
+ */
+int bitnet_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, const int32_t* from_len,
+                      const int32_t* to_len, int64_t page_size, int* dev_status, void* stream);
+
+/*
+ * Forks n sequences: row children[i] (which must hold no pages) becomes a copy of row parents[i].  Full pages are shared
+ * (refs + 1); a page filled in part is copied -- its rows in use, K and V, all layers -- to the lowest free page, in the order
+ * of the list.  No row may be a child and appear again in either list.  workspace: bitnet_kv_workspace_bytes(num_pages, n) bytes,
+ * 16-byte aligned, any contents; not to be shared by calls that overlap.
+ */
+size_t bitnet_kv_workspace_bytes(int64_t num_pages, int64_t n);
+int bitnet_kv_fork(const bitnet_kv_cache_t* cache, int32_t* refs, int32_t* table, int64_t seqs, int64_t table_width, int32_t* kv_len,
+                   const int32_t* parents, const int32_t* children, int64_t n, void* workspace, size_t workspace_bytes, int* dev_status,
+                   void* stream);
+
+/* Gives up the rows list[0..n): every page's count falls by one, the row becomes -1 and its length 0. */
+int bitnet_kv_free(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, int32_t* kv_len,
+                   const int32_t* list, int64_t n, int* dev_status, void* stream);
+
+/* Gives up, in every row, the pages that attention with this window and these sinks no longer reads: those wholly at positions
+ * sinks <= p < kv_len - window.  Their entries become -1. */
+int bitnet_kv_trim(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, const int32_t* kv_len,
+                   int64_t page_size, int64_t window, int64_t sinks, void* stream);
+
+/*
+ * Packs the pages in use (refs > 0) into the pool's first places: with L of them, the i-th page in use at or beyond place L moves
+ * to the i-th free place below L (K and V, all layers); table entries and refs follow.  *live_out (nullable device int) = L.
+ * workspace: bitnet_kv_workspace_bytes(num_pages, 0) bytes.
+ */
+int bitnet_kv_compact(const bitnet_kv_cache_t* cache, int32_t* refs, int32_t* table, int64_t seqs, int64_t table_width,
+                      int32_t* live_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies pages src[i] to dst[i] (K and V, all layers).  No page may be in dst and appear again in either list. */
+int bitnet_kv_copy_pages(const bitnet_kv_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n, int* dev_status,
+                         void* stream);
+
+/*
+ * Attention.  A query at position p sees the tokens c <= p with (window = 0) or c > p - window or c < sinks:
+ *   out[t][h] = sum_c softmax_c(scale * <q[t][h], K[c][g]>) V[c][g],  g = h / (q_heads / kv_heads);  a query that sees nothing: 0.
+ * q: [tokens][q_heads][head_dim], strides in elements (multiples of 4), 16-byte aligned; out: [tokens][q_heads][head_dim]
+ * contiguous, of q's type.  Cached values that no query sees (the rest of a page, released pages) may hold anything.
+ * workspace: bitnet_attn_workspace_bytes bytes, zeroed once with bitnet_workspace_init; every completed call leaves its counters
+ * zeroed.  It may serve calls with fewer tokens and any head layout that needs no more bytes, but no two calls that overlap.
+ *
+ * bitnet_attn_decode: one new token per sequence (token i belongs to sequence i), q in fp32 or in the cache's type.
+ * bitnet_attn_prompt: any number of new tokens per sequence (q_start; at most max_new of one sequence), q in the cache's type.  Their K and V
+ * rows are appended before.
+ */
+size_t bitnet_attn_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim);
+int bitnet_attn_decode(const bitnet_kv_cache_t* cache, int64_t layer, const void* q, int io_dtype, int64_t q_heads,
+                       int64_t stride_token, int64_t stride_head, const int32_t* table, int64_t table_width, const int32_t* kv_len,
+                       int64_t seqs, float scale, int64_t window, int64_t sinks, void* out, void* workspace, size_t workspace_bytes,
+                       int* dev_status, void* stream);
+int bitnet_attn_prompt(const bitnet_kv_cache_t* cache, int64_t layer, const void* q, int io_dtype, int64_t q_heads,
+                       int64_t stride_token, int64_t stride_head, int64_t tokens, const int32_t* table, int64_t table_width,
+                       const int32_t* kv_len, const int32_t* q_start, int64_t seqs, int64_t max_new, float scale, int64_t window,
+                       int64_t sinks, void* out, void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,8 @@ SYMBOLS = [
     "bitnet_tl_num_groups", "bitnet_tl_build_lut_debug", "bitnet_mpgemv_tl_noalloc", "bitnet_device_status",
     "bitnet_set_early_start", "bitnet_set_tl2_lookup", "bitnet_device_status_clear", "bitnet_debug_wait_timeout_probe", "bitnet_linear_group", "bitnet_linear_segments", "bitnet_microbench_read_stream", "bitnet_microbench_issue",
     "bitnet_elut_packed_bytes", "bitnet_pack_elut", "bitnet_unpack_elut", "bitnet_elut_linear_group",
+    "bitnet_kv_cache_init", "bitnet_kv_append", "bitnet_kv_reserve", "bitnet_kv_workspace_bytes", "bitnet_kv_fork", "bitnet_kv_free",
+    "bitnet_kv_trim", "bitnet_kv_compact", "bitnet_kv_copy_pages", "bitnet_attn_workspace_bytes", "bitnet_attn_decode", "bitnet_attn_prompt",
 ]
 
 _lib = None
@@ -84,6 +86,20 @@ def lib():
         L.bitnet_pack_elut.argtypes = [ci, ci, vp, i64, i64, vp, sz, vp, vp]
         L.bitnet_unpack_elut.argtypes = [ci, ci, vp, i64, i64, vp, vp, vp]
         L.bitnet_elut_linear_group.argtypes = [vp, i64, vp]
+        L.bitnet_kv_cache_init.argtypes = [vp]
+        L.bitnet_kv_append.argtypes = [vp, i64, vp, vp, ci, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp]
+        L.bitnet_kv_reserve.argtypes = [vp, i64, vp, i64, i64, vp, vp, i64, vp, vp]
+        L.bitnet_kv_workspace_bytes.argtypes = [i64, i64]
+        L.bitnet_kv_workspace_bytes.restype = sz
+        L.bitnet_kv_fork.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp, i64, vp, sz, vp, vp]
+        L.bitnet_kv_free.argtypes = [vp, i64, vp, i64, i64, vp, vp, i64, vp, vp]
+        L.bitnet_kv_trim.argtypes = [vp, i64, vp, i64, i64, vp, i64, i64, i64, vp]
+        L.bitnet_kv_compact.argtypes = [vp, vp, vp, i64, i64, vp, vp, sz, vp]
+        L.bitnet_kv_copy_pages.argtypes = [vp, vp, vp, i64, vp, vp]
+        L.bitnet_attn_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.bitnet_attn_workspace_bytes.restype = sz
+        L.bitnet_attn_decode.argtypes = [vp, i64, vp, ci, i64, i64, i64, vp, i64, vp, i64, fl, i64, i64, vp, vp, sz, vp, vp]
+        L.bitnet_attn_prompt.argtypes = [vp, i64, vp, ci, i64, i64, i64, i64, vp, i64, vp, vp, i64, i64, fl, i64, i64, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -472,3 +488,202 @@ def bitnet_mpgemv_tl_noalloc(fmt, packed, w_scale, M, K, q, act_scale, y, acc_ou
                                           _ptr(act_scale), T, _ptr(y), _ptr(acc_out), _stream(stream)),
            "bitnet_mpgemv_tl_noalloc")
     return y, acc_out
+
+
+# ---- paged key-value cache and the attention over it
+KV_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class KvCacheDesc(C.Structure):
+    """Mirror of bitnet_kv_cache_t."""
+    _fields_ = [("dtype", C.c_int32), ("kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32),
+                ("layers", C.c_int64), ("num_pages", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("stride_layer", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_row", C.c_int64),
+                ("ready", C.c_uint64), ("maps", C.c_uint64 * 32)]
+
+
+class KvCache:
+    """Handle of a cache whose pools are the CUDA tensors k and v [layers][pages][kv_heads][page_size][head_dim] (bf16 or
+    fp16, equal strides, head_dim contiguous; views in another order of the outer dimensions are fine).  Keeps the tensors alive."""
+
+    def __init__(self, k, v):
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise BitnetError("KvCache: k and v must be [layers][pages][kv_heads][page_size][head_dim] of one type with equal strides")
+        if not (k.is_cuda and v.is_cuda and k.device == v.device) or k.dtype not in (torch.bfloat16, torch.float16):
+            raise BitnetError("KvCache: expected CUDA tensors of bfloat16 or float16")
+        if k.stride(4) != 1 and k.shape[4] > 1:
+            raise BitnetError("KvCache: head_dim must be contiguous")
+        self.k, self.v = k, v
+        self.layers, self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        self.desc = KvCacheDesc(dtype=KV_DTYPE[k.dtype], kv_heads=self.kv_heads, page_size=self.page_size, head_dim=self.head_dim,
+                                layers=self.layers, num_pages=self.num_pages, k=k.data_ptr(), v=v.data_ptr(),
+                                stride_layer=k.stride(0), stride_page=k.stride(1), stride_head=k.stride(2), stride_row=k.stride(3))
+        _check(lib().bitnet_kv_cache_init(C.byref(self.desc)), "bitnet_kv_cache_init")
+        self.ref = C.addressof(self.desc)
+
+
+def new_kv_cache(layers, num_pages, kv_heads, page_size, head_dim, dtype=torch.bfloat16, device="cuda"):
+    """A cache with zeroed pools (rows padded to a multiple of 8 elements)."""
+    shape = (layers, num_pages, kv_heads, page_size, -(-head_dim // 8) * 8)
+    k, v = (torch.zeros(shape, dtype=dtype, device=device)[..., :head_dim] for _ in range(2))
+    return KvCache(k, v)
+
+
+def _book(t, name, dim):
+    if not (t.is_cuda and t.dtype == torch.int32 and t.dim() == dim and t.is_contiguous()):
+        raise BitnetError(f"{name}: expected a contiguous {dim}-D CUDA tensor of int32")
+    return t.data_ptr()
+
+
+def _opt(t, name):
+    return None if t is None else _book(t, name, 1)
+
+
+def _st(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _rows(t, name, heads, dim):
+    if not (t.is_cuda and t.dim() == 3 and t.dtype in KV_DTYPE and (heads is None or t.shape[1] == heads) and t.shape[2] == dim
+            and (t.stride(2) == 1 or dim == 1)):
+        raise BitnetError(f"{name}: expected a CUDA tensor [tokens][heads][head_dim] of fp32, bf16 or fp16, head_dim contiguous")
+    return t.data_ptr()
+
+
+def _lens(t, name, n):
+    if t.shape[0] < n:
+        raise BitnetError(f"{name}: expected {n} entries")
+
+
+def bitnet_kv_append(cache, layer, k, v, table, kv_len, q_start=None, dev_status=None, stream=None):
+    """Writes new tokens' rows k, v [tokens][kv_heads][head_dim] into their pages; kv_len [seqs] counts them already."""
+    kp, vp = _rows(k, "k", cache.kv_heads, cache.head_dim), _rows(v, "v", cache.kv_heads, cache.head_dim)
+    if k.dtype != v.dtype or k.stride() != v.stride() or k.shape != v.shape:
+        raise BitnetError("bitnet_kv_append: k and v must have one type, shape and strides")
+    seqs = table.shape[0] if q_start is None else q_start.shape[0] - 1
+    tp, lp, qp = _book(table, "table", 2), _book(kv_len, "kv_len", 1), _opt(q_start, "q_start")
+    _lens(table, "table", seqs)
+    _lens(kv_len, "kv_len", seqs)
+    _check(lib().bitnet_kv_append(cache.ref, layer, kp, vp, KV_DTYPE[k.dtype], k.stride(0), k.stride(1), k.shape[0], tp, table.shape[1],
+                                  lp, qp, seqs, _opt(dev_status, "dev_status"), _st(stream)), "bitnet_kv_append")
+
+
+def bitnet_kv_reserve(refs, table, from_len, to_len, page_size, dev_status=None, stream=None):
+    """Gives the rows of the table the pages that growing from from_len to to_len tokens takes, lowest free pages first."""
+    rp, tp, fp, lp = _book(refs, "refs", 1), _book(table, "table", 2), _book(from_len, "from_len", 1), _book(to_len, "to_len", 1)
+    _lens(from_len, "from_len", table.shape[0])
+    _lens(to_len, "to_len", table.shape[0])
+    _check(lib().bitnet_kv_reserve(rp, refs.shape[0], tp, table.shape[0], table.shape[1], fp, lp, page_size,
+                                   _opt(dev_status, "dev_status"), _st(stream)), "bitnet_kv_reserve")
+
+
+def bitnet_kv_workspace_bytes(num_pages, n) -> int:
+    return lib().bitnet_kv_workspace_bytes(num_pages, n)
+
+
+def new_kv_workspace(num_pages, n=0, device="cuda"):
+    """Workspace of bitnet_kv_fork (up to n children) and bitnet_kv_compact."""
+    size = bitnet_kv_workspace_bytes(num_pages, n)
+    if size == 0:
+        _check(1, "bitnet_kv_workspace_bytes")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def bitnet_kv_fork(cache, refs, table, kv_len, parents, children, workspace=None, dev_status=None, stream=None):
+    """Rows children[i] become copies of rows parents[i]: full pages shared, a page filled in part copied."""
+    if refs.shape[0] != cache.num_pages or parents.shape != children.shape:
+        raise BitnetError("bitnet_kv_fork: refs must have one entry per page, parents and children one length")
+    if workspace is None:
+        workspace = new_kv_workspace(cache.num_pages, parents.shape[0], cache.device)
+    _lens(kv_len, "kv_len", table.shape[0])
+    _check(lib().bitnet_kv_fork(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), table.shape[0], table.shape[1],
+                                _book(kv_len, "kv_len", 1), _book(parents, "parents", 1), _book(children, "children", 1), parents.shape[0],
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _opt(dev_status, "dev_status"),
+                                _st(stream)), "bitnet_kv_fork")
+
+
+def bitnet_kv_free(refs, table, kv_len, rows, dev_status=None, stream=None):
+    """Gives up the listed rows of the table: counts fall, the rows become -1, their lengths 0."""
+    _lens(kv_len, "kv_len", table.shape[0])
+    _check(lib().bitnet_kv_free(_book(refs, "refs", 1), refs.shape[0], _book(table, "table", 2), table.shape[0], table.shape[1],
+                                _book(kv_len, "kv_len", 1), _book(rows, "rows", 1), rows.shape[0], _opt(dev_status, "dev_status"),
+                                _st(stream)), "bitnet_kv_free")
+
+
+def bitnet_kv_trim(refs, table, kv_len, page_size, window, sinks=0, stream=None):
+    """Gives up the pages that attention with this window and these sinks no longer reads."""
+    _lens(kv_len, "kv_len", table.shape[0])
+    _check(lib().bitnet_kv_trim(_book(refs, "refs", 1), refs.shape[0], _book(table, "table", 2), table.shape[0], table.shape[1],
+                                _book(kv_len, "kv_len", 1), page_size, window, sinks, _st(stream)), "bitnet_kv_trim")
+
+
+def bitnet_kv_compact(cache, refs, table, live=None, workspace=None, stream=None):
+    """Moves the pages in use to the pool's first places; live (int32 [1], optional) receives their number."""
+    if refs.shape[0] != cache.num_pages:
+        raise BitnetError("bitnet_kv_compact: refs must have one entry per page")
+    if workspace is None:
+        workspace = new_kv_workspace(cache.num_pages, 0, cache.device)
+    _check(lib().bitnet_kv_compact(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), table.shape[0], table.shape[1],
+                                   _opt(live, "live"), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _st(stream)),
+           "bitnet_kv_compact")
+
+
+def bitnet_kv_copy_pages(cache, src, dst, dev_status=None, stream=None):
+    """Copies pages src[i] to dst[i], K and V, all layers."""
+    if src.shape != dst.shape:
+        raise BitnetError("bitnet_kv_copy_pages: src and dst must have one length")
+    _check(lib().bitnet_kv_copy_pages(cache.ref, _book(src, "src", 1), _book(dst, "dst", 1), src.shape[0], _opt(dev_status, "dev_status"),
+                                      _st(stream)), "bitnet_kv_copy_pages")
+
+
+def bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim) -> int:
+    return lib().bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim)
+
+
+def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
+    """A zeroed workspace for bitnet_attn_decode and bitnet_attn_prompt calls of up to `tokens` query tokens."""
+    size = bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim)
+    if size == 0:
+        _check(1, "bitnet_attn_workspace_bytes")
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    bitnet_workspace_init(ws)
+    return ws
+
+
+def _attn(name, cache, q, table, kv_len, seqs, out, workspace):
+    qp = _rows(q, "q", None, cache.head_dim)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif not (out.is_cuda and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()):
+        raise BitnetError(f"{name}: out must be contiguous, with q's shape and type")
+    _lens(table, "table", seqs)
+    _lens(kv_len, "kv_len", seqs)
+    if workspace is None and q.shape[0] > 0 and q.shape[1] % cache.kv_heads == 0:
+        workspace = new_attn_workspace(q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, q.device)
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return qp, out, ws, size
+
+
+def bitnet_attn_decode(cache, layer, q, table, kv_len, scale=None, window=0, sinks=0, out=None, workspace=None, dev_status=None,
+                       stream=None):
+    """Attention of one new token per sequence: q [seqs][q_heads][head_dim] (fp32 or the cache's type) -> out, same shape and type."""
+    qp, out, ws, size = _attn("bitnet_attn_decode", cache, q, table, kv_len, q.shape[0], out, workspace)
+    _check(lib().bitnet_attn_decode(cache.ref, layer, qp, KV_DTYPE[q.dtype], q.shape[1], q.stride(0), q.stride(1),
+                                    _book(table, "table", 2), table.shape[1], _book(kv_len, "kv_len", 1), q.shape[0],
+                                    cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
+                                    _opt(dev_status, "dev_status"), _st(stream)), "bitnet_attn_decode")
+    return out
+
+
+def bitnet_attn_prompt(cache, layer, q, table, kv_len, q_start, max_new, scale=None, window=0, sinks=0, out=None, workspace=None,
+                       dev_status=None, stream=None):
+    """Attention of prompts or chunks of prompts: q [tokens][q_heads][head_dim] in the cache's type; sequence s has the tokens
+    q_start[s] .. q_start[s + 1] - 1 (at most max_new), the last of them at position kv_len[s] - 1."""
+    seqs = q_start.shape[0] - 1
+    qp, out, ws, size = _attn("bitnet_attn_prompt", cache, q, table, kv_len, seqs, out, workspace)
+    _check(lib().bitnet_attn_prompt(cache.ref, layer, qp, KV_DTYPE[q.dtype], q.shape[1], q.stride(0), q.stride(1), q.shape[0],
+                                    _book(table, "table", 2), table.shape[1], _book(kv_len, "kv_len", 1), _book(q_start, "q_start", 1), seqs,
+                                    max_new, cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
+                                    _opt(dev_status, "dev_status"), _st(stream)), "bitnet_attn_prompt")
+    return out

@@ -103,6 +103,8 @@ const char* bitnet_status_string(int status) {
     case BITNET_ERR_BAD_WEIGHT: return "weight outside the format's alphabet or invalid packed code";
     case BITNET_ERR_CUDA: return "CUDA call failed (see bitnet_last_cuda_error)";
     case BITNET_ERR_TIMEOUT: return "bounded device-side wait gave up";
+    case BITNET_ERR_BAD_PAGE: return "page, sequence or position out of range";
+    case BITNET_ERR_NO_PAGE: return "too few free pages";
     default: return "unknown status";
   }
 }
@@ -122,7 +124,10 @@ int bitnet_device_status(int* status_out) {
   int d = 0;
   rc = gemm_i2s_stream_tc_status(&d);
   if (rc) return rc;
-  *status_out = a ? a : (b ? b : (c ? c : d));
+  int e = 0;
+  rc = attn_status(&e);
+  if (rc) return rc;
+  *status_out = a ? a : (b ? b : (c ? c : (d ? d : e)));
   return BITNET_OK;
 }
 
@@ -134,6 +139,8 @@ int bitnet_device_status_clear(void) {
   rc = gemm_prefill_status_clear();
   if (rc) return rc;
   rc = gemm_i2s_stream_tc_status_clear();
+  if (rc) return rc;
+  rc = attn_status_clear();
   if (rc) return rc;
   return gemv_tl_status_clear();
 }

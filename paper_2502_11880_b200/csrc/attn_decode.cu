@@ -1,0 +1,708 @@
+// Attention of single tokens over a paged key-value cache, split over the cache's length and joined.
+//
+//   s_c = scale * <q_h, K[c, g]>,  m = max_c s_c,  l = sum_c exp(s_c - m),  o_h = sum_c exp(s_c - m) V[c, g] / l
+//
+// over the tokens c that the query's position p sees: c <= p, and with a window either c > p - window or c < sinks.
+// Heads h of one kv head g share K and V.  Every K and V element is used for 4 * heads-per-kv-head flops, so the kernel is
+// bound by HBM; the design keeps the pool streaming:
+//   * the visible tokens of a row (a token and a kv head) are cut into tiles of 64; all rows' tiles together form one
+//     list that is dealt to the CTAs (one per SM) in equal contiguous parts, whatever the lengths are.  The list exists only on the
+//     device: every CTA derives its part from the lengths.
+//   * warp 8 brings tiles in by tensor copies (one per page, 64-column half and pool) into a ring of stages, 192 KB in flight;
+//     pages or halves of rows outside the visible range are not read.
+//   * warps 0-3 and 4-7 take the tiles in turns, 16 tokens a warp: S = Q K^T and O += P V on mma.sync m16n8k16 with the
+//     heads as the 16 rows.  At most 8 heads fill rows 0..7; rows 8..15 hold what rounding took from rows 0..7 (below).
+//   * every warp keeps its own running maximum and sum; the 8 warps' states meet in shared memory when a row ends, the parts of a
+//     row that lies on several CTAs in the workspace, joined by whichever part arrives last in the order of the parts (the
+//     result does not depend on who that is).
+// Rounding: scores, exponentials, sums and O are fp32.  The probabilities enter the second product as a 16-bit value plus a
+// 16-bit remainder (rows 8..15), 16 bits for bf16 and 22 for fp16, so that a 16-bit output is rounded once for all practical
+// purposes.  An fp32 query is split the same way; for a bf16 cache a third piece goes through a second product (24 bits).
+// fp16 probabilities are scaled by 2^12 and fp32 queries of an fp16 cache by a power of two per row, to keep the
+// remainders clear of fp16's smallest steps.
+#include <cstring>
+#include <type_traits>
+
+#include "kv_cache.cuh"
+
+namespace bitnet {
+namespace {
+
+constexpr int TILE = 64;                     // tokens per tile
+constexpr int CONSUMER_WARPS = 8;
+constexpr int THREADS = (CONSUMER_WARPS + 1) * 32;
+constexpr int HALF_BYTES = TILE * 128;       // 64 tokens x 64 columns
+constexpr int HEADS = 8;                     // query heads of one row
+
+static __device__ int g_attn_error = 0;
+
+struct DecodeArgs {
+  const void* q;
+  void* out;
+  int64_t q_stride_token, q_stride_head;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int64_t table_width;
+  int tokens, seqs;
+  int q_heads, kv_heads, group, head_blocks;  // group = query heads per kv head, in blocks of up to 8
+  int head_dim, page_shift, num_pages, layer;
+  int window, sinks, max_len;                 // max_len = table_width * page_size
+  int min_tiles;                              // fewest tiles of a CTA's part
+  float c;                                    // scale * log2(e)
+  int* counters;                              // [tokens * kv_heads * head_blocks], zero between calls
+  float2* part_ml;                            // [2 * grid][8] running maximum and sum of a part
+  float* part_o;                              // [2 * grid][8][D]
+  int* dev_status;
+};
+
+// The visible tokens of one row: [0, s_end) and [lo, len), as tiles.
+struct Range {
+  int len, s_end, lo, n0, t1, tiles, seq;
+};
+__device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
+  Range r;
+  r.seq = n;
+  int64_t len;
+  if (a.q_start) {
+    r.seq = kv_seq_of(a.q_start, a.seqs, n);
+    len = (int64_t)__ldg(a.kv_len + r.seq) - __ldg(a.q_start + r.seq + 1) + n + 1;
+  } else {
+    len = __ldg(a.kv_len + n);
+  }
+  r.len = (int)max((int64_t)0, min(len, (int64_t)a.max_len));
+  r.lo = a.window > 0 ? max(0, r.len - a.window) : 0;
+  r.s_end = min(a.sinks, r.lo);
+  if (r.lo <= a.sinks) r.lo = r.s_end = 0;
+  r.n0 = (r.s_end + TILE - 1) / TILE;
+  r.t1 = r.lo / TILE;
+  r.tiles = max(1, r.n0 + (r.len + TILE - 1) / TILE - r.t1);   // an empty row has one tile with nothing visible
+  return r;
+}
+// First token of tile t, and the visible part [lo, hi) of the range it belongs to.
+__device__ __forceinline__ void tile_of(const Range& r, int t, int& first, int& lo, int& hi) {
+  if (t < r.n0) {
+    first = t * TILE;
+    lo = 0;
+    hi = r.s_end;
+  } else {
+    first = (r.t1 + t - r.n0) * TILE;
+    lo = r.lo;
+    hi = r.len;
+  }
+}
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+};
+template <>
+struct Pair<__half> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  }
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+template <int DT>
+struct Layout {
+  static constexpr int D = DT * 16;                       // head_dim, padded
+  static constexpr int HALVES = DT > 4 ? 2 : 1;
+  static constexpr int TILE_BYTES = HALVES * HALF_BYTES;  // of K, and of V
+  // An even number: a stage then always belongs to the same group of warps, and a warp that waits for a stage's next
+  // fill has seen its previous one.  (A wait tells only the parity of a fill: with an odd number a group could take a
+  // fill two rounds old for the one it wants whenever the other group's copy in between was late.)
+  static constexpr int STAGES = HALVES == 2 ? 6 : 12;
+  static_assert(STAGES % 2 == 0, "a stage belongs to one group");
+  static constexpr int O_STRIDE = D + 8;                  // 8 heads x 4 lanes of float2 on distinct banks
+  struct Tail {
+    float o[4][HEADS][O_STRIDE];
+    float m[4][HEADS], l[4][HEADS];
+    uint64_t full_k[STAGES], full_v[STAGES], empty[STAGES];
+    int64_t scan[CONSUMER_WARPS + 2];
+    int64_t first_base;                                   // tiles before the token that the CTA's part begins in
+    int first_token;
+    int last_part;
+    int abort_flag;
+  };
+  static constexpr size_t SMEM = (size_t)STAGES * 2 * TILE_BYTES + sizeof(Tail) + 1024;
+};
+
+// KT: element type of the pools; F32: q and out are fp32; DT: head_dim in steps of 16.
+template <typename KT, bool F32, int DT>
+__global__ void __launch_bounds__(THREADS, 1)
+attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const DecodeArgs a) {
+  using L = Layout<DT>;
+  constexpr bool HALF_T = sizeof(KT) == 2 && !std::is_same<KT, __nv_bfloat16>::value;
+  constexpr bool THREE = F32 && !HALF_T;                  // third piece
+  constexpr float P_SHIFT = HALF_T ? 12.0f : 0.0f;
+  using P2 = Pair<KT>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  typename L::Tail& s = *reinterpret_cast<typename L::Tail*>(smem + L::STAGES * 2 * L::TILE_BYTES);
+  volatile int* abort_flag = &s.abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int i = 0; i < L::STAGES; ++i) {
+      kv_mbar_init(&s.full_k[i], 1);
+      kv_mbar_init(&s.full_v[i], 1);
+      kv_mbar_init(&s.empty[i], 4);
+    }
+    s.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap) : "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- the list of tiles: total, this CTA's part [item, end), and the token it begins in
+  const int rows_per_token = a.kv_heads * a.head_blocks;
+  int64_t total = 0;
+  int64_t my_excl = 0;                                     // of the last chunk of tokens looked at
+  int my_tiles = 0;
+  auto scan_chunk = [&](int n0, int64_t base) {            // tiles before token n0 + tid; returns the chunk's total
+    const int n = n0 + tid;
+    my_tiles = n < a.tokens ? range_of(a, n).tiles * rows_per_token : 0;
+    int64_t x = my_tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) s.scan[warp] = x;
+    __syncthreads();
+    int64_t before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < CONSUMER_WARPS + 1; ++w) {
+      const int64_t v = s.scan[w];
+      if (w < warp) before += v;
+      sum += v;
+    }
+    my_excl = base + before + x - my_tiles;
+    return sum;
+  };
+  for (int n0 = 0; n0 < a.tokens; n0 += THREADS) total += scan_chunk(n0, total);
+  const int64_t want = total / a.min_tiles;
+  const int64_t parts = want < 1 ? 1 : (want < (int64_t)gridDim.x ? want : (int64_t)gridDim.x);
+  if (blockIdx.x >= parts) return;
+  const int64_t begin = total * blockIdx.x / parts, end = total * (blockIdx.x + 1) / parts;
+  if (a.tokens <= THREADS) {
+    if (begin >= my_excl && begin < my_excl + my_tiles) {
+      s.first_token = tid;
+      s.first_base = my_excl;
+    }
+  } else {
+    int64_t base = 0;
+    for (int n0 = 0; n0 < a.tokens && base <= begin; n0 += THREADS) {
+      base += scan_chunk(n0, base);
+      if (begin >= my_excl && begin < my_excl + my_tiles) {
+        s.first_token = n0 + tid;
+        s.first_base = my_excl;
+      }
+    }
+  }
+  __syncthreads();
+
+  int n = s.first_token;
+  int64_t base = s.first_base;                             // tiles before token n
+  Range r = range_of(a, n);
+  int64_t item = begin;
+  uint32_t it = 0;                                         // tiles of this CTA so far
+
+  if (warp == CONSUMER_WARPS) {
+    // ------------------------------------------------------------ producer: lane = box of the tile
+    const int box_rows = min(1 << a.page_shift, TILE);
+    const int boxes = TILE / box_rows;
+    const int pool = lane / (boxes * L::HALVES);           // 0 = K, 1 = V
+    const int half = lane / boxes % L::HALVES;
+    const int box = lane % boxes;
+    const bool mine = pool < 2;
+    const uint32_t box_bytes = (uint32_t)box_rows * 128;
+    while (item < end) {
+      const int64_t off = item - base;
+      const int row = (int)(off / r.tiles);
+      const int t0 = (int)(off - (int64_t)row * r.tiles);
+      const int t_end = (int)min((int64_t)r.tiles, end - base - (int64_t)row * r.tiles);
+      const int head = row / a.head_blocks;
+      // the page of a tile's box, looked up one tile ahead
+      auto look_up = [&](int t, int& y) -> int {
+        int first, lo, hi;
+        tile_of(r, t, first, lo, hi);
+        const int tok = first + box * box_rows;
+        y = tok & ((1 << a.page_shift) - 1);
+        if (!mine || tok >= hi || tok + box_rows <= lo) return -2;   // nothing visible: not read
+        return __ldg(a.table + (int64_t)r.seq * a.table_width + (tok >> a.page_shift));
+      };
+      int y = 0, page = look_up(t0, y);
+      for (int t = t0; t < t_end; ++t, ++it) {
+        const int cur = page, cur_y = y;
+        if (t + 1 < t_end) page = look_up(t + 1, y);
+        const int st = it % L::STAGES;
+        kv_mbar_wait(&s.empty[st], ((it / L::STAGES) & 1u) ^ 1u, abort_flag, &g_attn_error);
+        if (*abort_flag) continue;
+        const bool issue = cur != -2;
+        const unsigned mask = __ballot_sync(0xffffffffu, issue);
+        const bool bad = issue && (cur < 0 || cur >= a.num_pages);
+        if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+        if (lane == 0) {
+          const int half_lanes = boxes * L::HALVES;
+          const unsigned k_mask = half_lanes >= 32 ? 0xffffffffu : (1u << half_lanes) - 1u;
+          kv_mbar_expect(&s.full_k[st], __popc(mask & k_mask) * box_bytes);
+          kv_mbar_expect(&s.full_v[st], __popc(mask & ~k_mask) * box_bytes);
+        }
+        __syncwarp();
+        if (issue) {
+          uint8_t* dst = smem + (st * 2 + pool) * L::TILE_BYTES + half * HALF_BYTES + box * box_bytes;
+          kv_box_copy(smem_u32(dst), pool ? &vmap : &kmap, half * 64, cur_y, head, bad ? -1 : cur, a.layer,
+                      pool ? &s.full_v[st] : &s.full_k[st]);
+        }
+      }
+      item += t_end - t0;
+      if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
+        base += (int64_t)r.tiles * rows_per_token;
+        r = range_of(a, ++n);
+      }
+    }
+    // a CTA that gave up leaves only when its copies have landed
+    if (*abort_flag)
+      for (uint32_t i = it > L::STAGES ? it - L::STAGES : 0; i < it; ++i)
+        for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.full_k[i % L::STAGES], (i / L::STAGES) & 1u) &&
+                                                   kv_mbar_try(&s.full_v[i % L::STAGES], (i / L::STAGES) & 1u)); ++k) {
+        }
+    return;
+  }
+
+  // -------------------------------------------------------------- consumers
+  const int grp = warp >> 2;                               // takes the tiles with it % 2 == grp
+  const int g = lane >> 2, t4 = lane & 3;                  // accumulator row (head) and column pair
+  const int tok_w = (warp & 3) * 16;                       // this warp's tokens within a tile
+  // lane's row and 16-byte piece in the ldmatrix of K (token = lane % 8 + 8 * (lane / 16), piece 2i + lane / 8 % 2) and of V
+  const int k_row = tok_w + (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;
+  const int v_row = tok_w + (lane & 15), v_piece = lane >> 4;
+  bool first_segment = true;
+
+  while (item < end) {
+    const int64_t off = item - base;
+    const int row = (int)(off / r.tiles);
+    const int t0 = (int)(off - (int64_t)row * r.tiles);
+    const int t_end = (int)min((int64_t)r.tiles, end - base - (int64_t)row * r.tiles);
+    const int head_kv = row / a.head_blocks, block = row % a.head_blocks;
+    const int heads = min(HEADS, a.group - block * HEADS);  // heads of this row
+    const int head0 = head_kv * a.group + block * HEADS;
+
+    // ---- the row's queries as operand A: rows 0..7 the values, rows 8..15 the remainders (and a third piece)
+    uint32_t qa[DT][4], qb[THREE ? DT : 1][2];
+    float c = a.c;
+    {
+      const bool have = g < heads;
+      const int64_t q_at = (int64_t)n * a.q_stride_token + (int64_t)(head0 + (have ? g : 0)) * a.q_stride_head;
+      if (F32) {
+        float2 x[DT][2];
+        const float* qp = static_cast<const float*>(a.q) + q_at;
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int d = 16 * i + 8 * j + 2 * t4;
+            x[i][j] = have && d < a.head_dim ? *reinterpret_cast<const float2*>(qp + d) : make_float2(0.0f, 0.0f);
+            top = fmaxf(top, fmaxf(fabsf(x[i][j].x), fabsf(x[i][j].y)));
+          }
+        if (HALF_T) {
+          // |q| scaled into [2^13, 2^14): fp16 then holds the value and its remainder to 2^-24
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int e = min(max((int)((__float_as_uint(top) >> 23) & 255) - 127 - 13, -100), 100);
+          const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+          c *= __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+          for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) x[i][j] = make_float2(x[i][j].x * down, x[i][j].y * down);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t h = P2::pack(x[i][j].x, x[i][j].y);
+            const float2 hf = P2::unpack(h);
+            const float rx = x[i][j].x - hf.x, ry = x[i][j].y - hf.y;
+            const uint32_t m = P2::pack(rx, ry);
+            qa[i][2 * j] = h;
+            qa[i][2 * j + 1] = m;
+            if (THREE) {
+              const float2 mf = P2::unpack(m);
+              qb[THREE ? i : 0][j] = P2::pack(rx - mf.x, ry - mf.y);
+            }
+          }
+      } else {
+        const uint8_t* qp = static_cast<const uint8_t*>(a.q) + q_at * 2;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int d = 16 * i + 8 * j + 2 * t4;
+            qa[i][2 * j] = have && d < a.head_dim ? *reinterpret_cast<const uint32_t*>(qp + d * 2) : 0u;
+            qa[i][2 * j + 1] = 0u;
+          }
+      }
+    }
+
+    float o[2 * DT][4];
+#pragma unroll
+    for (int j = 0; j < 2 * DT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+    float m = -INFINITY, l = 0.0f;                          // of head g over this warp's tokens (l: this lane's share)
+
+    for (int t = t0; t < t_end; ++t, ++it) {
+      if ((int)(it & 1u) != grp) continue;
+      const int st = it % L::STAGES;
+      const uint32_t par = (it / L::STAGES) & 1u;
+      int first, lo, hi;
+      tile_of(r, t, first, lo, hi);
+      const uint32_t kbase = smem_u32(smem + st * 2 * L::TILE_BYTES), vbase = kbase + L::TILE_BYTES;
+      kv_mbar_wait(&s.full_k[st], par, abort_flag, &g_attn_error);
+
+      float sc[2][4] = {};
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        uint32_t b[4];
+        ldsm4(kbase + (i >> 2) * HALF_BYTES + k_row * 128 + ((((2 * i & 7) + k_piece) ^ (k_row & 7)) << 4), b);
+        P2::mma(sc[0], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[0], b[1]);
+        P2::mma(sc[1], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[2], b[3]);
+        if (THREE) {
+          P2::mma(sc[0], qb[THREE ? i : 0][0], 0u, qb[THREE ? i : 0][1], 0u, b[0], b[1]);
+          P2::mma(sc[1], qb[THREE ? i : 0][0], 0u, qb[THREE ? i : 0][1], 0u, b[2], b[3]);
+        }
+      }
+      float x[4];                                           // scores of head g at tokens 2t, 2t+1, 2t+8, 2t+9 of the 16
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        x[2 * j] = (F32 ? sc[j][0] + sc[j][2] : sc[j][0]) * c;
+        x[2 * j + 1] = (F32 ? sc[j][1] + sc[j][3] : sc[j][1]) * c;
+      }
+      const bool edge = first + tok_w < lo || first + tok_w + 16 > hi;   // some of the 16 tokens are not visible
+      uint32_t vmask0 = 0xffffffffu, vmask1 = 0xffffffffu;
+      if (edge) {
+        bool in[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int tok = first + tok_w + 2 * t4 + (j & 1) + (j >> 1) * 8;
+          in[j] = tok >= lo && tok < hi;
+          if (!in[j]) x[j] = -INFINITY;
+        }
+        // V of tokens that are not visible may be anything (a page's stale end, NaN): it counts as 0
+        vmask0 = (in[0] ? 0xffffu : 0u) | (in[1] ? 0xffff0000u : 0u);
+        vmask1 = (in[2] ? 0xffffu : 0u) | (in[3] ? 0xffff0000u : 0u);
+      }
+      float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float m_new = fmaxf(m, top);
+      if (__any_sync(0xffffffffu, m_new > m)) {             // the maximum rose for some head: rescale what was summed
+        const float f = m_new == m ? 1.0f : exp2_approx(m - m_new);
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < 2 * DT; ++j) {
+          o[j][0] *= f;
+          o[j][1] *= f;
+          o[j][2] *= f;
+          o[j][3] *= f;
+        }
+        m = m_new;
+      }
+      const float ref = (m == -INFINITY ? 0.0f : m) - P_SHIFT;
+      float p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = exp2_approx(x[j] - ref);
+      l += (p[0] + p[1]) + (p[2] + p[3]);
+      uint32_t ph[2], pm[2], pl[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        ph[j] = P2::pack(p[2 * j], p[2 * j + 1]);
+        const float2 hf = P2::unpack(ph[j]);
+        const float rx = p[2 * j] - hf.x, ry = p[2 * j + 1] - hf.y;
+        pm[j] = P2::pack(rx, ry);
+        if (THREE) {
+          const float2 mf = P2::unpack(pm[j]);
+          pl[j] = P2::pack(rx - mf.x, ry - mf.y);
+        }
+      }
+      kv_mbar_wait(&s.full_v[st], par, abort_flag, &g_attn_error);
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        uint32_t b[4];
+        ldsm4_t(vbase + (i >> 2) * HALF_BYTES + v_row * 128 + ((((2 * i & 7) + v_piece) ^ (v_row & 7)) << 4), b);
+        if (edge) {
+          b[0] &= vmask0;
+          b[1] &= vmask1;
+          b[2] &= vmask0;
+          b[3] &= vmask1;
+        }
+        P2::mma(o[2 * i], ph[0], pm[0], ph[1], pm[1], b[0], b[1]);
+        P2::mma(o[2 * i + 1], ph[0], pm[0], ph[1], pm[1], b[2], b[3]);
+        if (THREE) {
+          P2::mma(o[2 * i], pl[0], 0u, pl[1], 0u, b[0], b[1]);
+          P2::mma(o[2 * i + 1], pl[0], 0u, pl[1], 0u, b[2], b[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) kv_mbar_arrive(&s.empty[st]);
+    }
+
+    // ---- the warps' states meet: those of the second group join the first group's, then four are summed
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    if (!first_segment) group_barrier(1, CONSUMER_WARPS * 32);   // the previous row's states have been read
+    const int ws = warp & 3;
+    if (grp == 1) {
+      if (t4 == 0) {
+        s.m[ws][g] = m;
+        s.l[ws][g] = l;
+      }
+#pragma unroll
+      for (int j = 0; j < 2 * DT; ++j)
+        *reinterpret_cast<float2*>(&s.o[ws][g][8 * j + 2 * t4]) = make_float2(o[j][0] + o[j][2], o[j][1] + o[j][3]);
+    }
+    group_barrier(1, CONSUMER_WARPS * 32);
+    if (grp == 0) {
+      const float m1 = s.m[ws][g], l1 = s.l[ws][g];
+      const float top = fmaxf(m, m1);
+      const float f0 = m == -INFINITY ? 0.0f : exp2_approx(m - top), f1 = m1 == -INFINITY ? 0.0f : exp2_approx(m1 - top);
+      __syncwarp();
+      if (t4 == 0) {
+        s.m[ws][g] = top;
+        s.l[ws][g] = l * f0 + l1 * f1;
+      }
+#pragma unroll
+      for (int j = 0; j < 2 * DT; ++j) {
+        float2* const at = reinterpret_cast<float2*>(&s.o[ws][g][8 * j + 2 * t4]);
+        const float2 x = *at;
+        *at = make_float2((o[j][0] + o[j][2]) * f0 + x.x * f1, (o[j][1] + o[j][3]) * f0 + x.y * f1);
+      }
+    }
+    group_barrier(1, CONSUMER_WARPS * 32);
+
+    const int hh = warp, d0 = lane * 4;                      // this thread joins 4 columns of head hh
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float big = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) big = fmaxf(big, s.m[w][hh]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = s.m[w][hh];
+      const float f = mw == -INFINITY ? 0.0f : exp2_approx(mw - big);
+      sum += f * s.l[w][hh];
+      if (d0 < L::D) {
+        const float4 v = *reinterpret_cast<const float4*>(&s.o[w][hh][d0]);
+        acc.x += f * v.x;
+        acc.y += f * v.y;
+        acc.z += f * v.z;
+        acc.w += f * v.w;
+      }
+    }
+
+    bool write = true;
+    if (t_end - t0 < r.tiles) {
+      // ---- the row lies on several CTAs: leave this part; the last to arrive joins them, in their order
+      const int64_t row_begin = base + (int64_t)row * r.tiles, row_last = row_begin + r.tiles - 1;
+      const int c0 = (int)(((row_begin + 1) * parts - 1) / total), c1 = (int)(((row_last + 1) * parts - 1) / total);
+      const int slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
+      if (d0 < L::D) *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * HEADS + hh) * L::D + d0) = acc;
+      if (lane == 0) a.part_ml[slot * HEADS + hh] = make_float2(big, sum);
+      __threadfence();
+      group_barrier(1, CONSUMER_WARPS * 32);
+      int* counter = a.counters + (int64_t)n * rows_per_token + row;
+      if (tid == 0) {
+        const int done = atomicAdd(counter, 1);
+        s.last_part = done == c1 - c0;
+        if (done == c1 - c0) *counter = 0;                  // the workspace is left as it was
+        __threadfence();
+      }
+      group_barrier(1, CONSUMER_WARPS * 32);
+      write = s.last_part != 0;
+      if (write) {
+        // parts of CTAs after c0 are those CTAs' first; c0's is its first too if it begins with this row
+        const int first_slot = 2 * c0 + (total * c0 / parts < row_begin ? 1 : 0);
+        big = -INFINITY;
+        for (int cta = c0 + lane; cta <= c1; cta += 32)
+          big = fmaxf(big, __ldcg(&a.part_ml[(cta == c0 ? first_slot : 2 * cta) * HEADS + hh]).x);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+        acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        sum = 0.0f;
+#pragma unroll 4
+        for (int cta = c0; cta <= c1; ++cta) {
+          const int sl = cta == c0 ? first_slot : 2 * cta;
+          const float2 ml = __ldcg(&a.part_ml[sl * HEADS + hh]);
+          const float f = ml.x == -INFINITY ? 0.0f : exp2_approx(ml.x - big);
+          sum += f * ml.y;
+          if (d0 < L::D) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)sl * HEADS + hh) * L::D + d0));
+            acc.x += f * v.x;
+            acc.y += f * v.y;
+            acc.z += f * v.z;
+            acc.w += f * v.w;
+          }
+        }
+      }
+    }
+    if (write && hh < heads && d0 < a.head_dim) {
+      const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);   // nothing visible: 0; NaN stays NaN
+      const int64_t at = ((int64_t)n * a.q_heads + head0 + hh) * a.head_dim + d0;
+      if (F32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      } else {
+        *reinterpret_cast<uint2*>(static_cast<KT*>(a.out) + at) =
+            make_uint2(P2::pack(acc.x * inv, acc.y * inv), P2::pack(acc.z * inv, acc.w * inv));
+      }
+    }
+    first_segment = false;
+    item += t_end - t0;
+    if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
+      base += (int64_t)r.tiles * rows_per_token;
+      r = range_of(a, ++n);
+    }
+  }
+}
+
+int padded_steps(int head_dim) {
+  const int dt = (head_dim + 15) / 16;
+  return dt <= 4 ? 4 : dt <= 6 ? 6 : dt;
+}
+
+template <typename KT, bool F32, int DT>
+int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
+  auto kernel = attn_decode_kernel<KT, F32, DT>;
+  constexpr size_t smem = Layout<DT>::SMEM;
+  static_assert(smem <= 232448, "shared memory of one CTA");
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return note_cuda_error(e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early_start_enabled(st) ? 1 : 0;
+  e = cudaLaunchKernelEx(&cfg, kernel, km, vm, d);
+  return e == cudaSuccess ? check_launch() : note_cuda_error(e);
+}
+template <typename KT, bool F32>
+int launch_dt(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
+  switch (padded_steps(d.head_dim)) {
+    case 4: return launch_one<KT, F32, 4>(km, vm, d, grid, st);
+    case 6: return launch_one<KT, F32, 6>(km, vm, d, grid, st);
+    case 7: return launch_one<KT, F32, 7>(km, vm, d, grid, st);
+    default: return launch_one<KT, F32, 8>(km, vm, d, grid, st);
+  }
+}
+
+size_t counters_bytes(int64_t tokens, int q_heads, int kv_heads) {
+  const int64_t blocks = ceil_div(q_heads / kv_heads, HEADS);
+  return (size_t)ceil_div(tokens * kv_heads * blocks * 4, 16) * 16;
+}
+
+}  // namespace
+
+size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, int head_dim) {
+  const size_t slots = 2 * (size_t)dev_info().sm_count * HEADS;
+  return counters_bytes(tokens, q_heads, kv_heads) + slots * (8 + (size_t)padded_steps(head_dim) * 64);
+}
+
+int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
+  CUtensorMap km, vm;
+  memcpy(&km, c->maps[0], sizeof km);
+  memcpy(&vm, c->maps[1], sizeof vm);
+  DecodeArgs d;
+  d.q = x.q;
+  d.out = x.out;
+  d.q_stride_token = x.q_stride_token;
+  d.q_stride_head = x.q_stride_head;
+  d.table = x.table;
+  d.kv_len = x.kv_len;
+  d.q_start = x.q_start;
+  d.table_width = x.table_width;
+  d.tokens = (int)x.tokens;
+  d.seqs = (int)x.seqs;
+  d.q_heads = x.q_heads;
+  d.kv_heads = c->kv_heads;
+  d.group = x.q_heads / c->kv_heads;
+  d.head_blocks = (int)ceil_div(d.group, HEADS);
+  d.head_dim = c->head_dim;
+  d.page_shift = __builtin_ctz((unsigned)c->page_size);
+  d.num_pages = (int)c->num_pages;
+  d.layer = x.layer;
+  d.window = x.window;
+  d.sinks = x.sinks;
+  const int64_t most = x.table_width * c->page_size;
+  d.max_len = most > 0x7fffff00 ? 0x7fffff00 : (int)most;
+  d.min_tiles = 1;
+  d.c = x.scale * 1.4426950408889634f;
+  const int grid = dev_info().sm_count;
+  const size_t slots = 2 * (size_t)grid * HEADS;
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  d.counters = reinterpret_cast<int*>(w);
+  w += counters_bytes(x.tokens, x.q_heads, c->kv_heads);
+  d.part_ml = reinterpret_cast<float2*>(w);
+  d.part_o = reinterpret_cast<float*>(w + slots * 8);
+  d.dev_status = x.dev_status;
+  log_launch("attn_decode_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.q_heads, d.kv_heads, d.head_dim,
+             d.window, grid);
+  if (x.dtype == BITNET_KV_BF16)
+    return x.io_f32 ? launch_dt<__nv_bfloat16, true>(km, vm, d, grid, st) : launch_dt<__nv_bfloat16, false>(km, vm, d, grid, st);
+  return x.io_f32 ? launch_dt<__half, true>(km, vm, d, grid, st) : launch_dt<__half, false>(km, vm, d, grid, st);
+}
+
+int attn_status(int* out) {
+  cudaError_t e = cudaMemcpyFromSymbol(out, g_attn_error, sizeof(int));
+  return e == cudaSuccess ? BITNET_OK : note_cuda_error(e);
+}
+int attn_status_clear() {
+  const int zero = 0;
+  cudaError_t e = cudaMemcpyToSymbol(g_attn_error, &zero, sizeof(int));
+  return e == cudaSuccess ? BITNET_OK : note_cuda_error(e);
+}
+
+}  // namespace bitnet

@@ -218,6 +218,8 @@ int gemv_tl_status(int* out);
 int gemm_prefill_status_clear();
 int gemv_tl_status_clear();
 int gemv_i2s_stream_status_clear();
+int attn_status(int* out);
+int attn_status_clear();
 int launch_wait_timeout_probe(cudaStream_t st);
 
 }  // namespace bitnet

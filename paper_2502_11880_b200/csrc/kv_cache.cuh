@@ -1,0 +1,138 @@
+// What the kernels over the paged key-value cache share (internal): the pool's geometry, bounded barrier waits, tensor
+// copies of page boxes, exp2.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "device_utils.cuh"
+
+namespace bitnet {
+
+// Element strides of the K and V pools [layers][pages][kv_heads][page_size][head_dim]; rows of head_dim are contiguous.
+struct KvView {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t stride_layer, stride_page, stride_head, stride_row;
+  int layers, num_pages, kv_heads, page_size, head_dim;
+};
+
+// Rows of one box of a tensor copy: a page, or 64 rows of a larger one.
+inline int kv_box_rows(int page_size) { return page_size < 64 ? page_size : 64; }
+// Tensor maps of both pools (64 columns x kv_box_rows rows per box, 128-byte swizzle), into two CUtensorMap.
+int encode_kv_maps(void* kmap, void* vmap, const KvView& v, int dtype);
+
+inline KvView kv_view(const bitnet_kv_cache_t* c) {
+  KvView v;
+  v.k = static_cast<uint8_t*>(c->k);
+  v.v = static_cast<uint8_t*>(c->v);
+  v.stride_layer = c->stride_layer;
+  v.stride_page = c->stride_page;
+  v.stride_head = c->stride_head;
+  v.stride_row = c->stride_row;
+  v.layers = (int)c->layers;
+  v.num_pages = (int)c->num_pages;
+  v.kv_heads = c->kv_heads;
+  v.page_size = c->page_size;
+  v.head_dim = c->head_dim;
+  return v;
+}
+
+// ---- launchers (one per .cu file)
+struct AttnArgs {
+  const void* q;            // [tokens][q_heads][head_dim]
+  void* out;                // [tokens][q_heads][head_dim], contiguous
+  int64_t q_stride_token, q_stride_head;   // elements
+  const int32_t* table;     // [seqs][table_width] page ids
+  const int32_t* kv_len;    // [seqs]
+  const int32_t* q_start;   // [seqs + 1] first token of each sequence; null: token i belongs to sequence i
+  int64_t tokens, seqs, table_width;
+  int64_t max_new;          // most tokens of one sequence (q_start)
+  int q_heads, layer, window, sinks;
+  float scale;
+  int io_f32;               // q and out are fp32; otherwise they have the cache's type
+  int dtype;
+  int* dev_status;
+};
+size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, int head_dim);
+int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
+
+int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
+                     int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
+                     int dtype, int* dev_status, cudaStream_t st);
+int launch_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* from_len,
+                      const int32_t* to_len, int page_size, int* dev_status, cudaStream_t st);
+int launch_kv_fork(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* parents,
+                   const int32_t* children, int64_t n, void* ws, int* dev_status, cudaStream_t st);
+int launch_kv_release(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* list,
+                      int64_t n, int page_size, int window, int sinks, bool trim, int* dev_status, cudaStream_t st);
+int launch_kv_compact(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs, int64_t width, int32_t* live_out, void* ws,
+                      cudaStream_t st);
+int launch_kv_copy_pages(const KvView& kv, const int32_t* src, const int32_t* dst, int64_t n, int* dev_status, cudaStream_t st);
+size_t kv_workspace_bytes(int64_t num_pages, int64_t n);
+
+#ifdef __CUDACC__
+// ---- device side
+constexpr uint32_t KV_WAIT_LIMIT = 1u << 22;
+
+__device__ __forceinline__ void kv_mbar_init(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void kv_mbar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void kv_mbar_expect(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool kv_mbar_try(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Bounded wait.  One that gives up raises the CTA's abort flag and the device status; the caller goes on (every loop
+// of these kernels is counted, so all roles reach their ends), and later waits give up at once.
+__device__ __forceinline__ void kv_mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* error) {
+  if (kv_mbar_try(bar, parity)) return;
+  for (uint32_t it = 0; it < KV_WAIT_LIMIT; ++it) {
+    if (kv_mbar_try(bar, parity)) return;
+    if ((it & 255u) == 0u && *abort_flag) return;
+  }
+  *abort_flag = 1;
+  atomicExch(error, BITNET_ERR_TIMEOUT);
+}
+
+// One box of the pool: columns [x, x + 64), rows from `row` of (head, page, layer).  Anything outside the pool reads as 0.
+__device__ __forceinline__ void kv_box_copy(uint32_t dst, const CUtensorMap* map, int x, int row, int head, int page, int layer,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(row), "r"(head), "r"(page), "r"(layer), "r"(smem_u32(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Sequence of token n: the number of i in 1..seqs with q_start[i] <= n (sequences without tokens are passed over).
+__device__ __forceinline__ int kv_seq_of(const int32_t* q_start, int seqs, int n) {
+  int lo = 0, hi = seqs;            // q_start[lo] <= n < q_start[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(q_start + mid) <= n) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+#endif
+
+}  // namespace bitnet
