@@ -127,7 +127,10 @@ int bitnet_device_status(int* status_out) {
   int e = 0;
   rc = attn_status(&e);
   if (rc) return rc;
-  *status_out = a ? a : (b ? b : (c ? c : (d ? d : e)));
+  int f = 0;
+  rc = attn_prompt_status(&f);
+  if (rc) return rc;
+  *status_out = a ? a : (b ? b : (c ? c : (d ? d : (e ? e : f))));
   return BITNET_OK;
 }
 
@@ -141,6 +144,8 @@ int bitnet_device_status_clear(void) {
   rc = gemm_i2s_stream_tc_status_clear();
   if (rc) return rc;
   rc = attn_status_clear();
+  if (rc) return rc;
+  rc = attn_prompt_status_clear();
   if (rc) return rc;
   return gemv_tl_status_clear();
 }

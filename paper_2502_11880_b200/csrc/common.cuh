@@ -220,6 +220,8 @@ int gemv_tl_status_clear();
 int gemv_i2s_stream_status_clear();
 int attn_status(int* out);
 int attn_status_clear();
+int attn_prompt_status(int* out);
+int attn_prompt_status_clear();
 int launch_wait_timeout_probe(cudaStream_t st);
 
 }  // namespace bitnet

@@ -201,7 +201,7 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
   if (tokens == 0) return BITNET_OK;
   if (max_new < 1) return BITNET_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < attn_decode_workspace_bytes(tokens, a.q_heads, c->kv_heads, c->head_dim)) return BITNET_ERR_WORKSPACE;
-  return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
+  return launch_attn_prompt(c, a, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -57,6 +57,7 @@ struct AttnArgs {
 };
 size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, int head_dim);
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
+int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
                      int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
