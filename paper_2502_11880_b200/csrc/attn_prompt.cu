@@ -63,18 +63,26 @@ __device__ __forceinline__ uint64_t desc_n_major(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(HALF >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// One lane of the warp, in a form that tells the compiler so: the operands of the instructions below are warp-uniform registers,
+// and behind a test of the lane's number each of them would be brought there by a loop over the lanes (measured: 130
+// instead of 64 cycles per product issued).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "l"(a), "l"(b), "r"(idesc), "r"(add)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "r"(a), "l"(b), "r"(idesc), "r"(add)
       : "memory");
 }
 __device__ __forceinline__ void commit(uint64_t* bar) {
@@ -284,26 +292,27 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
     } else if (warp == 9) {
       // ---------------------------------------------------------- MMA issuer
-      if (lane == 0 && nb > 0) {
+      if (nb > 0 && elect_one()) {
         constexpr uint32_t FMT = std::is_same<KT, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t base = (1u << 4) | (FMT << 7) | (FMT << 10) | ((uint32_t)(ROWS >> 4) << 24);
         const uint32_t id_s = base | ((uint32_t)(KB >> 3) << 17);
         const uint32_t id_o = base | (1u << 16) | ((uint32_t)(steps * 2) << 17);     // N = 16 * steps, B N-major
         const uint32_t q_addr = smem_u32(smem + L::Q_OFF);
         uint32_t cleaned = 0;                                  // parity of each stage's next cleaning
-        auto qk = [&](int u, int j) {
-          const uint64_t da = desc_k_major(q_addr + u * L::TILE_BYTES);
-          const uint64_t db = desc_k_major(smem_u32(smem + L::K_OFF + (j % STAGES) * L::TILE_BYTES));
-          for (int i = 0; i < steps; ++i) {
-            const uint64_t off = (uint64_t)(((i >> 2) * HALF + (i & 3) * 32) >> 4);
-            mma_ss(tmem + u * KB, da + off, db + off, id_s, i > 0);
-          }
+        const uint64_t dq = desc_k_major(q_addr);
+        const uint64_t dk = desc_k_major(smem_u32(smem + L::K_OFF)), dv = desc_n_major(smem_u32(smem + L::V_OFF));
+        auto qk = [&](int u, int st) {
+          const uint64_t da = dq + (uint64_t)(u * (L::TILE_BYTES >> 4)), db = dk + (uint64_t)(st * (L::TILE_BYTES >> 4));
+#pragma unroll
+          for (int i = 0; i < 4 * HALVES; ++i)
+            if (i < steps) mma_ss(tmem + u * KB, da + (((i >> 2) * HALF + (i & 3) * 32) >> 4), db + (((i >> 2) * HALF + (i & 3) * 32) >> 4), id_s, i > 0);
           commit(&s.s_full[u]);
         };
-        auto pv = [&](int u, int j) {
-          const uint64_t db = desc_n_major(smem_u32(smem + L::V_OFF + (j % STAGES) * L::TILE_BYTES));
+        auto pv = [&](int u, int st, uint32_t add) {
+          const uint64_t db = dv + (uint64_t)(st * (L::TILE_BYTES >> 4));
+#pragma unroll
           for (int i = 0; i < KB / 16; ++i)
-            mma_ts(tmem + 256 + u * 128, tmem + u * KB + 8 * i, db + (uint64_t)((i * 16 * 128) >> 4), id_o, j > 0 || i > 0);
+            mma_ts(tmem + 256 + u * 128, tmem + u * KB + 8 * i, db + ((i * 16 * 128) >> 4), id_o, i > 0 ? 1u : add);
         };
         auto wait_v = [&](int j) {
           kv_mbar_wait(&s.v_full[j % STAGES], (j / STAGES) & 1u, abort_flag, &g_prompt_error);
@@ -315,17 +324,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         kv_mbar_wait(&s.q_full, 0, abort_flag, &g_prompt_error);
         for (int j = 0; j <= nb; ++j) {
           if (j < nb) kv_mbar_wait(&s.k_full[j % STAGES], (j / STAGES) & 1u, abort_flag, &g_prompt_error);
+#pragma unroll
           for (int u = 0; u < 2; ++u) {
             if (j > 0) {
               kv_mbar_wait(&s.p_full[u], (j - 1) & 1u, abort_flag, &g_prompt_error);
               if (u == 0) wait_v(j - 1);
               fence_after();
-              pv(u, j - 1);
+              pv(u, (j - 1) % STAGES, j > 1);
               if (j == nb) commit(&s.o_full[u]);
             }
             if (j < nb) {
               if (j == 0) fence_after();
-              qk(u, j);
+              qk(u, j % STAGES);
             }
           }
           if (j > 0) commit(&s.v_empty[(j - 1) % STAGES]);
@@ -363,23 +373,23 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int p = valid ? (int)min((int64_t)x.pos0 + tok, (int64_t)a.max_len - 1) : -1;   // position; < 0 sees nothing
     const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;         // first token of its window
 
-    // ---- Q: the warp's 32 rows, 8 bytes per lane and step, into the swizzled layout of operand A
+    // ---- Q: the warp's 32 rows, one row of 8 bytes per lane at a time, into the swizzled layout of operand A
+    uint8_t* const stage = smem + L::Q_OFF + u * L::TILE_BYTES + (warp & 3) * 32 * 128;   // this warp's rows of the tile
+    auto staged = [&](int r, int d) { return stage + (d >> 6) * HALF + r * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4) + (d & 4) * 2; };
     if (nb > 0) {
-      uint8_t* dst = smem + L::Q_OFF + u * L::TILE_BYTES;
-#pragma unroll 8
-      for (int i = 0; i < 32; ++i) {
-        const int r = (warp & 3) * 32 + i;
-        const int rt = x.tok0 + u * a.tile_tokens + r / a.per_block, rh = r % a.per_block;
-        const bool ok = __shfl_sync(0xffffffffu, (int)valid, i) != 0;
-        const int d = lane * 4;
-        uint2 w = make_uint2(0u, 0u);
-        if (ok && d < a.head_dim)
-          w = __ldg(reinterpret_cast<const uint2*>(
-              a.q + 2 * ((int64_t)(x.q0 + rt) * a.q_stride_token + (int64_t)(x.head0 + rh) * a.q_stride_head + d)));
-        w.x ^= a.q_sign;
-        w.y ^= a.q_sign;
+      const int64_t at = valid ? (int64_t)(x.q0 + tok) * a.q_stride_token + (int64_t)(x.head0 + hd) * a.q_stride_head : -1;
+      const int d = lane * 4;
+#pragma unroll
+      for (int i0 = 0; i0 < 32; i0 += 16) {
+        uint2 w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int64_t from = __shfl_sync(0xffffffffu, at, i0 + i);
+          w[i] = from >= 0 && d < a.head_dim ? __ldg(reinterpret_cast<const uint2*>(a.q + 2 * (from + d))) : make_uint2(0u, 0u);
+        }
         if (d < HALVES * 64)
-          *reinterpret_cast<uint2*>(dst + (d >> 6) * HALF + r * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4) + (d & 4) * 2) = w;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) *reinterpret_cast<uint2*>(staged(i0 + i, d)) = make_uint2(w[i].x ^ a.q_sign, w[i].y ^ a.q_sign);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -448,26 +458,33 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       kv_mbar_wait(&s.o_full[u], 0, abort_flag, &g_prompt_error);
       fence_after();
     }
+    // through this warp's rows of Q's place (every product has read it) and out as whole rows
     const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
-    uint8_t* dst = a.out + 2 * (((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim);
-#pragma unroll 1
-    for (int i = 0; i < steps * 16; i += 32) {
-      uint32_t o[32];
-      if (nb > 0) {
+    if (nb > 0) {
+#pragma unroll
+      for (int i = 0; i < 64 * HALVES; i += 32) {
+        uint32_t o[32];
+        if (i >= steps * 16) break;
         tm_ld32(o_addr + i, o);
         wait_ld();
-      }
-      if (valid) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4) {
-          if (i + k < a.head_dim) {
-            uint2 w = make_uint2(0u, 0u);
-            if (nb > 0)
-              w = make_uint2(pack16<KT>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv),
-                             pack16<KT>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv));
-            *reinterpret_cast<uint2*>(dst + 2 * (i + k)) = w;
-          }
-        }
+        for (int k = 0; k < 32; k += 8)
+          *reinterpret_cast<uint4*>(staged(lane, i + k)) =
+              make_uint4(pack16<KT>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv),
+                         pack16<KT>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv),
+                         pack16<KT>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv),
+                         pack16<KT>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv));
+      }
+      __syncwarp();
+    }
+    {
+      const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
+      const int d = lane * 4;
+#pragma unroll 8
+      for (int i = 0; i < 32; ++i) {
+        const int64_t to = __shfl_sync(0xffffffffu, at, i);
+        if (to >= 0 && d < a.head_dim)
+          *reinterpret_cast<uint2*>(a.out + 2 * (to + d)) = nb > 0 ? *reinterpret_cast<const uint2*>(staged(i, d)) : make_uint2(0u, 0u);
       }
     }
   }
