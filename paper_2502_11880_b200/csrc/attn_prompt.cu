@@ -5,17 +5,21 @@
 //
 // in one pass over K and V with a running maximum m per row.  The rows of a tile are (token, query head) pairs of ONE kv head:
 // with g query heads per kv head a tile of 128 rows holds 128 / g tokens, so K and V are read once for all heads that share them, and
-// a window's edges waste fewer columns than a tile of 128 tokens would.  A CTA has two such tiles that work on the same
-// blocks of 128 cached tokens:
-//   * warp 8: tensor copies of K and V blocks (one box per page and 64-column half, 128-byte swizzle) into two rings;
-//   * warp 9: one thread issues tcgen05.mma -- S = Q K^T from shared memory, O += P V with P in tensor memory -- for the two
+// a window's edges waste fewer columns than a tile of 128 tokens would.  A work item is two such tiles that work on the same
+// blocks of 128 cached tokens; one persistent CTA per SM walks items, the last (longest) first:
+//   * warp 8 finds the items and brings K and V blocks in by tensor copies (one box per page and 64-column half, 128-byte
+//     swizzle) into two rings;
+//   * warp 9: one lane issues tcgen05.mma -- S = Q K^T from shared memory, O += P V with P in tensor memory -- for the two
 //     tiles in turn, so that the tensor cores work on one tile while the other tile's exponentials are taken;
-//   * warps 0-3 and 4-7, one row per thread: the row of S from tensor memory, mask, maximum, exponentials, P back into the
-//     tensor-memory columns that S had, rows of O at the end.  O is rescaled only when a row's maximum has risen by more
+//   * warps 0-3 and 4-7, one thread per row: S from tensor memory (once for the maximum, once for the exponentials), P back
+//     into the tensor-memory columns that S had, rows of O at the end.  O is rescaled only when a row's maximum has risen by more
 //     than 2^8 (P and the sums stay below 2^8 times their range, which fp32 and both 16-bit types hold), so rarely;
-//   * warps 10, 11 clear the V rows of a block that no query of the CTA sees (the end of a page, a place between the sinks
-//     and the window), since 0 * NaN would reach O.
+//   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
+//     place between the sinks and the window), since 0 * NaN would reach O.
 // Blocks that no row sees are not visited: those of the sinks, then those from the first row's window to the last row.
+// Exponentials: the unit that takes them does 16 per SM and cycle, which for head_dim 128 is as long as both products take;
+// a share of the columns goes through a polynomial on the fp32 units instead (2^x = 2^n * p(x - n), degree 4, relative error
+// 2.6e-6, far below the rounding of P).
 // Rounding: S, m, the sums and O are fp32; P is rounded to the cache's 16-bit type, which is what the tensor cores take
 // as an operand beside a V of that type (a second 16-bit piece would take half as many products again); out is rounded once.
 #include <cmath>
@@ -29,10 +33,16 @@ namespace {
 
 constexpr int ROWS = 128;                     // rows of a tile (MMA M, tensor-memory lanes)
 constexpr int KB = 128;                       // cached tokens of a block
-constexpr int THREADS = 384;
+constexpr int SOFT_WARPS = 8;                 // one thread per row of the two tiles
+constexpr int THREADS = (SOFT_WARPS + 4) * 32;
 constexpr int HALF = KB * 128;                // 128 rows x 64 columns of 16 bits
 constexpr int STAGES = 2;                     // of K, and of V
 constexpr float LAZY = 8.0f;                  // log2 of how far a maximum may rise before O is rescaled
+
+#ifndef POLY_EVERY_
+#define POLY_EVERY_ 4
+#endif
+constexpr int POLY_EVERY = POLY_EVERY_;       // every so-manieth pair of columns takes the polynomial
 
 static __device__ int g_prompt_error = 0;
 
@@ -50,7 +60,8 @@ struct PromptArgs {
   int head_dim, page_shift, num_pages, layer;
   int window, sinks, max_len;
   float c;                                            // |scale| * log2(e), above 0 so that -inf stays -inf
-  uint32_t q_sign;                                    // flips q where scale < 0
+  uint32_t q_neg;                                     // scale < 0: the products take -Q
+  int64_t items;                                      // no item has this number or a higher one
   int* dev_status;
 };
 
@@ -90,7 +101,13 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for this thread's tensor-memory loads; the N registers count as written here, so that nothing reads them earlier.
+template <int N>
+__device__ __forceinline__ void wait_ld(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(v[i]));
+}
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* v) {
@@ -116,6 +133,22 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* v) {
       : "memory");
 }
 
+__device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+      "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+
 template <typename KT>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   uint32_t r;
@@ -124,15 +157,57 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return r;
 }
 
-// What a CTA works on.
+// Pairs of fp32 values (one instruction for two).
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^x for x <= 2^7 by a polynomial (x below -126 counts as -126): n = round(x) through the sum with 1.5 * 2^23, whose low bits
+// then go to the exponent; p is the degree-4 minimax fit (relative error, own exchange iteration) of 2^f on [-1/2, 1/2].
+__device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
+  float2 x = unpair(x2);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.0f));
+  x2 = pair(x.x, x.y);
+  const uint64_t t = add2(x2, pair(12582912.0f, 12582912.0f));
+  const uint64_t n = add2(t, pair(-12582912.0f, -12582912.0f));
+  const uint64_t f = fma2(n, pair(-1.0f, -1.0f), x2);
+  uint64_t p = fma2(f, pair(0.009570102207362652f, 0.009570102207362652f), pair(0.05591785907745361f, 0.05591785907745361f));
+  p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
+  p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
+  p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
+  const float2 e = unpair(t), m = unpair(p);
+  return make_float2(__uint_as_float(__float_as_uint(m.x) + (__float_as_uint(e.x) << 23)),
+                     __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
+}
+
+// What a CTA works on at a time.
 struct Item {
   int seq, head_kv, head0, heads;   // heads: query heads of the rows, from head0
   int q0, n_new;                    // first token and number of new tokens of the sequence
-  int tok0;                         // first new token of the CTA
+  int tok0;                         // first new token of the item
   int pos0;                         // position of new token 0
-  int p_last;                       // position of the CTA's last token
-  int lo;                           // first token that the CTA's first row sees through its window
-  int n0, t1, nb;                   // blocks: 0 .. n0-1 (sinks), then t1 ..; nb in all
+  int p_last;                       // position of the item's last token
+  int lo;                           // first token that the item's first row sees through its window
+  int n0, t1;                       // blocks: 0 .. n0-1 (sinks), then t1 ..
+  int nb;                           // blocks in all; -1: no more items
+  int two;                          // the second tile has rows
 };
 
 template <int HALVES>
@@ -141,14 +216,16 @@ struct Layout {
   static constexpr int Q_OFF = 0, K_OFF = 2 * TILE_BYTES, V_OFF = K_OFF + STAGES * TILE_BYTES, TAIL = V_OFF + STAGES * TILE_BYTES;
 };
 struct Tail {
-  uint64_t q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], v_clean[STAGES], s_full[2], p_full[2], o_full[2];
-  Item item;
+  uint4 stage[SOFT_WARPS][64];                  // 32 rows x 16 columns of O on their way out, per warp
+  Item item[2];
+  uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], v_clean[STAGES];
+  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2], item_full[2], item_empty[2];
   uint32_t tmem;
-  int abort_flag, found;
+  int abort_flag;
 };
 
 __device__ __forceinline__ int block_start(const Item& x, int j) { return (j < x.n0 ? j : x.t1 + j - x.n0) * KB; }
-// Whether the block holds tokens that no row of the CTA sees, and which of its rows those are.
+// Whether the block holds tokens that no row of the item sees, and which of its rows those are.
 __device__ __forceinline__ bool unseen(const PromptArgs& a, const Item& x, int c) { return c > x.p_last || (c >= a.sinks && c < x.lo); }
 __device__ __forceinline__ bool has_unseen(const PromptArgs& a, const Item& x, int c0) {
   return c0 + KB - 1 > x.p_last || (c0 < x.lo && c0 + KB > a.sinks);
@@ -166,7 +243,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    kv_mbar_init(&s.q_full, 8);
+    kv_mbar_init(&s.q_full, 2);
+    kv_mbar_init(&s.q_empty, 1);
     for (int i = 0; i < STAGES; ++i) {
       kv_mbar_init(&s.k_full[i], 1);
       kv_mbar_init(&s.k_empty[i], 1);
@@ -178,63 +256,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       kv_mbar_init(&s.s_full[u], 1);
       kv_mbar_init(&s.p_full[u], 4);
       kv_mbar_init(&s.o_full[u], 1);
+      kv_mbar_init(&s.o_empty[u], 4);
+      kv_mbar_init(&s.item_full[u], 1);
+      kv_mbar_init(&s.item_empty[u], SOFT_WARPS + 3);
     }
     s.abort_flag = 0;
-    s.found = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap) : "memory");
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  // ---- which tile pair this CTA has: the last sequence's last first (a causal row's work grows with its position)
-  if (warp == 8) {
-    const int heads = a.kv_heads * a.blocks;
-    const int64_t want = blockIdx.x / heads;
-    const int hb = blockIdx.x % heads;
-    const int span = 2 * a.tile_tokens;
-    int64_t before = 0;
-    for (int s1 = a.seqs; s1 > 0 && before <= want; s1 -= 32) {
-      const int i = s1 - 1 - lane;
-      const int q0 = i >= 0 ? __ldg(a.q_start + i) : 0;
-      const int n = i >= 0 ? max(0, __ldg(a.q_start + i + 1) - q0) : 0;
-      const int64_t tiles = (n + span - 1) / span;
-      int64_t x = tiles;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
-      }
-      const int64_t excl = before + x - tiles;
-      if (want >= excl && want < excl + tiles) {
-        Item t;
-        t.seq = i;
-        t.head_kv = hb / a.blocks;
-        const int b0 = hb % a.blocks * a.per_block;
-        t.head0 = t.head_kv * a.group + b0;
-        t.heads = min(a.per_block, a.group - b0);
-        t.q0 = q0;
-        t.n_new = n;
-        t.tok0 = (int)(tiles - 1 - (want - excl)) * span;
-        const int64_t pos0 = (int64_t)__ldg(a.kv_len + i) - n;
-        t.pos0 = (int)pos0;                                // |pos0| < 2^31: both terms are at least 0 or the sequence is empty
-        const int64_t most = a.max_len - 1;
-        t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
-        t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
-        t.n0 = t.t1 = t.nb = 0;
-        if (t.p_last >= 0) {
-          t.t1 = t.lo / KB;
-          t.n0 = min((min(a.sinks, t.lo) + KB - 1) / KB, t.t1);
-          t.nb = t.n0 + t.p_last / KB + 1 - t.t1;
-        }
-        s.item = t;
-        s.found = 1;
-      }
-      before += __shfl_sync(0xffffffffu, x, 31);
-    }
-  }
-  if (warp == 9) {
+  if (warp == SOFT_WARPS + 1) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -242,249 +273,404 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   fence_before();
   __syncthreads();
   fence_after();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = s.tmem;
-  const Item x = s.item;
-  const int nb = s.found ? x.nb : 0;
   const int steps = (a.head_dim + 15) / 16;                 // of 16 columns of head_dim
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 8) {
-      // ---------------------------------------------------------- producer: lane = box of a block
+  // The `it`-th item of this CTA (every role but the one that finds them).
+  auto next_item = [&](int it) -> Item {
+    kv_mbar_wait(&s.item_full[it & 1], (it >> 1) & 1u, abort_flag, &g_prompt_error);
+    Item x = s.item[it & 1];
+    if (*abort_flag) x.nb = -1;                             // somebody gave up: no more work
+    return x;
+  };
+
+  if (warp >= SOFT_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    if (warp == SOFT_WARPS) {
+      // ---------------------------------------------------------- items, K and V; lane = box of a block
       const int box_rows = min(1 << a.page_shift, 64);
       const int boxes = KB / box_rows;                       // <= 16
       const int half = lane / boxes, box = lane % boxes;
       const bool mine = half < HALVES;
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
-      auto look_up = [&](int j, int& y) -> int {
-        const int tok = block_start(x, j) + box * box_rows;
-        y = tok & ((1 << a.page_shift) - 1);
-        if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
-        return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
-      };
-      int y = 0, page = nb > 0 ? look_up(0, y) : 0;
-      for (int j = 0; j < nb; ++j) {
-        const int cur = page, cur_y = y;
-        if (j + 1 < nb) page = look_up(j + 1, y);
-        const bool issue = cur != -2;
-        const bool bad = issue && (cur < 0 || cur >= a.num_pages);
-        if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
-        const int st = j % STAGES;
-        const uint32_t par = ((j / STAGES) & 1u) ^ 1u;
+      uint32_t kb = 0;                                       // blocks so far
+      for (int it = 0;; ++it) {
+        kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
+        __syncwarp();
+        // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
+        const int heads = a.kv_heads * a.blocks, span = 2 * a.tile_tokens;
+        const int64_t id = blockIdx.x + (int64_t)it * gridDim.x, want = id / heads;
+        const int hb = (int)(id % heads);
+        if (lane == 0) s.item[it & 1].nb = -1;
+        __syncwarp();
+        bool found = false;
+        int64_t before = 0;
+        for (int s1 = id < a.items && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
+          const int i = s1 - 1 - lane;
+          const int q0 = i >= 0 ? __ldg(a.q_start + i) : 0;
+          const int n = i >= 0 ? max(0, __ldg(a.q_start + i + 1) - q0) : 0;
+          const int64_t tiles = (n + span - 1) / span;
+          int64_t sum = tiles;
 #pragma unroll
-        for (int pool = 0; pool < 2; ++pool) {
-          uint64_t* full = pool ? &s.v_full[st] : &s.k_full[st];
-          kv_mbar_wait(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
-          __syncwarp();
-          if (*abort_flag) continue;
-          if (lane == 0) kv_mbar_expect(full, bytes);
-          __syncwarp();
-          if (issue)
-            kv_box_copy(smem_u32(smem + (pool ? L::V_OFF : L::K_OFF) + st * L::TILE_BYTES + half * HALF + box * box_bytes),
-                        pool ? &vmap : &kmap, half * 64, cur_y, x.head_kv, bad ? -1 : cur, a.layer, full);
+          for (int d = 1; d < 32; d <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+          }
+          const int64_t excl = before + sum - tiles;
+          const bool here = want >= excl && want < excl + tiles;
+          if (here) {
+            Item t;
+            t.seq = i;
+            t.head_kv = hb / a.blocks;
+            const int b0 = hb % a.blocks * a.per_block;
+            t.head0 = t.head_kv * a.group + b0;
+            t.heads = min(a.per_block, a.group - b0);
+            t.q0 = q0;
+            t.n_new = n;
+            t.tok0 = (int)(tiles - 1 - (want - excl)) * span;
+            t.two = t.tok0 + a.tile_tokens < n;
+            const int64_t pos0 = (int64_t)__ldg(a.kv_len + i) - n, most = a.max_len - 1;
+            t.pos0 = (int)pos0;                              // |pos0| < 2^31
+            t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
+            t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
+            t.n0 = t.t1 = t.nb = 0;
+            if (t.p_last >= 0) {
+              t.t1 = t.lo / KB;
+              t.n0 = min((min(a.sinks, t.lo) + KB - 1) / KB, t.t1);
+              t.nb = t.n0 + t.p_last / KB + 1 - t.t1;
+            }
+            s.item[it & 1] = t;
+          }
+          found = found || __any_sync(0xffffffffu, here);
+          before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        __syncwarp();
+        const Item x = s.item[it & 1];
+        __syncwarp();
+        if (lane == 0) kv_mbar_arrive(&s.item_full[it & 1]);
+        if (!found) break;
+        auto look_up = [&](int j, int& y) -> int {
+          const int tok = block_start(x, j) + box * box_rows;
+          y = tok & ((1 << a.page_shift) - 1);
+          if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
+          return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
+        };
+        int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
+        for (int j = 0; j < x.nb; ++j, ++kb) {
+          const int cur = page, cur_y = y;
+          if (j + 1 < x.nb) page = look_up(j + 1, y);
+          const bool issue = cur != -2;
+          const bool bad = issue && (cur < 0 || cur >= a.num_pages);
+          if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+          const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
+          const int st = kb % STAGES;
+          const uint32_t par = ((kb / STAGES) & 1u) ^ 1u;
+#pragma unroll
+          for (int pool = 0; pool < 2; ++pool) {
+            uint64_t* full = pool ? &s.v_full[st] : &s.k_full[st];
+            kv_mbar_wait(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
+            __syncwarp();
+            if (*abort_flag) continue;
+            if (lane == 0) kv_mbar_expect(full, bytes);
+            __syncwarp();
+            if (issue)
+              kv_box_copy(smem_u32(smem + (pool ? L::V_OFF : L::K_OFF) + st * L::TILE_BYTES + half * HALF + box * box_bytes),
+                          pool ? &vmap : &kmap, half * 64, cur_y, x.head_kv, bad ? -1 : cur, a.layer, full);
+          }
         }
       }
       if (*abort_flag)                                        // leave only when the copies have landed
-        for (int j = max(0, nb - STAGES); j < nb; ++j)
-          for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.k_full[j % STAGES], (j / STAGES) & 1u) &&
-                                                     kv_mbar_try(&s.v_full[j % STAGES], (j / STAGES) & 1u)); ++k) {
+        for (uint32_t i = kb > STAGES ? kb - STAGES : 0; i < kb; ++i)
+          for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.k_full[i % STAGES], (i / STAGES) & 1u) &&
+                                                     kv_mbar_try(&s.v_full[i % STAGES], (i / STAGES) & 1u)); ++k) {
           }
-    } else if (warp == 9) {
-      // ---------------------------------------------------------- MMA issuer
-      if (nb > 0 && elect_one()) {
+    } else if (warp == SOFT_WARPS + 1) {
+      // ---------------------------------------------------------- products
+      if (elect_one()) {
         constexpr uint32_t FMT = std::is_same<KT, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t base = (1u << 4) | (FMT << 7) | (FMT << 10) | ((uint32_t)(ROWS >> 4) << 24);
-        const uint32_t id_s = base | ((uint32_t)(KB >> 3) << 17);
+        const uint32_t id_s = base | ((uint32_t)(KB >> 3) << 17) | (a.q_neg << 13);  // bit 13: operand A negated
         const uint32_t id_o = base | (1u << 16) | ((uint32_t)(steps * 2) << 17);     // N = 16 * steps, B N-major
-        const uint32_t q_addr = smem_u32(smem + L::Q_OFF);
-        uint32_t cleaned = 0;                                  // parity of each stage's next cleaning
-        const uint64_t dq = desc_k_major(q_addr);
+        const uint64_t dq = desc_k_major(smem_u32(smem + L::Q_OFF));
         const uint64_t dk = desc_k_major(smem_u32(smem + L::K_OFF)), dv = desc_n_major(smem_u32(smem + L::V_OFF));
-        auto qk = [&](int u, int st) {
-          const uint64_t da = dq + (uint64_t)(u * (L::TILE_BYTES >> 4)), db = dk + (uint64_t)(st * (L::TILE_BYTES >> 4));
-#pragma unroll
-          for (int i = 0; i < 4 * HALVES; ++i)
-            if (i < steps) mma_ss(tmem + u * KB, da + (((i >> 2) * HALF + (i & 3) * 32) >> 4), db + (((i >> 2) * HALF + (i & 3) * 32) >> 4), id_s, i > 0);
+        // (rolled: this lane runs a few instructions every thousand cycles, and each line of code it needs is then fetched anew)
+        auto qk = [&](int u, uint32_t st) {
+          uint64_t da = dq + (uint64_t)(u * (L::TILE_BYTES >> 4)), db = dk + (uint64_t)(st * (L::TILE_BYTES >> 4));
+#pragma unroll 1
+          for (int i = 0; i < steps; ++i) {
+            mma_ss(tmem + u * KB, da, db, id_s, i > 0);
+            const uint64_t next = (i & 3) == 3 ? (HALF - 96) >> 4 : 32 >> 4;
+            da += next;
+            db += next;
+          }
           commit(&s.s_full[u]);
         };
-        auto pv = [&](int u, int st, uint32_t add) {
-          const uint64_t db = dv + (uint64_t)(st * (L::TILE_BYTES >> 4));
-#pragma unroll
-          for (int i = 0; i < KB / 16; ++i)
-            mma_ts(tmem + 256 + u * 128, tmem + u * KB + 8 * i, db + ((i * 16 * 128) >> 4), id_o, i > 0 ? 1u : add);
-        };
-        auto wait_v = [&](int j) {
-          kv_mbar_wait(&s.v_full[j % STAGES], (j / STAGES) & 1u, abort_flag, &g_prompt_error);
-          if (has_unseen(a, x, block_start(x, j))) {
-            kv_mbar_wait(&s.v_clean[j % STAGES], (cleaned >> (j % STAGES)) & 1u, abort_flag, &g_prompt_error);
-            cleaned ^= 1u << (j % STAGES);
+        auto pv = [&](int u, uint32_t st, uint32_t add) {
+          uint64_t db = dv + (uint64_t)(st * (L::TILE_BYTES >> 4));
+#pragma unroll 1
+          for (int i = 0; i < KB / 16; ++i) {
+            mma_ts(tmem + 256 + u * 128, tmem + u * KB + 8 * i, db, id_o, add);
+            add = 1;
+            db += (16 * 128) >> 4;
           }
         };
-        kv_mbar_wait(&s.q_full, 0, abort_flag, &g_prompt_error);
-        for (int j = 0; j <= nb; ++j) {
-          if (j < nb) kv_mbar_wait(&s.k_full[j % STAGES], (j / STAGES) & 1u, abort_flag, &g_prompt_error);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if (j > 0) {
-              kv_mbar_wait(&s.p_full[u], (j - 1) & 1u, abort_flag, &g_prompt_error);
-              if (u == 0) wait_v(j - 1);
-              fence_after();
-              pv(u, (j - 1) % STAGES, j > 1);
-              if (j == nb) commit(&s.o_full[u]);
+        uint32_t kb = 0, cleaned = 0, items = 0;               // blocks, parities of the stages' next cleaning, items with blocks
+        uint32_t p_par = 0, o_par = 3;                         // parities to wait for, one bit per tile
+        for (int it = 0;; ++it) {
+          const Item x = next_item(it);
+          kv_mbar_arrive(&s.item_empty[it & 1]);
+          if (x.nb < 0) break;
+          if (x.nb == 0) continue;
+          kv_mbar_wait(&s.q_full, items & 1u, abort_flag, &g_prompt_error);
+          for (int j = 0; j <= x.nb; ++j) {
+            const uint32_t cur = kb + j, prev = cur - 1;
+            if (j < x.nb) kv_mbar_wait(&s.k_full[cur % STAGES], (cur / STAGES) & 1u, abort_flag, &g_prompt_error);
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+              if (u == 0 || x.two) {
+                if (j > 0) {
+                  kv_mbar_wait(&s.p_full[u], (p_par >> u) & 1u, abort_flag, &g_prompt_error);
+                  p_par ^= 1u << u;
+                  if (u == 0) {
+                    kv_mbar_wait(&s.v_full[prev % STAGES], (prev / STAGES) & 1u, abort_flag, &g_prompt_error);
+                    if (has_unseen(a, x, block_start(x, j - 1))) {
+                      kv_mbar_wait(&s.v_clean[prev % STAGES], (cleaned >> (prev % STAGES)) & 1u, abort_flag, &g_prompt_error);
+                      cleaned ^= 1u << (prev % STAGES);
+                    }
+                  }
+                  if (j == 1) {                                // the previous item's O has been read
+                    kv_mbar_wait(&s.o_empty[u], (o_par >> u) & 1u, abort_flag, &g_prompt_error);
+                    o_par ^= 1u << u;
+                  }
+                  fence_after();
+                  pv(u, prev % STAGES, j > 1);
+                  if (j == x.nb) commit(&s.o_full[u]);
+                }
+                if (j < x.nb) {
+                  if (j == 0) fence_after();
+                  qk(u, cur % STAGES);
+                }
+              }
             }
-            if (j < nb) {
-              if (j == 0) fence_after();
-              qk(u, j % STAGES);
-            }
+            if (j == x.nb - 1) commit(&s.q_empty);
+            if (j > 0) commit(&s.v_empty[prev % STAGES]);
+            if (j < x.nb) commit(&s.k_empty[cur % STAGES]);
           }
-          if (j > 0) commit(&s.v_empty[(j - 1) % STAGES]);
-          if (j < nb) commit(&s.k_empty[j % STAGES]);
+          kb += x.nb;
+          ++items;
         }
       }
     } else {
-      // ---------------------------------------------------------- V rows that no query sees count as 0
-      const int t = tid - 320;                                // 0..63
-      for (int j = 0; j < nb; ++j) {
-        const int c0 = block_start(x, j);
-        kv_mbar_wait(&s.v_full[j % STAGES], (j / STAGES) & 1u, abort_flag, &g_prompt_error);
-        if (has_unseen(a, x, c0)) {
-          uint8_t* v = smem + L::V_OFF + (j % STAGES) * L::TILE_BYTES;
-          for (int i = t; i < KB * 8; i += 64)
-            if (unseen(a, x, c0 + (i >> 3)))
-#pragma unroll
-              for (int h = 0; h < HALVES; ++h) *reinterpret_cast<uint4*>(v + h * HALF + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) kv_mbar_arrive(&s.v_clean[j % STAGES]);
-        }
-        // every block is seen, not only those to be cleaned: a wait tells only a fill's parity
+      // ---------------------------------------------------------- Q of the next item; V rows that no query sees count as 0
+      const int t = tid - (SOFT_WARPS + 2) * 32;              // 0..63
+      const int u = t >> 5;
+      constexpr int LANES = HALVES * 16, PER = 32 / LANES;    // lanes per row of Q (8 bytes each), rows at a time
+      uint32_t kb = 0, items = 0;
+      for (int it = 0;; ++it) {
+        const Item x = next_item(it);
         __syncwarp();
-        if (lane == 0) kv_mbar_arrive(&s.v_empty[j % STAGES]);
+        if (lane == 0) kv_mbar_arrive(&s.item_empty[it & 1]);
+        if (x.nb < 0) break;
+        if (x.nb == 0) continue;
+        int64_t at[4];                                        // where rows lane, lane + 32, .. of this warp's tile begin
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = lane + 32 * k;
+          const int rt = x.tok0 + u * a.tile_tokens + r / a.per_block, rh = r % a.per_block;
+          const bool ok = r < a.tile_tokens * a.per_block && rh < x.heads && rt < x.n_new && x.q0 >= 0 && (int64_t)x.q0 + rt < a.tokens;
+          at[k] = ok ? (int64_t)(x.q0 + rt) * a.q_stride_token + (int64_t)(x.head0 + rh) * a.q_stride_head : -1;
+        }
+        kv_mbar_wait(&s.q_empty, (items & 1u) ^ 1u, abort_flag, &g_prompt_error);
+        __syncwarp();
+        if (u == 0 || x.two) {
+          const int d = (lane % LANES) * 4;
+          const uint32_t dst = smem_u32(smem + L::Q_OFF + u * L::TILE_BYTES) + (d >> 6) * HALF + (d & 4) * 2;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll 8
+            for (int i = 0; i < 32; i += PER) {
+              const int r = i + lane / LANES;
+              const int64_t from = __shfl_sync(0xffffffffu, at[k], r);
+              const bool ok = from >= 0 && d < a.head_dim;
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + (32 * k + r) * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4)),
+                           "l"(a.q + 2 * (ok ? from + d : 0)), "r"(ok ? 8 : 0)
+                           : "memory");
+            }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
+        if (lane == 0) kv_mbar_arrive(&s.q_full);
+        ++items;
+        for (int j = 0; j < x.nb; ++j, ++kb) {
+          const int c0 = block_start(x, j), st = kb % STAGES;
+          kv_mbar_wait(&s.v_full[st], (kb / STAGES) & 1u, abort_flag, &g_prompt_error);
+          if (has_unseen(a, x, c0)) {
+            uint8_t* v = smem + L::V_OFF + st * L::TILE_BYTES;
+            for (int i = t; i < KB * 8; i += 64)
+              if (unseen(a, x, c0 + (i >> 3)))
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) *reinterpret_cast<uint4*>(v + h * HALF + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) kv_mbar_arrive(&s.v_clean[st]);
+          }
+          // every block is seen, not only those to be cleaned: a wait tells only a fill's parity
+          __syncwarp();
+          if (lane == 0) kv_mbar_arrive(&s.v_empty[st]);
+        }
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    // ------------------------------------------------------------ one row per thread
-    const int u = warp >> 2, row = tid & 127;
-    const int tok = x.tok0 + u * a.tile_tokens + row / a.per_block, hd = row % a.per_block;
-    const bool valid = s.found && row < a.tile_tokens * a.per_block && hd < x.heads && tok < x.n_new && x.q0 >= 0 &&
-                       (int64_t)x.q0 + tok < a.tokens;
-    const int p = valid ? (int)min((int64_t)x.pos0 + tok, (int64_t)a.max_len - 1) : -1;   // position; < 0 sees nothing
-    const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;         // first token of its window
-
-    // ---- Q: the warp's 32 rows, one row of 8 bytes per lane at a time, into the swizzled layout of operand A
-    uint8_t* const stage = smem + L::Q_OFF + u * L::TILE_BYTES + (warp & 3) * 32 * 128;   // this warp's rows of the tile
-    auto staged = [&](int r, int d) { return stage + (d >> 6) * HALF + r * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4) + (d & 4) * 2; };
-    if (nb > 0) {
-      const int64_t at = valid ? (int64_t)(x.q0 + tok) * a.q_stride_token + (int64_t)(x.head0 + hd) * a.q_stride_head : -1;
-      const int d = lane * 4;
-#pragma unroll
-      for (int i0 = 0; i0 < 32; i0 += 16) {
-        uint2 w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int64_t from = __shfl_sync(0xffffffffu, at, i0 + i);
-          w[i] = from >= 0 && d < a.head_dim ? __ldg(reinterpret_cast<const uint2*>(a.q + 2 * (from + d))) : make_uint2(0u, 0u);
-        }
-        if (d < HALVES * 64)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) *reinterpret_cast<uint2*>(staged(i0 + i, d)) = make_uint2(w[i].x ^ a.q_sign, w[i].y ^ a.q_sign);
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) kv_mbar_arrive(&s.q_full);
-    }
-
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    // ------------------------------------------------------------ one thread per row
+    const int u = warp >> 2, quarter = warp & 3, row = tid & 127;
+    const int row_tok = row / a.per_block, hd = row % a.per_block;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tmem + lanes + u * KB, o_addr = tmem + lanes + 256 + u * 128;
-    float m = -INFINITY, l = 0.0f;
-    for (int j = 0; j < nb; ++j) {
-      kv_mbar_wait(&s.s_full[u], j & 1u, abort_flag, &g_prompt_error);
-      fence_after();
-      uint32_t v[KB];
+    const uint64_t c2 = pair(a.c, a.c);
+    uint32_t s_cnt = 0, items = 0;
+    for (int it = 0;; ++it) {
+      const Item x = next_item(it);
+      __syncwarp();
+      if (lane == 0) kv_mbar_arrive(&s.item_empty[it & 1]);
+      if (x.nb < 0) break;
+      const int tok = x.tok0 + u * a.tile_tokens + row_tok;
+      const bool valid = row < a.tile_tokens * a.per_block && hd < x.heads && tok < x.n_new && x.q0 >= 0 && (int64_t)x.q0 + tok < a.tokens;
+      if (u == 1 && !x.two) continue;
+      const int p = valid ? (int)min((int64_t)x.pos0 + tok, (int64_t)a.max_len - 1) : -1;   // position; < 0 sees nothing
+      const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;                          // first token of its window
+      float m = -INFINITY;
+      uint64_t l2 = 0;                                        // a pair of sums
+      for (int j = 0; j < x.nb; ++j, ++s_cnt) {
+        const int c0 = block_start(x, j);
+        const bool edge = __any_sync(0xffffffffu, c0 + KB - 1 > p || (c0 < wlo && c0 + KB > a.sinks));
+        kv_mbar_wait(&s.s_full[u], s_cnt & 1u, abort_flag, &g_prompt_error);
+        fence_after();
+        // ---- the row's maximum; a block at an edge goes back with -inf where the row does not see
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        uint32_t v[64];
+        tm_ld32(s_addr, v);
+        tm_ld32(s_addr + 32, v + 32);
 #pragma unroll
-      for (int i = 0; i < KB; i += 32) tm_ld32(s_addr + i, v + i);
-      wait_ld();
-      const int c0 = block_start(x, j);
-      const bool edge = c0 + KB - 1 > p || (c0 < wlo && c0 + KB > a.sinks);
-      if (__any_sync(0xffffffffu, edge)) {
-        const int hi = p - c0, lo = wlo - c0, sk = a.sinks - c0;
+        for (int g = 0; g < 2; ++g) {
+          wait_ld<64>(v);
+          if (edge) {
+            const int hi = p - c0 - 64 * g, lo = wlo - c0 - 64 * g, sk = a.sinks - c0 - 64 * g;
 #pragma unroll
-        for (int i = 0; i < KB; ++i)
-          if (!(i <= hi && (i >= lo || i < sk))) v[i] = 0xff800000u;
-      }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            for (int i = 0; i < 64; ++i)
+              if (!(i <= hi && (i >= lo || i < sk))) v[i] = 0xff800000u;
+            tm_st32(s_addr + 64 * g, v);
+            tm_st32(s_addr + 64 * g + 32, v + 32);
+          }
 #pragma unroll
-      for (int i = 0; i < KB; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
-      const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      const float m_new = fmaxf(m, big * a.c);
-      if (__any_sync(0xffffffffu, m_new > m + LAZY)) {
-        const float f = m == -INFINITY ? 0.0f : exp2_approx(m - m_new);   // (-inf before the first visible token: O is 0)
-        m = m_new;
-        l *= f;
-        if (j > 0) {
-#pragma unroll 1
-          for (int i = 0; i < steps * 16; i += 32) {
-            uint32_t o[32];
-            tm_ld32(o_addr + i, o);
-            wait_ld();
+          for (int i = 0; i < 64; i += 8)
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-            tm_st32(o_addr + i, o);
+            for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], __uint_as_float(v[i + 2 * k])), __uint_as_float(v[i + 2 * k + 1]));
+          if (g == 0) {
+            tm_ld32(s_addr + 64, v);
+            tm_ld32(s_addr + 96, v + 32);
           }
         }
-      }
-      const float ref = m == -INFINITY ? 0.0f : m;
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (edge) wait_st();
+        tm_ld32(s_addr, v);                                   // on its way again for the exponentials
+        const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float m_new = fmaxf(m, big * a.c);
+        if (__any_sync(0xffffffffu, m_new > m + LAZY)) {
+          const float f = m == -INFINITY ? 0.0f : exp2_approx(m - m_new);   // (-inf before the first visible token: O is 0)
+          m = m_new;
+          l2 = fma2(l2, pair(f, f), 0);
+          if (j > 0) {
+#pragma unroll 1
+            for (int i = 0; i < steps * 16; i += 16) {
+              uint32_t o[16];
+              tm_ld16(o_addr + i, o);
+              wait_ld<16>(o);
 #pragma unroll
-      for (int i = 0; i < KB; i += 2) {
-        const float e0 = exp2_approx(fmaf(__uint_as_float(v[i]), a.c, -ref));
-        const float e1 = exp2_approx(fmaf(__uint_as_float(v[i + 1]), a.c, -ref));
-        sum[(i >> 1) & 3] += e0 + e1;
-        v[i >> 1] = pack16<KT>(e0, e1);
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tm_st16(o_addr + i, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        const uint64_t r2 = pair(-ref, -ref);
+        // ---- exponentials of 32 columns, which become 16 of P; the next 32 are on their way meanwhile
+        auto exps = [&](uint32_t* w) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const uint64_t e = fma2(pair(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), c2, r2);
+            float2 y;
+            if ((i >> 1) % POLY_EVERY == POLY_EVERY - 1) {
+              y = exp2_poly(e);
+            } else {
+              y = unpair(e);
+              y.x = exp2_approx(y.x);
+              y.y = exp2_approx(y.y);
+            }
+            l2 = add2(l2, pair(y.x, y.y));
+            w[i >> 1] = pack16<KT>(y.x, y.y);
+          }
+        };
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+          wait_ld<32>(v);
+          tm_ld32(s_addr + 64 * g + 32, v + 32);
+          exps(v);
+          tm_st16(s_addr + 32 * g, v);                        // (over columns of S that have been read)
+          wait_ld<32>(v + 32);
+          if (g == 0) tm_ld32(s_addr + 64, v);
+          exps(v + 32);
+          tm_st16(s_addr + 32 * g + 16, v + 32);
+        }
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tm_st32(s_addr, v);
-      tm_st32(s_addr + 32, v + 32);
-      wait_st();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
-    }
 
-    // ---- rows of O
-    if (nb > 0) {
-      kv_mbar_wait(&s.o_full[u], 0, abort_flag, &g_prompt_error);
-      fence_after();
-    }
-    // through this warp's rows of Q's place (every product has read it) and out as whole rows
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
-    if (nb > 0) {
-#pragma unroll
-      for (int i = 0; i < 64 * HALVES; i += 32) {
-        uint32_t o[32];
-        if (i >= steps * 16) break;
-        tm_ld32(o_addr + i, o);
-        wait_ld();
-#pragma unroll
-        for (int k = 0; k < 32; k += 8)
-          *reinterpret_cast<uint4*>(staged(lane, i + k)) =
-              make_uint4(pack16<KT>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv),
-                         pack16<KT>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv),
-                         pack16<KT>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv),
-                         pack16<KT>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv));
+      // ---- rows of O, 16 columns at a time through this warp's staging rows and out as whole sectors
+      float inv = 0.0f;                                       // (a row that saw nothing is 0)
+      if (x.nb > 0) {
+        const float2 l = unpair(l2);
+        if (m != -INFINITY) inv = 1.0f / (l.x + l.y);
+        kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
+        fence_after();
+        ++items;
       }
-      __syncwarp();
-    }
-    {
       const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
-      const int d = lane * 4;
-#pragma unroll 8
-      for (int i = 0; i < 32; ++i) {
-        const int64_t to = __shfl_sync(0xffffffffu, at, i);
-        if (to >= 0 && d < a.head_dim)
-          *reinterpret_cast<uint2*>(a.out + 2 * (to + d)) = nb > 0 ? *reinterpret_cast<const uint2*>(staged(i, d)) : make_uint2(0u, 0u);
+      uint4* const stage = s.stage[warp];
+#pragma unroll 1
+      for (int i = 0; i < steps * 16; i += 16) {
+        uint32_t o[16];
+        if (x.nb > 0) {
+          tm_ld16(o_addr + i, o);
+          wait_ld<16>(o);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            w[e] = inv == 0.0f ? 0u : pack16<KT>(__uint_as_float(o[8 * k + 2 * e]) * inv, __uint_as_float(o[8 * k + 2 * e + 1]) * inv);
+          stage[lane * 2 + (k ^ ((lane >> 2) & 1))] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+        const int d = i + (lane & 3) * 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + (lane >> 2);
+          const int64_t to = __shfl_sync(0xffffffffu, at, r);
+          const uint2 w = reinterpret_cast<const uint2*>(stage + r * 2 + (((lane >> 1) & 1) ^ ((r >> 2) & 1)))[lane & 1];
+          if (to >= 0 && d < a.head_dim) *reinterpret_cast<uint2*>(a.out + 2 * (to + d)) = w;
+        }
+      }
+      if (x.nb > 0) {
+        fence_before();
+        __syncwarp();
+        if (lane == 0) kv_mbar_arrive(&s.o_empty[u]);
       }
     }
   }
@@ -493,7 +679,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (warp == SOFT_WARPS + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 template <typename KT, int HALVES>
@@ -548,13 +734,13 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, cudaStream
   a.sinks = x.sinks;
   const int64_t most = x.table_width * c->page_size;
   a.max_len = most > 0x3fffff00 ? 0x3fffff00 : (int)most;
-  a.q_sign = x.scale < 0.0f ? 0x80008000u : 0u;
+  a.q_neg = x.scale < 0.0f ? 1u : 0u;
   a.c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-30f);
   a.dev_status = x.dev_status;
   // a sequence has at most one tile pair that is not full; which CTA has which is found on the device
   const int64_t pairs = x.tokens / (2 * a.tile_tokens) + (x.seqs < x.tokens ? x.seqs : x.tokens);
-  const int64_t grid = pairs * a.kv_heads * a.blocks;
-  if (grid > 0x7fffffff) return BITNET_ERR_UNSUPPORTED_SHAPE;
+  a.items = pairs * a.kv_heads * a.blocks;
+  const int64_t sms = dev_info().sm_count, grid = a.items < sms ? a.items : sms;
   log_launch("attn_prompt_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%lld", a.tokens, a.q_heads, a.kv_heads,
              a.head_dim, a.window, (long long)grid);
   const bool two = a.head_dim > 64;
