@@ -39,10 +39,8 @@ constexpr int HALF = KB * 128;                // 128 rows x 64 columns of 16 bit
 constexpr int STAGES = 2;                     // of K, and of V
 constexpr float LAZY = 8.0f;                  // log2 of how far a maximum may rise before O is rescaled
 
-#ifndef POLY_EVERY_
-#define POLY_EVERY_ 4
-#endif
-constexpr int POLY_EVERY = POLY_EVERY_;       // every so-manieth pair of columns takes the polynomial
+constexpr int POLY_EVERY = 4;                 // every fourth pair of columns takes the polynomial (none / 8th / 4th / 2nd pair measured
+                                              // 97 / 94 / 94 / 100 us on chunks of 4 x 512 tokens)
 
 static __device__ int g_prompt_error = 0;
 
@@ -74,9 +72,8 @@ __device__ __forceinline__ uint64_t desc_n_major(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(HALF >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-// One lane of the warp, in a form that tells the compiler so: the operands of the instructions below are warp-uniform registers,
-// and behind a test of the lane's number each of them would be brought there by a loop over the lanes (measured: 130
-// instead of 64 cycles per product issued).
+// One lane of the warp, in a form that tells the compiler so: the operands of the instructions below are warp-uniform registers
+// (against a test of the lane's number: 4 % of a long prompt's time).
 __device__ __forceinline__ bool elect_one() {
   uint32_t e;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
@@ -216,7 +213,7 @@ struct Layout {
   static constexpr int Q_OFF = 0, K_OFF = 2 * TILE_BYTES, V_OFF = K_OFF + STAGES * TILE_BYTES, TAIL = V_OFF + STAGES * TILE_BYTES;
 };
 struct Tail {
-  uint4 stage[SOFT_WARPS][64];                  // 32 rows x 16 columns of O on their way out, per warp
+  uint4 stage[SOFT_WARPS][128];                 // 32 rows x 32 columns of O on their way out, per warp
   Item item[2];
   uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], v_clean[STAGES];
   uint64_t s_full[2], p_full[2], o_full[2], o_empty[2], item_full[2], item_empty[2];
@@ -395,7 +392,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         const uint32_t id_o = base | (1u << 16) | ((uint32_t)(steps * 2) << 17);     // N = 16 * steps, B N-major
         const uint64_t dq = desc_k_major(smem_u32(smem + L::Q_OFF));
         const uint64_t dk = desc_k_major(smem_u32(smem + L::K_OFF)), dv = desc_n_major(smem_u32(smem + L::V_OFF));
-        // (rolled: this lane runs a few instructions every thousand cycles, and each line of code it needs is then fetched anew)
+        // (rolled: the loop's own instructions hide behind the 64 cycles of each product)
         auto qk = [&](int u, uint32_t st) {
           uint64_t da = dq + (uint64_t)(u * (L::TILE_BYTES >> 4)), db = dk + (uint64_t)(st * (L::TILE_BYTES >> 4));
 #pragma unroll 1
@@ -427,19 +424,20 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           for (int j = 0; j <= x.nb; ++j) {
             const uint32_t cur = kb + j, prev = cur - 1;
             if (j < x.nb) kv_mbar_wait(&s.k_full[cur % STAGES], (cur / STAGES) & 1u, abort_flag, &g_prompt_error);
+            // (before P, so that little lies between it and its product)
+            if (j > 0) {
+              kv_mbar_wait(&s.v_full[prev % STAGES], (prev / STAGES) & 1u, abort_flag, &g_prompt_error);
+              if (has_unseen(a, x, block_start(x, j - 1))) {
+                kv_mbar_wait(&s.v_clean[prev % STAGES], (cleaned >> (prev % STAGES)) & 1u, abort_flag, &g_prompt_error);
+                cleaned ^= 1u << (prev % STAGES);
+              }
+            }
 #pragma unroll 1
             for (int u = 0; u < 2; ++u) {
               if (u == 0 || x.two) {
                 if (j > 0) {
                   kv_mbar_wait(&s.p_full[u], (p_par >> u) & 1u, abort_flag, &g_prompt_error);
                   p_par ^= 1u << u;
-                  if (u == 0) {
-                    kv_mbar_wait(&s.v_full[prev % STAGES], (prev / STAGES) & 1u, abort_flag, &g_prompt_error);
-                    if (has_unseen(a, x, block_start(x, j - 1))) {
-                      kv_mbar_wait(&s.v_clean[prev % STAGES], (cleaned >> (prev % STAGES)) & 1u, abort_flag, &g_prompt_error);
-                      cleaned ^= 1u << (prev % STAGES);
-                    }
-                  }
                   if (j == 1) {                                // the previous item's O has been read
                     kv_mbar_wait(&s.o_empty[u], (o_par >> u) & 1u, abort_flag, &g_prompt_error);
                     o_par ^= 1u << u;
@@ -531,6 +529,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tmem + lanes + u * KB, o_addr = tmem + lanes + 256 + u * 128;
     const uint64_t c2 = pair(a.c, a.c);
+    const bool wide = a.head_dim % 8 == 0;                    // rows of out begin at multiples of 16 bytes
     uint32_t s_cnt = 0, items = 0;
     for (int it = 0;; ++it) {
       const Item x = next_item(it);
@@ -544,6 +543,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;                          // first token of its window
       float m = -INFINITY;
       uint64_t l2 = 0;                                        // a pair of sums
+      uint32_t v[64];
       for (int j = 0; j < x.nb; ++j, ++s_cnt) {
         const int c0 = block_start(x, j);
         const bool edge = __any_sync(0xffffffffu, c0 + KB - 1 > p || (c0 < wlo && c0 + KB > a.sinks));
@@ -551,7 +551,6 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         fence_after();
         // ---- the row's maximum; a block at an edge goes back with -inf where the row does not see
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        uint32_t v[64];
         tm_ld32(s_addr, v);
         tm_ld32(s_addr + 32, v + 32);
 #pragma unroll
@@ -630,41 +629,52 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
       }
 
-      // ---- rows of O, 16 columns at a time through this warp's staging rows and out as whole sectors
+      // ---- rows of O, 32 columns at a time through this warp's staging rows and out as whole sectors
       float inv = 0.0f;                                       // (a row that saw nothing is 0)
       if (x.nb > 0) {
         const float2 l = unpair(l2);
         if (m != -INFINITY) inv = 1.0f / (l.x + l.y);
+      }
+      const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
+      const int piece = lane & 3;                             // 8 columns; rows 8 k + lane / 4
+      int64_t to[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        to[k] = __shfl_sync(0xffffffffu, at, 8 * k + (lane >> 2));
+        to[k] = to[k] < 0 ? -1 : to[k] + piece * 8;
+      }
+      uint4* const stage = s.stage[warp];
+      if (x.nb > 0) {
         kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
         fence_after();
         ++items;
       }
-      const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
-      uint4* const stage = s.stage[warp];
 #pragma unroll 1
-      for (int i = 0; i < steps * 16; i += 16) {
-        uint32_t o[16];
-        if (x.nb > 0) {
-          tm_ld16(o_addr + i, o);
-          wait_ld<16>(o);
-        }
-        __syncwarp();
+      for (int i = 0; i < steps * 16; i += 32) {
+        uint32_t* const o = v;
+        if (x.nb > 0) tm_ld32(o_addr + i, o);
+        wait_ld<32>(o);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t w[4];
+        for (int e = 0; e < 16; ++e)
+          o[e] = inv == 0.0f ? 0u : pack16<KT>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            w[e] = inv == 0.0f ? 0u : pack16<KT>(__uint_as_float(o[8 * k + 2 * e]) * inv, __uint_as_float(o[8 * k + 2 * e + 1]) * inv);
-          stage[lane * 2 + (k ^ ((lane >> 2) & 1))] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int k = 0; k < 4; ++k) stage[lane * 4 + (k ^ ((lane >> 1) & 3))] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         __syncwarp();
-        const int d = i + (lane & 3) * 4;
+        uint4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = stage[(8 * k + (lane >> 2)) * 4 + (piece ^ ((lane >> 3) & 3))];
+        __syncwarp();
+        const int left = a.head_dim - i - piece * 8;          // columns from this piece on
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = 8 * k + (lane >> 2);
-          const int64_t to = __shfl_sync(0xffffffffu, at, r);
-          const uint2 w = reinterpret_cast<const uint2*>(stage + r * 2 + (((lane >> 1) & 1) ^ ((r >> 2) & 1)))[lane & 1];
-          if (to >= 0 && d < a.head_dim) *reinterpret_cast<uint2*>(a.out + 2 * (to + d)) = w;
+          uint8_t* const dst = a.out + 2 * (to[k] + i);
+          if (to[k] < 0 || left <= 0) continue;
+          if (wide) {
+            *reinterpret_cast<uint4*>(dst) = w[k];
+          } else {
+            *reinterpret_cast<uint2*>(dst) = make_uint2(w[k].x, w[k].y);
+            if (left > 4) *reinterpret_cast<uint2*>(dst + 8) = make_uint2(w[k].z, w[k].w);
+          }
         }
       }
       if (x.nb > 0) {

@@ -109,6 +109,25 @@ __device__ __forceinline__ void kv_mbar_wait(uint64_t* bar, uint32_t parity, vol
   atomicExch(error, BITNET_ERR_TIMEOUT);
 }
 
+// The same by polling: a suspended wait takes some hundred cycles to resume, a poll some tens, at the price of issue slots.
+__device__ __forceinline__ void kv_mbar_poll(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* error) {
+  const uint32_t addr = smem_u32(bar);
+  for (uint32_t it = 0; it < 16 * KV_WAIT_LIMIT; ++it) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    if (ok) return;
+    if ((it & 255u) == 255u && *abort_flag) return;
+  }
+  *abort_flag = 1;
+  atomicExch(error, BITNET_ERR_TIMEOUT);
+}
+
 // One box of the pool: columns [x, x + 64), rows from `row` of (head, page, layer).  Anything outside the pool reads as 0.
 __device__ __forceinline__ void kv_box_copy(uint32_t dst, const CUtensorMap* map, int x, int row, int head, int page, int layer,
                                             uint64_t* bar) {

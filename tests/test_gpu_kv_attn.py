@@ -227,6 +227,32 @@ def test_prompt_single_tokens_agree_with_decode():
     assert torch.allclose(a.float(), b.float(), rtol=2 ** -7, atol=2 ** -7)
 
 
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
+def test_prompt_scales(scale):
+    """Negative scales (the largest exponent belongs to the smallest product), 0 (all alike) and sharp ones."""
+    p = Paged([150, 40], 2, 64, 16, BF, seed=14)
+    start, seq, pos = prompt_args([(30, 120), (0, 40)])
+    q = p.queries(160, 4, 64, BF)
+    out = run_prompt(p, q, start, 120, scale=scale, window=77, sinks=2)
+    check_attn(out, p.ref(q, pos, seq, scale, 77, 2), PROMPT_P[BF])
+
+
+def test_prompt_rising_maxima():
+    """Scores that grow along the context, so that the running maximum rises block after block."""
+    p = Paged([1500], 1, 64, 64, BF, seed=15)
+    grow = torch.linspace(0.2, 12.0, 1500, device="cuda")
+    ids = p.table[0].long()
+    for e in range(-(-1500 // 64)):
+        rows = min(64, 1500 - e * 64)
+        p.k[p.layer, ids[e], 0, :rows] = (p.k[p.layer, ids[e], 0, :rows].float().abs() * grow[e * 64:e * 64 + rows, None]).to(BF)
+    start, seq, pos = prompt_args([(1300, 200)])
+    q = p.queries(200, 2, 64, BF).abs()
+    out = run_prompt(p, q, start, 200)
+    check_attn(out, p.ref(q, pos, seq, 0.125, 0, 0), PROMPT_P[BF])
+    d = run_decode(p, q[-1:].contiguous())
+    check_attn(d, p.ref(q[-1:], [1499], [0], 0.125, 0, 0), DECODE_P[BF, False])
+
+
 def test_prompt_strided_queries_negative_positions_and_stream():
     """Tokens before the start of the context (kv_len smaller than the number of new tokens) see nothing."""
     p = Paged([5, 60], 2, 64, 16, HF, seed=12, nhd=True)
