@@ -530,9 +530,16 @@ def new_kv_cache(layers, num_pages, kv_heads, page_size, head_dim, dtype=torch.b
     return KvCache(k, v)
 
 
-def _book(t, name, dim):
-    if not (t.is_cuda and t.dtype == torch.int32 and t.dim() == dim and t.is_contiguous()):
+_I32 = torch.int32
+_raw_stream = torch._C._cuda_getCurrentRawStream     # (a Stream object costs 3 us to make)
+
+
+def _book(t, name, dim, rows=0):
+    """Address of an int32 array of the books with at least `rows` rows."""
+    if not (t.is_cuda and t.dtype is _I32 and t.dim() == dim and t.is_contiguous()):
         raise BitnetError(f"{name}: expected a contiguous {dim}-D CUDA tensor of int32")
+    if rows and t.size(0) < rows:
+        raise BitnetError(f"{name}: expected {rows} entries")
     return t.data_ptr()
 
 
@@ -540,42 +547,41 @@ def _opt(t, name):
     return None if t is None else _book(t, name, 1)
 
 
-def _st(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _st(stream, device):
+    return _raw_stream(device.index or 0) if stream is None else stream.cuda_stream
 
 
 def _rows(t, name, heads, dim):
-    if not (t.is_cuda and t.dim() == 3 and t.dtype in KV_DTYPE and (heads is None or t.shape[1] == heads) and t.shape[2] == dim
-            and (t.stride(2) == 1 or dim == 1)):
-        raise BitnetError(f"{name}: expected a CUDA tensor [tokens][heads][head_dim] of fp32, bf16 or fp16, head_dim contiguous")
-    return t.data_ptr()
-
-
-def _lens(t, name, n):
-    if t.shape[0] < n:
-        raise BitnetError(f"{name}: expected {n} entries")
+    """Shape, strides and type code of [tokens][heads][head_dim] rows."""
+    code = KV_DTYPE.get(t.dtype)
+    if t.dim() != 3 or not t.is_cuda or code is None:
+        raise BitnetError(f"{name}: expected a CUDA tensor [tokens][heads][head_dim] of fp32, bf16 or fp16")
+    n, h, d = t.shape
+    sn, sh, sd = t.stride()
+    if d != dim or (heads is not None and h != heads) or (sd != 1 and dim > 1):
+        raise BitnetError(f"{name}: expected [tokens][{'heads' if heads is None else heads}][{dim}] with the last dimension contiguous")
+    return n, h, sn, sh, code
 
 
 def bitnet_kv_append(cache, layer, k, v, table, kv_len, q_start=None, dev_status=None, stream=None):
     """Writes new tokens' rows k, v [tokens][kv_heads][head_dim] into their pages; kv_len [seqs] counts them already."""
-    kp, vp = _rows(k, "k", cache.kv_heads, cache.head_dim), _rows(v, "v", cache.kv_heads, cache.head_dim)
-    if k.dtype != v.dtype or k.stride() != v.stride() or k.shape != v.shape:
+    rows = _rows(k, "k", cache.kv_heads, cache.head_dim)
+    if rows != _rows(v, "v", cache.kv_heads, cache.head_dim):
         raise BitnetError("bitnet_kv_append: k and v must have one type, shape and strides")
-    seqs = table.shape[0] if q_start is None else q_start.shape[0] - 1
-    tp, lp, qp = _book(table, "table", 2), _book(kv_len, "kv_len", 1), _opt(q_start, "q_start")
-    _lens(table, "table", seqs)
-    _lens(kv_len, "kv_len", seqs)
-    _check(lib().bitnet_kv_append(cache.ref, layer, kp, vp, KV_DTYPE[k.dtype], k.stride(0), k.stride(1), k.shape[0], tp, table.shape[1],
-                                  lp, qp, seqs, _opt(dev_status, "dev_status"), _st(stream)), "bitnet_kv_append")
+    n, _, sn, sh, code = rows
+    height, width = table.shape
+    seqs = height if q_start is None else q_start.size(0) - 1
+    _check(lib().bitnet_kv_append(cache.ref, layer, k.data_ptr(), v.data_ptr(), code, sn, sh, n, _book(table, "table", 2, seqs), width,
+                                  _book(kv_len, "kv_len", 1, seqs), _opt(q_start, "q_start"), seqs, _opt(dev_status, "dev_status"),
+                                  _st(stream, cache.device)), "bitnet_kv_append")
 
 
 def bitnet_kv_reserve(refs, table, from_len, to_len, page_size, dev_status=None, stream=None):
     """Gives the rows of the table the pages that growing from from_len to to_len tokens takes, lowest free pages first."""
-    rp, tp, fp, lp = _book(refs, "refs", 1), _book(table, "table", 2), _book(from_len, "from_len", 1), _book(to_len, "to_len", 1)
-    _lens(from_len, "from_len", table.shape[0])
-    _lens(to_len, "to_len", table.shape[0])
-    _check(lib().bitnet_kv_reserve(rp, refs.shape[0], tp, table.shape[0], table.shape[1], fp, lp, page_size,
-                                   _opt(dev_status, "dev_status"), _st(stream)), "bitnet_kv_reserve")
+    seqs, width = table.shape
+    _check(lib().bitnet_kv_reserve(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
+                                   _book(from_len, "from_len", 1, seqs), _book(to_len, "to_len", 1, seqs), page_size,
+                                   _opt(dev_status, "dev_status"), _st(stream, table.device)), "bitnet_kv_reserve")
 
 
 def bitnet_kv_workspace_bytes(num_pages, n) -> int:
@@ -592,49 +598,48 @@ def new_kv_workspace(num_pages, n=0, device="cuda"):
 
 def bitnet_kv_fork(cache, refs, table, kv_len, parents, children, workspace=None, dev_status=None, stream=None):
     """Rows children[i] become copies of rows parents[i]: full pages shared, a page filled in part copied."""
-    if refs.shape[0] != cache.num_pages or parents.shape != children.shape:
+    n, (seqs, width) = parents.size(0), table.shape
+    if refs.size(0) != cache.num_pages or children.size(0) != n:
         raise BitnetError("bitnet_kv_fork: refs must have one entry per page, parents and children one length")
     if workspace is None:
-        workspace = new_kv_workspace(cache.num_pages, parents.shape[0], cache.device)
-    _lens(kv_len, "kv_len", table.shape[0])
-    _check(lib().bitnet_kv_fork(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), table.shape[0], table.shape[1],
-                                _book(kv_len, "kv_len", 1), _book(parents, "parents", 1), _book(children, "children", 1), parents.shape[0],
-                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _opt(dev_status, "dev_status"),
-                                _st(stream)), "bitnet_kv_fork")
+        workspace = new_kv_workspace(cache.num_pages, n, cache.device)
+    _check(lib().bitnet_kv_fork(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), seqs, width, _book(kv_len, "kv_len", 1, seqs),
+                                _book(parents, "parents", 1), _book(children, "children", 1), n, workspace.data_ptr(), workspace.nbytes,
+                                _opt(dev_status, "dev_status"), _st(stream, cache.device)), "bitnet_kv_fork")
 
 
 def bitnet_kv_free(refs, table, kv_len, rows, dev_status=None, stream=None):
     """Gives up the listed rows of the table: counts fall, the rows become -1, their lengths 0."""
-    _lens(kv_len, "kv_len", table.shape[0])
-    _check(lib().bitnet_kv_free(_book(refs, "refs", 1), refs.shape[0], _book(table, "table", 2), table.shape[0], table.shape[1],
-                                _book(kv_len, "kv_len", 1), _book(rows, "rows", 1), rows.shape[0], _opt(dev_status, "dev_status"),
-                                _st(stream)), "bitnet_kv_free")
+    seqs, width = table.shape
+    _check(lib().bitnet_kv_free(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
+                                _book(kv_len, "kv_len", 1, seqs), _book(rows, "rows", 1), rows.size(0), _opt(dev_status, "dev_status"),
+                                _st(stream, table.device)), "bitnet_kv_free")
 
 
 def bitnet_kv_trim(refs, table, kv_len, page_size, window, sinks=0, stream=None):
     """Gives up the pages that attention with this window and these sinks no longer reads."""
-    _lens(kv_len, "kv_len", table.shape[0])
-    _check(lib().bitnet_kv_trim(_book(refs, "refs", 1), refs.shape[0], _book(table, "table", 2), table.shape[0], table.shape[1],
-                                _book(kv_len, "kv_len", 1), page_size, window, sinks, _st(stream)), "bitnet_kv_trim")
+    seqs, width = table.shape
+    _check(lib().bitnet_kv_trim(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
+                                _book(kv_len, "kv_len", 1, seqs), page_size, window, sinks, _st(stream, table.device)), "bitnet_kv_trim")
 
 
 def bitnet_kv_compact(cache, refs, table, live=None, workspace=None, stream=None):
     """Moves the pages in use to the pool's first places; live (int32 [1], optional) receives their number."""
-    if refs.shape[0] != cache.num_pages:
+    if refs.size(0) != cache.num_pages:
         raise BitnetError("bitnet_kv_compact: refs must have one entry per page")
     if workspace is None:
         workspace = new_kv_workspace(cache.num_pages, 0, cache.device)
-    _check(lib().bitnet_kv_compact(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), table.shape[0], table.shape[1],
-                                   _opt(live, "live"), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _st(stream)),
-           "bitnet_kv_compact")
+    seqs, width = table.shape
+    _check(lib().bitnet_kv_compact(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), seqs, width, _opt(live, "live"),
+                                   workspace.data_ptr(), workspace.nbytes, _st(stream, cache.device)), "bitnet_kv_compact")
 
 
 def bitnet_kv_copy_pages(cache, src, dst, dev_status=None, stream=None):
     """Copies pages src[i] to dst[i], K and V, all layers."""
     if src.shape != dst.shape:
         raise BitnetError("bitnet_kv_copy_pages: src and dst must have one length")
-    _check(lib().bitnet_kv_copy_pages(cache.ref, _book(src, "src", 1), _book(dst, "dst", 1), src.shape[0], _opt(dev_status, "dev_status"),
-                                      _st(stream)), "bitnet_kv_copy_pages")
+    _check(lib().bitnet_kv_copy_pages(cache.ref, _book(src, "src", 1), _book(dst, "dst", 1), src.size(0), _opt(dev_status, "dev_status"),
+                                      _st(stream, cache.device)), "bitnet_kv_copy_pages")
 
 
 def bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim) -> int:
@@ -651,28 +656,32 @@ def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
     return ws
 
 
-def _attn(name, cache, q, table, kv_len, seqs, out, workspace):
-    qp = _rows(q, "q", None, cache.head_dim)
+def _attn_out(name, q, out):
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif not (out.is_cuda and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()):
+        return torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if not (out.is_cuda and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()):
         raise BitnetError(f"{name}: out must be contiguous, with q's shape and type")
-    _lens(table, "table", seqs)
-    _lens(kv_len, "kv_len", seqs)
-    if workspace is None and q.shape[0] > 0 and q.shape[1] % cache.kv_heads == 0:
-        workspace = new_attn_workspace(q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, q.device)
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    return qp, out, ws, size
+    return out
+
+
+def _attn_ws(workspace, cache, n, heads):
+    if workspace is None:
+        if n == 0 or heads % cache.kv_heads:
+            return None, 0, None
+        workspace = new_attn_workspace(n, heads, cache.kv_heads, cache.head_dim, cache.device)
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def bitnet_attn_decode(cache, layer, q, table, kv_len, scale=None, window=0, sinks=0, out=None, workspace=None, dev_status=None,
                        stream=None):
     """Attention of one new token per sequence: q [seqs][q_heads][head_dim] (fp32 or the cache's type) -> out, same shape and type."""
-    qp, out, ws, size = _attn("bitnet_attn_decode", cache, q, table, kv_len, q.shape[0], out, workspace)
-    _check(lib().bitnet_attn_decode(cache.ref, layer, qp, KV_DTYPE[q.dtype], q.shape[1], q.stride(0), q.stride(1),
-                                    _book(table, "table", 2), table.shape[1], _book(kv_len, "kv_len", 1), q.shape[0],
-                                    cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
-                                    _opt(dev_status, "dev_status"), _st(stream)), "bitnet_attn_decode")
+    n, heads, sn, sh, code = _rows(q, "q", None, cache.head_dim)
+    out = _attn_out("bitnet_attn_decode", q, out)
+    ws, size, _keep = _attn_ws(workspace, cache, n, heads)
+    _check(lib().bitnet_attn_decode(cache.ref, layer, q.data_ptr(), code, heads, sn, sh, _book(table, "table", 2, n), table.size(1),
+                                    _book(kv_len, "kv_len", 1, n), n, cache.head_dim ** -0.5 if scale is None else scale, window, sinks,
+                                    out.data_ptr(), ws, size, _opt(dev_status, "dev_status"), _st(stream, cache.device)),
+           "bitnet_attn_decode")
     return out
 
 
@@ -680,10 +689,12 @@ def bitnet_attn_prompt(cache, layer, q, table, kv_len, q_start, max_new, scale=N
                        dev_status=None, stream=None):
     """Attention of prompts or chunks of prompts: q [tokens][q_heads][head_dim] in the cache's type; sequence s has the tokens
     q_start[s] .. q_start[s + 1] - 1 (at most max_new), the last of them at position kv_len[s] - 1."""
-    seqs = q_start.shape[0] - 1
-    qp, out, ws, size = _attn("bitnet_attn_prompt", cache, q, table, kv_len, seqs, out, workspace)
-    _check(lib().bitnet_attn_prompt(cache.ref, layer, qp, KV_DTYPE[q.dtype], q.shape[1], q.stride(0), q.stride(1), q.shape[0],
-                                    _book(table, "table", 2), table.shape[1], _book(kv_len, "kv_len", 1), _book(q_start, "q_start", 1), seqs,
-                                    max_new, cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
-                                    _opt(dev_status, "dev_status"), _st(stream)), "bitnet_attn_prompt")
+    n, heads, sn, sh, code = _rows(q, "q", None, cache.head_dim)
+    seqs = q_start.size(0) - 1
+    out = _attn_out("bitnet_attn_prompt", q, out)
+    ws, size, _keep = _attn_ws(workspace, cache, n, heads)
+    _check(lib().bitnet_attn_prompt(cache.ref, layer, q.data_ptr(), code, heads, sn, sh, n, _book(table, "table", 2, seqs), table.size(1),
+                                    _book(kv_len, "kv_len", 1, seqs), _book(q_start, "q_start", 1), seqs, max_new,
+                                    cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
+                                    _opt(dev_status, "dev_status"), _st(stream, cache.device)), "bitnet_attn_prompt")
     return out

@@ -614,8 +614,9 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d
   auto kernel = attn_decode_kernel<KT, F32, DT>;
   constexpr size_t smem = Layout<DT>::SMEM;
   static_assert(smem <= 232448, "shared memory of one CTA");
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return note_cuda_error(e);
+  static std::atomic<uint64_t> have{0};                  // devices on which the kernel may take that much shared memory
+  int rc = allow_smem(kernel, (int)smem, &have);
+  if (rc) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
@@ -626,7 +627,7 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = early_start_enabled(st) ? 1 : 0;
-  e = cudaLaunchKernelEx(&cfg, kernel, km, vm, d);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, km, vm, d);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
 template <typename KT, bool F32>

@@ -697,8 +697,9 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const PromptArgs& a
   auto kernel = attn_prompt_kernel<KT, HALVES>;
   constexpr size_t smem = Layout<HALVES>::TAIL + sizeof(Tail) + 1024;
   static_assert(smem <= 232448, "shared memory of one CTA");
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return note_cuda_error(e);
+  static std::atomic<uint64_t> have{0};                  // devices on which the kernel may take that much shared memory
+  int rc = allow_smem(kernel, (int)smem, &have);
+  if (rc) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
@@ -709,7 +710,7 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const PromptArgs& a
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = early_start_enabled(st) ? 1 : 0;
-  e = cudaLaunchKernelEx(&cfg, kernel, km, vm, a);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, km, vm, a);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
 

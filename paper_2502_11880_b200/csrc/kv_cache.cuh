@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "device_utils.cuh"
 
@@ -72,6 +74,19 @@ int launch_kv_compact(const KvView& kv, int32_t* refs, int32_t* table, int64_t s
                       cudaStream_t st);
 int launch_kv_copy_pages(const KvView& kv, const int32_t* src, const int32_t* dst, int64_t n, int* dev_status, cudaStream_t st);
 size_t kv_workspace_bytes(int64_t num_pages, int64_t n);
+
+// Raises a kernel's limit of dynamic shared memory, once per device (`have`: one bit for each; a device beyond 63 every time).
+template <typename K>
+int allow_smem(K kernel, int bytes, std::atomic<uint64_t>* have) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return note_cuda_error(cudaGetLastError());
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (have->load(std::memory_order_acquire) & bit) return BITNET_OK;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return note_cuda_error(e);
+  have->fetch_or(bit, std::memory_order_release);
+  return BITNET_OK;
+}
 
 #ifdef __CUDACC__
 // ---- device side
