@@ -434,7 +434,8 @@ typedef struct bitnet_kv_cache {
   int64_t stride_layer, stride_page, stride_head, stride_row;   /* elements, multiples of 8; of both pools         */
   /* filled in by bitnet_kv_cache_init */
   uint64_t ready;
-  uint64_t maps[2][16];          /* how the tensor copies address the pools                                      */
+  uint64_t maps[4][16];          /* how the tensor copies address the pools                                      */
+  int64_t layer_pages;           /* > 0: a layer further is so many pages further (the third and fourth map)     */
 } bitnet_kv_cache_t;
 
 /* Checks the description and completes it (host only; nothing is launched).  The handle stays valid while the pools stay

@@ -499,7 +499,7 @@ class KvCacheDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32),
                 ("layers", C.c_int64), ("num_pages", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("stride_layer", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_row", C.c_int64),
-                ("ready", C.c_uint64), ("maps", C.c_uint64 * 32)]
+                ("ready", C.c_uint64), ("maps", C.c_uint64 * 64), ("layer_pages", C.c_int64)]
 
 
 class KvCache:

@@ -8,8 +8,9 @@
 //   * the visible tokens of a row (a token and a kv head) are cut into tiles of 64; all rows' tiles together form one
 //     list that is dealt to the CTAs (one per SM) in equal contiguous parts, whatever the lengths are.  The list exists only on the
 //     device: every CTA derives its part from the lengths.
-//   * warp 8 brings tiles in by tensor copies (one per page, 64-column half and pool) into a ring of stages, 192 KB in flight;
-//     pages or halves of rows outside the visible range are not read.
+//   * warp 8 brings tiles in by tensor copies (one per page and pool, and per 64-column half where head_dim is not 128: with
+//     pages of 16 tokens twice as many copies took 261 instead of 221 us for the batch below) into a ring of stages,
+//     192 KB in flight; pages outside the visible range are not read.
 //   * warps 0-3 and 4-7 take the tiles in turns, 16 tokens a warp: S = Q K^T and O += P V on mma.sync m16n8k16 with the
 //     heads as the 16 rows.  At most 8 heads fill rows 0..7; rows 8..15 hold what rounding took from rows 0..7 (below).
 //   * every warp keeps its own running maximum and sum; the 8 warps' states meet in shared memory when a row ends, the parts of a
@@ -48,7 +49,7 @@ struct DecodeArgs {
   int q_heads, kv_heads, group, head_blocks;  // group = query heads per kv head, in blocks of up to 8
   int head_dim, page_shift, num_pages, layer;
   int window, sinks, max_len;                 // max_len = table_width * page_size
-  int min_tiles;                              // fewest tiles of a CTA's part
+  int layer_pages;                            // > 0: the maps take both 64-column halves of a row in one box
   float c;                                    // scale * log2(e)
   int* counters;                              // [tokens * kv_heads * head_blocks], zero between calls
   float2* part_ml;                            // [2 * grid][8] running maximum and sum of a part
@@ -154,11 +155,14 @@ struct Layout {
   struct Tail {
     float o[4][HEADS][O_STRIDE];
     float m[4][HEADS], l[4][HEADS];
+    uint2 q3[DT][32];                                     // third pieces of an fp32 query, as a lane's operand words
     uint64_t full_k[STAGES], full_v[STAGES], empty[STAGES];
     int64_t scan[CONSUMER_WARPS + 2];
     int64_t first_base;                                   // tiles before the token that the CTA's part begins in
+    int64_t begin, end;
+    int most[CONSUMER_WARPS + 2];
     int first_token;
-    int last_part;
+    int last_part[2];
     int abort_flag;
   };
   static constexpr size_t SMEM = (size_t)STAGES * 2 * TILE_BYTES + sizeof(Tail) + 1024;
@@ -196,19 +200,25 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   // ---- the list of tiles: total, this CTA's part [item, end), and the token it begins in
   const int rows_per_token = a.kv_heads * a.head_blocks;
   int64_t total = 0;
+  int longest = 0;                                         // tiles of the longest row
   int64_t my_excl = 0;                                     // of the last chunk of tokens looked at
-  int my_tiles = 0;
+  int my_tiles = 0, my_row = 0;
   auto scan_chunk = [&](int n0, int64_t base) {            // tiles before token n0 + tid; returns the chunk's total
     const int n = n0 + tid;
-    my_tiles = n < a.tokens ? range_of(a, n).tiles * rows_per_token : 0;
+    my_row = n < a.tokens ? range_of(a, n).tiles : 0;
+    my_tiles = my_row * rows_per_token;
     int64_t x = my_tiles;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
       if (lane >= d) x += y;
     }
+    const int most = __reduce_max_sync(0xffffffffu, my_row);
     __syncthreads();
-    if (lane == 31) s.scan[warp] = x;
+    if (lane == 31) {
+      s.scan[warp] = x;
+      s.most[warp] = most;
+    }
     __syncthreads();
     int64_t before = 0, sum = 0;
 #pragma unroll
@@ -216,31 +226,47 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int64_t v = s.scan[w];
       if (w < warp) before += v;
       sum += v;
+      longest = max(longest, s.most[w]);
     }
     my_excl = base + before + x - my_tiles;
     return sum;
   };
   for (int n0 = 0; n0 < a.tokens; n0 += THREADS) total += scan_chunk(n0, total);
-  const int64_t want = total / a.min_tiles;
-  const int64_t parts = want < 1 ? 1 : (want < (int64_t)gridDim.x ? want : (int64_t)gridDim.x);
+  // How the list is cut:
+  //   short rows: at the rows' first tiles, so that no row has parts to be joined.  A join costs about 4 us, a tile 0.6 us
+  //     (one sequence, 8 kv heads, 5 tiles a row: 9.8 us whole, 10.4 in parts; 9 tiles: 12.4 and 11.0; 64 ragged sequences of up to
+  //     8 tiles, where every CTA has several rows: 39.4 and 45.3);
+  //   few rows, all alike: as many parts of a row as fit the CTAs, so that none holds parts of two rows (4096 tokens, 8 kv
+  //     heads: 18.5 -> 14.9 us);
+  //   otherwise into equal parts.
+  const int64_t rows = (int64_t)a.tokens * rows_per_token;
+  const bool whole = longest <= 6 || (longest <= 10 && 2 * longest * (int64_t)gridDim.x <= total);
+  int64_t parts = min((int64_t)gridDim.x, total);
+  if (whole) parts = min((int64_t)gridDim.x, rows);
+  else if (rows <= gridDim.x && total == rows * longest) parts = rows * min((int64_t)gridDim.x / rows, (int64_t)longest);
   if (blockIdx.x >= parts) return;
-  const int64_t begin = total * blockIdx.x / parts, end = total * (blockIdx.x + 1) / parts;
-  if (a.tokens <= THREADS) {
-    if (begin >= my_excl && begin < my_excl + my_tiles) {
-      s.first_token = tid;
+  const int64_t cut0 = total * blockIdx.x / parts, cut1 = total * (blockIdx.x + 1) / parts;
+  auto find_cuts = [&](int n0) {
+    const int64_t mine = my_excl + my_tiles;
+    if (cut0 >= my_excl && cut0 < mine) {
+      s.first_token = n0 + tid;
       s.first_base = my_excl;
+      s.begin = whole ? my_excl + (cut0 - my_excl) / my_row * my_row : cut0;
     }
+    if (cut1 == total && tid == 0) s.end = total;
+    if (cut1 >= my_excl && cut1 < mine) s.end = whole ? my_excl + (cut1 - my_excl) / my_row * my_row : cut1;
+  };
+  if (a.tokens <= THREADS) {
+    find_cuts(0);
   } else {
     int64_t base = 0;
-    for (int n0 = 0; n0 < a.tokens && base <= begin; n0 += THREADS) {
+    for (int n0 = 0; n0 < a.tokens && base <= cut1; n0 += THREADS) {
       base += scan_chunk(n0, base);
-      if (begin >= my_excl && begin < my_excl + my_tiles) {
-        s.first_token = n0 + tid;
-        s.first_base = my_excl;
-      }
+      find_cuts(n0);
     }
   }
   __syncthreads();
+  const int64_t begin = s.begin, end = s.end;
 
   int n = s.first_token;
   int64_t base = s.first_base;                             // tiles before token n
@@ -252,49 +278,66 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // ------------------------------------------------------------ producer: lane = box of the tile
     const int box_rows = min(1 << a.page_shift, TILE);
     const int boxes = TILE / box_rows;
-    const int pool = lane / (boxes * L::HALVES);           // 0 = K, 1 = V
-    const int half = lane / boxes % L::HALVES;
+    const bool both = L::HALVES == 2 && a.layer_pages > 0; // a box has both halves
+    const int per_pool = both ? boxes : boxes * L::HALVES;
+    const int pool = lane / per_pool;                      // 0 = K, 1 = V
+    const int half = both ? 0 : lane / boxes % L::HALVES;
     const int box = lane % boxes;
     const bool mine = pool < 2;
-    const uint32_t box_bytes = (uint32_t)box_rows * 128;
+    const uint32_t box_bytes = (uint32_t)box_rows * (both ? 256 : 128);
     while (item < end) {
       const int64_t off = item - base;
       const int row = (int)(off / r.tiles);
       const int t0 = (int)(off - (int64_t)row * r.tiles);
       const int t_end = (int)min((int64_t)r.tiles, end - base - (int64_t)row * r.tiles);
       const int head = row / a.head_blocks;
-      // the page of a tile's box, looked up one tile ahead
-      auto look_up = [&](int t, int& y) -> int {
+      // the page of a tile's box; -2: nothing visible, not read
+      auto look_up = [&](int t) -> int {
         int first, lo, hi;
         tile_of(r, t, first, lo, hi);
         const int tok = first + box * box_rows;
-        y = tok & ((1 << a.page_shift) - 1);
-        if (!mine || tok >= hi || tok + box_rows <= lo) return -2;   // nothing visible: not read
+        if (t >= t_end || !mine || tok >= hi || tok + box_rows <= lo) return -2;
         return __ldg(a.table + (int64_t)r.seq * a.table_width + (tok >> a.page_shift));
       };
-      int y = 0, page = look_up(t0, y);
-      for (int t = t0; t < t_end; ++t, ++it) {
-        const int cur = page, cur_y = y;
-        if (t + 1 < t_end) page = look_up(t + 1, y);
-        const int st = it % L::STAGES;
-        kv_mbar_wait(&s.empty[st], ((it / L::STAGES) & 1u) ^ 1u, abort_flag, &g_attn_error);
-        if (*abort_flag) continue;
-        const bool issue = cur != -2;
-        const unsigned mask = __ballot_sync(0xffffffffu, issue);
-        const bool bad = issue && (cur < 0 || cur >= a.num_pages);
-        if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-        if (lane == 0) {
-          const int half_lanes = boxes * L::HALVES;
-          const unsigned k_mask = half_lanes >= 32 ? 0xffffffffu : (1u << half_lanes) - 1u;
-          kv_mbar_expect(&s.full_k[st], __popc(mask & k_mask) * box_bytes);
-          kv_mbar_expect(&s.full_v[st], __popc(mask & ~k_mask) * box_bytes);
+      // (four tiles' pages are looked up while the four before are copied: one at a time the look-up's latency, 0.7 us, was
+      // every tile's time)
+      int page[4], next[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) page[k] = look_up(t0 + k);
+      for (int tb = t0; tb < t_end; tb += 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) next[k] = look_up(tb + 4 + k);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int t = tb + k, cur = page[k];
+          if (t >= t_end) break;
+          const int st = it % L::STAGES;
+          kv_mbar_wait(&s.empty[st], ((it / L::STAGES) & 1u) ^ 1u, abort_flag, &g_attn_error);
+          ++it;
+          if (*abort_flag) continue;
+          const bool issue = cur != -2;
+          const unsigned mask = __ballot_sync(0xffffffffu, issue);
+          const bool bad = issue && (cur < 0 || cur >= a.num_pages);
+          if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+          if (lane == 0) {
+            const unsigned k_mask = (1u << per_pool) - 1u;     // (at most 16 boxes of a pool)
+            kv_mbar_expect(&s.full_k[st], __popc(mask & k_mask) * box_bytes);
+            kv_mbar_expect(&s.full_v[st], __popc(mask & ~k_mask) * box_bytes);
+          }
+          __syncwarp();
+          if (issue) {
+            int first, lo, hi;
+            tile_of(r, t, first, lo, hi);
+            const int y = (first + box * box_rows) & ((1 << a.page_shift) - 1);
+            // a tile lies in shared memory as [box][half][row][64 columns]
+            uint8_t* dst = smem + (st * 2 + pool) * L::TILE_BYTES + box * box_rows * (128 * L::HALVES) + half * box_rows * 128;
+            uint64_t* full = pool ? &s.full_v[st] : &s.full_k[st];
+            if (both) kv_box_copy2(smem_u32(dst), pool ? &vmap : &kmap, y, head, bad ? -1 : cur + a.layer * a.layer_pages, full);
+            else kv_box_copy(smem_u32(dst), pool ? &vmap : &kmap, half * 64, y, head, bad ? -1 : cur, a.layer, full);
+          }
         }
-        __syncwarp();
-        if (issue) {
-          uint8_t* dst = smem + (st * 2 + pool) * L::TILE_BYTES + half * HALF_BYTES + box * box_bytes;
-          kv_box_copy(smem_u32(dst), pool ? &vmap : &kmap, half * 64, cur_y, head, bad ? -1 : cur, a.layer,
-                      pool ? &s.full_v[st] : &s.full_k[st]);
-        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) page[k] = next[k];
       }
       item += t_end - t0;
       if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
@@ -318,7 +361,25 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   // lane's row and 16-byte piece in the ldmatrix of K (token = lane % 8 + 8 * (lane / 16), piece 2i + lane / 8 % 2) and of V
   const int k_row = tok_w + (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;
   const int v_row = tok_w + (lane & 15), v_piece = lane >> 4;
+  const int box_shift = min(a.page_shift, 6), half_bytes = 128 << box_shift;
+  const uint32_t k_off = (uint32_t)((k_row >> box_shift) * half_bytes * L::HALVES + (k_row & ((1 << box_shift) - 1)) * 128);
+  const uint32_t v_off = (uint32_t)((v_row >> box_shift) * half_bytes * L::HALVES + (v_row & ((1 << box_shift) - 1)) * 128);
   bool first_segment = true;
+  struct Pending {                                         // a row of which this CTA has a part: its first, its last
+    int n, head0, heads, c0, c1, first_slot;
+  } pending[2];
+  pending[0].n = pending[1].n = -1;
+  auto write_row = [&](int tok, int h0, int heads, int hh, int d0, const float4& acc, float sum) {
+    if (hh >= heads || d0 >= a.head_dim) return;
+    const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);   // nothing visible: 0; NaN stays NaN
+    const int64_t at = ((int64_t)tok * a.q_heads + h0 + hh) * a.head_dim + d0;
+    if (F32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+      *reinterpret_cast<uint2*>(static_cast<KT*>(a.out) + at) =
+          make_uint2(P2::pack(acc.x * inv, acc.y * inv), P2::pack(acc.z * inv, acc.w * inv));
+    }
+  };
 
   while (item < end) {
     const int64_t off = item - base;
@@ -330,7 +391,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int head0 = head_kv * a.group + block * HEADS;
 
     // ---- the row's queries as operand A: rows 0..7 the values, rows 8..15 the remainders (and a third piece)
-    uint32_t qa[DT][4], qb[THREE ? DT : 1][2];
+    uint32_t qa[DT][4];
     float c = a.c;
     {
       const bool have = g < heads;
@@ -369,11 +430,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             const uint32_t m = P2::pack(rx, ry);
             qa[i][2 * j] = h;
             qa[i][2 * j + 1] = m;
-            if (THREE) {
+            if (THREE && i % CONSUMER_WARPS == warp) {        // (every warp holds the same)
               const float2 mf = P2::unpack(m);
-              qb[THREE ? i : 0][j] = P2::pack(rx - mf.x, ry - mf.y);
+              reinterpret_cast<uint32_t*>(&s.q3[i][lane])[j] = P2::pack(rx - mf.x, ry - mf.y);
             }
           }
+        if (THREE) group_barrier(1, CONSUMER_WARPS * 32);
       } else {
         const uint8_t* qp = static_cast<const uint8_t*>(a.q) + q_at * 2;
 #pragma unroll
@@ -401,24 +463,36 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const uint32_t kbase = smem_u32(smem + st * 2 * L::TILE_BYTES), vbase = kbase + L::TILE_BYTES;
       kv_mbar_wait(&s.full_k[st], par, abort_flag, &g_attn_error);
 
-      float sc[2][4] = {};
+      // (operands four steps at a time, so that their latencies overlap; two chains of sums for each 8 tokens)
+      float sc[2][2][4] = {};
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        uint32_t b[4];
-        ldsm4(kbase + (i >> 2) * HALF_BYTES + k_row * 128 + ((((2 * i & 7) + k_piece) ^ (k_row & 7)) << 4), b);
-        P2::mma(sc[0], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[0], b[1]);
-        P2::mma(sc[1], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[2], b[3]);
-        if (THREE) {
-          P2::mma(sc[0], qb[THREE ? i : 0][0], 0u, qb[THREE ? i : 0][1], 0u, b[0], b[1]);
-          P2::mma(sc[1], qb[THREE ? i : 0][0], 0u, qb[THREE ? i : 0][1], 0u, b[2], b[3]);
+      for (int i0 = 0; i0 < DT; i0 += 4) {
+        uint32_t b[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i0 + k < DT) ldsm4(kbase + k_off + (i0 >> 2) * half_bytes + (((2 * k + k_piece) ^ (k_row & 7)) << 4), b[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + k;
+          if (i < DT) {
+            P2::mma(sc[k & 1][0], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[k][0], b[k][1]);
+            P2::mma(sc[k & 1][1], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[k][2], b[k][3]);
+            if (THREE) {
+              const uint2 q3 = s.q3[i][lane];
+              P2::mma(sc[k & 1 ^ 1][0], q3.x, 0u, q3.y, 0u, b[k][0], b[k][1]);
+              P2::mma(sc[k & 1 ^ 1][1], q3.x, 0u, q3.y, 0u, b[k][2], b[k][3]);
+            }
+          }
         }
       }
       float x[4];                                           // scores of head g at tokens 2t, 2t+1, 2t+8, 2t+9 of the 16
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        x[2 * j] = (F32 ? sc[j][0] + sc[j][2] : sc[j][0]) * c;
-        x[2 * j + 1] = (F32 ? sc[j][1] + sc[j][3] : sc[j][1]) * c;
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float hi = sc[0][j][e] + sc[1][j][e];
+          x[2 * j + e] = (F32 ? hi + (sc[0][j][2 + e] + sc[1][j][2 + e]) : hi) * c;
+        }
       const bool edge = first + tok_w < lo || first + tok_w + 16 > hi;   // some of the 16 tokens are not visible
       uint32_t vmask0 = 0xffffffffu, vmask1 = 0xffffffffu;
       if (edge) {
@@ -468,20 +542,28 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       }
       kv_mbar_wait(&s.full_v[st], par, abort_flag, &g_attn_error);
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        uint32_t b[4];
-        ldsm4_t(vbase + (i >> 2) * HALF_BYTES + v_row * 128 + ((((2 * i & 7) + v_piece) ^ (v_row & 7)) << 4), b);
-        if (edge) {
-          b[0] &= vmask0;
-          b[1] &= vmask1;
-          b[2] &= vmask0;
-          b[3] &= vmask1;
-        }
-        P2::mma(o[2 * i], ph[0], pm[0], ph[1], pm[1], b[0], b[1]);
-        P2::mma(o[2 * i + 1], ph[0], pm[0], ph[1], pm[1], b[2], b[3]);
-        if (THREE) {
-          P2::mma(o[2 * i], pl[0], 0u, pl[1], 0u, b[0], b[1]);
-          P2::mma(o[2 * i + 1], pl[0], 0u, pl[1], 0u, b[2], b[3]);
+      for (int i0 = 0; i0 < DT; i0 += 4) {
+        uint32_t b[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i0 + k < DT) ldsm4_t(vbase + v_off + (i0 >> 2) * half_bytes + (((2 * k + v_piece) ^ (v_row & 7)) << 4), b[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + k;
+          if (i < DT) {
+            if (edge) {
+              b[k][0] &= vmask0;
+              b[k][1] &= vmask1;
+              b[k][2] &= vmask0;
+              b[k][3] &= vmask1;
+            }
+            P2::mma(o[2 * i], ph[0], pm[0], ph[1], pm[1], b[k][0], b[k][1]);
+            P2::mma(o[2 * i + 1], ph[0], pm[0], ph[1], pm[1], b[k][2], b[k][3]);
+            if (THREE) {
+              P2::mma(o[2 * i], pl[0], 0u, pl[1], 0u, b[k][0], b[k][1]);
+              P2::mma(o[2 * i + 1], pl[0], 0u, pl[1], 0u, b[k][2], b[k][3]);
+            }
+          }
         }
       }
       __syncwarp();
@@ -540,59 +622,30 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       }
     }
 
-    bool write = true;
-    if (t_end - t0 < r.tiles) {
-      // ---- the row lies on several CTAs: leave this part; the last to arrive joins them, in their order
-      const int64_t row_begin = base + (int64_t)row * r.tiles, row_last = row_begin + r.tiles - 1;
-      const int c0 = (int)(((row_begin + 1) * parts - 1) / total), c1 = (int)(((row_last + 1) * parts - 1) / total);
+    if (t_end - t0 == r.tiles) {
+      write_row(n, head0, heads, hh, d0, acc, sum);
+    } else {
+      // ---- the row lies on several CTAs: this part goes to the workspace; the last to arrive joins them, at its end
       const int slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
       if (d0 < L::D) *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * HEADS + hh) * L::D + d0) = acc;
       if (lane == 0) a.part_ml[slot * HEADS + hh] = make_float2(big, sum);
-      __threadfence();
+      Pending& p = pending[first_segment ? 0 : 1];
+      const int64_t row_begin = base + (int64_t)row * r.tiles, row_last = row_begin + r.tiles - 1;
+      p.n = n;
+      p.head0 = head0;
+      p.heads = heads;
+      p.c0 = (int)(((row_begin + 1) * parts - 1) / total);
+      p.c1 = (int)(((row_last + 1) * parts - 1) / total);
+      // parts of CTAs after c0 are those CTAs' first; c0's is its first too if it begins with this row
+      p.first_slot = 2 * p.c0 + (total * p.c0 / parts < row_begin ? 1 : 0);
       group_barrier(1, CONSUMER_WARPS * 32);
-      int* counter = a.counters + (int64_t)n * rows_per_token + row;
       if (tid == 0) {
+        int* counter = a.counters + (int64_t)n * rows_per_token + row;
+        __threadfence();                                    // (of all that the barrier ordered before)
         const int done = atomicAdd(counter, 1);
-        s.last_part = done == c1 - c0;
-        if (done == c1 - c0) *counter = 0;                  // the workspace is left as it was
+        s.last_part[first_segment ? 0 : 1] = done == p.c1 - p.c0;
+        if (done == p.c1 - p.c0) *counter = 0;              // the workspace is left as it was
         __threadfence();
-      }
-      group_barrier(1, CONSUMER_WARPS * 32);
-      write = s.last_part != 0;
-      if (write) {
-        // parts of CTAs after c0 are those CTAs' first; c0's is its first too if it begins with this row
-        const int first_slot = 2 * c0 + (total * c0 / parts < row_begin ? 1 : 0);
-        big = -INFINITY;
-        for (int cta = c0 + lane; cta <= c1; cta += 32)
-          big = fmaxf(big, __ldcg(&a.part_ml[(cta == c0 ? first_slot : 2 * cta) * HEADS + hh]).x);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
-        acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        sum = 0.0f;
-#pragma unroll 4
-        for (int cta = c0; cta <= c1; ++cta) {
-          const int sl = cta == c0 ? first_slot : 2 * cta;
-          const float2 ml = __ldcg(&a.part_ml[sl * HEADS + hh]);
-          const float f = ml.x == -INFINITY ? 0.0f : exp2_approx(ml.x - big);
-          sum += f * ml.y;
-          if (d0 < L::D) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)sl * HEADS + hh) * L::D + d0));
-            acc.x += f * v.x;
-            acc.y += f * v.y;
-            acc.z += f * v.z;
-            acc.w += f * v.w;
-          }
-        }
-      }
-    }
-    if (write && hh < heads && d0 < a.head_dim) {
-      const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);   // nothing visible: 0; NaN stays NaN
-      const int64_t at = ((int64_t)n * a.q_heads + head0 + hh) * a.head_dim + d0;
-      if (F32) {
-        *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      } else {
-        *reinterpret_cast<uint2*>(static_cast<KT*>(a.out) + at) =
-            make_uint2(P2::pack(acc.x * inv, acc.y * inv), P2::pack(acc.z * inv, acc.w * inv));
       }
     }
     first_segment = false;
@@ -601,6 +654,36 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       base += (int64_t)r.tiles * rows_per_token;
       r = range_of(a, ++n);
     }
+  }
+
+  // ---- joins, in the order of the parts whoever does it
+  group_barrier(1, CONSUMER_WARPS * 32);
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const Pending p = pending[k];
+    if (p.n < 0 || !s.last_part[k]) continue;
+    const int hh = warp, d0 = lane * 4;
+    float big = -INFINITY, sum = 0.0f;
+    for (int cta = p.c0 + lane; cta <= p.c1; cta += 32)
+      big = fmaxf(big, __ldcg(&a.part_ml[(cta == p.c0 ? p.first_slot : 2 * cta) * HEADS + hh]).x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int cta = p.c0; cta <= p.c1; ++cta) {
+      const int sl = cta == p.c0 ? p.first_slot : 2 * cta;
+      const float2 ml = __ldcg(&a.part_ml[sl * HEADS + hh]);
+      const float f = ml.x == -INFINITY ? 0.0f : exp2_approx(ml.x - big);
+      sum += f * ml.y;
+      if (d0 < L::D) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)sl * HEADS + hh) * L::D + d0));
+        acc.x += f * v.x;
+        acc.y += f * v.y;
+        acc.z += f * v.z;
+        acc.w += f * v.w;
+      }
+    }
+    write_row(p.n, p.head0, p.heads, hh, d0, acc, sum);
   }
 }
 
@@ -654,9 +737,11 @@ size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, in
 
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
   CUtensorMap km, vm;
-  memcpy(&km, c->maps[0], sizeof km);
-  memcpy(&vm, c->maps[1], sizeof vm);
+  const int first = c->layer_pages > 0 ? 2 : 0;
+  memcpy(&km, c->maps[first], sizeof km);
+  memcpy(&vm, c->maps[first + 1], sizeof vm);
   DecodeArgs d;
+  d.layer_pages = (int)c->layer_pages;
   d.q = x.q;
   d.out = x.out;
   d.q_stride_token = x.q_stride_token;
@@ -679,7 +764,6 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   d.sinks = x.sinks;
   const int64_t most = x.table_width * c->page_size;
   d.max_len = most > 0x7fffff00 ? 0x7fffff00 : (int)most;
-  d.min_tiles = 1;
   d.c = x.scale * 1.4426950408889634f;
   const int grid = dev_info().sm_count;
   const size_t slots = 2 * (size_t)grid * HEADS;

@@ -80,7 +80,7 @@ int bitnet_kv_cache_init(bitnet_kv_cache_t* c) {
   for (int64_t s : strides)
     if (s < 0 || s % 8 || s >= (int64_t)1 << 38) return BITNET_ERR_INVALID_ARG;
   if (c->stride_row < c->head_dim) return BITNET_ERR_INVALID_ARG;
-  const int rc = encode_kv_maps(c->maps[0], c->maps[1], kv_view(c), c->dtype);
+  const int rc = encode_kv_maps(c->maps, &c->layer_pages, kv_view(c), c->dtype);
   if (rc == BITNET_OK) c->ready = READY;
   return rc;
 }

@@ -22,8 +22,10 @@ struct KvView {
 
 // Rows of one box of a tensor copy: a page, or 64 rows of a larger one.
 inline int kv_box_rows(int page_size) { return page_size < 64 ? page_size : 64; }
-// Tensor maps of both pools (64 columns x kv_box_rows rows per box, 128-byte swizzle), into two CUtensorMap.
-int encode_kv_maps(void* kmap, void* vmap, const KvView& v, int dtype);
+// Tensor maps of both pools.  maps[0], maps[1]: boxes of 64 columns x kv_box_rows rows, 128-byte swizzle; coordinates
+// (column, row, head, page, layer).  maps[2], maps[3], where head_dim is 128 and a layer is a whole number of pages away: boxes of
+// both 64-column halves, [half][row][64]; coordinates (column in the half, row, half, head, page + layer * *layer_pages).
+int encode_kv_maps(uint64_t (*maps)[16], int64_t* layer_pages, const KvView& v, int dtype);
 
 inline KvView kv_view(const bitnet_kv_cache_t* c) {
   KvView v;
@@ -149,6 +151,14 @@ __device__ __forceinline__ void kv_box_copy(uint32_t dst, const CUtensorMap* map
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
       "l"(map), "r"(x), "r"(row), "r"(head), "r"(page), "r"(layer), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// One box of both halves of rows of 128 columns.
+__device__ __forceinline__ void kv_box_copy2(uint32_t dst, const CUtensorMap* map, int row, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(smem_u32(bar))
       : "memory");
 }
 

@@ -31,25 +31,36 @@ EncodeTiledFn encode_fn() {
 }
 }  // namespace
 
-int encode_kv_maps(void* kmap, void* vmap, const KvView& v, int dtype) {
+int encode_kv_maps(uint64_t (*maps)[16], int64_t* layer_pages, const KvView& v, int dtype) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return note_cuda_error(cudaErrorNotSupported);
-  const cuuint64_t dim[5] = {(cuuint64_t)v.head_dim, (cuuint64_t)v.page_size, (cuuint64_t)v.kv_heads, (cuuint64_t)v.num_pages,
-                             (cuuint64_t)v.layers};
-  // the stride of a dimension of extent 1 is never used, but has to be one that the encoder takes
-  const cuuint64_t stride[4] = {(cuuint64_t)v.stride_row * 2, v.kv_heads > 1 ? (cuuint64_t)v.stride_head * 2 : 16,
-                                v.num_pages > 1 ? (cuuint64_t)v.stride_page * 2 : 16, v.layers > 1 ? (cuuint64_t)v.stride_layer * 2 : 16};
-  const cuuint32_t box[5] = {64, (cuuint32_t)kv_box_rows(v.page_size), 1, 1, 1};
-  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   const CUtensorMapDataType t = dtype == BITNET_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   void* const pool[2] = {v.k, v.v};
-  void* const out[2] = {kmap, vmap};
-  for (int i = 0; i < 2; ++i) {
+  // the stride of a dimension of extent 1 is never used, but has to be one that the encoder takes
+  auto bytes = [](int64_t extent, int64_t stride) { return extent > 1 ? (cuuint64_t)stride * 2 : (cuuint64_t)16; };
+  const cuuint32_t rows = (cuuint32_t)kv_box_rows(v.page_size), estr[5] = {1, 1, 1, 1, 1};
+  auto encode = [&](int i, const cuuint64_t* dim, const cuuint64_t* stride, const cuuint32_t* box) {
     CUtensorMap m;
-    if (enc(&m, t, 5, pool[i], dim, stride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    if (enc(&m, t, 5, pool[i & 1], dim, stride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return note_cuda_error(cudaErrorInvalidValue);
-    memcpy(out[i], &m, sizeof m);
+      return false;
+    memcpy(maps[i], &m, sizeof m);
+    return true;
+  };
+  const cuuint64_t dim[5] = {(cuuint64_t)v.head_dim, (cuuint64_t)v.page_size, (cuuint64_t)v.kv_heads, (cuuint64_t)v.num_pages,
+                             (cuuint64_t)v.layers};
+  const cuuint64_t stride[4] = {(cuuint64_t)v.stride_row * 2, bytes(v.kv_heads, v.stride_head), bytes(v.num_pages, v.stride_page),
+                                bytes(v.layers, v.stride_layer)};
+  const cuuint32_t box[5] = {64, rows, 1, 1, 1};
+  for (int i = 0; i < 2; ++i)
+    if (!encode(i, dim, stride, box)) return note_cuda_error(cudaErrorInvalidValue);
+  *layer_pages = 0;
+  const int64_t apart = v.layers == 1 ? v.num_pages : v.stride_page > 0 && v.stride_layer % v.stride_page == 0 ? v.stride_layer / v.stride_page : 0;
+  if (v.head_dim == 128 && apart >= v.num_pages && apart * v.layers < 0x7fffffff) {
+    const cuuint64_t dim2[5] = {64, (cuuint64_t)v.page_size, 2, (cuuint64_t)v.kv_heads, (cuuint64_t)(apart * (v.layers - 1) + v.num_pages)};
+    const cuuint64_t stride2[4] = {(cuuint64_t)v.stride_row * 2, 128, bytes(v.kv_heads, v.stride_head), bytes((int64_t)dim2[4], v.stride_page)};
+    const cuuint32_t box2[5] = {64, rows, 2, 1, 1};
+    if (encode(2, dim2, stride2, box2) && encode(3, dim2, stride2, box2)) *layer_pages = apart;
   }
   return BITNET_OK;
 }
