@@ -1,4 +1,5 @@
-"""Python binding of libbitnet_b200.so: same names as the C ABI, argument marshalling only.
+"""Python binding of libbitnet_b200.so: same names as the C ABI, argument marshalling only (ctypes; the calls of the key-value
+cache and the attention, which a decode step makes by the dozen, through a small compiled module).
 
 Every step of the path (quantiser, packers, mpGEMV / mpGEMM, rescale) runs in the library's CUDA
 kernels.  PyTorch supplies device memory and streams.  There is no CPU fallback: if the shared
@@ -521,6 +522,7 @@ class KvCache:
                                 stride_layer=k.stride(0), stride_page=k.stride(1), stride_head=k.stride(2), stride_row=k.stride(3))
         _check(lib().bitnet_kv_cache_init(C.byref(self.desc)), "bitnet_kv_cache_init")
         self.ref = C.addressof(self.desc)
+        self.scale = self.head_dim ** -0.5
 
 
 def new_kv_cache(layers, num_pages, kv_heads, page_size, head_dim, dtype=torch.bfloat16, device="cuda"):
@@ -530,58 +532,42 @@ def new_kv_cache(layers, num_pages, kv_heads, page_size, head_dim, dtype=torch.b
     return KvCache(k, v)
 
 
-_I32 = torch.int32
-_raw_stream = torch._C._cuda_getCurrentRawStream     # (a Stream object costs 3 us to make)
+_fast = None
 
 
-def _book(t, name, dim, rows=0):
-    """Address of an int32 array of the books with at least `rows` rows."""
-    if not (t.is_cuda and t.dtype is _I32 and t.dim() == dim and t.is_contiguous()):
-        raise BitnetError(f"{name}: expected a contiguous {dim}-D CUDA tensor of int32")
-    if rows and t.size(0) < rows:
-        raise BitnetError(f"{name}: expected {rows} entries")
-    return t.data_ptr()
+def _binding():
+    """The compiled part of the binding (csrc/binding.cpp), tied to the loaded library.  Raises if it has not been built."""
+    global _fast
+    if _fast is None:
+        import importlib.machinery
+        import importlib.util
+        path = os.path.join(_PKG, "_binding.so")
+        if not os.path.exists(path):
+            raise BitnetError(f"{path} is missing: run `python -m paper_2502_11880_b200.build` (there is no fallback path)")
+        loader = importlib.machinery.ExtensionFileLoader(__name__ + "._binding", path)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location(__name__ + "._binding", path, loader=loader))
+        loader.exec_module(m)
+        L = lib()
+        m.bind(BitnetError, _check, tuple(C.cast(f, C.c_void_p).value for f in (
+            L.bitnet_kv_append, L.bitnet_kv_reserve, L.bitnet_kv_fork, L.bitnet_kv_free, L.bitnet_kv_trim, L.bitnet_kv_compact,
+            L.bitnet_kv_copy_pages, L.bitnet_attn_decode, L.bitnet_attn_prompt)))
+        _fast = m
+    return _fast
 
 
-def _opt(t, name):
-    return None if t is None else _book(t, name, 1)
-
-
-def _st(stream, device):
-    return _raw_stream(device.index or 0) if stream is None else stream.cuda_stream
-
-
-def _rows(t, name, heads, dim):
-    """Shape, strides and type code of [tokens][heads][head_dim] rows."""
-    code = KV_DTYPE.get(t.dtype)
-    if t.dim() != 3 or not t.is_cuda or code is None:
-        raise BitnetError(f"{name}: expected a CUDA tensor [tokens][heads][head_dim] of fp32, bf16 or fp16")
-    n, h, d = t.shape
-    sn, sh, sd = t.stride()
-    if d != dim or (heads is not None and h != heads) or (sd != 1 and dim > 1):
-        raise BitnetError(f"{name}: expected [tokens][{'heads' if heads is None else heads}][{dim}] with the last dimension contiguous")
-    return n, h, sn, sh, code
+def _st(stream):
+    """None: the current stream of the tensors' device."""
+    return None if stream is None else stream.cuda_stream
 
 
 def bitnet_kv_append(cache, layer, k, v, table, kv_len, q_start=None, dev_status=None, stream=None):
     """Writes new tokens' rows k, v [tokens][kv_heads][head_dim] into their pages; kv_len [seqs] counts them already."""
-    rows = _rows(k, "k", cache.kv_heads, cache.head_dim)
-    if rows != _rows(v, "v", cache.kv_heads, cache.head_dim):
-        raise BitnetError("bitnet_kv_append: k and v must have one type, shape and strides")
-    n, _, sn, sh, code = rows
-    height, width = table.shape
-    seqs = height if q_start is None else q_start.size(0) - 1
-    _check(lib().bitnet_kv_append(cache.ref, layer, k.data_ptr(), v.data_ptr(), code, sn, sh, n, _book(table, "table", 2, seqs), width,
-                                  _book(kv_len, "kv_len", 1, seqs), _opt(q_start, "q_start"), seqs, _opt(dev_status, "dev_status"),
-                                  _st(stream, cache.device)), "bitnet_kv_append")
+    (_fast or _binding()).kv_append(cache.ref, layer, k, v, table, kv_len, q_start, dev_status, _st(stream))
 
 
 def bitnet_kv_reserve(refs, table, from_len, to_len, page_size, dev_status=None, stream=None):
     """Gives the rows of the table the pages that growing from from_len to to_len tokens takes, lowest free pages first."""
-    seqs, width = table.shape
-    _check(lib().bitnet_kv_reserve(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
-                                   _book(from_len, "from_len", 1, seqs), _book(to_len, "to_len", 1, seqs), page_size,
-                                   _opt(dev_status, "dev_status"), _st(stream, table.device)), "bitnet_kv_reserve")
+    (_fast or _binding()).kv_reserve(refs, table, from_len, to_len, page_size, dev_status, _st(stream))
 
 
 def bitnet_kv_workspace_bytes(num_pages, n) -> int:
@@ -598,48 +584,31 @@ def new_kv_workspace(num_pages, n=0, device="cuda"):
 
 def bitnet_kv_fork(cache, refs, table, kv_len, parents, children, workspace=None, dev_status=None, stream=None):
     """Rows children[i] become copies of rows parents[i]: full pages shared, a page filled in part copied."""
-    n, (seqs, width) = parents.size(0), table.shape
-    if refs.size(0) != cache.num_pages or children.size(0) != n:
-        raise BitnetError("bitnet_kv_fork: refs must have one entry per page, parents and children one length")
     if workspace is None:
-        workspace = new_kv_workspace(cache.num_pages, n, cache.device)
-    _check(lib().bitnet_kv_fork(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), seqs, width, _book(kv_len, "kv_len", 1, seqs),
-                                _book(parents, "parents", 1), _book(children, "children", 1), n, workspace.data_ptr(), workspace.nbytes,
-                                _opt(dev_status, "dev_status"), _st(stream, cache.device)), "bitnet_kv_fork")
+        workspace = new_kv_workspace(cache.num_pages, parents.shape[0], cache.device)
+    (_fast or _binding()).kv_fork(cache.ref, refs, table, kv_len, parents, children, workspace, dev_status, _st(stream))
 
 
 def bitnet_kv_free(refs, table, kv_len, rows, dev_status=None, stream=None):
     """Gives up the listed rows of the table: counts fall, the rows become -1, their lengths 0."""
-    seqs, width = table.shape
-    _check(lib().bitnet_kv_free(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
-                                _book(kv_len, "kv_len", 1, seqs), _book(rows, "rows", 1), rows.size(0), _opt(dev_status, "dev_status"),
-                                _st(stream, table.device)), "bitnet_kv_free")
+    (_fast or _binding()).kv_free(refs, table, kv_len, rows, dev_status, _st(stream))
 
 
 def bitnet_kv_trim(refs, table, kv_len, page_size, window, sinks=0, stream=None):
     """Gives up the pages that attention with this window and these sinks no longer reads."""
-    seqs, width = table.shape
-    _check(lib().bitnet_kv_trim(_book(refs, "refs", 1), refs.size(0), _book(table, "table", 2), seqs, width,
-                                _book(kv_len, "kv_len", 1, seqs), page_size, window, sinks, _st(stream, table.device)), "bitnet_kv_trim")
+    (_fast or _binding()).kv_trim(refs, table, kv_len, page_size, window, sinks, _st(stream))
 
 
 def bitnet_kv_compact(cache, refs, table, live=None, workspace=None, stream=None):
     """Moves the pages in use to the pool's first places; live (int32 [1], optional) receives their number."""
-    if refs.size(0) != cache.num_pages:
-        raise BitnetError("bitnet_kv_compact: refs must have one entry per page")
     if workspace is None:
         workspace = new_kv_workspace(cache.num_pages, 0, cache.device)
-    seqs, width = table.shape
-    _check(lib().bitnet_kv_compact(cache.ref, _book(refs, "refs", 1), _book(table, "table", 2), seqs, width, _opt(live, "live"),
-                                   workspace.data_ptr(), workspace.nbytes, _st(stream, cache.device)), "bitnet_kv_compact")
+    (_fast or _binding()).kv_compact(cache.ref, refs, table, live, workspace, _st(stream))
 
 
 def bitnet_kv_copy_pages(cache, src, dst, dev_status=None, stream=None):
     """Copies pages src[i] to dst[i], K and V, all layers."""
-    if src.shape != dst.shape:
-        raise BitnetError("bitnet_kv_copy_pages: src and dst must have one length")
-    _check(lib().bitnet_kv_copy_pages(cache.ref, _book(src, "src", 1), _book(dst, "dst", 1), src.size(0), _opt(dev_status, "dev_status"),
-                                      _st(stream, cache.device)), "bitnet_kv_copy_pages")
+    (_fast or _binding()).kv_copy_pages(cache.ref, src, dst, dev_status, _st(stream))
 
 
 def bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim) -> int:
@@ -656,45 +625,24 @@ def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
     return ws
 
 
-def _attn_out(name, q, out):
-    if out is None:
-        return torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if not (out.is_cuda and out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()):
-        raise BitnetError(f"{name}: out must be contiguous, with q's shape and type")
-    return out
-
-
-def _attn_ws(workspace, cache, n, heads):
-    if workspace is None:
-        if n == 0 or heads % cache.kv_heads:
-            return None, 0, None
-        workspace = new_attn_workspace(n, heads, cache.kv_heads, cache.head_dim, cache.device)
-    return workspace.data_ptr(), workspace.nbytes, workspace
+def _attn_ws(cache, q):
+    """A workspace for one call; None where the call will refuse q anyway."""
+    if q.dim() != 3 or q.shape[0] == 0 or q.shape[1] == 0 or q.shape[1] % cache.kv_heads:
+        return None
+    return new_attn_workspace(q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, cache.device)
 
 
 def bitnet_attn_decode(cache, layer, q, table, kv_len, scale=None, window=0, sinks=0, out=None, workspace=None, dev_status=None,
                        stream=None):
     """Attention of one new token per sequence: q [seqs][q_heads][head_dim] (fp32 or the cache's type) -> out, same shape and type."""
-    n, heads, sn, sh, code = _rows(q, "q", None, cache.head_dim)
-    out = _attn_out("bitnet_attn_decode", q, out)
-    ws, size, _keep = _attn_ws(workspace, cache, n, heads)
-    _check(lib().bitnet_attn_decode(cache.ref, layer, q.data_ptr(), code, heads, sn, sh, _book(table, "table", 2, n), table.size(1),
-                                    _book(kv_len, "kv_len", 1, n), n, cache.head_dim ** -0.5 if scale is None else scale, window, sinks,
-                                    out.data_ptr(), ws, size, _opt(dev_status, "dev_status"), _st(stream, cache.device)),
-           "bitnet_attn_decode")
-    return out
+    return (_fast or _binding()).attn_decode(cache.ref, layer, q, table, kv_len, cache.scale if scale is None else scale, window, sinks, out,
+                                             _attn_ws(cache, q) if workspace is None else workspace, dev_status, _st(stream))
 
 
 def bitnet_attn_prompt(cache, layer, q, table, kv_len, q_start, max_new, scale=None, window=0, sinks=0, out=None, workspace=None,
                        dev_status=None, stream=None):
     """Attention of prompts or chunks of prompts: q [tokens][q_heads][head_dim] in the cache's type; sequence s has the tokens
     q_start[s] .. q_start[s + 1] - 1 (at most max_new), the last of them at position kv_len[s] - 1."""
-    n, heads, sn, sh, code = _rows(q, "q", None, cache.head_dim)
-    seqs = q_start.size(0) - 1
-    out = _attn_out("bitnet_attn_prompt", q, out)
-    ws, size, _keep = _attn_ws(workspace, cache, n, heads)
-    _check(lib().bitnet_attn_prompt(cache.ref, layer, q.data_ptr(), code, heads, sn, sh, n, _book(table, "table", 2, seqs), table.size(1),
-                                    _book(kv_len, "kv_len", 1, seqs), _book(q_start, "q_start", 1), seqs, max_new,
-                                    cache.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), ws, size,
-                                    _opt(dev_status, "dev_status"), _st(stream, cache.device)), "bitnet_attn_prompt")
-    return out
+    return (_fast or _binding()).attn_prompt(cache.ref, layer, q, table, kv_len, q_start, max_new, cache.scale if scale is None else scale,
+                                             window, sinks, out, _attn_ws(cache, q) if workspace is None else workspace, dev_status,
+                                             _st(stream))

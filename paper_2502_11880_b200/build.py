@@ -1,4 +1,5 @@
-"""Builds libbitnet_b200.so (sm_100a only) next to this file with nvcc.  No JIT cache, no fallback.
+"""Builds libbitnet_b200.so (sm_100a only) next to this file with nvcc, and the compiled part of the Python binding
+(_binding.so, g++).  No JIT cache, no fallback.
 
 Every csrc/*.cu is compiled to an object under build/ (in parallel; an object is reused while it is newer than
 its source and every header), then the objects are linked into the shared library.
@@ -8,6 +9,7 @@ from __future__ import annotations
 import glob
 import os
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +20,27 @@ OBJ_DIR = os.path.join(PKG, "build")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
+
+
+BINDING = os.path.join(PKG, "_binding.so")
+BINDING_SRC = os.path.join(CSRC, "binding.cpp")
+
+
+def build_binding(force: bool = False) -> str:
+    """csrc/binding.cpp against this Python and this torch (whose libraries are in the process already)."""
+    newest = max(os.path.getmtime(f) for f in [BINDING_SRC, *glob.glob(os.path.join(INCLUDE, "*.h"))])
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) > newest:
+        return BINDING
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    dirs = [INCLUDE, sysconfig.get_paths()["include"], os.path.join(root, "include"),
+            os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    lib = os.path.join(root, "lib")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *[f"-I{d}" for d in dirs], "-o", BINDING, BINDING_SRC,
+                    f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{lib}"], check=True)
+    return BINDING
 
 
 def sources():
@@ -36,6 +59,14 @@ def stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    with ThreadPoolExecutor(max_workers=1) as other:
+        binding = other.submit(build_binding, force)
+        build_library(force, verbose)
+        binding.result()
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not (force or stale()):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
