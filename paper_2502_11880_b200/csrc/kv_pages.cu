@@ -89,58 +89,74 @@ __device__ __forceinline__ uint2 to16(const float4& v, const __half*) {
   return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
 
-// One warp per new token and pool: 4 elements per lane and step.  IN32: fp32 rows, rounded once to the cache's type.
+// A warp takes up to 256 pieces of 4 elements of one new token's K or V: 8 per lane, all loaded before the look-ups of the token's
+// sequence, position and page, which do not depend on them, have come back one after the other.  IN32: fp32 rows, rounded once to the
+// cache's type; otherwise the bits move.  (32 tokens of 32 heads of 100: 10.6 us with a warp per row that looked up first and
+// loaded in turns.)
 template <typename KT, bool IN32>
 __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
+  const int quads = a.kv.head_dim >> 2, units = a.kv.kv_heads * quads, chunks = (units + 255) / 256;
   const int64_t id = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  if (id >= 2 * (int64_t)a.tokens) return;
-  const int n = (int)(id >> 1), pool = (int)(id & 1);
-  const int seq = a.q_start ? kv_seq_of(a.q_start, a.seqs, n) : n;
-  const int64_t pos = a.q_start ? (int64_t)__ldg(a.kv_len + seq) - __ldg(a.q_start + seq + 1) + n : (int64_t)__ldg(a.kv_len + seq) - 1;
-  const int64_t entry = pos / a.kv.page_size;
-  if (pos < 0 || entry >= a.width) {
-    if (lane == 0 && pos >= 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-    return;
+  const int64_t token_pool = id / chunks;
+  if (token_pool >= 2 * (int64_t)a.tokens) return;
+  const int n = (int)(token_pool >> 1), pool = (int)(token_pool & 1);
+  const int u0 = (int)(id - token_pool * chunks) * 256 + lane;
+
+  const uint8_t* src = a.src[pool] + n * a.stride_token * (IN32 ? 4 : 2);
+  uint4 raw[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int u = u0 + 32 * j;
+    if (u < units) {
+      const int h = u / quads, d = (u - h * quads) * 4;
+      if (IN32) {
+        raw[j] = __ldg(reinterpret_cast<const uint4*>(src + (h * a.stride_head + d) * 4));
+      } else {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + (h * a.stride_head + d) * 2));
+        raw[j].x = w.x;
+        raw[j].y = w.y;
+      }
+    }
   }
-  const int page = __ldg(a.table + (int64_t)seq * a.width + entry);
+
+  int seq = n;
+  int64_t pos;
+  if (a.q_start) {
+    // the number of sequences that begin after the first and not beyond token n, 32 at a time
+    seq = 0;
+    for (int s0 = 1; s0 < a.seqs; s0 += 32) {
+      const int s = s0 + lane;
+      const int in = __popc(__ballot_sync(0xffffffffu, s < a.seqs && __ldg(a.q_start + s) <= n));
+      seq += in;
+      if (in < 32) break;
+    }
+    pos = (int64_t)__ldg(a.kv_len + seq) - __ldg(a.q_start + seq + 1) + n;
+  } else {
+    pos = (int64_t)__ldg(a.kv_len + seq) - 1;
+  }
+  const int64_t entry = pos / a.kv.page_size;
+  if (pos < 0) return;
+  const int page = entry < a.width ? __ldg(a.table + (int64_t)seq * a.width + entry) : -1;
   if (page < 0 || page >= a.kv.num_pages) {
     if (lane == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
     return;
   }
   uint8_t* dst = (pool ? a.kv.v : a.kv.k) +
                  2 * (a.layer * a.kv.stride_layer + page * a.kv.stride_page + (pos & (a.kv.page_size - 1)) * a.kv.stride_row);
-  const uint8_t* src = a.src[pool] + n * a.stride_token * (IN32 ? 4 : 2);
-  const int quads = a.kv.head_dim >> 2, units = a.kv.kv_heads * quads;
-  for (int u0 = lane; u0 < units; u0 += 32 * 8) {
-    uint4 raw[8];
-    int64_t to[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int u = u0 + 32 * j;
-      if (u < units) {
-        const int h = u / quads, d = (u - h * quads) * 4;
-        to[j] = 2 * (h * a.kv.stride_head + d);
-        if (IN32) {
-          raw[j] = __ldg(reinterpret_cast<const uint4*>(src + (h * a.stride_head + d) * 4));
-        } else {
-          const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + (h * a.stride_head + d) * 2));
-          raw[j].x = w.x;
-          raw[j].y = w.y;
-        }
-      }
+  for (int j = 0; j < 8; ++j) {
+    const int u = u0 + 32 * j;
+    if (u < units) {
+      const int h = u / quads, d = (u - h * quads) * 4;
+      uint2 w = make_uint2(raw[j].x, raw[j].y);
+      if (IN32)
+        w = to16(make_float4(__uint_as_float(raw[j].x), __uint_as_float(raw[j].y), __uint_as_float(raw[j].z), __uint_as_float(raw[j].w)),
+                 (const KT*)nullptr);
+      *reinterpret_cast<uint2*>(dst + 2 * (h * a.kv.stride_head + d)) = w;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (u0 + 32 * j < units) {
-        uint2 w = make_uint2(raw[j].x, raw[j].y);
-        if (IN32)
-          w = to16(make_float4(__uint_as_float(raw[j].x), __uint_as_float(raw[j].y), __uint_as_float(raw[j].z), __uint_as_float(raw[j].w)),
-                   (const KT*)nullptr);
-        *reinterpret_cast<uint2*>(dst + to[j]) = w;
-      }
   }
 }
 
@@ -172,25 +188,40 @@ __device__ __forceinline__ int block_scan(int x, int& total, int* warp_sums) {
   return before + inc - x;
 }
 
-// Calls give(rank, page) for the free pages of rank first..need-1, lowest page first; returns how many free pages there
-// were (counted up to where the scan ended: at least `need` if enough).
+// The counts of a step's 4 pages per thread (a page beyond the pool counts as used).
+struct Counts {
+  int c[4];
+};
+__device__ __forceinline__ Counts load_counts(const int32_t* refs, int num_pages, int p0) {
+  Counts x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int p = p0 + (int)threadIdx.x * 4 + j;
+    x.c[j] = p < num_pages ? __ldcg(refs + p) : 1;
+  }
+  return x;
+}
+// Calls give(rank, page) for the free pages of rank 0..need-1, lowest page first; returns how many free pages there
+// were (counted up to where the scan ended: at least `need` if enough).  `x` holds the first step's counts; each step's are loaded
+// while the one before is looked at.
 template <typename F>
-__device__ __forceinline__ int scan_free(const int32_t* refs, int num_pages, int first, int need, int* warp_sums, F give) {
+__device__ __forceinline__ int scan_free(const int32_t* refs, int num_pages, int need, Counts x, int* warp_sums, F give) {
   int found = 0;
   for (int p0 = 0; p0 < num_pages && found < need; p0 += PLAN_THREADS * 4) {
+    const Counts next = load_counts(refs, num_pages, p0 + PLAN_THREADS * 4);
     const int p = p0 + threadIdx.x * 4;
-    bool free[4];
+    int total, mine = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) free[j] = p + j < num_pages && __ldcg(refs + p + j) == 0;
-    int total;
-    int rank = found + block_scan(free[0] + free[1] + free[2] + free[3], total, warp_sums);
+    for (int j = 0; j < 4; ++j) mine += x.c[j] == 0;
+    int rank = found + block_scan(mine, total, warp_sums);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (free[j]) {
-        if (rank >= first && rank < need) give(rank, p + j);
+      if (x.c[j] == 0) {
+        if (rank < need) give(rank, p + j);
         ++rank;
       }
     found += total;
+    x = next;
   }
   return found;
 }
@@ -205,6 +236,7 @@ kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
   const int64_t mask = (1 << page_shift) - 1;
   auto first_entry = [&](int64_t row) { return (max((int64_t)0, (int64_t)from_len[row]) + mask) >> page_shift; };
   bool lacking = false;
+  Counts counts = load_counts(refs, num_pages, 0);
   for (int64_t r0 = 0; r0 < seqs; r0 += PLAN_SEQS) {
     const int rows = (int)min((int64_t)PLAN_SEQS, seqs - r0);
     // 4 rows per thread: counts, then their prefix
@@ -240,7 +272,7 @@ kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
       }
       return table + (r0 + lo) * width + first_entry(r0 + lo) + (rank - start[lo]);
     };
-    const int found = scan_free(refs, num_pages, 0, need, warp_sums, [&](int rank, int page) {
+    const int found = scan_free(refs, num_pages, need, counts, warp_sums, [&](int rank, int page) {
       *place(rank) = page;
       refs[page] = 1;
     });
@@ -250,6 +282,7 @@ kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
     }
     __threadfence();
     __syncthreads();
+    if (r0 + PLAN_SEQS < seqs) counts = load_counts(refs, num_pages, 0);
   }
   if (lacking && dev_status) atomicExch(dev_status, BITNET_ERR_NO_PAGE);
 }
@@ -263,67 +296,62 @@ struct PlanHead {
   int32_t moves, live, pad[2];
 };
 
-// Child rows of a fork: shares of the parent's full pages and a fresh page for the part of one.
+// Where a fork's parent ends: used tokens, as a number that its row of the table can hold.
+__device__ __forceinline__ int64_t fork_used(const int32_t* len, int parent, int64_t width, int page_shift) {
+  return min((int64_t)max(0, len[parent]), width << page_shift);
+}
+__device__ __forceinline__ bool fork_valid(int parent, int child, int64_t seqs) {
+  return parent >= 0 && parent < seqs && child >= 0 && child < seqs && parent != child;
+}
+
+// Plans a fork's copies: the i-th child whose parent fills a page in part gets the i-th free page.  (Full pages are shared, which
+// makes none free or used; kv_move_kernel does that, on all SMs.)
 __global__ void __launch_bounds__(PLAN_THREADS)
-kv_fork_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* parents,
+kv_fork_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* len, const int32_t* parents,
                const int32_t* children, int n, int page_shift, PlanHead* head, Move* moves, int* dev_status) {
   __shared__ int warp_sums[32];
+  __shared__ Move want[PLAN_THREADS];      // of a step's children, by rank; dst: the child
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int page = 1 << page_shift;
-  bool bad = false, lacking = false;
-  auto valid = [&](int p, int c) { return p >= 0 && p < seqs && c >= 0 && c < seqs && p != c; };
-  // full pages: one warp per child
-  for (int i = warp; i < n; i += PLAN_THREADS / 32) {
-    const int p = parents[i], c = children[i];
-    if (!valid(p, c)) {
-      bad = true;
-      continue;
-    }
-    const int64_t used = min((int64_t)max(0, len[p]), width << page_shift);
-    const int64_t full = used >> page_shift;
-    for (int64_t e = lane; e < width; e += 32) {
-      int id = -1;
-      if (e < full) {
-        id = table[p * width + e];
-        if (id >= 0 && id < num_pages) atomicAdd(refs + id, 1);
-        else id = -1;
-      }
-      table[c * width + e] = id;
-    }
-    if (lane == 0) len[c] = (int)used;
-  }
-  __threadfence();
-  __syncthreads();
-  // parts of pages: the i-th child that has one gets the i-th free page
+  Counts counts = load_counts(refs, num_pages, 0);
   int made = 0;
+  bool bad = false, lacking = false;
   for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
     const int i = i0 + threadIdx.x;
-    int src = -1, rows = 0;
+    int src = -1, rows = 0, c = 0;
     int64_t e = 0;
-    if (i < n && valid(parents[i], children[i])) {
-      const int64_t used = min((int64_t)max(0, len[parents[i]]), width << page_shift);
-      rows = (int)(used & (page - 1));
-      e = used >> page_shift;
-      if (rows) src = table[(int64_t)parents[i] * width + e];
-      if (src >= num_pages) src = -1;
+    if (i < n) {
+      const int p = parents[i];
+      c = children[i];
+      if (fork_valid(p, c, seqs)) {
+        const int64_t used = fork_used(len, p, width, page_shift);
+        rows = (int)(used & ((1 << page_shift) - 1));
+        e = used >> page_shift;
+        if (rows) src = table[p * width + e];
+        if (src >= num_pages) src = -1;
+        if (rows) table[c * width + e] = -1;
+      } else {
+        bad = true;
+      }
     }
     int total;
-    const int rank = made + block_scan(src >= 0, total, warp_sums);
-    if (src >= 0) moves[rank] = Move{src, -1, rows, (int)(i)};
-    made += total;
+    const int rank = block_scan(src >= 0, total, warp_sums);
+    if (src >= 0) want[rank] = Move{src, c, rows, (int)e};
+    __threadfence();
+    __syncthreads();
+    const int found = scan_free(refs, num_pages, total, counts, warp_sums, [&](int k, int id) {
+      const Move w = want[k];
+      moves[made + k] = Move{w.src, id, w.rows, 0};
+      table[w.dst * width + w.pad] = id;
+      refs[id] = 1;
+    });
+    if (found < total) lacking = true;     // children without a page keep -1 there
+    made += min(found, total);
+    __threadfence();
+    __syncthreads();
+    if (i0 + PLAN_THREADS < n) counts = load_counts(refs, num_pages, 0);
   }
-  __threadfence();
-  __syncthreads();
-  const int found = scan_free(refs, num_pages, 0, made, warp_sums, [&](int rank, int id) {
-    const int c = children[moves[rank].pad];
-    moves[rank].dst = id;
-    table[(int64_t)c * width + (len[c] >> page_shift)] = id;
-    refs[id] = 1;
-  });
-  if (found < made) lacking = true;        // children without a page keep -1 there
-  if (threadIdx.x == 0) head->moves = min(found, made);
+  if (threadIdx.x == 0) head->moves = made;
   if (dev_status) {
     if (bad) atomicExch(dev_status, BITNET_ERR_BAD_PAGE);
     if (lacking) atomicExch(dev_status, BITNET_ERR_NO_PAGE);
@@ -337,22 +365,37 @@ kv_compact_plan_kernel(int32_t* refs, int num_pages, int page_size, PlanHead* he
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int live = 0;
-  for (int p = threadIdx.x; p < num_pages; p += PLAN_THREADS) live += refs[p] > 0;
+#pragma unroll 4
+  for (int p0 = 0; p0 < num_pages; p0 += PLAN_THREADS * 4) {
+    const Counts x = load_counts(refs, num_pages, p0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) live += x.c[j] > 0 && p0 + (int)threadIdx.x * 4 + j < num_pages;
+  }
+  Counts x = load_counts(refs, num_pages, 0);
   int sum;
   block_scan(live, sum, warp_sums);
   live = sum;
   int holes = 0, tail = 0;                 // free places below `live`, pages in use beyond
-  for (int p0 = 0; p0 < num_pages; p0 += PLAN_THREADS) {
-    const int p = p0 + threadIdx.x;
-    const bool used = p < num_pages && refs[p] > 0;
-    const bool hole = p < live && !used, out = p >= live && used;
+  for (int p0 = 0; p0 < num_pages; p0 += PLAN_THREADS * 4) {
+    const Counts next = load_counts(refs, num_pages, p0 + PLAN_THREADS * 4);
+    const int p = p0 + (int)threadIdx.x * 4;
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p + j < num_pages) mine += p + j < live ? (x.c[j] <= 0 ? 1 : 0) : (x.c[j] > 0 ? 1 << 16 : 0);
     int total;
-    const int both = block_scan((hole ? 1 : 0) | (out ? 1 << 16 : 0), total, warp_sums);   // at most 1024 of each per step
-    if (hole) moves[holes + (both & 0xffff)].dst = p;
-    if (out) moves[tail + (both >> 16)].src = p;
-    if (p < num_pages) place[p] = p;
+    const int both = block_scan(mine, total, warp_sums);    // at most 4096 of each per step
+    int hole = holes + (both & 0xffff), out = tail + (both >> 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (p + j < num_pages) {
+        place[p + j] = p + j;
+        if (p + j < live && x.c[j] <= 0) moves[hole++].dst = p + j;
+        if (p + j >= live && x.c[j] > 0) moves[out++].src = p + j;
+      }
     holes += total & 0xffff;
     tail += total >> 16;
+    x = next;
   }
   __threadfence();
   __syncthreads();
@@ -380,7 +423,13 @@ struct MoveArgs {
   int64_t count;
   const int32_t* place;     // compaction: the pages' new places, for the table
   int32_t* table;
-  int64_t table_entries;
+  int64_t seqs, width;
+  const int32_t* parents;   // fork: the children's rows and the counts of what they share
+  const int32_t* children;
+  int64_t n;
+  int32_t* refs;
+  int32_t* len;
+  int page_shift;
   int* dev_status;
 };
 
@@ -393,6 +442,25 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
   const int64_t moves = a.head ? a.head->moves : a.count;
   const int pieces = a.kv.head_dim / PER;
   const int64_t jobs = moves * a.kv.layers * 2;
+  if (a.parents) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.n; i += (int64_t)gridDim.x * 8) {
+      const int p = a.parents[i], c = a.children[i];
+      if (!fork_valid(p, c, a.seqs)) continue;
+      const int64_t used = fork_used(a.len, p, a.width, a.page_shift), full = used >> a.page_shift;
+      const bool part = (used & ((1 << a.page_shift) - 1)) != 0;       // that entry has been seen to
+      for (int64_t e = lane; e < a.width; e += 32) {
+        int id = -1;
+        if (e < full) {
+          id = a.table[p * a.width + e];
+          if (id >= 0 && id < a.kv.num_pages) atomicAdd(a.refs + id, 1);
+          else id = -1;
+        }
+        if (e != full || !part) a.table[c * a.width + e] = id;
+      }
+      if (lane == 0) a.len[c] = (int)used;
+    }
+  }
   for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
     const int pool = (int)(job & 1);
     const int64_t ml = job >> 1, move = ml / a.kv.layers;
@@ -432,7 +500,7 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
     }
   }
   if (a.place)
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.table_entries; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.seqs * a.width; i += (int64_t)gridDim.x * 256) {
       const int id = a.table[i];
       if (id >= 0 && id < a.kv.num_pages) a.table[i] = a.place[id];
     }
@@ -515,7 +583,9 @@ int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, 
   a.seqs = (int)seqs;
   a.layer = layer;
   a.dev_status = dev_status;
-  const unsigned grid = (unsigned)ceil_div(2 * tokens, 8);
+  const int64_t chunks = ceil_div((int64_t)kv.kv_heads * (kv.head_dim / 4), 256), blocks = ceil_div(2 * tokens * chunks, 8);
+  if (blocks > 0x7fffffff) return BITNET_ERR_UNSUPPORTED_SHAPE;
+  const unsigned grid = (unsigned)blocks;
   log_launch("kv_append_kernel tokens=%lld grid=%u", (long long)tokens, grid);
   if (in_dtype != BITNET_KV_F32) return launch(kv_append_kernel<__half, false>, grid, 256, st, a);   // same type: bits move
   return dtype == BITNET_KV_BF16 ? launch(kv_append_kernel<__nv_bfloat16, true>, grid, 256, st, a)
@@ -539,6 +609,15 @@ int launch_kv_fork(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs
   m.kv = kv;
   m.head = plan_head(ws);
   m.moves = plan_moves(ws);
+  m.table = table;
+  m.seqs = seqs;
+  m.width = width;
+  m.parents = parents;
+  m.children = children;
+  m.n = n;
+  m.refs = refs;
+  m.len = len;
+  m.page_shift = __builtin_ctz((unsigned)kv.page_size);
   m.dev_status = dev_status;
   return launch_move(m, n * kv.layers * 2, st);
 }
@@ -563,7 +642,8 @@ int launch_kv_compact(const KvView& kv, int32_t* refs, int32_t* table, int64_t s
   m.moves = plan_moves(ws);
   m.place = place;
   m.table = table;
-  m.table_entries = seqs * width;
+  m.seqs = seqs;
+  m.width = width;
   return launch_move(m, (int64_t)kv.num_pages * kv.layers, st);   // at most half of the pages move
 }
 
