@@ -407,7 +407,8 @@ int bitnet_tl_build_lut_debug(bitnet_fmt_t fmt, const int8_t* q_row, int64_t K, 
  * Paged key-value cache and the attention over it: what lies between the Q/K/V linear and the O linear of a decoder layer.
  *
  * A cache is two pools K and V [layers][num_pages][kv_heads][page_size][head_dim] of 16-bit values (any order of the outer
- * dimensions: the strides say where things are) and its books, which are plain device arrays of the caller:
+ * dimensions: the strides say where things are; a row is stride_row elements long, of which those beyond head_dim, up to the next
+ * multiple of 8, may be read but are never used or written) and its books, which are plain device arrays of the caller:
  *   table[seqs][table_width] int32   row s holds the pages of sequence s: its token at position p is row p % page_size of page
  *                                    table[s][p / page_size]; -1 = no page;
  *   kv_len[seqs] int32               tokens of each sequence;
@@ -496,12 +497,14 @@ int bitnet_kv_copy_pages(const bitnet_kv_cache_t* cache, const int32_t* src, con
  *   out[t][h] = sum_c softmax_c(scale * <q[t][h], K[c][g]>) V[c][g],  g = h / (q_heads / kv_heads);  a query that sees nothing: 0.
  * q: [tokens][q_heads][head_dim], strides in elements (multiples of 4), 16-byte aligned; out: [tokens][q_heads][head_dim]
  * contiguous, of q's type.  Cached values that no query sees (the rest of a page, released pages) may hold anything.
- * workspace: bitnet_attn_workspace_bytes bytes, zeroed once with bitnet_workspace_init; every completed call leaves its counters
- * zeroed.  It may serve calls with fewer tokens and any head layout that needs no more bytes, but no two calls that overlap.
+ * workspace: bitnet_attn_workspace_bytes bytes; its first 64 KB are zeroed once with bitnet_workspace_init, and every completed call
+ * leaves them zeroed.  tokens is the most new tokens of a prompt call; with 0 the workspace (1.3 MB) serves decode calls, and prompt
+ * calls without cutting the blocks of one tile between CTAs.  One workspace may serve calls of any sizes and both kinds, but no
+ * two calls that overlap.
  *
  * bitnet_attn_decode: one new token per sequence (token i belongs to sequence i), q in fp32 or in the cache's type.
  * bitnet_attn_prompt: any number of new tokens per sequence (q_start; at most max_new of one sequence), q in the cache's type.  Their K and V
- * rows are appended before.
+ * rows are appended before.  (With max_new of 1 or 2 the decode kernel serves the call.)
  */
 size_t bitnet_attn_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim);
 int bitnet_attn_decode(const bitnet_kv_cache_t* cache, int64_t layer, const void* q, int io_dtype, int64_t q_heads,

@@ -611,17 +611,21 @@ def bitnet_kv_copy_pages(cache, src, dst, dev_status=None, stream=None):
     (_fast or _binding()).kv_copy_pages(cache.ref, src, dst, dev_status, _st(stream))
 
 
+ATTN_WORKSPACE_HEAD = 65536      # the bytes of a workspace that have to be zero before its first call
+
+
 def bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim) -> int:
     return lib().bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim)
 
 
 def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
-    """A zeroed workspace for bitnet_attn_decode and bitnet_attn_prompt calls of up to `tokens` query tokens."""
+    """A workspace for bitnet_attn_decode and bitnet_attn_prompt calls, its counters zeroed.  tokens: the most new tokens of a prompt
+    call (0: decode calls only, 1.3 MB; otherwise some 60 MB for the parts of prompt calls with few rows)."""
     size = bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim)
     if size == 0:
         _check(1, "bitnet_attn_workspace_bytes")
     ws = torch.empty(size, dtype=torch.uint8, device=device)
-    bitnet_workspace_init(ws)
+    bitnet_workspace_init(ws[:ATTN_WORKSPACE_HEAD])
     return ws
 
 

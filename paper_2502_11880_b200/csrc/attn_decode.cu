@@ -50,8 +50,11 @@ struct DecodeArgs {
   int head_dim, page_shift, num_pages, layer;
   int window, sinks, max_len;                 // max_len = table_width * page_size
   int layer_pages;                            // > 0: the maps take both 64-column halves of a row in one box
+  const uint8_t *k, *v;                       // DENSE: the layer's pools, and their strides in bytes
+  int64_t page_bytes, head_bytes;
+  int row_bytes;
   float c;                                    // scale * log2(e)
-  int* counters;                              // [tokens * kv_heads * head_blocks], zero between calls
+  int* counters;                              // [grid], of the row in parts that begins in a CTA; zero between calls
   float2* part_ml;                            // [2 * grid][8] running maximum and sum of a part
   float* part_o;                              // [2 * grid][8][D]
   int* dev_status;
@@ -169,7 +172,10 @@ struct Layout {
 };
 
 // KT: element type of the pools; F32: q and out are fp32; DT: head_dim in steps of 16.
-template <typename KT, bool F32, int DT>
+// DENSE: a page's rows lie one after the other and each is an odd number of 16-byte pieces (head_dim 100: 13).  A page of a head is then one
+// plain bulk copy, and ldmatrix meets distinct banks without a swizzle; tensor copies, whose 128-byte box rows begin at odd
+// multiples of 16 bytes there, took 114 instead of 85 us for 9 windows of 4096 tokens, 32 heads of 100.
+template <typename KT, bool F32, int DT, bool DENSE>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const DecodeArgs a) {
   using L = Layout<DT>;
@@ -278,13 +284,13 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // ------------------------------------------------------------ producer: lane = box of the tile
     const int box_rows = min(1 << a.page_shift, TILE);
     const int boxes = TILE / box_rows;
-    const bool both = L::HALVES == 2 && a.layer_pages > 0; // a box has both halves
+    const bool both = DENSE || (L::HALVES == 2 && a.layer_pages > 0);   // a box has both halves
     const int per_pool = both ? boxes : boxes * L::HALVES;
     const int pool = lane / per_pool;                      // 0 = K, 1 = V
     const int half = both ? 0 : lane / boxes % L::HALVES;
     const int box = lane % boxes;
     const bool mine = pool < 2;
-    const uint32_t box_bytes = (uint32_t)box_rows * (both ? 256 : 128);
+    const uint32_t box_bytes = (uint32_t)box_rows * (DENSE ? a.row_bytes : both ? 256 : 128);
     while (item < end) {
       const int64_t off = item - base;
       const int row = (int)(off / r.tiles);
@@ -316,9 +322,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           ++it;
           if (*abort_flag) continue;
           const bool issue = cur != -2;
-          const unsigned mask = __ballot_sync(0xffffffffu, issue);
           const bool bad = issue && (cur < 0 || cur >= a.num_pages);
           if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+          const unsigned mask = __ballot_sync(0xffffffffu, issue && !(DENSE && bad));
+          if (DENSE && bad) {                                  // (a tensor copy from outside the pool writes zeros by itself)
+            uint8_t* dst = smem + (st * 2 + pool) * L::TILE_BYTES + box * box_bytes;
+            for (uint32_t i = 0; i < box_bytes; i += 16) *reinterpret_cast<uint4*>(dst + i) = make_uint4(0u, 0u, 0u, 0u);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          __syncwarp();
           if (lane == 0) {
             const unsigned k_mask = (1u << per_pool) - 1u;     // (at most 16 boxes of a pool)
             kv_mbar_expect(&s.full_k[st], __popc(mask & k_mask) * box_bytes);
@@ -332,7 +344,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             // a tile lies in shared memory as [box][half][row][64 columns]
             uint8_t* dst = smem + (st * 2 + pool) * L::TILE_BYTES + box * box_rows * (128 * L::HALVES) + half * box_rows * 128;
             uint64_t* full = pool ? &s.full_v[st] : &s.full_k[st];
-            if (both) kv_box_copy2(smem_u32(dst), pool ? &vmap : &kmap, y, head, bad ? -1 : cur + a.layer * a.layer_pages, full);
+            if (DENSE) {
+              if (!bad)
+                kv_bulk_copy(smem_u32(smem + (st * 2 + pool) * L::TILE_BYTES + box * box_bytes),
+                             (pool ? a.v : a.k) + cur * a.page_bytes + head * a.head_bytes + (int64_t)y * a.row_bytes, box_bytes, full);
+            } else if (both) kv_box_copy2(smem_u32(dst), pool ? &vmap : &kmap, y, head, bad ? -1 : cur + a.layer * a.layer_pages, full);
             else kv_box_copy(smem_u32(dst), pool ? &vmap : &kmap, half * 64, y, head, bad ? -1 : cur, a.layer, full);
           }
         }
@@ -362,8 +378,13 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const int k_row = tok_w + (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;
   const int v_row = tok_w + (lane & 15), v_piece = lane >> 4;
   const int box_shift = min(a.page_shift, 6), half_bytes = 128 << box_shift;
-  const uint32_t k_off = (uint32_t)((k_row >> box_shift) * half_bytes * L::HALVES + (k_row & ((1 << box_shift) - 1)) * 128);
-  const uint32_t v_off = (uint32_t)((v_row >> box_shift) * half_bytes * L::HALVES + (v_row & ((1 << box_shift) - 1)) * 128);
+  // DENSE: a row's pieces lie one after the other
+  auto piece_at = [&](int row, int i0, int k, int p) -> uint32_t {       // piece 2 (i0 + k) + p of a row, i0 a multiple of 4
+    if (DENSE) return (uint32_t)((2 * (i0 + k) + p) << 4);
+    return (uint32_t)((i0 >> 2) * half_bytes + (((2 * k + p) ^ (row & 7)) << 4));
+  };
+  const uint32_t k_off = DENSE ? (uint32_t)(k_row * a.row_bytes) : (uint32_t)((k_row >> box_shift) * half_bytes * L::HALVES + (k_row & ((1 << box_shift) - 1)) * 128);
+  const uint32_t v_off = DENSE ? (uint32_t)(v_row * a.row_bytes) : (uint32_t)((v_row >> box_shift) * half_bytes * L::HALVES + (v_row & ((1 << box_shift) - 1)) * 128);
   bool first_segment = true;
   struct Pending {                                         // a row of which this CTA has a part: its first, its last
     int n, head0, heads, c0, c1, first_slot;
@@ -470,11 +491,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         uint32_t b[4][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (i0 + k < DT) ldsm4(kbase + k_off + (i0 >> 2) * half_bytes + (((2 * k + k_piece) ^ (k_row & 7)) << 4), b[k]);
+          if (i0 + k < DT) ldsm4(kbase + k_off + piece_at(k_row, i0, k, k_piece), b[k]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int i = i0 + k;
           if (i < DT) {
+            if (DENSE && 16 * i + 16 > a.head_dim) {            // beyond the row lies something else: it counts as 0
+              const uint32_t m0 = 16 * i + 2 * t4 < a.head_dim ? 0xffffffffu : 0u, m1 = 16 * i + 8 + 2 * t4 < a.head_dim ? 0xffffffffu : 0u;
+              b[k][0] &= m0;
+              b[k][1] &= m1;
+              b[k][2] &= m0;
+              b[k][3] &= m1;
+            }
             P2::mma(sc[k & 1][0], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[k][0], b[k][1]);
             P2::mma(sc[k & 1][1], qa[i][0], qa[i][1], qa[i][2], qa[i][3], b[k][2], b[k][3]);
             if (THREE) {
@@ -546,7 +574,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         uint32_t b[4][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (i0 + k < DT) ldsm4_t(vbase + v_off + (i0 >> 2) * half_bytes + (((2 * k + v_piece) ^ (v_row & 7)) << 4), b[k]);
+          if (i0 + k < DT) ldsm4_t(vbase + v_off + piece_at(v_row, i0, k, v_piece), b[k]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int i = i0 + k;
@@ -640,7 +668,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       p.first_slot = 2 * p.c0 + (total * p.c0 / parts < row_begin ? 1 : 0);
       group_barrier(1, CONSUMER_WARPS * 32);
       if (tid == 0) {
-        int* counter = a.counters + (int64_t)n * rows_per_token + row;
+        int* counter = a.counters + p.c0;                   // (at most one row in parts begins in a CTA)
         __threadfence();                                    // (of all that the barrier ordered before)
         const int done = atomicAdd(counter, 1);
         s.last_part[first_segment ? 0 : 1] = done == p.c1 - p.c0;
@@ -692,9 +720,9 @@ int padded_steps(int head_dim) {
   return dt <= 4 ? 4 : dt <= 6 ? 6 : dt;
 }
 
-template <typename KT, bool F32, int DT>
+template <typename KT, bool F32, int DT, bool DENSE = false>
 int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
-  auto kernel = attn_decode_kernel<KT, F32, DT>;
+  auto kernel = attn_decode_kernel<KT, F32, DT, DENSE>;
   constexpr size_t smem = Layout<DT>::SMEM;
   static_assert(smem <= 232448, "shared memory of one CTA");
   static std::atomic<uint64_t> have{0};                  // devices on which the kernel may take that much shared memory
@@ -715,6 +743,13 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d
 }
 template <typename KT, bool F32>
 int launch_dt(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
+  if (d.row_bytes) {
+    switch (padded_steps(d.head_dim)) {
+      case 6: return launch_one<KT, F32, 6, true>(km, vm, d, grid, st);
+      case 7: return launch_one<KT, F32, 7, true>(km, vm, d, grid, st);
+      default: return launch_one<KT, F32, 8, true>(km, vm, d, grid, st);
+    }
+  }
   switch (padded_steps(d.head_dim)) {
     case 4: return launch_one<KT, F32, 4>(km, vm, d, grid, st);
     case 6: return launch_one<KT, F32, 6>(km, vm, d, grid, st);
@@ -723,17 +758,10 @@ int launch_dt(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d,
   }
 }
 
-size_t counters_bytes(int64_t tokens, int q_heads, int kv_heads) {
-  const int64_t blocks = ceil_div(q_heads / kv_heads, HEADS);
-  return (size_t)ceil_div(tokens * kv_heads * blocks * 4, 16) * 16;
-}
-
 }  // namespace
 
-size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, int head_dim) {
-  const size_t slots = 2 * (size_t)dev_info().sm_count * HEADS;
-  return counters_bytes(tokens, q_heads, kv_heads) + slots * (8 + (size_t)padded_steps(head_dim) * 64);
-}
+// The parts of one call: two per CTA, whatever the call.
+size_t attn_decode_parts_bytes() { return 2 * (size_t)dev_info().sm_count * HEADS * (8 + 128 * 4); }
 
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
   CUtensorMap km, vm;
@@ -742,6 +770,12 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   memcpy(&vm, c->maps[first + 1], sizeof vm);
   DecodeArgs d;
   d.layer_pages = (int)c->layer_pages;
+  d.k = static_cast<const uint8_t*>(c->k) + 2 * x.layer * c->stride_layer;
+  d.v = static_cast<const uint8_t*>(c->v) + 2 * x.layer * c->stride_layer;
+  d.page_bytes = 2 * c->stride_page;
+  d.head_bytes = 2 * c->stride_head;
+  const bool dense = c->head_dim > 64 && c->stride_row / 8 == ceil_div(c->head_dim, 8) && c->stride_row / 8 % 2 == 1;
+  d.row_bytes = dense ? (int)c->stride_row * 2 : 0;
   d.q = x.q;
   d.out = x.out;
   d.q_stride_token = x.q_stride_token;
@@ -767,9 +801,8 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   d.c = x.scale * 1.4426950408889634f;
   const int grid = dev_info().sm_count;
   const size_t slots = 2 * (size_t)grid * HEADS;
-  uint8_t* w = static_cast<uint8_t*>(ws);
-  d.counters = reinterpret_cast<int*>(w);
-  w += counters_bytes(x.tokens, x.q_heads, c->kv_heads);
+  d.counters = attn_counters(ws);
+  uint8_t* const w = attn_decode_parts(ws);
   d.part_ml = reinterpret_cast<float2*>(w);
   d.part_o = reinterpret_cast<float*>(w + slots * 8);
   d.dev_status = x.dev_status;

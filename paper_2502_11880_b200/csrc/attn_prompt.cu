@@ -37,6 +37,7 @@ constexpr int SOFT_WARPS = 8;                 // one thread per row of the two t
 constexpr int THREADS = (SOFT_WARPS + 4) * 32;
 constexpr int HALF = KB * 128;                // 128 rows x 64 columns of 16 bits
 constexpr int STAGES = 2;                     // of K, and of V
+constexpr int PART_BLOCKS = 4;                // fewest blocks of a part of an item
 constexpr float LAZY = 8.0f;                  // log2 of how far a maximum may rise before O is rescaled
 
 constexpr int POLY_EVERY = 4;                 // every fourth pair of columns takes the polynomial (none / 8th / 4th / 2nd pair measured
@@ -59,7 +60,10 @@ struct PromptArgs {
   int window, sinks, max_len;
   float c;                                            // |scale| * log2(e), above 0 so that -inf stays -inf
   uint32_t q_neg;                                     // scale < 0: the products take -Q
-  int64_t items;                                      // no item has this number or a higher one
+  int room;                                           // parts of items that the workspace has room for
+  int* counters;                                      // [items][8 warps]: parts that have arrived; zero between calls
+  float2* part_ml;                                    // [units][2 tiles][128 rows]: maximum and sum
+  float4* part_o;                                     // [units][8 warps][32 pieces of 4 columns][32 rows]
   int* dev_status;
 };
 
@@ -203,8 +207,11 @@ struct Item {
   int p_last;                       // position of the item's last token
   int lo;                           // first token that the item's first row sees through its window
   int n0, t1;                       // blocks: 0 .. n0-1 (sinks), then t1 ..
-  int nb;                           // blocks in all; -1: no more items
+  int b0, nb;                       // the part's first block, and its blocks; nb = -1: no more items
   int two;                          // the second tile has rows
+  int parts;                        // of the item, which join if there are several
+  int part;
+  int64_t unit0, id;                // the first part's place in the workspace, the item's number
 };
 
 template <int HALVES>
@@ -221,7 +228,10 @@ struct Tail {
   int abort_flag;
 };
 
-__device__ __forceinline__ int block_start(const Item& x, int j) { return (j < x.n0 ? j : x.t1 + j - x.n0) * KB; }
+__device__ __forceinline__ int block_start(const Item& x, int j) {
+  j += x.b0;
+  return (j < x.n0 ? j : x.t1 + j - x.n0) * KB;
+}
 // Whether the block holds tokens that no row of the item sees, and which of its rows those are.
 __device__ __forceinline__ bool unseen(const PromptArgs& a, const Item& x, int c) { return c > x.p_last || (c >= a.sinks && c < x.lo); }
 __device__ __forceinline__ bool has_unseen(const PromptArgs& a, const Item& x, int c0) {
@@ -293,18 +303,32 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const bool mine = half < HALVES;
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
       uint32_t kb = 0;                                       // blocks so far
-      for (int it = 0;; ++it) {
+      // With few items for the SMs the blocks of an item go to several CTAs: as many as make one part per SM at most (more of
+      // them, and the joins cost more than the SMs give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM
+      // 76, 191, 353 us)
+      int64_t pairs = 0;
+      for (int s0 = 0; s0 < a.seqs; s0 += 32) {
+        const int i = s0 + lane;
+        const int n = i < a.seqs ? max(0, __ldg(a.q_start + i + 1) - __ldg(a.q_start + i)) : 0;
+        pairs += (n + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens);
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) pairs += __shfl_xor_sync(0xffffffffu, pairs, d);
+      const int64_t items = pairs * a.kv_heads * a.blocks;
+      const int parts = items > 0 && 2 * items <= a.room ? (int)(a.room / items) : 1;
+      int64_t unit = blockIdx.x;
+      for (int it = 0;; unit += gridDim.x) {
         kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
         const int heads = a.kv_heads * a.blocks, span = 2 * a.tile_tokens;
-        const int64_t id = blockIdx.x + (int64_t)it * gridDim.x, want = id / heads;
-        const int hb = (int)(id % heads);
+        const int64_t id = unit / parts, want = id / heads;
+        const int hb = (int)(id % heads), part = (int)(unit % parts);
         if (lane == 0) s.item[it & 1].nb = -1;
         __syncwarp();
         bool found = false;
         int64_t before = 0;
-        for (int s1 = id < a.items && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
+        for (int s1 = unit < items * parts && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
           const int i = s1 - 1 - lane;
           const int q0 = i >= 0 ? __ldg(a.q_start + i) : 0;
           const int n = i >= 0 ? max(0, __ldg(a.q_start + i + 1) - q0) : 0;
@@ -332,11 +356,22 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             t.pos0 = (int)pos0;                              // |pos0| < 2^31
             t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
             t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
-            t.n0 = t.t1 = t.nb = 0;
+            t.n0 = t.t1 = t.b0 = t.nb = 0;
+            t.unit0 = id * parts;
+            t.part = part;
+            t.id = id;
+            int all = 0;
             if (t.p_last >= 0) {
               t.t1 = t.lo / KB;
               t.n0 = min((min(a.sinks, t.lo) + KB - 1) / KB, t.t1);
-              t.nb = t.n0 + t.p_last / KB + 1 - t.t1;
+              all = t.n0 + t.p_last / KB + 1 - t.t1;
+            }
+            t.parts = max(1, min(parts, all / PART_BLOCKS));
+            if (part < t.parts) {
+              t.b0 = (int)((int64_t)all * part / t.parts);
+              t.nb = (int)((int64_t)all * (part + 1) / t.parts) - t.b0;
+            } else {
+              t.nb = -2;                                     // the item has fewer parts than that
             }
             s.item[it & 1] = t;
           }
@@ -346,7 +381,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         __syncwarp();
         const Item x = s.item[it & 1];
         __syncwarp();
+        if (found && x.nb == -2) continue;                   // (the place is free still)
         if (lane == 0) kv_mbar_arrive(&s.item_full[it & 1]);
+        ++it;
         if (!found) break;
         auto look_up = [&](int j, int& y) -> int {
           const int tok = block_start(x, j) + box * box_rows;
@@ -633,7 +670,51 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       float inv = 0.0f;                                       // (a row that saw nothing is 0)
       if (x.nb > 0) {
         const float2 l = unpair(l2);
-        if (m != -INFINITY) inv = 1.0f / (l.x + l.y);
+        const float sum = l.x + l.y;
+        if (m != -INFINITY) inv = 1.0f / sum;
+        kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
+        fence_after();
+        ++items;
+        if (x.parts > 1) {
+          // ---- a part: to the workspace; each warp's last part to arrive joins its 32 rows, in the order of the parts
+          float4* const mine = a.part_o + ((x.unit0 + x.part) * 8 + warp) * 1024 + lane;
+          a.part_ml[((x.unit0 + x.part) * 2 + u) * ROWS + row] = make_float2(m, sum);
+#pragma unroll 1
+          for (int i = 0; i < steps * 16; i += 32) {
+            tm_ld32(o_addr + i, v);
+            wait_ld<32>(v);
+            if (valid)
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                mine[(i / 4 + k) * 32] = make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]), __uint_as_float(v[4 * k + 2]),
+                                                     __uint_as_float(v[4 * k + 3]));
+          }
+          fence_before();
+          __syncwarp();
+          int last = 0;
+          if (lane == 0) {
+            kv_mbar_arrive(&s.o_empty[u]);                    // O has been read
+            int* counter = a.counters + x.id * 8 + warp;
+            __threadfence();                                  // (of all that the warp's barrier ordered before)
+            last = atomicAdd(counter, 1) == x.parts - 1;
+            if (last) *counter = 0;                           // the workspace is left as it was
+            __threadfence();
+          }
+          last = __shfl_sync(0xffffffffu, last, 0);
+          __syncwarp();
+          if (!last) continue;
+          m = -INFINITY;
+          const float2* const ml = a.part_ml + (x.unit0 * 2 + u) * ROWS + row;
+#pragma unroll 4
+          for (int k = 0; k < x.parts; ++k) m = fmaxf(m, __ldcg(ml + k * 2 * ROWS).x);
+          float all = 0.0f;
+#pragma unroll 4
+          for (int k = 0; k < x.parts; ++k) {
+            const float2 y = __ldcg(ml + k * 2 * ROWS);
+            all += y.x == -INFINITY ? 0.0f : exp2_approx(y.x - m) * y.y;
+          }
+          inv = m == -INFINITY ? 0.0f : 1.0f / all;
+        }
       }
       const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
       const int piece = lane & 3;                             // 8 columns; rows 8 k + lane / 4
@@ -644,16 +725,35 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         to[k] = to[k] < 0 ? -1 : to[k] + piece * 8;
       }
       uint4* const stage = s.stage[warp];
-      if (x.nb > 0) {
-        kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
-        fence_after();
-        ++items;
-      }
 #pragma unroll 1
       for (int i = 0; i < steps * 16; i += 32) {
         uint32_t* const o = v;
-        if (x.nb > 0) tm_ld32(o_addr + i, o);
-        wait_ld<32>(o);
+        if (x.parts > 1) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+          if (valid) {
+            const float2* const ml = a.part_ml + (x.unit0 * 2 + u) * ROWS + row;
+            const float4* const from = a.part_o + (x.unit0 * 8 + warp) * 1024 + lane + (i / 4) * 32;
+#pragma unroll 3
+            for (int k = 0; k < x.parts; ++k) {
+              float4 w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) w[e] = __ldcg(from + (int64_t)k * 8 * 1024 + e * 32);
+              const float pm = __ldcg(ml + k * 2 * ROWS).x;
+              const float f = pm == -INFINITY ? 0.0f : exp2_approx(pm - m);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                o[4 * e] = __float_as_uint(__uint_as_float(o[4 * e]) + f * w[e].x);
+                o[4 * e + 1] = __float_as_uint(__uint_as_float(o[4 * e + 1]) + f * w[e].y);
+                o[4 * e + 2] = __float_as_uint(__uint_as_float(o[4 * e + 2]) + f * w[e].z);
+                o[4 * e + 3] = __float_as_uint(__uint_as_float(o[4 * e + 3]) + f * w[e].w);
+              }
+            }
+          }
+        } else {
+          if (x.nb > 0) tm_ld32(o_addr + i, o);
+          wait_ld<32>(o);
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           o[e] = inv == 0.0f ? 0u : pack16<KT>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
@@ -677,7 +777,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
         }
       }
-      if (x.nb > 0) {
+      if (x.nb > 0 && x.parts == 1) {
         fence_before();
         __syncwarp();
         if (lane == 0) kv_mbar_arrive(&s.o_empty[u]);
@@ -716,7 +816,15 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const PromptArgs& a
 
 }  // namespace
 
-int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, cudaStream_t st) {
+static constexpr size_t PART_BYTES = 2 * ROWS * 8 + 8 * 1024 * 16;
+
+// Room for the parts of any call of up to so many tokens: one part per SM, unless even one token has too many items to be cut.
+size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads) {
+  const int64_t least = (int64_t)kv_heads * ceil_div(q_heads / kv_heads, ROWS), sms = dev_info().sm_count;
+  return tokens > 0 && 2 * least <= sms ? (size_t)sms * PART_BYTES : 0;
+}
+
+int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, size_t ws_bytes, cudaStream_t st) {
   CUtensorMap km, vm;
   memcpy(&km, c->maps[0], sizeof km);
   memcpy(&vm, c->maps[1], sizeof vm);
@@ -748,10 +856,14 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, cudaStream
   a.q_neg = x.scale < 0.0f ? 1u : 0u;
   a.c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-30f);
   a.dev_status = x.dev_status;
-  // a sequence has at most one tile pair that is not full; which CTA has which is found on the device
+  // a sequence has at most one pair of tiles that is not full; which CTA has which, in how many parts, is found on the device
   const int64_t pairs = x.tokens / (2 * a.tile_tokens) + (x.seqs < x.tokens ? x.seqs : x.tokens);
-  a.items = pairs * a.kv_heads * a.blocks;
-  const int64_t sms = dev_info().sm_count, grid = a.items < sms ? a.items : sms;
+  const int64_t sms = dev_info().sm_count, items = pairs * a.kv_heads * a.blocks;
+  a.room = ws_bytes >= attn_decode_workspace_bytes() + (size_t)sms * PART_BYTES ? (int)sms : 0;
+  a.counters = attn_counters(ws);
+  a.part_o = reinterpret_cast<float4*>(attn_prompt_parts(ws));
+  a.part_ml = reinterpret_cast<float2*>(attn_prompt_parts(ws) + (size_t)sms * (8 * 1024 * 16));
+  const int64_t grid = a.room || items > sms ? sms : items;
   log_launch("attn_prompt_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%lld", a.tokens, a.q_heads, a.kv_heads,
              a.head_dim, a.window, (long long)grid);
   const bool two = a.head_dim > 64;

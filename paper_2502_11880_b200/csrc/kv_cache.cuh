@@ -59,9 +59,17 @@ struct AttnArgs {
   int dtype;
   int* dev_status;
 };
-size_t attn_decode_workspace_bytes(int64_t tokens, int q_heads, int kv_heads, int head_dim);
+// The workspace: counters that are zero between calls (of fixed number, so that no call's parts ever lie where another call's
+// counters are), the parts of decode rows, the parts of prompt items (where the caller gave the room for them).
+size_t attn_decode_parts_bytes();
+inline size_t attn_counters_bytes() { return 65536; }
+inline int* attn_counters(void* ws) { return static_cast<int*>(ws); }
+inline uint8_t* attn_decode_parts(void* ws) { return static_cast<uint8_t*>(ws) + attn_counters_bytes(); }
+inline uint8_t* attn_prompt_parts(void* ws) { return attn_decode_parts(ws) + attn_decode_parts_bytes(); }
+inline size_t attn_decode_workspace_bytes() { return attn_counters_bytes() + attn_decode_parts_bytes(); }
+size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads);
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
-int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, cudaStream_t st);
+int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, size_t ws_bytes, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
                      int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
@@ -160,6 +168,13 @@ __device__ __forceinline__ void kv_box_copy2(uint32_t dst, const CUtensorMap* ma
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
       "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(smem_u32(bar))
       : "memory");
+}
+
+// `bytes` contiguous bytes (a multiple of 16, both addresses too).
+__device__ __forceinline__ void kv_bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(smem_u32(bar))
+               : "memory");
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {

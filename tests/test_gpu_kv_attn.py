@@ -81,6 +81,9 @@ DECODE = [
     ([1000, 640, 3, 66], 8, 8, 100, 16, HF, F32, 100, 4),
     ([900, 130, 80], 8, 2, 64, 32, HF, HF, 63, 70),            # sinks over more than a tile
     ([900, 130, 80], 4, 2, 128, 8, BF, BF, 5, 2000),           # sinks beyond the context: everything
+    ([300, 70, 9], 6, 3, 72, 8, BF, F32, 0, 0),                # rows of an odd number of 16-byte pieces
+    ([300, 70, 1], 4, 4, 120, 256, HF, HF, 90, 3),
+    ([500, 64], 8, 1, 88, 32, BF, BF, 0, 0),
     ([400], 8, 2, 128, 8, BF, BF, 390, 9),                     # sinks meet the window's first tile
 ]
 
@@ -132,9 +135,10 @@ def test_decode_strided_queries_other_pool_order_and_stream():
     check_attn(out, p.ref(q, [332, 39, 6], range(3), 0.1, 0, 0), DECODE_P[BF, True])
 
 
-def test_decode_bad_pages_are_reported_and_not_read():
-    p = Paged([100, 50], 2, 64, 16, BF, seed=8)
-    q = p.queries(2, 4, 64, BF)
+@pytest.mark.parametrize("dim", [64, 100, 128])
+def test_decode_bad_pages_are_reported_and_not_read(dim):
+    p = Paged([100, 50], 2, dim, 16, BF, seed=8)
+    q = p.queries(2, 4, dim, BF)
     good = run_decode(p, q)
     for bad in (-1, p.cache.num_pages, 2 ** 31 - 1, -2 ** 31):
         table = p.table.clone()
@@ -142,7 +146,7 @@ def test_decode_bad_pages_are_reported_and_not_read():
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
         out = bn.bitnet_attn_decode(p.cache, p.layer, q, table, p.len, dev_status=status)
         torch.cuda.synchronize()
-        assert int(status) == 7 and torch.equal(out[1], good[1])
+        assert int(status) == 7 and torch.equal(out[1], good[1]) and torch.isfinite(out[0]).all()
 
 
 def test_decode_length_beyond_the_table_stops_at_its_end():
@@ -225,6 +229,47 @@ def test_prompt_single_tokens_agree_with_decode():
     start = torch.arange(4, dtype=torch.int32, device="cuda")
     a, b = run_prompt(p, q, start, 1, window=50, sinks=3), run_decode(p, q, window=50, sinks=3)
     assert torch.allclose(a.float(), b.float(), rtol=2 ** -7, atol=2 ** -7)
+
+
+SPLIT = [
+    # few rows over long contexts: the blocks of a tile go to several CTAs and are joined
+    ([(5000, 3)], 8, 2, 128, 64, BF, 0, 0),
+    ([(2000, 40), (0, 5), (700, 1), (3, 130)], 8, 2, 128, 16, HF, 0, 0),
+    ([(4100, 20)], 6, 1, 100, 32, HF, 1500, 7),
+    ([(1500, 60)], 4, 4, 64, 128, BF, 0, 0),
+]
+
+
+@pytest.mark.parametrize("room", [True, False])
+@pytest.mark.parametrize("spans,hq,hkv,dim,page,dtype,window,sinks", SPLIT)
+def test_prompt_parts(spans, hq, hkv, dim, page, dtype, window, sinks, room):
+    """With room for parts in the workspace and without; the workspace then serves decode, and the prompt again."""
+    p = Paged([b + n for b, n in spans], hkv, dim, page, dtype, seed=dim + 3)
+    start, seq, pos = prompt_args(spans)
+    q = p.queries(len(seq), hq, dim, dtype)
+    ws = bn.new_attn_workspace(len(seq) if room else 0, hq, hkv, dim)
+    most = max(n for _, n in spans)
+    call = lambda: bn.bitnet_attn_prompt(p.cache, p.layer, q, p.table, p.len, start, most, window=window, sinks=sinks, workspace=ws)
+    out = call()
+    check_attn(out, p.ref(q, pos, seq, dim ** -0.5, window, sinks), PROMPT_P[dtype])
+    last = q[start[1:].long() - 1].contiguous()
+    d = bn.bitnet_attn_decode(p.cache, p.layer, last, p.table, p.len, window=window, sinks=sinks, workspace=ws)
+    assert torch.equal(d, run_decode(p, last, window=window, sinks=sinks))
+    for _ in range(4):
+        assert torch.equal(call(), out)
+    assert int(ws[:bn.ATTN_WORKSPACE_HEAD].sum()) == 0
+
+
+def test_decode_one_workspace_for_calls_of_all_sizes():
+    big = Paged([900 + 7 * i for i in range(40)], 4, 64, 16, BF, seed=21)
+    small = Paged([30000], 1, 128, 64, HF, seed=22)
+    ws = bn.new_attn_workspace(0, 16, 4, 64)
+    qb, qs = big.queries(40, 16, 64, BF), small.queries(1, 4, 128, F32)
+    wb, wsm = run_decode(big, qb), run_decode(small, qs)
+    for _ in range(3):
+        assert torch.equal(bn.bitnet_attn_decode(small.cache, 1, qs, small.table, small.len, workspace=ws), wsm)
+        assert torch.equal(bn.bitnet_attn_decode(big.cache, 1, qb, big.table, big.len, workspace=ws), wb)
+    assert int(ws[:bn.ATTN_WORKSPACE_HEAD].sum()) == 0
 
 
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
