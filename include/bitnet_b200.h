@@ -407,8 +407,8 @@ int bitnet_tl_build_lut_debug(bitnet_fmt_t fmt, const int8_t* q_row, int64_t K, 
  * Paged key-value cache and the attention over it: what lies between the Q/K/V linear and the O linear of a decoder layer.
  *
  * A cache is two pools K and V [layers][num_pages][kv_heads][page_size][head_dim] of 16-bit values (any order of the outer
- * dimensions: the strides say where things are; a row is stride_row elements long, of which those beyond head_dim, up to the next
- * multiple of 8, may be read but are never used or written) and its books, which are plain device arrays of the caller:
+ * dimensions: the strides say where things are; a row takes head_dim elements rounded up to a multiple of 8, and what lies in the
+ * padding is never used, but copied with pages and cleared by appends) and its books, which are plain device arrays of the caller:
  *   table[seqs][table_width] int32   row s holds the pages of sequence s: its token at position p is row p % page_size of page
  *                                    table[s][p / page_size]; -1 = no page;
  *   kv_len[seqs] int32               tokens of each sequence;

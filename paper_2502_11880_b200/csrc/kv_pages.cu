@@ -80,44 +80,52 @@ struct AppendArgs {
   int* dev_status;
 };
 
-__device__ __forceinline__ uint2 to16(const float4& v, const __nv_bfloat16*) {
-  __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-  return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+__device__ __forceinline__ uint32_t to16(uint32_t lo, uint32_t hi, const __nv_bfloat16*) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint2 to16(const float4& v, const __half*) {
-  __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
-  return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+__device__ __forceinline__ uint32_t to16(uint32_t lo, uint32_t hi, const __half*) {
+  const __half2 v = __floats2half2_rn(__uint_as_float(lo), __uint_as_float(hi));
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// A warp takes up to 256 pieces of 4 elements of one new token's K or V: 8 per lane, all loaded before the look-ups of the token's
-// sequence, position and page, which do not depend on them, have come back one after the other.  IN32: fp32 rows, rounded once to the
-// cache's type; otherwise the bits move.  (32 tokens of 32 heads of 100: 10.6 us with a warp per row that looked up first and
-// loaded in turns.)
-template <typename KT, bool IN32>
+enum AppendIn { IN_F32, IN_16, IN_16_ALIGNED };
+
+// A warp takes up to 128 pieces of 8 elements of one new token's K or V: 4 per lane, all loaded before the look-ups of the token's
+// sequence, position and page, which do not depend on them, have come back one after the other.  fp32 rows are rounded
+// once to the cache's type; otherwise the bits move.  A row's last piece, where head_dim is no multiple of 8, ends with zeros in the
+// row's padding, so that whole sectors are written.  (32 tokens of 32 heads of 100: 10.6 us with a warp per row that looked up
+// first and loaded in turns.)
+template <typename KT, int IN>
 __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
-  const int quads = a.kv.head_dim >> 2, units = a.kv.kv_heads * quads, chunks = (units + 255) / 256;
+  const int pieces = (a.kv.head_dim + 7) >> 3, units = a.kv.kv_heads * pieces, chunks = (units + 127) / 128;
   const int64_t id = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int64_t token_pool = id / chunks;
   if (token_pool >= 2 * (int64_t)a.tokens) return;
   const int n = (int)(token_pool >> 1), pool = (int)(token_pool & 1);
-  const int u0 = (int)(id - token_pool * chunks) * 256 + lane;
+  const int u0 = (int)(id - token_pool * chunks) * 128 + lane;
 
-  const uint8_t* src = a.src[pool] + n * a.stride_token * (IN32 ? 4 : 2);
-  uint4 raw[8];
+  const uint8_t* src = a.src[pool] + n * a.stride_token * (IN == IN_F32 ? 4 : 2);
+  uint4 lo[4], hi[4];                                      // 8 fp32 values, or 8 of 16 bits in lo
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 4; ++j) {
     const int u = u0 + 32 * j;
+    lo[j] = hi[j] = make_uint4(0u, 0u, 0u, 0u);
     if (u < units) {
-      const int h = u / quads, d = (u - h * quads) * 4;
-      if (IN32) {
-        raw[j] = __ldg(reinterpret_cast<const uint4*>(src + (h * a.stride_head + d) * 4));
+      const int h = u / pieces, d = (u - h * pieces) * 8;
+      const bool full = d + 8 <= a.kv.head_dim;
+      const uint8_t* at = src + (h * a.stride_head + d) * (IN == IN_F32 ? 4 : 2);
+      if (IN == IN_F32) {
+        lo[j] = __ldg(reinterpret_cast<const uint4*>(at));
+        if (full) hi[j] = __ldg(reinterpret_cast<const uint4*>(at) + 1);
+      } else if (IN == IN_16_ALIGNED) {
+        lo[j] = __ldg(reinterpret_cast<const uint4*>(at));
       } else {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + (h * a.stride_head + d) * 2));
-        raw[j].x = w.x;
-        raw[j].y = w.y;
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(at)), y = full ? __ldg(reinterpret_cast<const uint2*>(at) + 1) : make_uint2(0u, 0u);
+        lo[j] = make_uint4(x.x, x.y, y.x, y.y);
       }
     }
   }
@@ -147,15 +155,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
   uint8_t* dst = (pool ? a.kv.v : a.kv.k) +
                  2 * (a.layer * a.kv.stride_layer + page * a.kv.stride_page + (pos & (a.kv.page_size - 1)) * a.kv.stride_row);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 4; ++j) {
     const int u = u0 + 32 * j;
     if (u < units) {
-      const int h = u / quads, d = (u - h * quads) * 4;
-      uint2 w = make_uint2(raw[j].x, raw[j].y);
-      if (IN32)
-        w = to16(make_float4(__uint_as_float(raw[j].x), __uint_as_float(raw[j].y), __uint_as_float(raw[j].z), __uint_as_float(raw[j].w)),
-                 (const KT*)nullptr);
-      *reinterpret_cast<uint2*>(dst + 2 * (h * a.kv.stride_head + d)) = w;
+      const int h = u / pieces, d = (u - h * pieces) * 8;
+      uint4 w = lo[j];
+      if (IN == IN_F32) {
+        const KT* t = nullptr;
+        w = make_uint4(to16(lo[j].x, lo[j].y, t), to16(lo[j].z, lo[j].w, t), to16(hi[j].x, hi[j].y, t), to16(hi[j].z, hi[j].w, t));
+      }
+      *reinterpret_cast<uint4*>(dst + 2 * (h * a.kv.stride_head + d)) = w;
     }
   }
 }
@@ -433,14 +442,15 @@ struct MoveArgs {
   int* dev_status;
 };
 
-// One block per (move, layer, pool) at a time; a thread moves pieces of VEC bytes of the rows.
-template <typename VEC>
+// A block takes `jobs` -- a move in one layer of one pool each -- one at a time where a page has many 16-byte pieces, otherwise as
+// many at a time as give every thread four: 4 per thread in flight carry the copy.  A row is copied with its padding up to a whole
+// piece (8-byte pieces of rows of 100 without it: 3.3 instead of 5.9 TB/s).
+template <bool LARGE>
 __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  constexpr int PER = sizeof(VEC) / 2;     // elements of a piece
   const int64_t moves = a.head ? a.head->moves : a.count;
-  const int pieces = a.kv.head_dim / PER;
+  const int pieces = (a.kv.head_dim + 7) >> 3;
   const int64_t jobs = moves * a.kv.layers * 2;
   if (a.parents) {
     const int lane = threadIdx.x & 31;
@@ -461,42 +471,78 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
       if (lane == 0) a.len[c] = (int)used;
     }
   }
-  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int pool = (int)(job & 1);
+  struct Job {
+    const uint8_t* from;
+    uint8_t* to;
+    int rows;
+  };
+  auto job_of = [&](int64_t job) -> Job {
     const int64_t ml = job >> 1, move = ml / a.kv.layers;
     const int layer = (int)(ml - move * a.kv.layers);
     int src, dst, rows = a.kv.page_size;
     if (a.head) {
-      src = a.moves[move].src;
-      dst = a.moves[move].dst;
-      rows = a.moves[move].rows;
+      const Move m = a.moves[move];
+      src = m.src;
+      dst = m.dst;
+      rows = m.rows;
     } else {
       src = a.src[move];
       dst = a.dst[move];
     }
     if (src < 0 || src >= a.kv.num_pages || dst < 0 || dst >= a.kv.num_pages) {
-      if (threadIdx.x == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-      continue;
+      if (a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+      return Job{nullptr, nullptr, 0};
     }
-    uint8_t* base = (pool ? a.kv.v : a.kv.k) + 2 * layer * a.kv.stride_layer;
-    const uint8_t* from = base + 2 * src * a.kv.stride_page;
-    uint8_t* to = base + 2 * dst * a.kv.stride_page;
-    const int units = a.kv.kv_heads * rows * pieces;
-    for (int u0 = threadIdx.x; u0 < units; u0 += 256 * 4) {
-      VEC w[4];
-      int64_t at[4];
+    uint8_t* base = (job & 1 ? a.kv.v : a.kv.k) + 2 * layer * a.kv.stride_layer;
+    return Job{base + 2 * src * a.kv.stride_page, base + 2 * dst * a.kv.stride_page, rows};
+  };
+  const int page_units = a.kv.kv_heads * a.kv.page_size * pieces;
+  if (LARGE) {
+    for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+      const Job x = job_of(job);
+      const int units = a.kv.kv_heads * x.rows * pieces;
+      for (int u0 = threadIdx.x; u0 < units; u0 += 256 * 4) {
+        uint4 w[4];
+        int64_t at[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int u = u0 + 256 * j;
+          if (u < units) {
+            const int hr = u / pieces, h = hr / x.rows;
+            at[j] = 2 * (h * a.kv.stride_head + (hr - h * x.rows) * a.kv.stride_row + (u - hr * pieces) * 8);
+            w[j] = *reinterpret_cast<const uint4*>(x.from + at[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (u0 + 256 * j < units) *reinterpret_cast<uint4*>(x.to + at[j]) = w[j];
+      }
+    }
+  } else {
+    const int64_t units = jobs * page_units;
+    for (int64_t base = (int64_t)blockIdx.x * 1024; base < units; base += (int64_t)gridDim.x * 1024) {
+      const int64_t job0 = base / page_units;
+      const int skip = (int)(base - job0 * page_units), end = (int)min((int64_t)1024, units - base) + skip;
+      uint4 w[4];
+      uint8_t* to[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int u = u0 + 256 * j;
-        if (u < units) {
-          const int hr = u / pieces, h = hr / rows;
-          at[j] = 2 * (h * a.kv.stride_head + (hr - h * rows) * a.kv.stride_row + (u - hr * pieces) * PER);
-          w[j] = *reinterpret_cast<const VEC*>(from + at[j]);
+        const int u = skip + (int)threadIdx.x + 256 * j;
+        to[j] = nullptr;
+        if (u < end) {
+          const int job = u / page_units;
+          const Job x = job_of(job0 + job);
+          const int v = u - job * page_units, hr = v / pieces, h = hr / a.kv.page_size, row = hr - h * a.kv.page_size;
+          if (row < x.rows) {
+            const int64_t at = 2 * (h * a.kv.stride_head + row * a.kv.stride_row + (v - hr * pieces) * 8);
+            w[j] = *reinterpret_cast<const uint4*>(x.from + at);
+            to[j] = x.to + at;
+          }
         }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (u0 + 256 * j < units) *reinterpret_cast<VEC*>(to + at[j]) = w[j];
+        if (to[j]) *reinterpret_cast<uint4*>(to[j]) = w[j];
     }
   }
   if (a.place)
@@ -556,12 +602,15 @@ PlanHead* plan_head(void* ws) { return static_cast<PlanHead*>(ws); }
 Move* plan_moves(void* ws) { return reinterpret_cast<Move*>(static_cast<uint8_t*>(ws) + sizeof(PlanHead)); }
 int32_t* plan_place(void* ws, int64_t moves) { return reinterpret_cast<int32_t*>(plan_moves(ws) + moves); }
 
-// 16-byte pieces where a head's row is a whole number of them, 8-byte pieces otherwise (every row is a multiple of 8 bytes).
+// Up to 32 blocks per SM, which the hardware deals out as others end (8 / 32 / 128 of them: compaction of 1.7 GB 312 / 280 / 275 us,
+// 128 forks of 0.6 GB 98 / 90 / 90 us); 16 where a page has fewer than 1024 pieces.
 int launch_move(const MoveArgs& a, int64_t jobs, cudaStream_t st) {
-  const int64_t most = (int64_t)dev_info().sm_count * 8;
+  const int page_units = a.kv.kv_heads * a.kv.page_size * ((a.kv.head_dim + 7) / 8);
+  const bool large = page_units >= 1024;
+  const int64_t most = (int64_t)dev_info().sm_count * (large ? 32 : 16);
   const unsigned grid = (unsigned)(jobs < 1 ? 1 : jobs < most ? jobs : most);
   log_launch("kv_move_kernel jobs=%lld grid=%u", (long long)jobs, grid);
-  return a.kv.head_dim % 8 == 0 ? launch(kv_move_kernel<uint4>, grid, 256, st, a) : launch(kv_move_kernel<uint2>, grid, 256, st, a);
+  return large ? launch(kv_move_kernel<true>, grid, 256, st, a) : launch(kv_move_kernel<false>, grid, 256, st, a);
 }
 
 }  // namespace
@@ -583,13 +632,17 @@ int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, 
   a.seqs = (int)seqs;
   a.layer = layer;
   a.dev_status = dev_status;
-  const int64_t chunks = ceil_div((int64_t)kv.kv_heads * (kv.head_dim / 4), 256), blocks = ceil_div(2 * tokens * chunks, 8);
+  const int64_t chunks = ceil_div((int64_t)kv.kv_heads * ceil_div(kv.head_dim, 8), 128), blocks = ceil_div(2 * tokens * chunks, 8);
   if (blocks > 0x7fffffff) return BITNET_ERR_UNSUPPORTED_SHAPE;
   const unsigned grid = (unsigned)blocks;
   log_launch("kv_append_kernel tokens=%lld grid=%u", (long long)tokens, grid);
-  if (in_dtype != BITNET_KV_F32) return launch(kv_append_kernel<__half, false>, grid, 256, st, a);   // same type: bits move
-  return dtype == BITNET_KV_BF16 ? launch(kv_append_kernel<__nv_bfloat16, true>, grid, 256, st, a)
-                                 : launch(kv_append_kernel<__half, true>, grid, 256, st, a);
+  if (in_dtype != BITNET_KV_F32) {
+    // same type: bits move, in 16-byte pieces where every row begins at a multiple of 16 bytes and is a whole number of them
+    const bool whole = kv.head_dim % 8 == 0 && stride_token % 8 == 0 && stride_head % 8 == 0 && aligned16(k) && aligned16(v);
+    return whole ? launch(kv_append_kernel<__half, IN_16_ALIGNED>, grid, 256, st, a) : launch(kv_append_kernel<__half, IN_16>, grid, 256, st, a);
+  }
+  return dtype == BITNET_KV_BF16 ? launch(kv_append_kernel<__nv_bfloat16, IN_F32>, grid, 256, st, a)
+                                 : launch(kv_append_kernel<__half, IN_F32>, grid, 256, st, a);
 }
 
 int launch_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* from_len,

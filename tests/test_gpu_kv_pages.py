@@ -25,10 +25,9 @@ class Books:
         self.full = [torch.randn(shape, generator=g, device="cuda").to(dtype) for _ in range(2)]
         pools = [t.permute(0, 1, 3, 2, 4) if nhd else t for t in self.full]
         self.k, self.v = (t[..., :dim] for t in pools)
-        self.pad = [t[..., dim:].clone() for t in pools]
-        self.pad_now = [t[..., dim:] for t in pools]
-        self.page, self.pages = page, pages
-        self.hk, self.hv = self.k.cpu().clone(), self.v.cpu().clone()
+        self.rows_k, self.rows_v = pools                   # rows with their padding, which pages carry along
+        self.page, self.pages, self.dim = page, pages, dim
+        self.hk, self.hv = self.rows_k.cpu().clone(), self.rows_v.cpu().clone()
         self.cache = bn.KvCache(self.k, self.v)
         self.refs, self.table, self.len = [0] * pages, [[-1] * width for _ in range(seqs)], [0] * seqs
         self.d_refs, self.d_table, self.d_len = i32(self.refs), i32(self.table), i32(self.len)
@@ -83,6 +82,12 @@ class Books:
         for s in range(len(self.table)):
             self.release(s, lambda e: e * self.page < sinks or (e + 1) * self.page > self.len[s] - window)
 
+    def put(self, layer, page, row, k, v):
+        """One token's rows; their padding becomes 0."""
+        for pool, x in ((self.hk, k), (self.hv, v)):
+            pool[layer, page, :, row] = 0
+            pool[layer, page, :, row, :self.dim] = x.to(pool.dtype).cpu()
+
     def compact(self):
         live = sum(r > 0 for r in self.refs)
         src = [i for i in range(live, self.pages) if self.refs[i] > 0]
@@ -100,10 +105,8 @@ class Books:
         assert self.d_refs.tolist() == self.refs
         assert self.d_table.tolist() == self.table
         assert self.d_len.tolist() == self.len
-        for now, want in ((self.k, self.hk), (self.v, self.hv)):
+        for now, want in ((self.rows_k, self.hk), (self.rows_v, self.hv)):
             assert torch.equal(now.cpu().view(torch.int16), want.view(torch.int16))
-        for now, before in zip(self.pad_now, self.pad):
-            assert torch.equal(now, before)            # the padding of rows is nobody's to write
         assert int(self.status) == status
 
 
@@ -228,8 +231,7 @@ def test_append(heads, page, dim, dtype, nhd, io32):
     for s, (a, n) in enumerate(spans):
         for j in range(n):
             p, row = b.table[s][(a + j) // page], (a + j) % page
-            b.hk[1, p, :, row] = k[start[s] + j].to(dtype).cpu()
-            b.hv[1, p, :, row] = v[start[s] + j].to(dtype).cpu()
+            b.put(1, p, row, k[start[s] + j], v[start[s] + j])
     bn.bitnet_kv_append(b.cache, 1, k, v, b.d_table, b.d_len, i32(start), dev_status=b.status)
     b.check()
     # one token each: no q_start
@@ -237,9 +239,21 @@ def test_append(heads, page, dim, dtype, nhd, io32):
     k, v = one[:, :heads * dim].view(-1, heads, dim), one[:, heads * dim:2 * heads * dim].view(-1, heads, dim)
     for s, (a, n) in enumerate(spans):
         p = a + n - 1
-        b.hk[0, b.table[s][p // page], :, p % page] = k[s].to(dtype).cpu()
-        b.hv[0, b.table[s][p // page], :, p % page] = v[s].to(dtype).cpu()
+        b.put(0, b.table[s][p // page], p % page, k[s], v[s])
     bn.bitnet_kv_append(b.cache, 0, k, v, b.d_table, b.d_len, dev_status=b.status)
+    b.check()
+
+
+def test_append_of_16_bit_rows_at_multiples_of_8_bytes():
+    b = Books(2, 1, 4, 3, 8, 24, seed=9)
+    b.table, b.len, b.refs = [[2], [0]], [3, 1], [1, 0, 1, 0]
+    b.load()
+    fused = torch.randn(2, 4 + 6 * 24 + 4, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(BF)
+    k, v = fused[:, 4:4 + 72].view(2, 3, 24), fused[:, 76:148].view(2, 3, 24)
+    assert k.data_ptr() % 16 == 8
+    b.put(1, 2, 2, k[0], v[0])
+    b.put(1, 0, 0, k[1], v[1])
+    bn.bitnet_kv_append(b.cache, 1, k, v, b.d_table, b.d_len, dev_status=b.status)
     b.check()
 
 
