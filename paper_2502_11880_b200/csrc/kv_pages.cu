@@ -554,17 +554,17 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
 
 // ------------------------------------------------------------------------------------------------ releasing
 // list: the rows to give up (null: rows 0..n-1).  trim: only pages wholly between the first `sinks` tokens and the last
-// `window`; otherwise the whole row, whose length becomes 0.  One warp per row; an entry is taken out by an exchange, so
-// a row that is listed twice is released once.
+// `window`; otherwise the whole row, whose length becomes 0.  One warp per 32 entries (a warp per row took 22 us for rows of 512); an
+// entry is taken out by an exchange, so a row that is listed twice is released once.
 __global__ void __launch_bounds__(256)
 kv_release_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* list, int64_t n,
                   int page_shift, int window, int sinks, int trim, int* dev_status) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
-  const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), chunks = (width + 31) / 32, i = id / chunks;
   if (i >= n) return;
-  const int64_t row = list ? list[i] : i;
+  const int64_t row = list ? list[i] : i, e = (id - i * chunks) * 32 + lane;
   if (row < 0 || row >= seqs) {
     if (lane == 0 && dev_status) atomicExch(dev_status, BITNET_ERR_BAD_PAGE);
     return;
@@ -574,13 +574,11 @@ kv_release_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
     first = ((int64_t)sinks + (1 << page_shift) - 1) >> page_shift;
     last = min(width, max((int64_t)0, (int64_t)len[row] - window) >> page_shift);
   }
-  for (int64_t e = first + lane; e < last; e += 32) {
-    if (table[row * width + e] < 0) continue;
+  if (e >= first && e < last && table[row * width + e] >= 0) {
     const int id = atomicExch(table + row * width + e, -1);
     if (id >= 0 && id < num_pages) atomicSub(refs + id, 1);
   }
-  __syncwarp();
-  if (!trim && lane == 0) len[row] = 0;
+  if (!trim && e == 0) len[row] = 0;
 }
 
 template <typename K, typename... A>
@@ -677,8 +675,10 @@ int launch_kv_fork(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs
 
 int launch_kv_release(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* list,
                       int64_t n, int page_size, int window, int sinks, bool trim, int* dev_status, cudaStream_t st) {
+  const int64_t blocks = ceil_div(n * ceil_div(width, 32), 8);
+  if (blocks > 0x7fffffff) return BITNET_ERR_UNSUPPORTED_SHAPE;
   log_launch("kv_release_kernel rows=%lld trim=%d", (long long)n, (int)trim);
-  return launch(kv_release_kernel, (unsigned)ceil_div(n, 8), 256, st, refs, (int)num_pages, table, seqs, width, len, list, n,
+  return launch(kv_release_kernel, (unsigned)blocks, 256, st, refs, (int)num_pages, table, seqs, width, len, list, n,
                 __builtin_ctz((unsigned)page_size), window, sinks, (int)trim, dev_status);
 }
 
