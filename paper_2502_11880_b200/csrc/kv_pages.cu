@@ -408,12 +408,23 @@ kv_compact_plan_kernel(int32_t* refs, int num_pages, int page_size, PlanHead* he
   }
   __threadfence();
   __syncthreads();
-  for (int i = threadIdx.x; i < tail; i += PLAN_THREADS) {
-    const int src = moves[i].src, dst = moves[i].dst;
-    moves[i].rows = page_size;
-    place[src] = dst;
-    refs[dst] = refs[src];
-    refs[src] = 0;
+  for (int i0 = threadIdx.x; i0 < tail; i0 += PLAN_THREADS * 4) {   // four at a time: their latencies overlap
+    Move m[4];
+    int count[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i0 + PLAN_THREADS * j < tail) m[j] = moves[i0 + PLAN_THREADS * j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i0 + PLAN_THREADS * j < tail) count[j] = refs[m[j].src];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i0 + PLAN_THREADS * j < tail) {
+        moves[i0 + PLAN_THREADS * j].rows = page_size;
+        place[m[j].src] = m[j].dst;
+        refs[m[j].dst] = count[j];
+        refs[m[j].src] = 0;
+      }
   }
   if (threadIdx.x == 0) {
     head->moves = tail;
