@@ -28,7 +28,7 @@ def desc(**kw):
 
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=2), 1), (dict(dtype=-1), 1), (dict(k=None), 1), (dict(v=4100), 1), (dict(kv_heads=0), 1), (dict(layers=0), 1),
-    (dict(num_pages=0), 1), (dict(page_size=24), 2), (dict(page_size=4), 2), (dict(page_size=1 << 21), 2), (dict(head_dim=0), 2),
+    (dict(num_pages=0), 1), (dict(page_size=24), 2), (dict(page_size=4), 2), (dict(kv_heads=256, page_size=1 << 20), 2), (dict(page_size=1 << 21), 2), (dict(head_dim=0), 2),
     (dict(head_dim=130, stride_row=136), 2), (dict(head_dim=66, stride_row=72), 2), (dict(stride_row=56), 1), (dict(stride_row=68), 1),
     (dict(stride_page=2052), 1), (dict(stride_head=-1024), 1), (dict(stride_layer=1 << 40), 1)])
 def test_handles_are_checked(L, change, code):
