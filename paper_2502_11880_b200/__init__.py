@@ -620,7 +620,7 @@ def bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim) -> int:
 
 def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
     """A workspace for bitnet_attn_decode and bitnet_attn_prompt calls, its counters zeroed.  tokens: the most new tokens of a prompt
-    call (0: decode calls only, 1.3 MB; otherwise some 60 MB for the parts of prompt calls with few rows)."""
+    call (0: decode calls only, 1.3 MB; otherwise 21 MB, for the parts of prompt calls with few rows)."""
     size = bitnet_attn_workspace_bytes(tokens, q_heads, kv_heads, head_dim)
     if size == 0:
         _check(1, "bitnet_attn_workspace_bytes")
