@@ -437,9 +437,11 @@ typedef struct bitnet_kv_cache {
   uint64_t ready;
   uint64_t maps[4][16];          /* how the tensor copies address the pools                                      */
   int64_t layer_pages;           /* > 0: a layer further is so many pages further (the third and fourth map)     */
+  int32_t device, reserved;      /* the pools' device: calls on another one are refused                         */
 } bitnet_kv_cache_t;
 
-/* Checks the description and completes it (host only; nothing is launched).  The handle stays valid while the pools stay
+/* Checks the description and completes it (host only; nothing is launched).  Every call that takes a handle has to be made with the
+ * pools' device current.  The handle stays valid while the pools stay
  * where they are; it may be copied, and shared by streams and threads. */
 int bitnet_kv_cache_init(bitnet_kv_cache_t* cache);
 

@@ -7,6 +7,7 @@ library is missing or fails to load, importing a symbol from here raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -500,7 +501,7 @@ class KvCacheDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32),
                 ("layers", C.c_int64), ("num_pages", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("stride_layer", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_row", C.c_int64),
-                ("ready", C.c_uint64), ("maps", C.c_uint64 * 64), ("layer_pages", C.c_int64)]
+                ("ready", C.c_uint64), ("maps", C.c_uint64 * 64), ("layer_pages", C.c_int64), ("device", C.c_int32), ("reserved", C.c_int32)]
 
 
 class KvCache:
@@ -560,6 +561,14 @@ def _st(stream):
     return None if stream is None else stream.cuda_stream
 
 
+_here = contextlib.nullcontext()
+
+
+def _on(stream):
+    """Calls that make tensors (results, workspaces) make them on the stream that they run on."""
+    return _here if stream is None else torch.cuda.stream(stream)
+
+
 def bitnet_kv_append(cache, layer, k, v, table, kv_len, q_start=None, dev_status=None, stream=None):
     """Writes new tokens' rows k, v [tokens][kv_heads][head_dim] into their pages; kv_len [seqs] counts them already."""
     (_fast or _binding()).kv_append(cache.ref, layer, k, v, table, kv_len, q_start, dev_status, _st(stream))
@@ -584,9 +593,10 @@ def new_kv_workspace(num_pages, n=0, device="cuda"):
 
 def bitnet_kv_fork(cache, refs, table, kv_len, parents, children, workspace=None, dev_status=None, stream=None):
     """Rows children[i] become copies of rows parents[i]: full pages shared, a page filled in part copied."""
-    if workspace is None:
-        workspace = new_kv_workspace(cache.num_pages, parents.shape[0], cache.device)
-    (_fast or _binding()).kv_fork(cache.ref, refs, table, kv_len, parents, children, workspace, dev_status, _st(stream))
+    with _on(stream):
+        if workspace is None:
+            workspace = new_kv_workspace(cache.num_pages, parents.shape[0], cache.device)
+        (_fast or _binding()).kv_fork(cache.ref, refs, table, kv_len, parents, children, workspace, dev_status, None)
 
 
 def bitnet_kv_free(refs, table, kv_len, rows, dev_status=None, stream=None):
@@ -601,9 +611,10 @@ def bitnet_kv_trim(refs, table, kv_len, page_size, window, sinks=0, stream=None)
 
 def bitnet_kv_compact(cache, refs, table, live=None, workspace=None, stream=None):
     """Moves the pages in use to the pool's first places; live (int32 [1], optional) receives their number."""
-    if workspace is None:
-        workspace = new_kv_workspace(cache.num_pages, 0, cache.device)
-    (_fast or _binding()).kv_compact(cache.ref, refs, table, live, workspace, _st(stream))
+    with _on(stream):
+        if workspace is None:
+            workspace = new_kv_workspace(cache.num_pages, 0, cache.device)
+        (_fast or _binding()).kv_compact(cache.ref, refs, table, live, workspace, None)
 
 
 def bitnet_kv_copy_pages(cache, src, dst, dev_status=None, stream=None):
@@ -629,24 +640,26 @@ def new_attn_workspace(tokens, q_heads, kv_heads, head_dim, device="cuda"):
     return ws
 
 
-def _attn_ws(cache, q):
-    """A workspace for one call; None where the call will refuse q anyway."""
+def _attn_ws(cache, q, prompt):
+    """A workspace for one call; None where the call will refuse q anyway, or has nothing to do."""
     if q.dim() != 3 or q.shape[0] == 0 or q.shape[1] == 0 or q.shape[1] % cache.kv_heads:
         return None
-    return new_attn_workspace(q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, cache.device)
+    return new_attn_workspace(prompt * q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, cache.device)
 
 
 def bitnet_attn_decode(cache, layer, q, table, kv_len, scale=None, window=0, sinks=0, out=None, workspace=None, dev_status=None,
                        stream=None):
     """Attention of one new token per sequence: q [seqs][q_heads][head_dim] (fp32 or the cache's type) -> out, same shape and type."""
-    return (_fast or _binding()).attn_decode(cache.ref, layer, q, table, kv_len, cache.scale if scale is None else scale, window, sinks, out,
-                                             _attn_ws(cache, q) if workspace is None else workspace, dev_status, _st(stream))
+    with _on(stream):
+        return (_fast or _binding()).attn_decode(cache.ref, layer, q, table, kv_len, cache.scale if scale is None else scale, window, sinks,
+                                                 out, _attn_ws(cache, q, 0) if workspace is None else workspace, dev_status, None)
 
 
 def bitnet_attn_prompt(cache, layer, q, table, kv_len, q_start, max_new, scale=None, window=0, sinks=0, out=None, workspace=None,
                        dev_status=None, stream=None):
     """Attention of prompts or chunks of prompts: q [tokens][q_heads][head_dim] in the cache's type; sequence s has the tokens
     q_start[s] .. q_start[s + 1] - 1 (at most max_new), the last of them at position kv_len[s] - 1."""
-    return (_fast or _binding()).attn_prompt(cache.ref, layer, q, table, kv_len, q_start, max_new, cache.scale if scale is None else scale,
-                                             window, sinks, out, _attn_ws(cache, q) if workspace is None else workspace, dev_status,
-                                             _st(stream))
+    with _on(stream):
+        return (_fast or _binding()).attn_prompt(cache.ref, layer, q, table, kv_len, q_start, max_new, cache.scale if scale is None else scale,
+                                                 window, sinks, out, _attn_ws(cache, q, 1) if workspace is None else workspace, dev_status,
+                                                 None)

@@ -16,6 +16,10 @@
 //     than 2^8 (P and the sums stay below 2^8 times their range, which fp32 and both 16-bit types hold), so rarely;
 //   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
 //     place between the sinks and the window), since 0 * NaN would reach O.
+// Bound by a tile's chain per block -- about 1630 cycles of softmax, 1024 of products, 650 until signals are seen -- of which two run in
+// turn: 3300 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 855 us = 0.96
+// PFLOP/s at the 1.34 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 92 us).  Blocks of 64 tokens with two
+// buffers of S, P through shared memory, two threads per row, P in halves or a lane per tile that issues were each slower.
 // Blocks that no row sees are not visited: those of the sinks, then those from the first row's window to the last row.
 // Exponentials: the unit that takes them does 16 per SM and cycle, which for head_dim 128 is as long as both products take;
 // a share of the columns goes through a polynomial on the fp32 units instead (2^x = 2^n * p(x - n), degree 4, relative error

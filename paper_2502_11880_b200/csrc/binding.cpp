@@ -7,6 +7,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -36,9 +37,13 @@ struct Refused {};                 // a Python exception is set
   throw Refused{};
 }
 
+thread_local int g_device;         // the current one, for this call
+
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) refuse(name, "expected a tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.is_cuda() && t.get_device() != g_device) refuse(name, "on another device than the current one");
+  return t;
 }
 int64_t integer(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
@@ -111,6 +116,8 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   }
   try {
+    c10::DeviceIndex current = -1;
+    g_device = c10::cuda::GetDevice(&current) == cudaSuccess ? current : -1;
     return F(a);
   } catch (const Refused&) {
     return nullptr;

@@ -18,16 +18,23 @@ int64_t clamp_int(int64_t x) { return x < MOST ? x : MOST; }
 
 // The books: table[seqs][width] and refs[num_pages].
 int check_books(const int32_t* refs, int64_t num_pages, const int32_t* table, int64_t seqs, int64_t width) {
-  if (!ints(refs) || !ints(table) || num_pages < 1 || num_pages > MOST || seqs < 1 || seqs > MOST || width < 1 || width > MOST)
-    return BITNET_ERR_INVALID_ARG;
-  return BITNET_OK;
+  if (!ints(refs) || num_pages < 1 || num_pages > MOST || seqs < 0 || seqs > MOST || width < 1 || width > MOST) return BITNET_ERR_INVALID_ARG;
+  return seqs == 0 || ints(table) ? BITNET_OK : BITNET_ERR_INVALID_ARG;
 }
-int check_cache(const bitnet_kv_cache_t* c) { return c && c->ready == READY ? BITNET_OK : BITNET_ERR_INVALID_ARG; }
+int check_cache(const bitnet_kv_cache_t* c) {
+  if (!c || c->ready != READY) return BITNET_ERR_INVALID_ARG;
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return note_cuda_error(e);
+  return dev == c->device ? BITNET_OK : BITNET_ERR_INVALID_ARG;
+}
 int check_tokens(const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start, int64_t tokens, int64_t seqs,
                  const int* dev_status) {
-  if (!ints(table) || !ints(kv_len) || !ints_or_null(q_start) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
-  if (width < 1 || width > MOST || seqs < 1 || seqs > MOST || tokens < 0 || tokens > MOST) return BITNET_ERR_INVALID_ARG;
+  if (seqs < 0 || seqs > MOST || tokens < 0 || tokens > MOST || !ints_or_null(q_start) || !ints_or_null(dev_status))
+    return BITNET_ERR_INVALID_ARG;
   if (!q_start && tokens != seqs) return BITNET_ERR_INVALID_ARG;
+  if (tokens == 0) return BITNET_OK;      // nothing to do, whatever else there is
+  if (!ints(table) || !ints(kv_len) || width < 1 || width > MOST || seqs < 1) return BITNET_ERR_INVALID_ARG;
   return BITNET_OK;
 }
 
@@ -81,6 +88,13 @@ int bitnet_kv_cache_init(bitnet_kv_cache_t* c) {
   for (int64_t s : strides)
     if (s < 0 || s % 8 || s >= (int64_t)1 << 38) return BITNET_ERR_INVALID_ARG;
   if (c->stride_row < c->head_dim) return BITNET_ERR_INVALID_ARG;
+  cudaPointerAttributes k_at, v_at;
+  cudaError_t e = cudaPointerGetAttributes(&k_at, c->k);
+  if (e == cudaSuccess) e = cudaPointerGetAttributes(&v_at, c->v);
+  if (e != cudaSuccess) return note_cuda_error(cudaGetLastError());
+  if ((k_at.type != cudaMemoryTypeDevice && k_at.type != cudaMemoryTypeManaged) || k_at.type != v_at.type || k_at.device != v_at.device)
+    return BITNET_ERR_INVALID_ARG;
+  c->device = k_at.device;
   const int rc = encode_kv_maps(c->maps, &c->layer_pages, kv_view(c), c->dtype);
   if (rc == BITNET_OK) c->ready = READY;
   return rc;
@@ -106,8 +120,9 @@ int bitnet_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t 
                       const int32_t* to_len, int64_t page_size, int* dev_status, void* stream) {
   const int rc = check_books(refs, num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (!ints(from_len) || !ints(to_len) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   if (!page_size_ok(page_size)) return BITNET_ERR_UNSUPPORTED_SHAPE;
+  if (seqs == 0) return BITNET_OK;
+  if (!ints(from_len) || !ints(to_len) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_reserve(refs, num_pages, table, seqs, table_width, from_len, to_len, (int)page_size, dev_status, (cudaStream_t)stream);
 }
 
@@ -123,8 +138,9 @@ int bitnet_kv_fork(const bitnet_kv_cache_t* c, int32_t* refs, int32_t* table, in
   if (rc) return rc;
   rc = check_books(refs, c->num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (!ints(kv_len) || !ints(parents) || !ints(children) || !ints_or_null(dev_status) || n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
+  if (n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
   if (n == 0) return BITNET_OK;
+  if (seqs < 1 || !ints(kv_len) || !ints(parents) || !ints(children) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < kv_workspace_bytes(1, n)) return BITNET_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_fork(kv_view(c), refs, table, seqs, table_width, kv_len, parents, children, n, workspace, dev_status,
@@ -135,8 +151,9 @@ int bitnet_kv_free(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seq
                    const int32_t* list, int64_t n, int* dev_status, void* stream) {
   const int rc = check_books(refs, num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (!ints(kv_len) || !ints(list) || !ints_or_null(dev_status) || n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
+  if (n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
   if (n == 0) return BITNET_OK;
+  if (seqs < 1 || !ints(kv_len) || !ints(list) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_release(refs, num_pages, table, seqs, table_width, kv_len, list, n, 8, 0, 0, false, dev_status, (cudaStream_t)stream);
 }
 
@@ -144,8 +161,10 @@ int bitnet_kv_trim(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seq
                    int64_t page_size, int64_t window, int64_t sinks, void* stream) {
   const int rc = check_books(refs, num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (!ints(kv_len) || window < 1 || sinks < 0) return BITNET_ERR_INVALID_ARG;
+  if (window < 1 || sinks < 0) return BITNET_ERR_INVALID_ARG;
   if (!page_size_ok(page_size)) return BITNET_ERR_UNSUPPORTED_SHAPE;
+  if (seqs == 0) return BITNET_OK;
+  if (!ints(kv_len)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_release(refs, num_pages, table, seqs, table_width, const_cast<int32_t*>(kv_len), nullptr, seqs, (int)page_size,
                            (int)clamp_int(window), (int)clamp_int(sinks), true, nullptr, (cudaStream_t)stream);
 }
@@ -186,6 +205,7 @@ int bitnet_attn_decode(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
                            scale, window, sinks, out, workspace, dev_status, &a);
   if (rc) return rc;
   if (io_dtype != BITNET_KV_F32 && io_dtype != c->dtype) return BITNET_ERR_INVALID_ARG;
+  if (seqs == 0) return BITNET_OK;
   if (!workspace || workspace_bytes < attn_decode_workspace_bytes()) return BITNET_ERR_WORKSPACE;
   return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
 }

@@ -313,6 +313,22 @@ def test_prompt_strided_queries_negative_positions_and_stream():
     check_attn(out, p.ref(q, pos, [0] * 9 + [1] * 31, 0.125, 0, 0), PROMPT_P[HF])
 
 
+def test_calls_without_workspace_on_another_stream():
+    """The result and the workspace that the call makes belong to the stream that it runs on."""
+    p = Paged([3000], 2, 128, 16, BF, seed=16)
+    q = p.queries(1, 8, 128, BF)
+    start = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    want, side = run_decode(p, q), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        out = bn.bitnet_attn_decode(p.cache, p.layer, q, p.table, p.len, stream=side)
+        junk = torch.full((1 << 22,), 7, dtype=torch.int32, device="cuda")     # would land in memory given back too early
+        out2 = bn.bitnet_attn_prompt(p.cache, p.layer, q, p.table, p.len, start, 1, stream=side)
+        side.synchronize()
+        assert torch.equal(out, want) and torch.equal(out2, want)
+        del junk, out, out2
+
+
 def test_refusals():
     p = Paged([20], 2, 64, 16, BF, seed=13)
     q = p.queries(1, 4, 64, BF)
@@ -353,6 +369,7 @@ def test_refusals():
     x = torch.zeros(1, 4, 2, 16, 100, dtype=BF, device="cuda")
     with pytest.raises(bn.BitnetError):
         bn.KvCache(x, x.clone())                                                     # rows of 200 bytes
+    assert bn.bitnet_attn_decode(p.cache, 0, q[:0], p.table[:0], p.len[:0]).shape == (0, 4, 64)
     empty = torch.empty(0, 4, 64, dtype=BF, device="cuda")
     none = torch.zeros(2, dtype=torch.int32, device="cuda")
     assert bn.bitnet_attn_prompt(p.cache, 0, empty, p.table, p.len, none, 0).shape == (0, 4, 64)

@@ -329,6 +329,16 @@ def test_refusals():
         bn.bitnet_kv_fork(b.cache, b.d_refs[:3], b.d_table, b.d_len, one, i32([1]))
     with pytest.raises(bn.BitnetError):
         bn.bitnet_kv_copy_pages(b.cache, one, i32([1, 2]))
+    none = torch.empty(0, 2, dtype=torch.int32, device="cuda")
+    nothing = torch.empty(0, dtype=torch.int32, device="cuda")
+    bn.bitnet_kv_reserve(b.d_refs, none, nothing, nothing, 8)                        # nothing to do
+    bn.bitnet_kv_trim(b.d_refs, none, nothing, 8, 5)
+    bn.bitnet_kv_free(b.d_refs, b.d_table, b.d_len, nothing)
+    bn.bitnet_kv_fork(b.cache, b.d_refs, b.d_table, b.d_len, nothing, nothing)
+    bn.bitnet_kv_copy_pages(b.cache, nothing, nothing)
+    bn.bitnet_kv_append(b.cache, 0, torch.empty(0, 1, 8, device="cuda"), torch.empty(0, 1, 8, device="cuda"), none, nothing)
+    with pytest.raises(bn.BitnetError):
+        bn.KvCache(torch.zeros(1, 2, 1, 8, 8, dtype=BF, device="cuda"), torch.zeros(1, 2, 1, 8, 8, dtype=BF))
     x = torch.zeros(2, 1, 8, device="cuda")
     with pytest.raises(bn.BitnetError):
         bn.bitnet_kv_append(b.cache, 2, x, x, b.d_table, b.d_len)                    # no such layer

@@ -51,7 +51,8 @@ def test_calls_refuse_handles_that_were_not_initialised(L):
 def test_books_are_checked(L):
     assert L.bitnet_kv_reserve(NULL, 8, FAKE, 1, 4, FAKE, FAKE, 16, NULL, NULL) == 1
     assert L.bitnet_kv_reserve(FAKE, 0, FAKE, 1, 4, FAKE, FAKE, 16, NULL, NULL) == 1
-    assert L.bitnet_kv_reserve(FAKE, 8, FAKE, 0, 4, FAKE, FAKE, 16, NULL, NULL) == 1
+    assert L.bitnet_kv_reserve(FAKE, 8, FAKE, -1, 4, FAKE, FAKE, 16, NULL, NULL) == 1
+    assert L.bitnet_kv_reserve(FAKE, 8, NULL, 0, 4, NULL, NULL, 16, NULL, NULL) == 0   # no rows
     assert L.bitnet_kv_reserve(FAKE, 8, FAKE, 1, 4, ODD, FAKE, 16, NULL, NULL) == 1
     assert L.bitnet_kv_reserve(FAKE, 8, FAKE, 1, 4, FAKE, FAKE, 10, NULL, NULL) == 2
     assert L.bitnet_kv_free(FAKE, 8, FAKE, 1, 4, FAKE, NULL, 1, NULL, NULL) == 1
