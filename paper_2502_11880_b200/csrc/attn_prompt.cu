@@ -11,8 +11,8 @@
 //     swizzle) into two rings;
 //   * warp 9: one lane issues tcgen05.mma -- S = Q K^T from shared memory, O += P V with P in tensor memory -- for the two
 //     tiles in turn, so that the tensor cores work on one tile while the other tile's exponentials are taken;
-//   * warps 0-3 and 4-7, one thread per row: S from tensor memory (once for the maximum, once for the exponentials), P back
-//     into the tensor-memory columns that S had, rows of O at the end.  O is rescaled only when a row's maximum has risen by more
+//   * warps 0-3 and 4-7, one thread per row: S from tensor memory, maximum, exponentials, P back into the tensor-memory
+//     columns that S had, rows of O at the end.  O is rescaled only when a row's maximum has risen by more
 //     than 2^8 (P and the sums stay below 2^8 times their range, which fp32 and both 16-bit types hold), so rarely;
 //   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
 //     place between the sinks and the window), since 0 * NaN would reach O.
@@ -44,8 +44,8 @@ constexpr int STAGES = 2;                     // of K, and of V
 constexpr int PART_BLOCKS = 4;                // fewest blocks of a part of an item
 constexpr float LAZY = 8.0f;                  // log2 of how far a maximum may rise before O is rescaled
 
-constexpr int POLY_EVERY = 4;                 // every fourth pair of columns takes the polynomial (none / 8th / 4th / 2nd pair measured
-                                              // 97 / 94 / 94 / 100 us on chunks of 4 x 512 tokens)
+constexpr int POLY_EVERY = 8;                 // every so-manieth pair of columns takes the polynomial (none / 16th / 8th / 4th: 842 / 849 /
+                                              // 831 / 854 us for the 8192 tokens above)
 
 static __device__ int g_prompt_error = 0;
 
@@ -202,6 +202,16 @@ __device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
                      __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
 }
 
+// Bits of the columns below n, of 32.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// -inf in those of 32 columns from c that a row at position p does not see.  (Selects by bits: compared column by column, with
+// branches, an edge block took as long as ten others.)
+__device__ __forceinline__ void hide_columns(uint32_t* x, int c, int p, int wlo, int sinks) {
+  const uint32_t see = bits_below(p - c + 1) & (~bits_below(wlo - c) | bits_below(sinks - c));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = see & (1u << i) ? x[i] : 0xff800000u;
+}
+
 // What a CTA works on at a time.
 struct Item {
   int seq, head_kv, head0, heads;   // heads: query heads of the rows, from head0
@@ -215,7 +225,7 @@ struct Item {
   int two;                          // the second tile has rows
   int parts;                        // of the item, which join if there are several
   int part;
-  int64_t unit0, id;                // the first part's place in the workspace, the item's number
+  int64_t unit0, id;                // the first part's place in the workspace, the item's number among those cut
 };
 
 template <int HALVES>
@@ -307,9 +317,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const bool mine = half < HALVES;
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
       uint32_t kb = 0;                                       // blocks so far
-      // With few items for the SMs the blocks of an item go to several CTAs: as many as make one part per SM at most (more of
-      // them, and the joins cost more than the SMs give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM
-      // 76, 191, 353 us)
+      // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
+      // into parts of their blocks: as many as make one part per SM at most (more of them, and the joins cost more than the SMs
+      // give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM 76, 191, 353 us)
       int64_t pairs = 0;
       for (int s0 = 0; s0 < a.seqs; s0 += 32) {
         const int i = s0 + lane;
@@ -319,20 +329,22 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
       for (int d = 16; d; d >>= 1) pairs += __shfl_xor_sync(0xffffffffu, pairs, d);
       const int64_t items = pairs * a.kv_heads * a.blocks;
-      const int parts = items > 0 && 2 * items <= a.room ? (int)(a.room / items) : 1;
+      const int64_t uncut = a.room ? items / a.room * a.room : items, rest = items - uncut;
+      const int parts = rest > 0 ? max(1, (int)(a.room / rest)) : 1;
       int64_t unit = blockIdx.x;
       for (int it = 0;; unit += gridDim.x) {
         kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
         const int heads = a.kv_heads * a.blocks, span = 2 * a.tile_tokens;
-        const int64_t id = unit / parts, want = id / heads;
-        const int hb = (int)(id % heads), part = (int)(unit % parts);
+        const bool whole = unit < uncut;
+        const int64_t id = whole ? unit : uncut + (unit - uncut) / parts, want = id / heads;
+        const int hb = (int)(id % heads), part = whole ? 0 : (int)((unit - uncut) % parts);
         if (lane == 0) s.item[it & 1].nb = -1;
         __syncwarp();
         bool found = false;
         int64_t before = 0;
-        for (int s1 = unit < items * parts && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
+        for (int s1 = unit < uncut + rest * parts && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
           const int i = s1 - 1 - lane;
           const int q0 = i >= 0 ? __ldg(a.q_start + i) : 0;
           const int n = i >= 0 ? max(0, __ldg(a.q_start + i + 1) - q0) : 0;
@@ -361,16 +373,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
             t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
             t.n0 = t.t1 = t.b0 = t.nb = 0;
-            t.unit0 = id * parts;
+            t.unit0 = (id - uncut) * parts;                   // (used by cut items only)
             t.part = part;
-            t.id = id;
+            t.id = id - uncut;
             int all = 0;
             if (t.p_last >= 0) {
               t.t1 = t.lo / KB;
               t.n0 = min((min(a.sinks, t.lo) + KB - 1) / KB, t.t1);
               all = t.n0 + t.p_last / KB + 1 - t.t1;
             }
-            t.parts = max(1, min(parts, all / PART_BLOCKS));
+            t.parts = whole ? 1 : max(1, min(parts, all / PART_BLOCKS));
             if (part < t.parts) {
               t.b0 = (int)((int64_t)all * part / t.parts);
               t.nb = (int)((int64_t)all * (part + 1) / t.parts) - t.b0;
@@ -584,38 +596,34 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;                          // first token of its window
       float m = -INFINITY;
       uint64_t l2 = 0;                                        // a pair of sums
-      uint32_t v[64];
+      uint32_t v[64], w[64];
       for (int j = 0; j < x.nb; ++j, ++s_cnt) {
         const int c0 = block_start(x, j);
         const bool edge = __any_sync(0xffffffffu, c0 + KB - 1 > p || (c0 < wlo && c0 + KB > a.sinks));
         kv_mbar_wait(&s.s_full[u], s_cnt & 1u, abort_flag, &g_prompt_error);
         fence_after();
-        // ---- the row's maximum; a block at an edge goes back with -inf where the row does not see
+        // ---- the row, -inf where it does not see, and its maximum
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        tm_ld32(s_addr, v);
-        tm_ld32(s_addr + 32, v + 32);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          wait_ld<64>(v);
-          if (edge) {
-            const int hi = p - c0 - 64 * g, lo = wlo - c0 - 64 * g, sk = a.sinks - c0 - 64 * g;
-#pragma unroll
-            for (int i = 0; i < 64; ++i)
-              if (!(i <= hi && (i >= lo || i < sk))) v[i] = 0xff800000u;
-            tm_st32(s_addr + 64 * g, v);
-            tm_st32(s_addr + 64 * g + 32, v + 32);
-          }
+        tm_ld32(s_addr, w);
+        tm_ld32(s_addr + 32, w + 32);
+        wait_ld<64>(w);
+        tm_ld32(s_addr + 64, v);
+        tm_ld32(s_addr + 96, v + 32);
+        auto mask = [&](uint32_t* x, int c) {
+          hide_columns(x, c, p, wlo, a.sinks);
+          hide_columns(x + 32, c + 32, p, wlo, a.sinks);
+        };
+        auto maxima = [&](const uint32_t* x) {
 #pragma unroll
           for (int i = 0; i < 64; i += 8)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], __uint_as_float(v[i + 2 * k])), __uint_as_float(v[i + 2 * k + 1]));
-          if (g == 0) {
-            tm_ld32(s_addr + 64, v);
-            tm_ld32(s_addr + 96, v + 32);
-          }
-        }
-        if (edge) wait_st();
-        tm_ld32(s_addr, v);                                   // on its way again for the exponentials
+            for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], __uint_as_float(x[i + 2 * k])), __uint_as_float(x[i + 2 * k + 1]));
+        };
+        if (edge) mask(w, c0);
+        maxima(w);
+        wait_ld<64>(v);
+        if (edge) mask(v, c0 + 64);
+        maxima(v);
         const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         const float m_new = fmaxf(m, big * a.c);
         if (__any_sync(0xffffffffu, m_new > m + LAZY)) {
@@ -636,11 +644,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         }
         const float ref = m == -INFINITY ? 0.0f : m;
         const uint64_t r2 = pair(-ref, -ref);
-        // ---- exponentials of 32 columns, which become 16 of P; the next 32 are on their way meanwhile
-        auto exps = [&](uint32_t* w) {
+        // ---- exponentials of 64 columns, which become 32 of P
+        auto exps = [&](uint32_t* x) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const uint64_t e = fma2(pair(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), c2, r2);
+          for (int i = 0; i < 64; i += 2) {
+            const uint64_t e = fma2(pair(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), c2, r2);
             float2 y;
             if ((i >> 1) % POLY_EVERY == POLY_EVERY - 1) {
               y = exp2_poly(e);
@@ -650,20 +658,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
               y.y = exp2_approx(y.y);
             }
             l2 = add2(l2, pair(y.x, y.y));
-            w[i >> 1] = pack16<KT>(y.x, y.y);
+            x[i >> 1] = pack16<KT>(y.x, y.y);
           }
         };
-#pragma unroll 1
-        for (int g = 0; g < 2; ++g) {
-          wait_ld<32>(v);
-          tm_ld32(s_addr + 64 * g + 32, v + 32);
-          exps(v);
-          tm_st16(s_addr + 32 * g, v);                        // (over columns of S that have been read)
-          wait_ld<32>(v + 32);
-          if (g == 0) tm_ld32(s_addr + 64, v);
-          exps(v + 32);
-          tm_st16(s_addr + 32 * g + 16, v + 32);
-        }
+        exps(v);
+        tm_st32(s_addr + 32, v);
+        exps(w);
+        tm_st32(s_addr, w);
         wait_st();
         fence_before();
         __syncwarp();
@@ -764,9 +765,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
         for (int k = 0; k < 4; ++k) stage[lane * 4 + (k ^ ((lane >> 1) & 3))] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         __syncwarp();
-        uint4 w[4];
+        uint4 y[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = stage[(8 * k + (lane >> 2)) * 4 + (piece ^ ((lane >> 3) & 3))];
+        for (int k = 0; k < 4; ++k) y[k] = stage[(8 * k + (lane >> 2)) * 4 + (piece ^ ((lane >> 3) & 3))];
         __syncwarp();
         const int left = a.head_dim - i - piece * 8;          // columns from this piece on
 #pragma unroll
@@ -774,10 +775,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           uint8_t* const dst = a.out + 2 * (to[k] + i);
           if (to[k] < 0 || left <= 0) continue;
           if (wide) {
-            *reinterpret_cast<uint4*>(dst) = w[k];
+            *reinterpret_cast<uint4*>(dst) = y[k];
           } else {
-            *reinterpret_cast<uint2*>(dst) = make_uint2(w[k].x, w[k].y);
-            if (left > 4) *reinterpret_cast<uint2*>(dst + 8) = make_uint2(w[k].z, w[k].w);
+            *reinterpret_cast<uint2*>(dst) = make_uint2(y[k].x, y[k].y);
+            if (left > 4) *reinterpret_cast<uint2*>(dst + 8) = make_uint2(y[k].z, y[k].w);
           }
         }
       }

@@ -237,6 +237,7 @@ SPLIT = [
     ([(2000, 40), (0, 5), (700, 1), (3, 130)], 8, 2, 128, 16, HF, 0, 0),
     ([(4100, 20)], 6, 1, 100, 32, HF, 1500, 7),
     ([(1500, 60)], 4, 4, 64, 128, BF, 0, 0),
+    ([(1100, 9), (900, 3)], 160, 80, 32, 16, HF, 0, 0),        # 160 items: one for each SM, and some that are cut
 ]
 
 
