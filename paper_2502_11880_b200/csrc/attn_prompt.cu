@@ -63,6 +63,7 @@ struct PromptArgs {
   int head_dim, page_shift, num_pages, layer;
   int window, sinks, max_len;
   float c;                                            // |scale| * log2(e), above 0 so that -inf stays -inf
+  int q_wide;                                         // rows of q are whole 16-byte pieces
   uint32_t q_neg;                                     // scale < 0: the products take -Q
   int room;                                           // parts of items that the workspace has room for
   int* counters;                                      // [items][8 warps]: parts that have arrived; zero between calls
@@ -320,12 +321,24 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
       // into parts of their blocks: as many as make one part per SM at most (more of them, and the joins cost more than the SMs
       // give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM 76, 191, 353 us)
-      int64_t pairs = 0;
-      for (int s0 = 0; s0 < a.seqs; s0 += 32) {
-        const int i = s0 + lane;
-        const int n = i < a.seqs ? max(0, __ldg(a.q_start + i + 1) - __ldg(a.q_start + i)) : 0;
-        pairs += (n + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens);
-      }
+      // A lane's sequence among the 32 that end before s1: first token, tokens, context.  (Those of the last 32 are kept: with
+      // look-ups for every item the first one was there 2.6 us after the start.)
+      struct Seq {
+        int i, q0, n, len;
+      };
+      auto seq_at = [&](int s1) -> Seq {
+        Seq q = {s1 - 1 - lane, 0, 0, 0};
+        if (q.i >= 0) {
+          q.q0 = __ldg(a.q_start + q.i);
+          q.n = max(0, __ldg(a.q_start + q.i + 1) - q.q0);
+          q.len = __ldg(a.kv_len + q.i);
+        }
+        return q;
+      };
+      const Seq tail = seq_at(a.seqs);
+      const int span = 2 * a.tile_tokens;
+      int64_t pairs = (tail.n + span - 1) / span;
+      for (int s1 = a.seqs - 32; s1 > 0; s1 -= 32) pairs += (seq_at(s1).n + span - 1) / span;
 #pragma unroll
       for (int d = 16; d; d >>= 1) pairs += __shfl_xor_sync(0xffffffffu, pairs, d);
       const int64_t items = pairs * a.kv_heads * a.blocks;
@@ -336,7 +349,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
-        const int heads = a.kv_heads * a.blocks, span = 2 * a.tile_tokens;
+        const int heads = a.kv_heads * a.blocks;
         const bool whole = unit < uncut;
         const int64_t id = whole ? unit : uncut + (unit - uncut) / parts, want = id / heads;
         const int hb = (int)(id % heads), part = whole ? 0 : (int)((unit - uncut) % parts);
@@ -345,9 +358,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         bool found = false;
         int64_t before = 0;
         for (int s1 = unit < uncut + rest * parts && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
-          const int i = s1 - 1 - lane;
-          const int q0 = i >= 0 ? __ldg(a.q_start + i) : 0;
-          const int n = i >= 0 ? max(0, __ldg(a.q_start + i + 1) - q0) : 0;
+          const Seq q = s1 == a.seqs ? tail : seq_at(s1);
+          const int i = q.i, q0 = q.q0, n = q.n;
           const int64_t tiles = (n + span - 1) / span;
           int64_t sum = tiles;
 #pragma unroll
@@ -368,7 +380,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             t.n_new = n;
             t.tok0 = (int)(tiles - 1 - (want - excl)) * span;
             t.two = t.tok0 + a.tile_tokens < n;
-            const int64_t pos0 = (int64_t)__ldg(a.kv_len + i) - n, most = a.max_len - 1;
+            const int64_t pos0 = (int64_t)q.len - n, most = a.max_len - 1;
             t.pos0 = (int)pos0;                              // |pos0| < 2^31
             t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
             t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
@@ -517,7 +529,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // ---------------------------------------------------------- Q of the next item; V rows that no query sees count as 0
       const int t = tid - (SOFT_WARPS + 2) * 32;              // 0..63
       const int u = t >> 5;
-      constexpr int LANES = HALVES * 16, PER = 32 / LANES;    // lanes per row of Q (8 bytes each), rows at a time
+      // 16 bytes per lane where every row of q begins at a multiple of 16 and is a whole number of them, otherwise 8
+      const int bytes = a.q_wide ? 16 : 8, lanes = HALVES * 128 / bytes, per = 32 / lanes;   // lanes per row, rows at a time
+      const int my_row = lane / lanes, d = lane % lanes * (bytes / 2);
       uint32_t kb = 0, items = 0;
       for (int it = 0;; ++it) {
         const Item x = next_item(it);
@@ -536,18 +550,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         kv_mbar_wait(&s.q_empty, (items & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         if (u == 0 || x.two) {
-          const int d = (lane % LANES) * 4;
           const uint32_t dst = smem_u32(smem + L::Q_OFF + u * L::TILE_BYTES) + (d >> 6) * HALF + (d & 4) * 2;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
 #pragma unroll 8
-            for (int i = 0; i < 32; i += PER) {
-              const int r = i + lane / LANES;
+            for (int i = 0; i < 32; i += per) {
+              const int r = i + my_row;
               const int64_t from = __shfl_sync(0xffffffffu, at[k], r);
               const bool ok = from >= 0 && d < a.head_dim;
-              asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + (32 * k + r) * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4)),
-                           "l"(a.q + 2 * (ok ? from + d : 0)), "r"(ok ? 8 : 0)
-                           : "memory");
+              const uint32_t to = dst + (32 * k + r) * 128 + ((((d & 63) >> 3) ^ (r & 7)) << 4);
+              const uint8_t* src = a.q + 2 * (ok ? from + d : 0);
+              if (a.q_wide) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(ok ? 16 : 0) : "memory");
+              else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(src), "r"(ok ? 8 : 0) : "memory");
             }
           asm volatile("cp.async.wait_all;" ::: "memory");
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -858,6 +872,7 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   a.sinks = x.sinks;
   const int64_t most = x.table_width * c->page_size;
   a.max_len = most > 0x3fffff00 ? 0x3fffff00 : (int)most;
+  a.q_wide = c->head_dim % 8 == 0 && x.q_stride_token % 8 == 0 && x.q_stride_head % 8 == 0;
   a.q_neg = x.scale < 0.0f ? 1u : 0u;
   a.c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-30f);
   a.dev_status = x.dev_status;
