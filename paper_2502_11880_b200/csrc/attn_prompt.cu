@@ -685,8 +685,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
       }
 
-      // ---- rows of O, 32 columns at a time through this warp's staging rows and out as whole sectors
       float inv = 0.0f;                                       // (a row that saw nothing is 0)
+      float top_all = m;                                      // maximum of all parts
+      bool mine_to_write = true;
       if (x.nb > 0) {
         const float2 l = unpair(l2);
         const float sum = l.x + l.y;
@@ -695,46 +696,53 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         fence_after();
         ++items;
         if (x.parts > 1) {
-          // ---- a part: to the workspace; each warp's last part to arrive joins its 32 rows, in the order of the parts
-          float4* const mine = a.part_o + ((x.unit0 + x.part) * 8 + warp) * 1024 + lane;
-          a.part_ml[((x.unit0 + x.part) * 2 + u) * ROWS + row] = make_float2(m, sum);
+          // ---- a part: each warp's last part to arrive joins its 32 rows, in the order of the parts; its own stay in tensor memory, and
+          //      go to the workspace only if the others are not known to be there yet
+          int* const counter = a.counters + x.id * 8 + warp;
+          int last = 0;
+          if (lane == 0) {
+            last = *reinterpret_cast<volatile int*>(counter) == x.parts - 1;
+            __threadfence();
+          }
+          last = __shfl_sync(0xffffffffu, last, 0);
+          if (!last) {
+            float4* const mine = a.part_o + ((x.unit0 + x.part) * 8 + warp) * 1024 + lane;
+            a.part_ml[((x.unit0 + x.part) * 2 + u) * ROWS + row] = make_float2(m, sum);
 #pragma unroll 1
-          for (int i = 0; i < steps * 16; i += 32) {
-            tm_ld32(o_addr + i, v);
-            wait_ld<32>(v);
-            if (valid)
+            for (int i = 0; i < steps * 16; i += 32) {
+              tm_ld32(o_addr + i, v);
+              wait_ld<32>(v);
 #pragma unroll
               for (int k = 0; k < 8; ++k)
                 mine[(i / 4 + k) * 32] = make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]), __uint_as_float(v[4 * k + 2]),
                                                      __uint_as_float(v[4 * k + 3]));
+            }
+            __syncwarp();
+            if (lane == 0) {
+              __threadfence();                                // (of all that the warp's barrier ordered before)
+              last = atomicAdd(counter, 1) == x.parts - 1;
+              __threadfence();
+            }
+            last = __shfl_sync(0xffffffffu, last, 0);
           }
-          fence_before();
           __syncwarp();
-          int last = 0;
-          if (lane == 0) {
-            kv_mbar_arrive(&s.o_empty[u]);                    // O has been read
-            int* counter = a.counters + x.id * 8 + warp;
-            __threadfence();                                  // (of all that the warp's barrier ordered before)
-            last = atomicAdd(counter, 1) == x.parts - 1;
-            if (last) *counter = 0;                           // the workspace is left as it was
-            __threadfence();
-          }
-          last = __shfl_sync(0xffffffffu, last, 0);
-          __syncwarp();
-          if (!last) continue;
-          m = -INFINITY;
-          const float2* const ml = a.part_ml + (x.unit0 * 2 + u) * ROWS + row;
+          mine_to_write = last;
+          if (last) {
+            if (lane == 0) *counter = 0;                      // the workspace is left as it was
+            const float2* const ml = a.part_ml + (x.unit0 * 2 + u) * ROWS + row;
+            float all = 0.0f;
 #pragma unroll 4
-          for (int k = 0; k < x.parts; ++k) m = fmaxf(m, __ldcg(ml + k * 2 * ROWS).x);
-          float all = 0.0f;
+            for (int k = 0; k < x.parts; ++k) top_all = fmaxf(top_all, k == x.part ? m : __ldcg(ml + k * 2 * ROWS).x);
 #pragma unroll 4
-          for (int k = 0; k < x.parts; ++k) {
-            const float2 y = __ldcg(ml + k * 2 * ROWS);
-            all += y.x == -INFINITY ? 0.0f : exp2_approx(y.x - m) * y.y;
+            for (int k = 0; k < x.parts; ++k) {
+              const float2 y = k == x.part ? make_float2(m, sum) : __ldcg(ml + k * 2 * ROWS);
+              all += y.x == -INFINITY ? 0.0f : exp2_approx(y.x - top_all) * y.y;
+            }
+            inv = top_all == -INFINITY ? 0.0f : 1.0f / all;
           }
-          inv = m == -INFINITY ? 0.0f : 1.0f / all;
         }
       }
+      // ---- O, 32 columns at a time, through this warp's staging rows and out as whole sectors
       const int64_t at = valid ? ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd) * a.head_dim : -1;
       const int piece = lane & 3;                             // 8 columns; rows 8 k + lane / 4
       int64_t to[4];
@@ -745,33 +753,35 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       }
       uint4* const stage = s.stage[warp];
 #pragma unroll 1
-      for (int i = 0; i < steps * 16; i += 32) {
+      for (int i = 0; i < steps * 16 && mine_to_write; i += 32) {
         uint32_t* const o = v;
-        if (x.parts > 1) {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = 0u;
-          if (valid) {
-            const float2* const ml = a.part_ml + (x.unit0 * 2 + u) * ROWS + row;
-            const float4* const from = a.part_o + (x.unit0 * 8 + warp) * 1024 + lane + (i / 4) * 32;
-#pragma unroll 3
-            for (int k = 0; k < x.parts; ++k) {
-              float4 w[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) w[e] = __ldcg(from + (int64_t)k * 8 * 1024 + e * 32);
-              const float pm = __ldcg(ml + k * 2 * ROWS).x;
-              const float f = pm == -INFINITY ? 0.0f : exp2_approx(pm - m);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                o[4 * e] = __float_as_uint(__uint_as_float(o[4 * e]) + f * w[e].x);
-                o[4 * e + 1] = __float_as_uint(__uint_as_float(o[4 * e + 1]) + f * w[e].y);
-                o[4 * e + 2] = __float_as_uint(__uint_as_float(o[4 * e + 2]) + f * w[e].z);
-                o[4 * e + 3] = __float_as_uint(__uint_as_float(o[4 * e + 3]) + f * w[e].w);
-              }
-            }
-          }
-        } else {
+        if (x.parts == 1) {
           if (x.nb > 0) tm_ld32(o_addr + i, o);
           wait_ld<32>(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0u;
+#pragma unroll 1
+          for (int k = 0; k < x.parts; ++k) {
+            const float mk = k == x.part ? m : __ldcg(a.part_ml + ((x.unit0 + k) * 2 + u) * ROWS + row).x;
+            if (k == x.part) {
+              tm_ld32(o_addr + i, w);
+              wait_ld<32>(w);
+            } else {
+              const float4* const from = a.part_o + ((x.unit0 + k) * 8 + warp) * 1024 + lane + (i / 4) * 32;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float4 y = __ldcg(from + e * 32);
+                w[4 * e] = __float_as_uint(y.x);
+                w[4 * e + 1] = __float_as_uint(y.y);
+                w[4 * e + 2] = __float_as_uint(y.z);
+                w[4 * e + 3] = __float_as_uint(y.w);
+              }
+            }
+            const float f = mk == -INFINITY ? 0.0f : exp2_approx(mk - top_all);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(f, __uint_as_float(w[e]), __uint_as_float(o[e])));
+          }
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -783,7 +793,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
         for (int k = 0; k < 4; ++k) y[k] = stage[(8 * k + (lane >> 2)) * 4 + (piece ^ ((lane >> 3) & 3))];
         __syncwarp();
-        const int left = a.head_dim - i - piece * 8;          // columns from this piece on
+        const int left = a.head_dim - i - piece * 8;      // columns from this piece on
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint8_t* const dst = a.out + 2 * (to[k] + i);
@@ -796,10 +806,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
         }
       }
-      if (x.nb > 0 && x.parts == 1) {
+      if (x.nb > 0) {
         fence_before();
         __syncwarp();
-        if (lane == 0) kv_mbar_arrive(&s.o_empty[u]);
+        if (lane == 0) kv_mbar_arrive(&s.o_empty[u]);         // O has been read
       }
     }
   }
