@@ -16,10 +16,11 @@
 //     than 2^8 (P and the sums stay below 2^8 times their range, which fp32 and both 16-bit types hold), so rarely;
 //   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
 //     place between the sinks and the window), since 0 * NaN would reach O.
-// Bound by a tile's chain per block -- about 1630 cycles of softmax, 1024 of products, 650 until signals are seen -- of which two run in
-// turn: 3300 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 855 us = 0.96
-// PFLOP/s at the 1.34 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 92 us).  Blocks of 64 tokens with two
-// buffers of S, P through shared memory, two threads per row, P in halves or a lane per tile that issues were each slower.
+// Bound by a tile's chain per block -- softmax, 1024 cycles of products, 650 until signals are seen -- of which two run in turn: 3100 to
+// 3200 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 800 to 840 us = about 1.0
+// PFLOP/s at the 1.3 to 1.4 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 78 us).  Blocks of 64 tokens
+// with two buffers of S, P through shared memory, two threads per row, P in halves, S in two products of 64 columns (the first one before
+// P) or a lane per tile that issues were each slower.
 // Blocks that no row sees are not visited: those of the sinks, then those from the first row's window to the last row.
 // Exponentials: the unit that takes them does 16 per SM and cycle, which for head_dim 128 is as long as both products take;
 // a share of the columns goes through a polynomial on the fp32 units instead (2^x = 2^n * p(x - n), degree 4, relative error
@@ -344,8 +345,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int64_t items = pairs * a.kv_heads * a.blocks;
       const int64_t uncut = a.room ? items / a.room * a.room : items, rest = items - uncut;
       const int parts = rest > 0 ? max(1, (int)(a.room / rest)) : 1;
-      int64_t unit = blockIdx.x;
-      for (int it = 0;; unit += gridDim.x) {
+      // dealt out in rounds, every other round backwards: units get shorter as they go on, and a CTA that had the longest of one
+      // round gets the shortest of the next
+      int it = 0;
+      for (int64_t round = 0;; ++round) {
+        const int64_t unit = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
