@@ -7,7 +7,7 @@
 // with g query heads per kv head a tile of 128 rows holds 128 / g tokens, so K and V are read once for all heads that share them, and
 // a window's edges waste fewer columns than a tile of 128 tokens would.  A work item is two such tiles that work on the same
 // blocks of 128 cached tokens; one persistent CTA per SM walks items, the last (longest) first:
-//   * warp 8 finds the items and brings K and V blocks in by tensor copies (one box per page and 64-column half, 128-byte
+//   * warp 8 draws the items and brings K and V blocks in by tensor copies (one box per page and 64-column half, 128-byte
 //     swizzle) into two rings;
 //   * warp 9: one lane issues tcgen05.mma -- S = Q K^T from shared memory, O += P V with P in tensor memory -- for the two
 //     tiles in turn, so that the tensor cores work on one tile while the other tile's exponentials are taken;
@@ -68,6 +68,7 @@ struct PromptArgs {
   uint32_t q_neg;                                     // scale < 0: the products take -Q
   int room;                                           // parts of items that the workspace has room for
   int* counters;                                      // [items][8 warps]: parts that have arrived; zero between calls
+  unsigned long long* drawn;                          // [0] units drawn so far, [1] CTAs that have finished; zero between calls
   float2* part_ml;                                    // [units][2 tiles][128 rows]: maximum and sum
   float4* part_o;                                     // [units][8 warps][32 pieces of 4 columns][32 rows]
   int* dev_status;
@@ -345,11 +346,21 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int64_t items = pairs * a.kv_heads * a.blocks;
       const int64_t uncut = a.room ? items / a.room * a.room : items, rest = items - uncut;
       const int parts = rest > 0 ? max(1, (int)(a.room / rest)) : 1;
-      // dealt out in rounds, every other round backwards: units get shorter as they go on, and a CTA that had the longest of one
-      // round gets the shortest of the next
+      // A CTA draws its next unit when the last copies of one are on their way.  Without a workspace they are dealt out in rounds, every
+      // other round backwards: units get shorter as they go on, and a CTA that had the longest of one round gets the shortest of the next.
+      // (Rounds all forwards / there and back / drawn: 4 x 512 tokens 78.5 / 78.6 / 76.4 us, 4096 tokens, 32/4 heads 168 to 184 / 137 to
+      // 165 / 141 to 149, 2048 tokens, 32/8 heads 59 / 45 to 48 / 45 to 46; a unit drawn one earlier was in between.)
+      const int64_t units = uncut + rest * parts;
       int it = 0;
-      for (int64_t round = 0;; ++round) {
-        const int64_t unit = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      for (int64_t round = 0, unit = blockIdx.x;; ++round) {
+        if (round > 0) {
+          if (a.room) {
+            if (lane == 0) unit = gridDim.x + (int64_t)atomicAdd(a.drawn, 1ull);
+            unit = __shfl_sync(0xffffffffu, unit, 0);
+          } else {
+            unit = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+          }
+        }
         kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
         __syncwarp();
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
@@ -361,7 +372,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         __syncwarp();
         bool found = false;
         int64_t before = 0;
-        for (int s1 = unit < uncut + rest * parts && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
+        for (int s1 = unit < units && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
           const Seq q = s1 == a.seqs ? tail : seq_at(s1);
           const int i = q.i, q0 = q.q0, n = q.n;
           const int64_t tiles = (n + span - 1) / span;
@@ -447,6 +458,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
         }
       }
+      if (a.room && lane == 0) {                              // the workspace is left as it was
+        __threadfence();
+        if (atomicAdd(a.drawn + 1, 1ull) == gridDim.x - 1) a.drawn[0] = a.drawn[1] = 0;
+      }
+      __syncwarp();
       if (*abort_flag)                                        // leave only when the copies have landed
         for (uint32_t i = kb > STAGES ? kb - STAGES : 0; i < kb; ++i)
           for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.k_full[i % STAGES], (i / STAGES) & 1u) &&
@@ -895,6 +911,7 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   const int64_t sms = dev_info().sm_count, items = pairs * a.kv_heads * a.blocks;
   a.room = ws_bytes >= attn_decode_workspace_bytes() + (size_t)sms * PART_BYTES ? (int)sms : 0;
   a.counters = attn_counters(ws);
+  a.drawn = reinterpret_cast<unsigned long long*>(static_cast<uint8_t*>(ws) + attn_counters_bytes()) - 2;
   a.part_o = reinterpret_cast<float4*>(attn_prompt_parts(ws));
   a.part_ml = reinterpret_cast<float2*>(attn_prompt_parts(ws) + (size_t)sms * (8 * 1024 * 16));
   const int64_t grid = a.room || items > sms ? sms : items;

@@ -60,7 +60,8 @@ struct AttnArgs {
   int* dev_status;
 };
 // The workspace: counters that are zero between calls (of fixed number, so that no call's parts ever lie where another call's
-// counters are), the parts of decode rows, the parts of prompt items (where the caller gave the room for them).
+// counters are; the last 16 bytes deal out prompt items), the parts of decode rows, the parts of prompt items (where the caller
+// gave the room for them).
 size_t attn_decode_parts_bytes();
 inline size_t attn_counters_bytes() { return 65536; }
 inline int* attn_counters(void* ws) { return static_cast<int*>(ws); }

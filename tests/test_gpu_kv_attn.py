@@ -261,6 +261,29 @@ def test_prompt_parts(spans, hq, hkv, dim, page, dtype, window, sinks, room):
     assert int(ws[:bn.ATTN_WORKSPACE_HEAD].sum()) == 0
 
 
+ROUNDS = [
+    # more items than SMs, several times over: CTAs draw them, or take them in rounds when there is no workspace
+    ([(100, 200), (0, 150), (637, 90)], 256, 64, 32, 32, BF, 120, 5),
+    ([(3 * i, 1 + i % 9) for i in range(70)], 8, 8, 16, 8, HF, 0, 0),      # sequences beyond the 32 that are kept at hand
+]
+
+
+@pytest.mark.parametrize("room", [True, False])
+@pytest.mark.parametrize("spans,hq,hkv,dim,page,dtype,window,sinks", ROUNDS)
+def test_prompt_many_items(spans, hq, hkv, dim, page, dtype, window, sinks, room):
+    p = Paged([b + n for b, n in spans], hkv, dim, page, dtype, seed=dim + 5)
+    start, seq, pos = prompt_args(spans)
+    q = p.queries(len(seq), hq, dim, dtype)
+    ws = bn.new_attn_workspace(len(seq) if room else 0, hq, hkv, dim)
+    most = max(n for _, n in spans)
+    call = lambda: bn.bitnet_attn_prompt(p.cache, p.layer, q, p.table, p.len, start, most, window=window, sinks=sinks, workspace=ws)
+    out = call()
+    check_attn(out, p.ref(q, pos, seq, dim ** -0.5, window, sinks), PROMPT_P[dtype])
+    for _ in range(4):
+        assert torch.equal(call(), out)
+    assert int(ws[:bn.ATTN_WORKSPACE_HEAD].sum()) == 0
+
+
 def test_decode_one_workspace_for_calls_of_all_sizes():
     big = Paged([900 + 7 * i for i in range(40)], 4, 64, 16, BF, seed=21)
     small = Paged([30000], 1, 128, 64, HF, seed=22)
