@@ -17,8 +17,8 @@
 //   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
 //     place between the sinks and the window), since 0 * NaN would reach O.
 // Bound by a tile's chain per block -- softmax, 1024 cycles of products, 650 until signals are seen -- of which two run in turn: 3100 to
-// 3200 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 800 to 840 us = about 1.0
-// PFLOP/s at the 1.3 to 1.4 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 78 us).  Blocks of 64 tokens
+// 3200 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 805 to 830 us = 1.0
+// PFLOP/s at the 1.3 to 1.4 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 76 to 82 us).  Blocks of 64 tokens
 // with two buffers of S, P through shared memory, two threads per row, P in halves, S in two products of 64 columns (the first one before
 // P) or a lane per tile that issues were each slower.
 // Blocks that no row sees are not visited: those of the sinks, then those from the first row's window to the last row.
