@@ -186,8 +186,14 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 // 2^x for x <= 2^7 by a polynomial (x below -126 counts as -126): n = round(x) through the sum with 1.5 * 2^23, whose low bits
-// then go to the exponent; p is the degree-4 minimax fit (relative error, own exchange iteration) of 2^f on [-1/2, 1/2].
+// are then the exponent of a factor; p is the degree-4 minimax fit (relative error, own exchange iteration) of 2^f on [-1/2, 1/2].
+// (A product by 2^n, where a sum of the exponents' bits would do for numbers, keeps a NaN: the sum makes FLT_MAX of it.)
 __device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
   float2 x = unpair(x2);
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
@@ -200,9 +206,8 @@ __device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
   p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
   p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
   p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
-  const float2 e = unpair(t), m = unpair(p);
-  return make_float2(__uint_as_float(__float_as_uint(m.x) + (__float_as_uint(e.x) << 23)),
-                     __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
+  const float2 e = unpair(t);
+  return unpair(mul2(p, pair(__uint_as_float((__float_as_uint(e.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(e.y) << 23) + 0x3f800000u))));
 }
 
 // Bits of the columns below n, of 32.
