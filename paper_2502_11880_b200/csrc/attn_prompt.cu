@@ -191,13 +191,14 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// 2^x for x <= 2^7 by a polynomial (x below -126 counts as -126): n = round(x) through the sum with 1.5 * 2^23, whose low bits
-// are then the exponent of a factor; p is the degree-4 minimax fit (relative error, own exchange iteration) of 2^f on [-1/2, 1/2].
-// (A product by 2^n, where a sum of the exponents' bits would do for numbers, keeps a NaN: the sum makes FLT_MAX of it.)
+// 2^x for x <= 2^7 by a polynomial, 0 where x rounds to -127 or less (as a hidden score, -inf, does): n = round(x) through the sum
+// with 1.5 * 2^23, whose low bits are then the exponent of a factor (bits of 0 for n = -127); p is the degree-4 minimax fit (relative
+// error, own exchange iteration) of 2^f on [-1/2, 1/2].  (A product by 2^n, where a sum of the exponents' bits would do for numbers,
+// keeps a NaN: the sum makes FLT_MAX of it.)
 __device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
   float2 x = unpair(x2);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.0f));
   x2 = pair(x.x, x.y);
   const uint64_t t = add2(x2, pair(12582912.0f, 12582912.0f));
   const uint64_t n = add2(t, pair(-12582912.0f, -12582912.0f));

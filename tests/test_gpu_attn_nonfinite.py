@@ -1,4 +1,4 @@
-"""NaN where queries see it and where they do not: a NaN that a query sees is in its result, by whichever
+"""NaN and huge values where queries see them and where they do not: a NaN that a query sees is in its result, by whichever
 kernel serves the call, and what a query does not see leaves its result as it is."""
 import pytest
 import torch
@@ -39,3 +39,22 @@ def test_prompt_nan_key_makes_nan_of_the_rows_that_see_it(dtype, column):
     assert torch.equal(out[:first], clean[:first])                 # before the key
     assert torch.equal(out[:, 2:], clean[:, 2:])                   # heads of the other kv head
     assert bool(out[first:, :2].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_prompt_hidden_tokens_have_no_weight(dtype):
+    """Values as large as the type holds, beside queries that do not see them."""
+    p = Paged([150], 1, 64, 16, dtype, seed=32)
+    start, _, _ = prompt_args([(0, 150)])
+    q = p.queries(150, 3, 64, dtype)
+    for window, sinks in ((0, 0), (20, 2)):
+        clean = prompt(p, q, start, 150, window=window, sinks=sinks)
+        for column in (46, 47, 63, 78):
+            page, row = at(p, 0, column)
+            kept = p.v[p.layer, page, 0, row].clone()
+            p.v[p.layer, page, 0, row] = torch.finfo(dtype).max
+            out = prompt(p, q, start, 150, window=window, sinks=sinks)
+            p.v[p.layer, page, 0, row] = kept
+            assert torch.equal(out[:column], clean[:column])
+            if window:
+                assert torch.equal(out[column + window:], clean[column + window:])
