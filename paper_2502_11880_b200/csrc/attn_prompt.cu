@@ -211,6 +211,10 @@ __device__ __forceinline__ float2 exp2_poly(uint64_t x2) {
   return unpair(mul2(p, pair(__uint_as_float((__float_as_uint(e.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(e.y) << 23) + 0x3f800000u))));
 }
 
+// What a row's sum is divided by, as a factor: a row that saw nothing is 0 (as one that saw only scores of -inf), and a NaN sum stays NaN,
+// also where all scores were NaN, which leaves the maximum at -inf.
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
+
 // Bits of the columns below n, of 32.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 // -inf in those of 32 columns from c that a row at position p does not see.  (Selects by bits: compared column by column, with
@@ -711,13 +715,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
       }
 
-      float inv = 0.0f;                                       // (a row that saw nothing is 0)
+      float inv = 0.0f;
       float top_all = m;                                      // maximum of all parts
       bool mine_to_write = true;
       if (x.nb > 0) {
         const float2 l = unpair(l2);
         const float sum = l.x + l.y;
-        if (m != -INFINITY) inv = 1.0f / sum;
+        inv = inverse(sum);
         kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
         fence_after();
         ++items;
@@ -762,9 +766,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll 4
             for (int k = 0; k < x.parts; ++k) {
               const float2 y = k == x.part ? make_float2(m, sum) : __ldcg(ml + k * 2 * ROWS);
-              all += y.x == -INFINITY ? 0.0f : exp2_approx(y.x - top_all) * y.y;
+              all += (y.x == -INFINITY ? 0.0f : exp2_approx(y.x - top_all)) * y.y;    // (y.y may be NaN)
             }
-            inv = top_all == -INFINITY ? 0.0f : 1.0f / all;
+            inv = inverse(all);
           }
         }
       }

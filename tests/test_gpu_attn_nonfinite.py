@@ -1,4 +1,4 @@
-"""NaN and huge values where queries see them and where they do not: a NaN that a query sees is in its result, by whichever
+"""NaN, infinities and huge values where queries see them and where they do not: a NaN that a query sees is in its result, by whichever
 kernel serves the call, and what a query does not see leaves its result as it is."""
 import pytest
 import torch
@@ -58,3 +58,58 @@ def test_prompt_hidden_tokens_have_no_weight(dtype):
             assert torch.equal(out[:column], clean[:column])
             if window:
                 assert torch.equal(out[column + window:], clean[column + window:])
+
+
+SPANS = [
+    ([(0, 200), (30, 5)], True),
+    ([(0, 200), (30, 5)], False),
+    ([(5000, 3)], True),                                           # blocks of the tile on several CTAs, joined
+    ([(5000, 3)], False),
+    ([(300, 2), (40, 1)], True),                                   # the kernel of single tokens
+]
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("spans,room", SPANS)
+def test_prompt_query_whose_scores_are_all_nan(spans, room, dtype, value):
+    """A NaN in a query, or infinities whose products cancel: NaN for that query, and nothing else changes."""
+    p = Paged([b + n for b, n in spans], 2, 64, 16, dtype, seed=33)
+    start, seq, _ = prompt_args(spans)
+    q, most = p.queries(len(seq), 8, 64, dtype), max(n for _, n in spans)
+    clean = prompt(p, q, start, most, room)
+    t = len(seq) // 2
+    for heads in ([3], list(range(8))):
+        bad = q.clone()
+        bad[t, heads] = value
+        out = prompt(p, bad, start, most, room)
+        others = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+        others[t, heads] = False
+        assert bool(out[~others].isnan().all())
+        assert torch.equal(out[others], clean[others])
+
+
+@pytest.mark.parametrize("room", [True, False])
+def test_prompt_first_token_with_a_nan_key(room):
+    """The first token sees itself alone: all that it sees is NaN."""
+    p = Paged([40], 1, 64, 16, BF, seed=34)
+    start, _, _ = prompt_args([(0, 40)])
+    q = p.queries(40, 2, 64, BF)
+    page, row = at(p, 0, 0)
+    p.k[p.layer, page, 0, row] = float("nan")
+    assert bool(prompt(p, q, start, 40, room).isnan().all())
+    d = bn.bitnet_attn_decode(p.cache, p.layer, q[-1:].contiguous(), p.table, p.len)
+    assert bool(d.isnan().all())
+
+
+@pytest.mark.parametrize("room", [True, False])
+def test_prompt_part_whose_keys_are_all_nan(room):
+    """The first four blocks of 128 tokens, which one CTA has by itself where the row's blocks go to several."""
+    p = Paged([6000], 1, 64, 64, BF, seed=35)
+    start, _, _ = prompt_args([(5995, 5)])
+    q = p.queries(5, 4, 64, BF)
+    clean = prompt(p, q, start, 5, room, window=5000)
+    for e in range(512 // 64):
+        p.k[p.layer, int(p.table[0, e])] = float("nan")
+    assert bool(prompt(p, q, start, 5, room).isnan().all())
+    assert torch.equal(prompt(p, q, start, 5, room, window=5000), clean)      # those keys are outside the window
