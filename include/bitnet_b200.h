@@ -417,9 +417,14 @@ int bitnet_tl_build_lut_debug(bitnet_fmt_t fmt, const int8_t* q_row, int64_t K, 
  * q_start[seqs] = tokens) says which are whose, and NULL that sequence i has exactly token i.  kv_len counts the new tokens: token j
  * of the n new ones of sequence s is at position kv_len[s] - n + j.
  *
- * Values that only the device sees are checked there: a page outside the pool, a position outside the table or a sequence out of
- * range is skipped (attention reads zeros) and reported in *dev_status (nullable device int) as BITNET_ERR_BAD_PAGE; nothing
- * outside the arrays is read or written.
+ * Values that only the device sees are checked there, and nothing outside the arrays is read or written.  What cannot be used is
+ * passed over and reported in *dev_status (nullable device int) as BITNET_ERR_BAD_PAGE:
+ *   a page outside the pool, or none where a token is read or written: not written to; attention reads zeros;
+ *   a sequence out of range: its entry of a list has no effect;
+ *   a position beyond the table (kv_len > table_width * page_size): not written; attention with a window sees what the window and the
+ *   sinks have of the table's tokens.  Attention without a window takes such a length for the table's own, and reports nothing.
+ * A position before the start (kv_len smaller than the number of new tokens; an idle row) is not written, sees nothing, and is not
+ * reported.
  */
 enum { BITNET_KV_BF16 = 0, BITNET_KV_F16 = 1, BITNET_KV_F32 = 2 };
 

@@ -61,9 +61,11 @@ struct DecodeArgs {
   int* dev_status;
 };
 
-// The visible tokens of one row: [0, s_end) and [lo, len), as tiles.
+// The visible tokens of one row: [0, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
+// tokens there are not there; without a window such a position means all of the table).
 struct Range {
   int len, s_end, lo, n0, t1, tiles, seq;
+  bool beyond;
 };
 __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
   Range r;
@@ -76,9 +78,11 @@ __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
     len = __ldg(a.kv_len + n);
   }
   r.len = (int)max((int64_t)0, min(len, (int64_t)a.max_len));
-  r.lo = a.window > 0 ? max(0, r.len - a.window) : 0;
+  r.beyond = a.window > 0 && len > a.max_len;
+  r.lo = a.window > 0 ? (int)min(max((int64_t)0, len - a.window), (int64_t)r.len) : 0;
   r.s_end = min(a.sinks, r.lo);
   if (r.lo <= a.sinks) r.lo = r.s_end = 0;
+  if (r.beyond && r.lo == r.len) r.lo = r.len = 0;             // the window lies beyond the table: the sinks alone
   r.n0 = (r.s_end + TILE - 1) / TILE;
   r.t1 = r.lo / TILE;
   r.tiles = max(1, r.n0 + (r.len + TILE - 1) / TILE - r.t1);   // an empty row has one tile with nothing visible
@@ -298,6 +302,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int t0 = (int)(off - (int64_t)row * r.tiles);
       const int t_end = (int)min((int64_t)r.tiles, end - base - (int64_t)row * r.tiles);
       const int head = row / a.head_blocks;
+      if (r.beyond && lane == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
       // the page of a tile's box; -2: nothing visible, not read
       auto look_up = [&](int t) -> int {
         int first, lo, hi;

@@ -405,10 +405,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             t.n_new = n;
             t.tok0 = (int)(tiles - 1 - (want - excl)) * span;
             t.two = t.tok0 + a.tile_tokens < n;
+            // (positions beyond the table: what their windows have of its tokens; without a window, all of them)
             const int64_t pos0 = (int64_t)q.len - n, most = a.max_len - 1;
             t.pos0 = (int)pos0;                              // |pos0| < 2^31
             t.p_last = (int)min(pos0 + min((int64_t)n, (int64_t)t.tok0 + span) - 1, most);
-            t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0, most) - a.window + 1) : 0;
+            t.lo = a.window > 0 ? (int)max((int64_t)0, min(pos0 + t.tok0 - a.window + 1, (int64_t)a.max_len)) : 0;
             t.n0 = t.t1 = t.b0 = t.nb = 0;
             t.unit0 = (id - uncut) * parts;                   // (used by cut items only)
             t.part = part;
@@ -438,6 +439,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (lane == 0) kv_mbar_arrive(&s.item_full[it & 1]);
         ++it;
         if (!found) break;
+        if (a.window > 0 && lane == 0 && a.dev_status && (int64_t)x.pos0 + min(x.n_new, x.tok0 + span) > a.max_len)
+          atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
         auto look_up = [&](int j, int& y) -> int {
           const int tok = block_start(x, j) + box * box_rows;
           y = tok & ((1 << a.page_shift) - 1);
@@ -636,8 +639,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int tok = x.tok0 + u * a.tile_tokens + row_tok;
       const bool valid = row < a.tile_tokens * a.per_block && hd < x.heads && tok < x.n_new && x.q0 >= 0 && (int64_t)x.q0 + tok < a.tokens;
       if (u == 1 && !x.two) continue;
-      const int p = valid ? (int)min((int64_t)x.pos0 + tok, (int64_t)a.max_len - 1) : -1;   // position; < 0 sees nothing
-      const int wlo = a.window > 0 ? max(0, p - a.window + 1) : 0;                          // first token of its window
+      const int64_t pos = valid ? (int64_t)x.pos0 + tok : -1;
+      const int p = (int)min(pos, (int64_t)a.max_len - 1);    // last token that the row may see; < 0: sees nothing
+      // first token of its window
+      const int wlo = a.window > 0 ? (int)max((int64_t)0, min(pos - a.window + 1, (int64_t)a.max_len)) : 0;
       float m = -INFINITY;
       uint64_t l2 = 0;                                        // a pair of sums
       uint32_t v[64], w[64];
