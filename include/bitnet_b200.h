@@ -470,7 +470,8 @@ int bitnet_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t 
 /*
  * Forks n sequences: row children[i] (which must hold no pages) becomes a copy of row parents[i].  Full pages are shared
  * (refs + 1); a page filled in part is copied -- its rows in use, K and V, all layers -- to the lowest free page, in the order
- * of the list.  No row may be a child and appear again in either list.  workspace: bitnet_kv_workspace_bytes(num_pages, n) bytes,
+ * of the list.  A page outside the pool, no page where the parent's last rows are, and a parent longer than its row of the table are
+ * reported; the child has -1 there, and the length that the table holds.  No row may be a child and appear again in either list.  workspace: bitnet_kv_workspace_bytes(num_pages, n) bytes,
  * 16-byte aligned, any contents; not to be shared by calls that overlap.
  */
 size_t bitnet_kv_workspace_bytes(int64_t num_pages, int64_t n);
@@ -478,18 +479,19 @@ int bitnet_kv_fork(const bitnet_kv_cache_t* cache, int32_t* refs, int32_t* table
                    const int32_t* parents, const int32_t* children, int64_t n, void* workspace, size_t workspace_bytes, int* dev_status,
                    void* stream);
 
-/* Gives up the rows list[0..n): every page's count falls by one, the row becomes -1 and its length 0. */
+/* Gives up the rows list[0..n): every page's count falls by one, the row becomes -1 and its length 0 (also where it names pages outside
+ * the pool, which are reported). */
 int bitnet_kv_free(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, int32_t* kv_len,
                    const int32_t* list, int64_t n, int* dev_status, void* stream);
 
 /* Gives up, in every row, the pages that attention with this window and these sinks no longer reads: those wholly at positions
- * sinks <= p < kv_len - window.  Their entries become -1. */
+ * sinks <= p < kv_len - window.  Their entries become -1 (ids outside the pool too, without a report). */
 int bitnet_kv_trim(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, const int32_t* kv_len,
                    int64_t page_size, int64_t window, int64_t sinks, void* stream);
 
 /*
  * Packs the pages in use (refs > 0) into the pool's first places: with L of them, the i-th page in use at or beyond place L moves
- * to the i-th free place below L (K and V, all layers); table entries and refs follow.  *live_out (nullable device int) = L.
+ * to the i-th free place below L (K and V, all layers); table entries and refs follow (entries outside the pool stay as they are).  *live_out (nullable device int) = L.
  * workspace: bitnet_kv_workspace_bytes(num_pages, 0) bytes.
  */
 int bitnet_kv_compact(const bitnet_kv_cache_t* cache, int32_t* refs, int32_t* table, int64_t seqs, int64_t table_width,

@@ -358,6 +358,8 @@ kv_fork_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, int64
         e = used >> page_shift;
         if (rows) src = table[p * width + e];
         if (src >= num_pages) src = -1;
+        // no page where rows are in use, or tokens beyond the table
+        if ((rows && src < 0) || ((int64_t)len[p] + (1 << page_shift) - 1) >> page_shift > width) bad = true;
         if (rows) table[c * width + e] = -1;
       } else {
         bad = true;
@@ -497,7 +499,10 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
         if (e < full) {
           id = a.table[p * a.width + e];
           if (id >= 0 && id < a.kv.num_pages) atomicAdd(a.refs + id, 1);
-          else id = -1;
+          else {
+            if (id >= 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);   // (-1: released)
+            id = -1;
+          }
         }
         if (e != full || !part) a.table[c * a.width + e] = id;
       }
@@ -613,6 +618,7 @@ kv_release_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
   if (e >= first && e < last && table[row * width + e] >= 0) {
     const int id = atomicExch(table + row * width + e, -1);
     if (id >= 0 && id < num_pages) atomicSub(refs + id, 1);
+    else if (id >= 0 && dev_status) atomicExch(dev_status, BITNET_ERR_BAD_PAGE);
   }
   if (!trim && e == 0) len[row] = 0;
 }

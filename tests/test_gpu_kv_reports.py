@@ -83,3 +83,44 @@ def test_positions_inside_the_table_are_not_reported():
     assert int(status) == 0
     pos = [123 + j for j in range(5)] + [3 - 7 + j for j in range(7)]
     check_attn(out, p.ref(q, pos, [0] * 5 + [1] * 7, 0.125, 9, 1), PROMPT_P[BF])
+
+
+@pytest.mark.parametrize("row,length,child", [
+    ([0, 40, 1, -1], 24, [0, -1, 1, -1]),        # a full page beyond the pool: not shared
+    ([0, 1, 40, -1], 20, [0, 1, -1, -1]),        # the page filled in part beyond the pool: not copied
+    ([0, 1, -1, -1], 20, [0, 1, -1, -1]),        # the page filled in part is none
+    ([0, 1, 2, 3], 33, [0, 1, 2, 3]),            # a length beyond the table: its row is shared up to its end
+])
+def test_fork_reports_what_it_cannot_take_over(row, length, child):
+    b = Books(3, 4, 6, 1, 8, 8, seed=11)
+    b.table[0], b.len[0] = row, length
+    b.refs = [int(i in row) for i in range(6)]
+    b.load()
+    bn.bitnet_kv_fork(b.cache, b.d_refs, b.d_table, b.d_len, i32([0]), i32([2]), dev_status=b.status)
+    b.table[2], b.len[2] = child, min(length, 32)
+    for e, page in enumerate(child):
+        if page >= 0:
+            b.refs[page] += 1
+    b.check(7)
+
+
+def test_fork_does_not_report_released_pages():
+    b = Books(2, 4, 6, 1, 8, 8, seed=12)
+    b.table[0], b.len[0], b.refs = [0, -1, 1, 3], 29, [1, 1, 0, 1, 0, 0]
+    b.load()
+    b.fork([0], [1])
+    bn.bitnet_kv_fork(b.cache, b.d_refs, b.d_table, b.d_len, i32([0]), i32([1]), dev_status=b.status)
+    b.check()
+
+
+def test_free_reports_pages_beyond_the_pool():
+    b = Books(2, 4, 6, 1, 8, 8, seed=13)
+    b.table, b.len, b.refs = [[0, 6, -1, 2 ** 31 - 1], [1, -1, -1, -1]], [25, 3], [1, 1, 0, 0, 0, 0]
+    b.load()
+    bn.bitnet_kv_free(b.d_refs, b.d_table, b.d_len, i32([0]), dev_status=b.status)
+    b.table[0], b.len[0], b.refs[0] = [-1] * 4, 0, 0
+    b.check(7)
+    b.status.zero_()
+    bn.bitnet_kv_free(b.d_refs, b.d_table, b.d_len, i32([1, 0]), dev_status=b.status)
+    b.table[1], b.len[1], b.refs[1] = [-1] * 4, 0, 0
+    b.check()
