@@ -389,6 +389,10 @@ int bitnet_microbench_issue(int kind, int iters, unsigned* sink, void* stream);
  * expects bytes that no copy ever delivers.  Nothing is in flight, nothing faults; afterwards
  * bitnet_device_status reports BITNET_ERR_TIMEOUT until bitnet_device_status_clear. */
 int bitnet_debug_wait_timeout_probe(void* stream);
+/* Until it is called with -1, every CTA of the attention kernels that comes to its `tile`-th tile of cached tokens takes the wait
+ * before it for one that has run out, and goes the way of a call that gives up: the output is not to be used, and bitnet_device_status
+ * reports BITNET_ERR_TIMEOUT until bitnet_device_status_clear. */
+void bitnet_debug_attn_give_up(int64_t tile);
 /* Inverse of the packers: packed -> w[M][K] int8.  dev_status set if an invalid code is met. */
 int bitnet_unpack_i2s(const void* packed, int64_t M, int64_t K, int8_t* w, int* dev_status,
                       void* stream);
@@ -507,7 +511,7 @@ int bitnet_kv_copy_pages(const bitnet_kv_cache_t* cache, const int32_t* src, con
  * q: [tokens][q_heads][head_dim], strides in elements (multiples of 4), 16-byte aligned; out: [tokens][q_heads][head_dim]
  * contiguous, of q's type.  Cached values that no query sees (the rest of a page, released pages) may hold anything.
  * workspace: bitnet_attn_workspace_bytes bytes; its first 64 KB are zeroed once with bitnet_workspace_init, and every completed call
- * leaves them zeroed.  tokens is the most new tokens of a prompt call; with 0 the workspace (1.3 MB) serves decode calls, and prompt
+ * leaves them zeroed (after one that gave up -- BITNET_ERR_TIMEOUT from bitnet_device_status -- they are zeroed anew).  tokens is the most new tokens of a prompt call; with 0 the workspace (1.3 MB) serves decode calls, and prompt
  * calls without cutting the blocks of one tile between CTAs.  One workspace may serve calls of any sizes and both kinds, but no
  * two calls that overlap.
  *

@@ -32,6 +32,7 @@ SYMBOLS = [
     "bitnet_elut_packed_bytes", "bitnet_pack_elut", "bitnet_unpack_elut", "bitnet_elut_linear_group",
     "bitnet_kv_cache_init", "bitnet_kv_append", "bitnet_kv_reserve", "bitnet_kv_workspace_bytes", "bitnet_kv_fork", "bitnet_kv_free",
     "bitnet_kv_trim", "bitnet_kv_compact", "bitnet_kv_copy_pages", "bitnet_attn_workspace_bytes", "bitnet_attn_decode", "bitnet_attn_prompt",
+    "bitnet_debug_attn_give_up",
 ]
 
 _lib = None
@@ -55,6 +56,8 @@ def lib():
         L.bitnet_last_cuda_error.restype = ci
         L.bitnet_device_status.argtypes = [vp]
         L.bitnet_debug_wait_timeout_probe.argtypes = [vp]
+        L.bitnet_debug_attn_give_up.argtypes = [i64]
+        L.bitnet_debug_attn_give_up.restype = None
         L.bitnet_set_early_start.argtypes = [ci]
         L.bitnet_set_early_start.restype = None
         L.bitnet_set_tl2_lookup.argtypes = [ci]
@@ -124,6 +127,11 @@ def bitnet_device_status_clear():
 def bitnet_debug_wait_timeout_probe(stream=None):
     """Test hook: a kernel whose bounded wait runs out (sets the device status flag to BITNET_ERR_TIMEOUT)."""
     _check(lib().bitnet_debug_wait_timeout_probe(_stream(stream)), "bitnet_debug_wait_timeout_probe")
+
+
+def bitnet_debug_attn_give_up(tile):
+    """Test hook: CTAs of the attention kernels give up before their tile-th tile of cached tokens (-1: off)."""
+    lib().bitnet_debug_attn_give_up(tile)
 
 
 def bitnet_set_early_start(enable: bool):

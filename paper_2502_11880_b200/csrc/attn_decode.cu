@@ -59,6 +59,7 @@ struct DecodeArgs {
   float2* part_ml;                            // [2 * grid][8] running maximum and sum of a part
   float* part_o;                              // [2 * grid][8][D]
   int* dev_status;
+  uint32_t give_up;                           // (test hook) the tile before which a CTA gives up
 };
 
 // The visible tokens of one row: [0, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
@@ -296,7 +297,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const int box = lane % boxes;
     const bool mine = pool < 2;
     const uint32_t box_bytes = (uint32_t)box_rows * (DENSE ? a.row_bytes : both ? 256 : 128);
-    while (item < end) {
+    bool stop = false;
+    while (item < end && !stop) {
       const int64_t off = item - base;
       const int row = (int)(off / r.tiles);
       const int t0 = (int)(off - (int64_t)row * r.tiles);
@@ -316,17 +318,18 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       int page[4], next[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) page[k] = look_up(t0 + k);
-      for (int tb = t0; tb < t_end; tb += 4) {
+      const int t_stop = (int)min((int64_t)t_end, (int64_t)t0 + (a.give_up - it));
+      for (int tb = t0; tb < t_stop && !stop; tb += 4) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) next[k] = look_up(tb + 4 + k);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int t = tb + k, cur = page[k];
-          if (t >= t_end) break;
+          if (t >= t_stop) break;
           const int st = it % L::STAGES;
-          kv_mbar_wait(&s.empty[st], ((it / L::STAGES) & 1u) ^ 1u, abort_flag, &g_attn_error);
+          stop = !kv_mbar_wait_warp(&s.empty[st], ((it / L::STAGES) & 1u) ^ 1u, abort_flag, &g_attn_error);
+          if (stop) break;
           ++it;
-          if (*abort_flag) continue;
           const bool issue = cur != -2;
           const bool bad = issue && (cur < 0 || cur >= a.num_pages);
           if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
@@ -361,18 +364,21 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
         for (int k = 0; k < 4; ++k) page[k] = next[k];
       }
+      if (t_stop < t_end) {
+        kv_give_up(abort_flag, &g_attn_error);
+        stop = true;
+      }
       item += t_end - t0;
       if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
         base += (int64_t)r.tiles * rows_per_token;
         r = range_of(a, ++n);
       }
     }
-    // a CTA that gave up leaves only when its copies have landed
-    if (*abort_flag)
-      for (uint32_t i = it > L::STAGES ? it - L::STAGES : 0; i < it; ++i)
-        for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.full_k[i % L::STAGES], (i / L::STAGES) & 1u) &&
-                                                   kv_mbar_try(&s.full_v[i % L::STAGES], (i / L::STAGES) & 1u)); ++k) {
-        }
+    // leaves only when its copies have landed, which matters where the warps that wait for them have given up
+    for (uint32_t i = it > L::STAGES ? it - L::STAGES : 0; i < it; ++i)
+      for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.full_k[i % L::STAGES], (i / L::STAGES) & 1u) &&
+                                                 kv_mbar_try(&s.full_v[i % L::STAGES], (i / L::STAGES) & 1u)); ++k) {
+      }
     return;
   }
 
@@ -812,6 +818,7 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   d.part_ml = reinterpret_cast<float2*>(w);
   d.part_o = reinterpret_cast<float*>(w + slots * 8);
   d.dev_status = x.dev_status;
+  d.give_up = x.give_up;
   log_launch("attn_decode_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.q_heads, d.kv_heads, d.head_dim,
              d.window, grid);
   if (x.dtype == BITNET_KV_BF16)

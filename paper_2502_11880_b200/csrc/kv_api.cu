@@ -15,6 +15,7 @@ bool ints(const void* p) { return p && aligned(p, 4); }
 bool ints_or_null(const void* p) { return aligned(p, 4); }
 bool page_size_ok(int64_t n) { return n >= 8 && n <= (1 << 20) && (n & (n - 1)) == 0; }
 int64_t clamp_int(int64_t x) { return x < MOST ? x : MOST; }
+std::atomic<uint32_t> g_give_up{0xffffffffu};       // bitnet_debug_attn_give_up
 
 // The books: table[seqs][width] and refs[num_pages].
 int check_books(const int32_t* refs, int64_t num_pages, const int32_t* table, int64_t seqs, int64_t width) {
@@ -69,6 +70,7 @@ int attn_args(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_d
   a->io_f32 = io_dtype == BITNET_KV_F32;
   a->dtype = c->dtype;
   a->dev_status = dev_status;
+  a->give_up = g_give_up.load(std::memory_order_relaxed);
   return BITNET_OK;
 }
 
@@ -196,6 +198,8 @@ size_t bitnet_attn_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t kv_h
     return 0;
   return attn_decode_workspace_bytes() + attn_prompt_parts_bytes(tokens, (int)q_heads, (int)kv_heads);
 }
+
+void bitnet_debug_attn_give_up(int64_t tile) { g_give_up = tile < 0 || tile >= 0xffffffffll ? 0xffffffffu : (uint32_t)tile; }
 
 int bitnet_attn_decode(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_dtype, int64_t q_heads, int64_t stride_token,
                        int64_t stride_head, const int32_t* table, int64_t table_width, const int32_t* kv_len, int64_t seqs, float scale,

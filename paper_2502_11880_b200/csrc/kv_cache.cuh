@@ -56,6 +56,7 @@ struct AttnArgs {
   int q_heads, layer, window, sinks;
   float scale;
   int io_f32;               // q and out are fp32; otherwise they have the cache's type
+  uint32_t give_up;         // the tile before which a CTA gives up (test hook; usually one that never comes)
   int dtype;
   int* dev_status;
 };
@@ -123,7 +124,11 @@ __device__ __forceinline__ bool kv_mbar_try(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait.  One that gives up raises the CTA's abort flag and the device status; the caller goes on (every loop
+__device__ __forceinline__ void kv_give_up(volatile int* abort_flag, int* error) {
+  *abort_flag = 1;
+  atomicExch(error, BITNET_ERR_TIMEOUT);
+}
+// Bounded wait.  One that gives up (2^22 tries of 4 us) raises the CTA's abort flag and the device status; the caller goes on (every loop
 // of these kernels is counted, so all roles reach their ends), and later waits give up at once.
 __device__ __forceinline__ void kv_mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* error) {
   if (kv_mbar_try(bar, parity)) return;
@@ -131,8 +136,14 @@ __device__ __forceinline__ void kv_mbar_wait(uint64_t* bar, uint32_t parity, vol
     if (kv_mbar_try(bar, parity)) return;
     if ((it & 255u) == 0u && *abort_flag) return;
   }
-  *abort_flag = 1;
-  atomicExch(error, BITNET_ERR_TIMEOUT);
+  kv_give_up(abort_flag, error);
+}
+// The same by all lanes of a warp, with one answer: whether the barrier's phase is over.  (Lanes may give up at different times, and
+// where full-warp steps follow, or a buffer is filled, all have to go the same way.)
+__device__ __forceinline__ bool kv_mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* error) {
+  if (__all_sync(0xffffffffu, kv_mbar_try(bar, parity))) return true;
+  kv_mbar_wait(bar, parity, abort_flag, error);
+  return __all_sync(0xffffffffu, *abort_flag == 0);
 }
 
 // The same by polling: a suspended wait takes some hundred cycles to resume, a poll some tens, at the price of issue slots.
