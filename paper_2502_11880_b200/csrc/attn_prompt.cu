@@ -250,7 +250,7 @@ struct Tail {
   uint4 stage[SOFT_WARPS][128];                 // 32 rows x 32 columns of O on their way out, per warp
   Item item[2];
   uint64_t q_full, q_empty, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], v_clean[STAGES];
-  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2], item_full[2], item_empty[2];
+  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2], item_full[2], item_empty[2], drained;
   uint32_t tmem;
   int abort_flag;
 };
@@ -294,6 +294,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       kv_mbar_init(&s.item_full[u], 1);
       kv_mbar_init(&s.item_empty[u], SOFT_WARPS + 3);
     }
+    kv_mbar_init(&s.drained, 1);
     s.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap) : "memory");
@@ -556,6 +557,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
           kb += x.nb;
           ++items;
+        }
+        // all products, and their signals, before the tensor memory goes back and the CTA ends
+        commit(&s.drained);
+        for (uint32_t k = 0; k < KV_WAIT_LIMIT && !kv_mbar_try(&s.drained, 0); ++k) {
         }
       }
     } else {
