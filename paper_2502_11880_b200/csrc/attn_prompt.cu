@@ -72,6 +72,7 @@ struct PromptArgs {
   float2* part_ml;                                    // [units][2 tiles][128 rows]: maximum and sum
   float4* part_o;                                     // [units][8 warps][32 pieces of 4 columns][32 rows]
   int* dev_status;
+  uint32_t give_up;                                   // (test hook) the block before which a CTA gives up
 };
 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t saddr) {      // rows of 128 bytes, 128-byte swizzle
@@ -313,11 +314,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const uint32_t tmem = s.tmem;
   const int steps = (a.head_dim + 15) / 16;                 // of 16 columns of head_dim
 
-  // The `it`-th item of this CTA (every role but the one that finds them).
+  // The `it`-th item of this CTA (every role but the one that finds them); none once somebody has given up.  In the second form all
+  // lanes of a warp ask, and get one answer.
   auto next_item = [&](int it) -> Item {
     kv_mbar_wait(&s.item_full[it & 1], (it >> 1) & 1u, abort_flag, &g_prompt_error);
     Item x = s.item[it & 1];
-    if (*abort_flag) x.nb = -1;                             // somebody gave up: no more work
+    if (*abort_flag) x.nb = -1;
+    return x;
+  };
+  auto next_item_warp = [&](int it) -> Item {
+    const bool there = kv_mbar_wait_warp(&s.item_full[it & 1], (it >> 1) & 1u, abort_flag, &g_prompt_error);
+    Item x = s.item[it & 1];
+    if (!there) x.nb = -1;
     return x;
   };
 
@@ -330,7 +338,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int half = lane / boxes, box = lane % boxes;
       const bool mine = half < HALVES;
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
-      uint32_t kb = 0;                                       // blocks so far
+      uint32_t kb = 0, kb_v = 0;                             // fills of K, of V so far
       // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
       // into parts of their blocks: as many as make one part per SM at most (more of them, and the joins cost more than the SMs
       // give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM 76, 191, 353 us)
@@ -372,8 +380,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             unit = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
           }
         }
-        kv_mbar_wait(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error);
-        __syncwarp();
+        // (a place that somebody may still read is left alone)
+        if (!kv_mbar_wait_warp(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error)) break;
         // the last sequence's last tokens first (a causal row's work grows with its position), its heads side by side
         const int heads = a.kv_heads * a.blocks;
         const bool whole = unit < uncut;
@@ -383,7 +391,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         __syncwarp();
         bool found = false;
         int64_t before = 0;
-        for (int s1 = unit < units && !*abort_flag ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
+        for (int s1 = unit < units ? a.seqs : 0; s1 > 0 && before <= want; s1 -= 32) {
           const Seq q = s1 == a.seqs ? tail : seq_at(s1);
           const int i = q.i, q0 = q.q0, n = q.n;
           const int64_t tiles = (n + span - 1) / span;
@@ -449,39 +457,47 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
         };
         int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
-        for (int j = 0; j < x.nb; ++j, ++kb) {
+        const int n_stop = (int)min((int64_t)x.nb, (int64_t)(a.give_up - kb));
+        bool stop = false;
+        for (int j = 0; j < n_stop; ++j) {
           const int cur = page, cur_y = y;
           if (j + 1 < x.nb) page = look_up(j + 1, y);
           const bool issue = cur != -2;
           const bool bad = issue && (cur < 0 || cur >= a.num_pages);
           if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
           const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
-          const int st = kb % STAGES;
-          const uint32_t par = ((kb / STAGES) & 1u) ^ 1u;
+          const int st = kb_v % STAGES;
+          const uint32_t par = ((kb_v / STAGES) & 1u) ^ 1u;
 #pragma unroll
           for (int pool = 0; pool < 2; ++pool) {
             uint64_t* full = pool ? &s.v_full[st] : &s.k_full[st];
-            kv_mbar_wait(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
-            __syncwarp();
-            if (*abort_flag) continue;
+            stop = !kv_mbar_wait_warp(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
+            if (stop) break;
             if (lane == 0) kv_mbar_expect(full, bytes);
             __syncwarp();
             if (issue)
               kv_box_copy(smem_u32(smem + (pool ? L::V_OFF : L::K_OFF) + st * L::TILE_BYTES + half * HALF + box * box_bytes),
                           pool ? &vmap : &kmap, half * 64, cur_y, x.head_kv, bad ? -1 : cur, a.layer, full);
+            ++(pool ? kb_v : kb);
           }
+          if (stop) break;
         }
+        if (n_stop < x.nb) {
+          kv_give_up(abort_flag, &g_prompt_error);
+          stop = true;
+        }
+        if (stop) break;
       }
       if (a.room && lane == 0) {                              // the workspace is left as it was
         __threadfence();
         if (atomicAdd(a.drawn + 1, 1ull) == gridDim.x - 1) a.drawn[0] = a.drawn[1] = 0;
       }
       __syncwarp();
-      if (*abort_flag)                                        // leave only when the copies have landed
-        for (uint32_t i = kb > STAGES ? kb - STAGES : 0; i < kb; ++i)
-          for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.k_full[i % STAGES], (i / STAGES) & 1u) &&
-                                                     kv_mbar_try(&s.v_full[i % STAGES], (i / STAGES) & 1u)); ++k) {
-          }
+      // leave only when the copies have landed, which matters where those that wait for them have given up
+      for (uint32_t i = kb > STAGES ? kb - STAGES : 0; i < kb; ++i)
+        for (uint32_t k = 0; k < KV_WAIT_LIMIT && !(kv_mbar_try(&s.k_full[i % STAGES], (i / STAGES) & 1u) &&
+                                                   (i >= kb_v || kv_mbar_try(&s.v_full[i % STAGES], (i / STAGES) & 1u))); ++k) {
+        }
     } else if (warp == SOFT_WARPS + 1) {
       // ---------------------------------------------------------- products
       if (elect_one()) {
@@ -572,7 +588,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int my_row = lane / lanes, d = lane % lanes * (bytes / 2);
       uint32_t kb = 0, items = 0;
       for (int it = 0;; ++it) {
-        const Item x = next_item(it);
+        const Item x = next_item_warp(it);
         __syncwarp();
         if (lane == 0) kv_mbar_arrive(&s.item_empty[it & 1]);
         if (x.nb < 0) break;
@@ -637,7 +653,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     const bool wide = a.head_dim % 8 == 0;                    // rows of out begin at multiples of 16 bytes
     uint32_t s_cnt = 0, items = 0;
     for (int it = 0;; ++it) {
-      const Item x = next_item(it);
+      const Item x = next_item_warp(it);
       __syncwarp();
       if (lane == 0) kv_mbar_arrive(&s.item_empty[it & 1]);
       if (x.nb < 0) break;
@@ -926,6 +942,7 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   a.q_neg = x.scale < 0.0f ? 1u : 0u;
   a.c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-30f);
   a.dev_status = x.dev_status;
+  a.give_up = x.give_up;
   // a sequence has at most one pair of tiles that is not full; which CTA has which, in how many parts, is found on the device
   const int64_t pairs = x.tokens / (2 * a.tile_tokens) + (x.seqs < x.tokens ? x.seqs : x.tokens);
   const int64_t sms = dev_info().sm_count, items = pairs * a.kv_heads * a.blocks;

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2502_11880_b200 as bn
-from test_gpu_kv_attn import BF, F32, HF, Paged
+from test_gpu_kv_attn import BF, F32, HF, Paged, prompt_args
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +54,29 @@ def test_decode_that_gives_up(give_up, lens, hq, hkv, dim, page, dtype, io, tile
     give_up(-1)
     bn.bitnet_workspace_init(ws[:bn.ATTN_WORKSPACE_HEAD])
     assert torch.equal(call(), want) and bn.bitnet_device_status() == 0
+
+
+PROMPT = [
+    ([(0, 600), (300, 200)], 8, 2, 128, 16, BF, True),
+    ([(0, 600), (300, 200)], 8, 2, 128, 16, BF, False),
+    ([(9000, 20)], 4, 1, 64, 64, HF, True),                # an item in parts
+    ([(100, 300)] * 5, 64, 32, 32, 32, BF, True),          # several items to a CTA
+    ([(100, 300)] * 5, 64, 32, 32, 32, BF, False),
+]
+
+
+@pytest.mark.parametrize("block", [0, 1, 2, 3])                # every case has a CTA with four blocks
+@pytest.mark.parametrize("spans,hq,hkv,dim,page,dtype,room", PROMPT)
+def test_prompt_that_gives_up(give_up, spans, hq, hkv, dim, page, dtype, room, block):
+    p = Paged([b + n for b, n in spans], hkv, dim, page, dtype, seed=62)
+    start, seq, _ = prompt_args(spans)
+    q, most = p.queries(len(seq), hq, dim, dtype), max(n for _, n in spans)
+    ws = bn.new_attn_workspace(len(seq) if room else 0, hq, hkv, dim)
+    call = lambda: bn.bitnet_attn_prompt(p.cache, p.layer, q, p.table, p.len, start, most, workspace=ws)
+    want = call()
+    give_up(block)
+    gives_up(call)
+    give_up(-1)
+    bn.bitnet_workspace_init(ws[:bn.ATTN_WORKSPACE_HEAD])
+    assert torch.equal(call(), want) and bn.bitnet_device_status() == 0
+    assert int(ws[:bn.ATTN_WORKSPACE_HEAD].sum()) == 0
