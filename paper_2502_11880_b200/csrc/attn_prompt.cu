@@ -340,8 +340,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
       uint32_t kb = 0, kb_v = 0;                             // fills of K, of V so far
       // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
-      // into parts of their blocks: as many as make one part per SM at most (more of them, and the joins cost more than the SMs
-      // give: 8 tokens over 32768, 8 kv heads: one, two, three parts per SM 76, 191, 353 us)
+      // into parts of their blocks: as many as make one part per SM at most.  (8 tokens over 32768, 8 kv heads: 353 us uncut, 67 in one part per SM;
+      // more parts than SMs, and the joins cost more than the SMs give.)
       // A lane's sequence among the 32 that end before s1: first token, tokens, context.  (Those of the last 32 are kept: with
       // look-ups for every item the first one was there 2.6 us after the start.)
       struct Seq {
@@ -903,7 +903,9 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const PromptArgs& a
 
 static constexpr size_t PART_BYTES = 2 * ROWS * 8 + 8 * 1024 * 16;
 
-// Room for the parts of any call of up to so many tokens: one part per SM, unless even one token has too many items to be cut.
+// Room for the parts of a call: one part per SM.  None where a pair of tiles is more than half as many items (kv heads, blocks of query
+// heads) as there are SMs: a call of one pair is not cut then.  (The rest of a call of several pairs could be -- two pairs of 80 items
+// leave 12 beyond 148 -- and is not.)
 size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads) {
   const int64_t least = (int64_t)kv_heads * ceil_div(q_heads / kv_heads, ROWS), sms = dev_info().sm_count;
   return tokens > 0 && 2 * least <= sms ? (size_t)sms * PART_BYTES : 0;
