@@ -41,7 +41,7 @@ int check_tokens(const int32_t* table, int64_t width, const int32_t* kv_len, con
 
 int attn_args(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_dtype, int64_t q_heads, int64_t stride_token,
               int64_t stride_head, int64_t tokens, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
-              int64_t seqs, int64_t max_new, float scale, int64_t window, int64_t sinks, void* out, void* ws, int* dev_status, AttnArgs* a) {
+              int64_t seqs, float scale, int64_t window, int64_t sinks, void* out, void* ws, int* dev_status, AttnArgs* a) {
   int rc = check_cache(c);
   if (rc) return rc;
   rc = check_tokens(table, width, kv_len, q_start, tokens, seqs, dev_status);
@@ -61,7 +61,6 @@ int attn_args(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_d
   a->tokens = tokens;
   a->seqs = seqs;
   a->table_width = width;
-  a->max_new = max_new;
   a->q_heads = (int)q_heads;
   a->layer = (int)layer;
   a->window = (int)clamp_int(window);
@@ -205,7 +204,7 @@ int bitnet_attn_decode(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
                        int64_t stride_head, const int32_t* table, int64_t table_width, const int32_t* kv_len, int64_t seqs, float scale,
                        int64_t window, int64_t sinks, void* out, void* workspace, size_t workspace_bytes, int* dev_status, void* stream) {
   AttnArgs a;
-  const int rc = attn_args(c, layer, q, io_dtype, q_heads, stride_token, stride_head, seqs, table, table_width, kv_len, nullptr, seqs, 1,
+  const int rc = attn_args(c, layer, q, io_dtype, q_heads, stride_token, stride_head, seqs, table, table_width, kv_len, nullptr, seqs,
                            scale, window, sinks, out, workspace, dev_status, &a);
   if (rc) return rc;
   if (io_dtype != BITNET_KV_F32 && io_dtype != c->dtype) return BITNET_ERR_INVALID_ARG;
@@ -220,7 +219,7 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
                        void* workspace, size_t workspace_bytes, int* dev_status, void* stream) {
   AttnArgs a;
   const int rc = attn_args(c, layer, q, io_dtype, q_heads, stride_token, stride_head, tokens, table, table_width, kv_len, q_start, seqs,
-                           max_new, scale, window, sinks, out, workspace, dev_status, &a);
+                           scale, window, sinks, out, workspace, dev_status, &a);
   if (rc) return rc;
   if (!q_start || io_dtype != c->dtype || max_new < 0 || max_new > tokens) return BITNET_ERR_INVALID_ARG;
   if (tokens == 0) return BITNET_OK;

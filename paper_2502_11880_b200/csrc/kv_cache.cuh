@@ -52,7 +52,6 @@ struct AttnArgs {
   const int32_t* kv_len;    // [seqs]
   const int32_t* q_start;   // [seqs + 1] first token of each sequence; null: token i belongs to sequence i
   int64_t tokens, seqs, table_width;
-  int64_t max_new;          // most tokens of one sequence (q_start)
   int q_heads, layer, window, sinks;
   float scale;
   int io_f32;               // q and out are fp32; otherwise they have the cache's type
@@ -144,25 +143,6 @@ __device__ __forceinline__ bool kv_mbar_wait_warp(uint64_t* bar, uint32_t parity
   if (__all_sync(0xffffffffu, kv_mbar_try(bar, parity))) return true;
   kv_mbar_wait(bar, parity, abort_flag, error);
   return __all_sync(0xffffffffu, *abort_flag == 0);
-}
-
-// The same by polling: a suspended wait takes some hundred cycles to resume, a poll some tens, at the price of issue slots.
-__device__ __forceinline__ void kv_mbar_poll(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* error) {
-  const uint32_t addr = smem_u32(bar);
-  for (uint32_t it = 0; it < 16 * KV_WAIT_LIMIT; ++it) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(addr), "r"(parity)
-        : "memory");
-    if (ok) return;
-    if ((it & 255u) == 255u && *abort_flag) return;
-  }
-  *abort_flag = 1;
-  atomicExch(error, BITNET_ERR_TIMEOUT);
 }
 
 // One box of the pool: columns [x, x + 64), rows from `row` of (head, page, layer).  Anything outside the pool reads as 0.
