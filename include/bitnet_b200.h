@@ -436,7 +436,7 @@ typedef struct bitnet_kv_cache {
   /* filled in by the caller */
   int32_t dtype;                 /* BITNET_KV_BF16 or BITNET_KV_F16                                             */
   int32_t kv_heads;
-  int32_t page_size;             /* tokens: a power of two, 8 to 2^20; kv_heads * page_size below 2^27            */
+  int32_t page_size;             /* tokens: a power of two, 8 to 2^20; kv_heads * page_size at most 2^27 - 64     */
   int32_t head_dim;              /* 4 to 128, a multiple of 4                                                     */
   int64_t layers, num_pages;
   void* k;                       /* 16-byte aligned                                                              */

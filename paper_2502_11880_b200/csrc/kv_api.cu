@@ -84,7 +84,8 @@ int bitnet_kv_cache_init(bitnet_kv_cache_t* c) {
   if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return BITNET_ERR_INVALID_ARG;
   if (c->kv_heads < 1 || c->layers < 1 || c->num_pages < 1 || c->layers > MOST || c->num_pages > MOST) return BITNET_ERR_INVALID_ARG;
   if (!page_size_ok(c->page_size) || c->head_dim < 4 || c->head_dim > 128 || c->head_dim % 4) return BITNET_ERR_UNSUPPORTED_SHAPE;
-  if ((int64_t)c->kv_heads * c->page_size * 16 > MOST) return BITNET_ERR_UNSUPPORTED_SHAPE;   // 16-byte pieces of a page, counted in int
+  // 16-byte pieces of a page (at most 16 in a row) are counted in int, by blocks that look 1024 of them ahead
+  if ((int64_t)c->kv_heads * c->page_size * 16 > MOST - 1023) return BITNET_ERR_UNSUPPORTED_SHAPE;
   const int64_t strides[4] = {c->stride_layer, c->stride_page, c->stride_head, c->stride_row};
   for (int64_t s : strides)
     if (s < 0 || s % 8 || s >= (int64_t)1 << 38) return BITNET_ERR_INVALID_ARG;
