@@ -782,8 +782,8 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   memcpy(&vm, c->maps[first + 1], sizeof vm);
   DecodeArgs d;
   d.layer_pages = (int)c->layer_pages;
-  d.k = static_cast<const uint8_t*>(c->k) + 2 * x.layer * c->stride_layer;
-  d.v = static_cast<const uint8_t*>(c->v) + 2 * x.layer * c->stride_layer;
+  d.k = static_cast<const uint8_t*>(c->k) + x.layer * c->stride_layer * 2;
+  d.v = static_cast<const uint8_t*>(c->v) + x.layer * c->stride_layer * 2;
   d.page_bytes = 2 * c->stride_page;
   d.head_bytes = 2 * c->stride_head;
   const bool dense = c->head_dim > 64 && c->stride_row / 8 == ceil_div(c->head_dim, 8) && c->stride_row / 8 % 2 == 1;

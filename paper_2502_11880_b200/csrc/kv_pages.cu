@@ -534,8 +534,8 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const MoveArgs a) {
       if (a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
       return Job{nullptr, nullptr, 0, by_rows};
     }
-    uint8_t* base = (job & 1 ? a.kv.v : a.kv.k) + 2 * layer * a.kv.stride_layer;
-    return Job{base + 2 * src * a.kv.stride_page, base + 2 * dst * a.kv.stride_page, rows, by_rows};
+    uint8_t* base = (job & 1 ? a.kv.v : a.kv.k) + layer * a.kv.stride_layer * 2;
+    return Job{base + src * a.kv.stride_page * 2, base + dst * a.kv.stride_page * 2, rows, by_rows};   // (products of 64 bits)
   };
   const int page_units = a.kv.kv_heads * a.kv.page_size * pieces;
   if (LARGE) {
