@@ -1,5 +1,5 @@
 """Builds libbitnet_b200.so (sm_100a only) next to this file with nvcc, and the compiled part of the Python binding
-(_binding.so, g++).  No JIT cache, no fallback.
+(_binding.so, g++, where the headers of Python and torch are there).  No JIT cache, no fallback.
 
 Every csrc/*.cu is compiled to an object under build/ (in parallel; an object is reused while it is newer than
 its source and every header), then the objects are linked into the shared library.
@@ -8,8 +8,10 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -26,20 +28,49 @@ BINDING = os.path.join(PKG, "_binding.so")
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 
 
-def build_binding(force: bool = False) -> str:
-    """csrc/binding.cpp against this Python and this torch (whose libraries are in the process already)."""
-    newest = max(os.path.getmtime(f) for f in [BINDING_SRC, *glob.glob(os.path.join(INCLUDE, "*.h"))])
-    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) > newest:
-        return BINDING
-    import torch
+def binding_tools():
+    """What the binding is compiled with, as (compiler, include directories, library directory, versions, C++ ABI), or a text that says what is
+    missing: a user of the C ABI alone needs neither a C++ compiler of its own nor the headers of Python and torch."""
+    cxx = os.environ.get("CXX", "g++")
+    if shutil.which(cxx.split()[0]) is None:
+        return f"no C++ compiler ({cxx})"
+    python = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(python, "Python.h")):
+        return f"no Python.h in {python}"
+    try:
+        import torch
+    except ImportError as e:
+        return f"no torch ({e})"
     root = os.path.dirname(torch.__file__)
+    if not os.path.exists(os.path.join(root, "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return f"no headers of torch in {root}"
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-    dirs = [INCLUDE, sysconfig.get_paths()["include"], os.path.join(root, "include"),
-            os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
-    lib = os.path.join(root, "lib")
-    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *[f"-I{d}" for d in dirs], "-o", BINDING, BINDING_SRC,
+    dirs = [INCLUDE, python, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+            os.path.join(cuda, "include")]
+    abi = int(torch.compiled_with_cxx11_abi())
+    return cxx, dirs, os.path.join(root, "lib"), f"python {sysconfig.get_python_version()} torch {torch.__version__} {root} abi {abi}", abi
+
+
+def build_binding(force: bool = False):
+    """csrc/binding.cpp against this Python and this torch (whose libraries are in the process already); again when its source, the header
+    or either of those has changed.  None, with a warning, where something that it takes is missing: the calls it serves then raise."""
+    tools = binding_tools()
+    if isinstance(tools, str):
+        warnings.warn(f"the compiled part of the Python binding is not built: {tools}")
+        return None
+    cxx, dirs, lib, versions, abi = tools
+    newest = max(os.path.getmtime(f) for f in [BINDING_SRC, *glob.glob(os.path.join(INCLUDE, "*.h"))])
+    made_for = os.path.join(OBJ_DIR, "binding_versions.txt")
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) > newest and os.path.exists(made_for):
+        with open(made_for) as f:
+            if f.read() == versions:
+                return BINDING
+    subprocess.run([*cxx.split(), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={abi}",
+                    *[f"-I{d}" for d in dirs], "-o", BINDING, BINDING_SRC,
                     f"-L{lib}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{lib}"], check=True)
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    with open(made_for, "w") as f:
+        f.write(versions)
     return BINDING
 
 
@@ -59,6 +90,7 @@ def stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Both; the library whatever becomes of the binding."""
     with ThreadPoolExecutor(max_workers=1) as other:
         binding = other.submit(build_binding, force)
         build_library(force, verbose)
