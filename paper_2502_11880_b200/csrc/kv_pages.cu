@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendArgs a) {
 
 // ------------------------------------------------------------------------------------------------ planning
 constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_SEQS = 4096;      // entries of the list that one pass plans
+constexpr int PLAN_SEQS = 4096;      // entries of the list that one pass plans at most
 
 // Exclusive prefix of `x` over the CTA; `total` is the sum.  All threads take part.
 __device__ __forceinline__ int block_scan(int x, int& total, int* warp_sums) {
@@ -254,10 +254,11 @@ __device__ __forceinline__ int scan_free(const int32_t* refs, int num_pages, int
   return found;
 }
 
-// Pages for the entries [ceil(from / page), ceil(to / page)) of every row, lowest free pages first in the order of the rows.
+// Pages for the entries [ceil(from / page), ceil(to / page)) of every row, lowest free pages first in the order of the rows; per_pass
+// rows (at most PLAN_SEQS) at a time.
 __global__ void __launch_bounds__(PLAN_THREADS)
 kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* from_len, const int32_t* to_len,
-                  int page_shift, int* dev_status) {
+                  int page_shift, int per_pass, int* dev_status) {
   __shared__ int warp_sums[32];
   __shared__ int start[PLAN_SEQS + 1];     // entries asked for before each row of the pass
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -265,8 +266,8 @@ kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
   auto first_entry = [&](int64_t row) { return (max((int64_t)0, (int64_t)from_len[row]) + mask) >> page_shift; };
   bool lacking = false;
   Counts counts = load_counts(refs, num_pages, 0);
-  for (int64_t r0 = 0; r0 < seqs; r0 += PLAN_SEQS) {
-    const int rows = (int)min((int64_t)PLAN_SEQS, seqs - r0);
+  for (int64_t r0 = 0; r0 < seqs; r0 += per_pass) {
+    const int rows = (int)min((int64_t)per_pass, seqs - r0);
     // 4 rows per thread: counts, then their prefix
     int cnt[PLAN_SEQS / PLAN_THREADS], sum = 0;
 #pragma unroll
@@ -306,11 +307,11 @@ kv_reserve_kernel(int32_t* refs, int num_pages, int32_t* table, int64_t seqs, in
     });
     if (found < need) {                    // the pool has no more: the entries left over hold no page
       lacking = true;
-      for (int k = found + threadIdx.x; k < need; k += PLAN_THREADS) *place(k) = -1;
+      for (int64_t k = found + threadIdx.x; k < need; k += PLAN_THREADS) *place((int)k) = -1;
     }
     __threadfence();
     __syncthreads();
-    if (r0 + PLAN_SEQS < seqs) counts = load_counts(refs, num_pages, 0);
+    if (r0 + per_pass < seqs) counts = load_counts(refs, num_pages, 0);
   }
   if (lacking && dev_status) atomicExch(dev_status, BITNET_ERR_NO_PAGE);
 }
@@ -691,9 +692,11 @@ int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, 
 
 int launch_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* from_len,
                       const int32_t* to_len, int page_size, int* dev_status, cudaStream_t st) {
+  // as many rows to a pass as have fewer than 2^31 entries together, which are counted in int
+  const int64_t most = 0x7fffffff / width, per_pass = most < 1 ? 1 : most < PLAN_SEQS ? most : PLAN_SEQS;
   log_launch("kv_reserve_kernel seqs=%lld", (long long)seqs);
   return launch(kv_reserve_kernel, 1, PLAN_THREADS, st, refs, (int)num_pages, table, seqs, width, from_len, to_len,
-                __builtin_ctz((unsigned)page_size), dev_status);
+                __builtin_ctz((unsigned)page_size), (int)per_pass, dev_status);
 }
 
 int launch_kv_fork(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* parents,

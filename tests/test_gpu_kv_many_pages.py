@@ -31,3 +31,17 @@ def test_pages_beyond_2_to_30():
     at = last * 8 + 56
     assert torch.equal(flat[0][at:at + 8], x.view(8).bfloat16()) and torch.equal(flat[1][at:at + 8], -x.view(8).bfloat16())
     assert int(status) == 0
+
+
+def test_reserve_of_more_than_2_to_31_entries():
+    """Rows that together ask for more pages than 31 bits count: the first few get what the pool has, the rest none, and it is reported."""
+    seqs, width, pages = 2049, 1 << 20, 10
+    table = torch.full((seqs, width), 7, dtype=torch.int32, device="cuda")
+    refs, zero = torch.zeros(pages, dtype=torch.int32, device="cuda"), torch.zeros(seqs, dtype=torch.int32, device="cuda")
+    refs[4] = 1
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bn.bitnet_kv_reserve(refs, table, zero, torch.full_like(zero, 8 * width), 8, dev_status=status)
+    assert int(status) == 8 and bool((refs == 1).all())
+    assert table[0, :9].tolist() == [0, 1, 2, 3, 5, 6, 7, 8, 9] and bool((table[0, 9:] == -1).all())
+    for s in range(1, seqs, 64):
+        assert bool((table[s:s + 64] == -1).all())
