@@ -421,6 +421,8 @@ int bitnet_tl_build_lut_debug(bitnet_fmt_t fmt, const int8_t* q_row, int64_t K, 
  * q_start[seqs] = tokens) says which are whose, and NULL that sequence i has exactly token i.  kv_len counts the new tokens: token j
  * of the n new ones of sequence s is at position kv_len[s] - n + j.
  *
+ * Pages, rows of a table, tokens and entries of a list number at most 2^31 - 8193 each.
+ *
  * Values that only the device sees are checked there, and nothing outside the arrays is read or written.  What cannot be used is
  * passed over and reported in *dev_status (nullable device int) as BITNET_ERR_BAD_PAGE:
  *   a page outside the pool, or none where a token is read or written: not written to; attention reads zeros;

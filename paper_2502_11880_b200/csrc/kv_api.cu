@@ -9,6 +9,7 @@ namespace {
 
 constexpr uint64_t READY = 0x6b76636163686531ull;   // set by bitnet_kv_cache_init
 constexpr int64_t MOST = 0x7fffffff;
+constexpr int64_t COUNT = MOST - 8192;              // most pages, rows, tokens, entries of a list: kernels step up to 8191 beyond the last in int
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool ints(const void* p) { return p && aligned(p, 4); }
@@ -19,7 +20,7 @@ std::atomic<uint32_t> g_give_up{0xffffffffu};       // bitnet_debug_attn_give_up
 
 // The books: table[seqs][width] and refs[num_pages].
 int check_books(const int32_t* refs, int64_t num_pages, const int32_t* table, int64_t seqs, int64_t width) {
-  if (!ints(refs) || num_pages < 1 || num_pages > MOST || seqs < 0 || seqs > MOST || width < 1 || width > MOST) return BITNET_ERR_INVALID_ARG;
+  if (!ints(refs) || num_pages < 1 || num_pages > COUNT || seqs < 0 || seqs > COUNT || width < 1 || width > MOST) return BITNET_ERR_INVALID_ARG;
   return seqs == 0 || ints(table) ? BITNET_OK : BITNET_ERR_INVALID_ARG;
 }
 int check_cache(const bitnet_kv_cache_t* c) {
@@ -31,7 +32,7 @@ int check_cache(const bitnet_kv_cache_t* c) {
 }
 int check_tokens(const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start, int64_t tokens, int64_t seqs,
                  const int* dev_status) {
-  if (seqs < 0 || seqs > MOST || tokens < 0 || tokens > MOST || !ints_or_null(q_start) || !ints_or_null(dev_status))
+  if (seqs < 0 || seqs > COUNT || tokens < 0 || tokens > COUNT || !ints_or_null(q_start) || !ints_or_null(dev_status))
     return BITNET_ERR_INVALID_ARG;
   if (!q_start && tokens != seqs) return BITNET_ERR_INVALID_ARG;
   if (tokens == 0) return BITNET_OK;      // nothing to do, whatever else there is
@@ -82,7 +83,7 @@ int bitnet_kv_cache_init(bitnet_kv_cache_t* c) {
   c->ready = 0;
   if (c->dtype != BITNET_KV_BF16 && c->dtype != BITNET_KV_F16) return BITNET_ERR_INVALID_ARG;
   if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return BITNET_ERR_INVALID_ARG;
-  if (c->kv_heads < 1 || c->layers < 1 || c->num_pages < 1 || c->layers > MOST || c->num_pages > MOST) return BITNET_ERR_INVALID_ARG;
+  if (c->kv_heads < 1 || c->layers < 1 || c->num_pages < 1 || c->layers > MOST || c->num_pages > COUNT) return BITNET_ERR_INVALID_ARG;
   if (!page_size_ok(c->page_size) || c->head_dim < 4 || c->head_dim > 128 || c->head_dim % 4) return BITNET_ERR_UNSUPPORTED_SHAPE;
   // 16-byte pieces of a page (at most 16 in a row) are counted in int, by blocks that look 1024 of them ahead
   if ((int64_t)c->kv_heads * c->page_size * 16 > MOST - 1023) return BITNET_ERR_UNSUPPORTED_SHAPE;
@@ -129,7 +130,7 @@ int bitnet_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t 
 }
 
 size_t bitnet_kv_workspace_bytes(int64_t num_pages, int64_t n) {
-  if (num_pages < 1 || num_pages > MOST || n < 0 || n > MOST) return 0;
+  if (num_pages < 1 || num_pages > COUNT || n < 0 || n > COUNT) return 0;
   return kv_workspace_bytes(num_pages, n);
 }
 
@@ -140,7 +141,7 @@ int bitnet_kv_fork(const bitnet_kv_cache_t* c, int32_t* refs, int32_t* table, in
   if (rc) return rc;
   rc = check_books(refs, c->num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
+  if (n < 0 || n > COUNT) return BITNET_ERR_INVALID_ARG;
   if (n == 0) return BITNET_OK;
   if (seqs < 1 || !ints(kv_len) || !ints(parents) || !ints(children) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < kv_workspace_bytes(1, n)) return BITNET_ERR_WORKSPACE;
@@ -153,7 +154,7 @@ int bitnet_kv_free(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seq
                    const int32_t* list, int64_t n, int* dev_status, void* stream) {
   const int rc = check_books(refs, num_pages, table, seqs, table_width);
   if (rc) return rc;
-  if (n < 0 || n > MOST) return BITNET_ERR_INVALID_ARG;
+  if (n < 0 || n > COUNT) return BITNET_ERR_INVALID_ARG;
   if (n == 0) return BITNET_OK;
   if (seqs < 1 || !ints(kv_len) || !ints(list) || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_release(refs, num_pages, table, seqs, table_width, kv_len, list, n, 8, 0, 0, false, dev_status, (cudaStream_t)stream);
@@ -186,14 +187,14 @@ int bitnet_kv_compact(const bitnet_kv_cache_t* c, int32_t* refs, int32_t* table,
 int bitnet_kv_copy_pages(const bitnet_kv_cache_t* c, const int32_t* src, const int32_t* dst, int64_t n, int* dev_status, void* stream) {
   const int rc = check_cache(c);
   if (rc) return rc;
-  if (n < 0 || n > MOST || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
+  if (n < 0 || n > COUNT || !ints_or_null(dev_status)) return BITNET_ERR_INVALID_ARG;
   if (n == 0) return BITNET_OK;
   if (!ints(src) || !ints(dst)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_copy_pages(kv_view(c), src, dst, n, dev_status, (cudaStream_t)stream);
 }
 
 size_t bitnet_attn_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim) {
-  if (tokens < 0 || tokens > MOST || kv_heads < 1 || q_heads < kv_heads || q_heads > 65536 || q_heads % kv_heads || head_dim < 4 ||
+  if (tokens < 0 || tokens > COUNT || kv_heads < 1 || q_heads < kv_heads || q_heads > 65536 || q_heads % kv_heads || head_dim < 4 ||
       head_dim > 128)
     return 0;
   return attn_decode_workspace_bytes() + attn_prompt_parts_bytes(tokens, (int)q_heads, (int)kv_heads);
