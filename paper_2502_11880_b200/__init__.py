@@ -517,7 +517,9 @@ class KvCache:
     fp16, equal strides, head_dim contiguous; views in another order of the outer dimensions are fine).  Keeps the tensors alive."""
 
     def __init__(self, k, v):
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        # (the stride of a dimension of one entry says nothing)
+        stride, other = ([t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim())] for t in (k, v))
+        if k.dim() != 5 or k.shape != v.shape or stride != other or k.dtype != v.dtype:
             raise BitnetError("KvCache: k and v must be [layers][pages][kv_heads][page_size][head_dim] of one type with equal strides")
         if not (k.is_cuda and v.is_cuda and k.device == v.device) or k.dtype not in (torch.bfloat16, torch.float16):
             raise BitnetError("KvCache: expected CUDA tensors of bfloat16 or float16")
@@ -528,7 +530,7 @@ class KvCache:
         self.dtype, self.device = k.dtype, k.device
         self.desc = KvCacheDesc(dtype=KV_DTYPE[k.dtype], kv_heads=self.kv_heads, page_size=self.page_size, head_dim=self.head_dim,
                                 layers=self.layers, num_pages=self.num_pages, k=k.data_ptr(), v=v.data_ptr(),
-                                stride_layer=k.stride(0), stride_page=k.stride(1), stride_head=k.stride(2), stride_row=k.stride(3))
+                                stride_layer=stride[0], stride_page=stride[1], stride_head=stride[2], stride_row=stride[3])
         _check(lib().bitnet_kv_cache_init(C.byref(self.desc)), "bitnet_kv_cache_init")
         self.ref = C.addressof(self.desc)
         self.scale = self.head_dim ** -0.5

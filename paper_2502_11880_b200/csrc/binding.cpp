@@ -83,6 +83,8 @@ const at::Tensor& rows(PyObject* o, const char* name, int64_t heads, int64_t dim
   if (t.stride(2) != 1 && dim > 1) refuse(name, "head_dim must be contiguous");
   return t;
 }
+// The stride of a dimension of one entry says nothing (torch may leave anything there).
+int64_t step(const at::Tensor& t, int dim) { return t.size(dim) > 1 ? t.stride(dim) : 0; }
 void* stream(PyObject* o, const at::Tensor& t) {
   if (o != Py_None) return PyLong_AsVoidPtr(o);
   return c10::cuda::getCurrentCUDAStream(t.get_device()).stream();
@@ -129,12 +131,12 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* append(PyObject* const* a) {
   const bitnet_kv_cache_t* c = cache(a[0]);
   const at::Tensor &k = rows(a[2], "k", c->kv_heads, c->head_dim), &v = rows(a[3], "v", c->kv_heads, c->head_dim);
-  if (k.scalar_type() != v.scalar_type() || k.size(0) != v.size(0) || k.stride(0) != v.stride(0) || k.stride(1) != v.stride(1))
+  if (k.scalar_type() != v.scalar_type() || k.size(0) != v.size(0) || k.size(1) != v.size(1) || step(k, 0) != step(v, 0) || step(k, 1) != step(v, 1))
     refuse("bitnet_kv_append", "k and v must have one type, shape and strides");
   const int32_t* q_start = book_or_none(a[6], "q_start");
   const int64_t seqs = q_start ? tensor(a[6], "q_start").size(0) - 1 : tensor(a[4], "table").size(0);
   const int32_t* table = book(a[4], "table", 2, seqs);
-  return done(g_fn.append(c, integer(a[1]), k.data_ptr(), v.data_ptr(), type_code(k), k.stride(0), k.stride(1), k.size(0), table,
+  return done(g_fn.append(c, integer(a[1]), k.data_ptr(), v.data_ptr(), type_code(k), step(k, 0), step(k, 1), k.size(0), table,
                           tensor(a[4], "table").size(1), book(a[5], "kv_len", 1, seqs), q_start, seqs, book_or_none(a[7], "dev_status"),
                           stream(a[8], k)),
               "bitnet_kv_append");
@@ -225,7 +227,7 @@ PyObject* decode(PyObject* const* a) {
   const int32_t *table = book(a[3], "table", 2, n), *len = book(a[4], "kv_len", 1, n);
   const at::Tensor out = output(a[8], q, "bitnet_attn_decode");
   const Space ws = space(a[9]);
-  const int rc = g_fn.decode(c, integer(a[1]), q.data_ptr(), type_code(q), q.size(1), q.stride(0), q.stride(1), table,
+  const int rc = g_fn.decode(c, integer(a[1]), q.data_ptr(), type_code(q), q.size(1), step(q, 0), step(q, 1), table,
                              tensor(a[3], "table").size(1), len, n, (float)real(a[5]), integer(a[6]), integer(a[7]), out.data_ptr(), ws.p,
                              ws.n, book_or_none(a[10], "dev_status"), stream(a[11], q));
   return rc ? done(rc, "bitnet_attn_decode") : THPVariable_Wrap(out);
@@ -240,7 +242,7 @@ PyObject* prompt(PyObject* const* a) {
   const int32_t *table = book(a[3], "table", 2, seqs), *len = book(a[4], "kv_len", 1, seqs);
   const at::Tensor out = output(a[10], q, "bitnet_attn_prompt");
   const Space ws = space(a[11]);
-  const int rc = g_fn.prompt(c, integer(a[1]), q.data_ptr(), type_code(q), q.size(1), q.stride(0), q.stride(1), q.size(0), table,
+  const int rc = g_fn.prompt(c, integer(a[1]), q.data_ptr(), type_code(q), q.size(1), step(q, 0), step(q, 1), q.size(0), table,
                              tensor(a[3], "table").size(1), len, q_start, seqs, integer(a[6]), (float)real(a[7]), integer(a[8]),
                              integer(a[9]), out.data_ptr(), ws.p, ws.n, book_or_none(a[12], "dev_status"), stream(a[13], q));
   return rc ? done(rc, "bitnet_attn_prompt") : THPVariable_Wrap(out);
