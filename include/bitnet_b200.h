@@ -511,7 +511,9 @@ int bitnet_kv_copy_pages(const bitnet_kv_cache_t* cache, const int32_t* src, con
  * Attention.  A query at position p sees the tokens c <= p with (window = 0) or c > p - window or c < sinks:
  *   out[t][h] = sum_c softmax_c(scale * <q[t][h], K[c][g]>) V[c][g],  g = h / (q_heads / kv_heads);  a query that sees nothing: 0.
  * q: [tokens][q_heads][head_dim], strides in elements (multiples of 4), 16-byte aligned; out: [tokens][q_heads][head_dim]
- * contiguous, of q's type.  Cached values that no query sees (the rest of a page, released pages) may hold anything.
+ * contiguous, of q's type.  Cached values that no query sees (the rest of a page, released pages) may hold anything.  In a prompt call a
+ * NaN or infinity in V that some query sees may reach queries that do not, up to 255 tokens from one that does (a product 0 * NaN).
+ * Prompts read at most the first 2^30 - 256 tokens of a row of the table, single tokens 2^31 - 256.
  * workspace: bitnet_attn_workspace_bytes bytes; its first 64 KB are zeroed once with bitnet_workspace_init, and every completed call
  * leaves them zeroed (after one that gave up -- BITNET_ERR_TIMEOUT from bitnet_device_status -- they are zeroed anew).  tokens is the most new tokens of a prompt call; with 0 the workspace (1.3 MB) serves decode calls, and prompt
  * calls without cutting the blocks of one tile between CTAs.  One workspace may serve calls of any sizes and both kinds, but no

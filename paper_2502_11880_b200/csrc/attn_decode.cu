@@ -5,7 +5,7 @@
 // over the tokens c that the query's position p sees: c <= p, and with a window either c > p - window or c < sinks.
 // Heads h of one kv head g share K and V.  Every K and V element is used for 4 * heads-per-kv-head flops, so the kernel is
 // bound by HBM; the design keeps the pool streaming (64 ragged sequences of up to 8192 tokens, 64/8 heads of 128, pages of 16,
-// 1.38 GB: 220 us = 6.3 TB/s; one of 131072: 91 us = 5.9 TB/s; one of 517, 32/8 heads: 11 us, all latency):
+// 1.38 GB: 218 to 227 us = 6.1 to 6.35 TB/s; one of 131072: 91 to 94 us; one of 517, 32/8 heads: 11 us, all latency):
 //   * the visible tokens of a row (a token and a kv head) are cut into tiles of 64; all rows' tiles together form one
 //     list that is dealt to the CTAs (one per SM) in equal contiguous parts, whatever the lengths are.  The list exists only on the
 //     device: every CTA derives its part from the lengths.
@@ -180,7 +180,8 @@ struct Layout {
 // KT: element type of the pools; F32: q and out are fp32; DT: head_dim in steps of 16.
 // DENSE: a page's rows lie one after the other and each is an odd number of 16-byte pieces (head_dim 100: 13).  A page of a head is then one
 // plain bulk copy, and ldmatrix meets distinct banks without a swizzle; tensor copies, whose 128-byte box rows begin at odd
-// multiples of 16 bytes there, took 114 instead of 85 us for 9 windows of 4096 tokens, 32 heads of 100.
+// multiples of 16 bytes there, took 114 instead of 85 us for 9 windows of 4096 tokens, 32 heads of 100.  (Rows of one 64-column half take
+// tensor copies whatever their length: not measured there.)
 template <typename KT, bool F32, int DT, bool DENSE>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const DecodeArgs a) {

@@ -17,8 +17,8 @@
 //   * warps 10, 11 bring Q in for the next item, and clear the V rows of a block that no query of the item sees (the end of a page, a
 //     place between the sinks and the window), since 0 * NaN would reach O.
 // Bound by a tile's chain per block -- softmax, 1024 cycles of products, 650 until signals are seen -- of which two run in turn: 3100 to
-// 3200 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 805 to 830 us = 1.0
-// PFLOP/s at the 1.3 to 1.4 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 76 to 82 us).  Blocks of 64 tokens
+// 3200 cycles a pair of blocks against 2048 of the tensor pipe (8192 tokens, 64/8 heads of 128, window 4096: 805 to 835 us = 1.0
+// PFLOP/s at the 1.3 to 1.4 GHz that the power cap leaves; 4 chunks of up to 512 tokens over 5003, 32/8 heads: 76 to 83 us).  Blocks of 64 tokens
 // with two buffers of S, P through shared memory, two threads per row, P in halves, S in two products of 64 columns (the first one before
 // P) or a lane per tile that issues were each slower.
 // Blocks that no row sees are not visited: those of the sinks, then those from the first row's window to the last row.
@@ -340,8 +340,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
       uint32_t kb = 0, kb_v = 0;                             // fills of K, of V so far
       // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
-      // into parts of their blocks: as many as make one part per SM at most.  (8 tokens over 32768, 8 kv heads: 353 us uncut, 67 in one part per SM;
-      // more parts than SMs, and the joins cost more than the SMs give.)
+      // into parts of their blocks: as many as make one part per SM at most.  (8 tokens over 32768, 32/8 heads of 128: 474 us uncut, 72 in one part per
+      // SM; with more parts than SMs the joins cost more than the SMs give.)
       // A lane's sequence among the 32 that end before s1: first token, tokens, context.  (Those of the last 32 are kept: with
       // look-ups for every item the first one was there 2.6 us after the start.)
       struct Seq {

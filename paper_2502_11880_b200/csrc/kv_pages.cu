@@ -6,8 +6,9 @@
 // move by integer atomics (any order gives the same) and the free pages come from an ordered scan of the counts by one
 // CTA.  That scan reads 4 bytes per page (100,000 pages: 0.4 MB) and ends as soon as enough pages are found.
 // Moves of data (whole pages for compaction and copies, rows in use for forks) are a grid-stride copy of 16-byte
-// pieces over the list of pages that the planning CTA left in the workspace; they are bound by HBM (compaction of 1.74 GB, read
-// and written: 278 us with its planning = 6.25 TB/s; 128 forks, 0.63 GB: 85 us).  Appends read fp32 rows once and write
+// pieces over the list of pages that the planning CTA left in the workspace; compaction is bound by HBM (1.74 GB, read and written: 277 to
+// 285 us with its planning = 6.1 to 6.25 TB/s).  Forks read a parent's rows once for every child, the later times from L2: 128 forks of 16
+// parents, 40 MB of distinct rows read and 317 MB written, take 83 to 91 us, of which HBM needs 54.  Appends read fp32 rows once and write
 // 16-bit rows: 8192 tokens of 8 heads of 128, 100 MB, in 23 us with the books' copy and the reserve before it.
 #include <cstring>
 
