@@ -140,7 +140,7 @@ def prepare(case, seed):
         if case["kind"] == "rope":
             s["rope"] = bn.Rope(**rope_args(case))
         if case["kind"] == "shared":
-            s["ws"] = bn.new_attn_shared_workspace(s["q"].shape[0], len(_ints(case["groups"])), case["heads"], case["kv_heads"], case["dim"])
+            s["ws"] = bn.new_attn_shared_workspace(s["q"].shape[0], case["heads"], case["kv_heads"], case["dim"])
     return s
 
 
