@@ -533,6 +533,103 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* cache, int64_t layer, const void
                        const int32_t* kv_len, const int32_t* q_start, int64_t seqs, int64_t max_new, float scale, int64_t window,
                        int64_t sinks, void* out, void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------
+ * The rest of a decode step around the linears and the cache: the norm before a linear, the rotation of queries and keys on their way
+ * into the cache, attention of samples that share a prefix, and the drawing of the next token.  (Element types are BITNET_KV_BF16,
+ * _F16 and _F32.)
+ */
+
+/*
+ * Residual addition, root-mean-square norm and Alg. 1 Phase 1 of the next linear:
+ *   h = residual + x (without residual: x);  r = 1 / sqrt(mean_k(h^2) + eps);  y = (h r) weight;  q, act_scale, act_sum as
+ *   bitnet_quant_act(y) gives them.
+ *   x[T][K], residual[T][K], residual_out[T][K], y[T][K]: each of its own element type; strides between rows in elements.
+ *   residual, weight[K] (NULL: 1), y and act_sum are nullable; residual_out goes with residual, has its type, and may be residual or x itself (then
+ *   with its stride).  No other buffers may overlap.
+ * The sum is binary32 rounded to residual's type, and that value is what is normed.  The squares are summed in 64 bits and r is rounded once; from
+ * there every step is one binary32 operation: q does not depend on T, on strides or on which kernel ran.  eps >= 0.  q and y are contiguous.
+ * Rows of up to 32768 elements (a multiple of 4, at strides of 4 elements, x and the others at 16-byte (16-bit types: 8-byte) addresses)
+ * are read once; any other row is walked three times.
+ */
+int bitnet_add_rmsnorm_quant(const void* x, int x_type, int64_t stride_x, const void* residual, int residual_type, int64_t stride_residual,
+                             void* residual_out, int64_t stride_residual_out, const void* weight, int weight_type, float eps, int64_t T,
+                             int64_t K, void* y, int y_type, int8_t* q, float* act_scale, int32_t* act_sum, void* stream);
+
+/*
+ * Rotary positions.  Element pairs (x[i], x[i + rot_dim / 2]) or, interleaved, (x[2i], x[2i + 1]), i < rot_dim / 2, turn by position * f[i]; what
+ * lies beyond rot_dim moves as it is.
+ *   f[i] = base^(-2i / rot_dim), then with scaling
+ *     BITNET_ROPE_LINEAR  f / factor (positions interpolated);
+ *     BITNET_ROPE_BANDS   by the turns n = f * context / (2 pi) that a pair makes within the original context: n >= high: f; n <= low: f / factor; in
+ *                         between (1 - s) f / factor + s f with s = (n - low) / (high - low).
+ *   freqs (HOST, rot_dim / 2 values, radians per position; read by bitnet_rope_init only) takes the place of all of that.
+ *   magnitude multiplies the sines and cosines (0 means 1).
+ * Angles are exact to 2^-31 of a turn at every position.  The description is plain host data, completed by bitnet_rope_init; it may be copied
+ * and is read during a call only.
+ */
+enum { BITNET_ROPE_NONE = 0, BITNET_ROPE_LINEAR = 1, BITNET_ROPE_BANDS = 2 };
+typedef struct bitnet_rope {
+  /* filled in by the caller */
+  int32_t rot_dim;               /* 2 to 128, even                                                               */
+  int32_t interleaved;
+  int32_t scaling;
+  int32_t reserved;
+  double base, factor, low, high, context, magnitude;
+  const double* freqs;           /* nullable                                                                     */
+  /* filled in by bitnet_rope_init */
+  uint64_t ready;
+  uint64_t step[64];             /* turns per position, in 2^-64                                                 */
+} bitnet_rope_t;
+int bitnet_rope_init(bitnet_rope_t* rope);
+
+/*
+ * bitnet_kv_append with rotation: writes the rotated rows of k and the rows of v into their pages, and the rotated rows of q to
+ * q_out[tokens][q_heads][head_dim] (contiguous, 16-byte aligned, fp32 or the cache's type), each value computed in binary32 and rounded once.  Tables, lengths and
+ * q_start as for bitnet_kv_append; positions are those of the tokens.
+ *   q, k, v: of `in_type` (fp32 or the cache's type), head_dim contiguous, any strides (multiples of 8 elements, and 16-byte addresses, are fastest); k and v
+ *   have one pair of strides.  q_heads = 0: q and q_out are not looked at.  q_out may be q itself where q is contiguous and of q_out's type.
+ * rot_dim may not exceed head_dim.  A token before the start (an idle row) is passed over, its row of q_out left as it was; one without a page is
+ * reported, its row of q_out is written.
+ */
+int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const bitnet_rope_t* rope, const void* q, int64_t q_heads,
+                          int64_t q_stride_token, int64_t q_stride_head, const void* k, const void* v, int in_type, int64_t stride_token,
+                          int64_t stride_head, int64_t tokens, const int32_t* table, int64_t table_width, const int32_t* kv_len,
+                          const int32_t* q_start, int64_t seqs, void* q_out, int out_type, int* dev_status, void* stream);
+
+/*
+ * bitnet_attn_decode for sequences that share beginnings: forked samples of one prompt, requests over one document.  Sequences
+ * group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1], ascending, group_start[0] = 0, group_start[groups] = seqs) have their first prefix_len[g] tokens
+ * (int32 [groups]; 0: none) in common: those are read through the row of the table of the group's first sequence (which has to hold their pages), once for the whole group, on the tensor cores;
+ * every sequence's own tokens after them through its own row.  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
+ * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
+ * and that the probabilities of the prefix are rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
+ * A sequence in no group (an array that is not as above) is taken by itself.  Reads at most the first 2^30 - 256 tokens of a prefix.
+ * workspace: bitnet_attn_shared_workspace_bytes bytes (20 MB, and 528 bytes per sequence and query head of 128); its first 64 KB as for the other attention
+ * calls, whose workspace it may be too.
+ */
+size_t bitnet_attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int64_t kv_heads, int64_t head_dim);
+int bitnet_attn_shared(const bitnet_kv_cache_t* cache, int64_t layer, const void* q, int io_dtype, int64_t q_heads, int64_t stride_token,
+                       int64_t stride_head, const int32_t* table, int64_t table_width, const int32_t* kv_len, int64_t seqs,
+                       const int32_t* group_start, const int32_t* prefix_len, int64_t groups, float scale, int64_t window, int64_t sinks,
+                       void* out, void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
+
+/*
+ * Draws one token per row of logits[rows][vocab] (fp32, bf16 or fp16; stride between rows in elements, any):
+ *   w[i] = exp((x[i] - max x) / temperature);  the order: larger x first, of equal ones the lower index first;
+ *   kept are the first top_k of the order; of those the shortest beginning whose w sum to at least top_p times theirs (at least one);
+ *   of those the ones with w >= min_p;
+ *   tokens[r] = the first index at which the sum of kept w, in the order of the vocabulary, exceeds u * (their sum); prob[r] = its share of that sum.
+ *   u[rows] fp32 in [0, 1) (what lies outside counts as 0 or as the largest below 1).  temperature, top_p, min_p [rows] fp32, top_k [rows] int32: device arrays,
+ *   each nullable; off are temperature 1, top_k <= 0 or >= vocab, top_p >= 1, min_p <= 0, and those that are no numbers; min_p above 1 counts as 1; top_p <= 0 keeps one.
+ *   temperature <= 0 or not a number: the largest logit of lowest index, prob 1.  tokens[rows] int32; prob[rows] fp32, nullable.
+ * A logit that is no number counts as -infinity, which is never drawn; infinite ones share all weight.  A row of nothing but those gives token -1, prob 0.
+ * Weights are kept as 32-bit fixed point of the largest (those below 2^-33 of it count as 0), and added exactly: the token does not depend on rows, strides or
+ * how the work is split.  vocab at most 2^30.
+ */
+int bitnet_sample(const void* logits, int type, int64_t stride, int64_t rows, int64_t vocab, const float* u, const float* temperature,
+                  const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* prob, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,8 @@ SYMBOLS = [
     "bitnet_elut_packed_bytes", "bitnet_pack_elut", "bitnet_unpack_elut", "bitnet_elut_linear_group",
     "bitnet_kv_cache_init", "bitnet_kv_append", "bitnet_kv_reserve", "bitnet_kv_workspace_bytes", "bitnet_kv_fork", "bitnet_kv_free",
     "bitnet_kv_trim", "bitnet_kv_compact", "bitnet_kv_copy_pages", "bitnet_attn_workspace_bytes", "bitnet_attn_decode", "bitnet_attn_prompt",
-    "bitnet_debug_attn_give_up",
+    "bitnet_debug_attn_give_up", "bitnet_attn_shared", "bitnet_attn_shared_workspace_bytes", "bitnet_rope_init", "bitnet_kv_append_rope",
+    "bitnet_add_rmsnorm_quant", "bitnet_sample",
 ]
 
 _lib = None
@@ -105,6 +106,13 @@ def lib():
         L.bitnet_attn_workspace_bytes.restype = sz
         L.bitnet_attn_decode.argtypes = [vp, i64, vp, ci, i64, i64, i64, vp, i64, vp, i64, fl, i64, i64, vp, vp, sz, vp, vp]
         L.bitnet_attn_prompt.argtypes = [vp, i64, vp, ci, i64, i64, i64, i64, vp, i64, vp, vp, i64, i64, fl, i64, i64, vp, vp, sz, vp, vp]
+        L.bitnet_attn_shared_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.bitnet_attn_shared_workspace_bytes.restype = sz
+        L.bitnet_attn_shared.argtypes = [vp, i64, vp, ci, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, fl, i64, i64, vp, vp, sz, vp, vp]
+        L.bitnet_rope_init.argtypes = [vp]
+        L.bitnet_kv_append_rope.argtypes = [vp, i64, vp, vp, i64, i64, i64, vp, vp, ci, i64, i64, i64, vp, i64, vp, vp, i64, vp, ci, vp, vp]
+        L.bitnet_add_rmsnorm_quant.argtypes = [vp, ci, i64, vp, ci, i64, vp, i64, vp, ci, fl, i64, i64, vp, ci, vp, vp, vp, vp]
+        L.bitnet_sample.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -561,7 +569,8 @@ def _binding():
         L = lib()
         m.bind(BitnetError, _check, tuple(C.cast(f, C.c_void_p).value for f in (
             L.bitnet_kv_append, L.bitnet_kv_reserve, L.bitnet_kv_fork, L.bitnet_kv_free, L.bitnet_kv_trim, L.bitnet_kv_compact,
-            L.bitnet_kv_copy_pages, L.bitnet_attn_decode, L.bitnet_attn_prompt)))
+            L.bitnet_kv_copy_pages, L.bitnet_attn_decode, L.bitnet_attn_prompt, L.bitnet_attn_shared, L.bitnet_kv_append_rope,
+            L.bitnet_add_rmsnorm_quant, L.bitnet_sample)))
         _fast = m
     return _fast
 
@@ -673,3 +682,84 @@ def bitnet_attn_prompt(cache, layer, q, table, kv_len, q_start, max_new, scale=N
         return (_fast or _binding()).attn_prompt(cache.ref, layer, q, table, kv_len, q_start, max_new, cache.scale if scale is None else scale,
                                                  window, sinks, out, _attn_ws(cache, q, 1) if workspace is None else workspace, dev_status,
                                                  None)
+
+
+def bitnet_attn_shared_workspace_bytes(seqs, q_heads, kv_heads, head_dim) -> int:
+    return lib().bitnet_attn_shared_workspace_bytes(seqs, q_heads, kv_heads, head_dim)
+
+
+def new_attn_shared_workspace(seqs, q_heads, kv_heads, head_dim, device="cuda"):
+    """A workspace for bitnet_attn_shared calls of up to so many sequences, its counters zeroed."""
+    size = bitnet_attn_shared_workspace_bytes(seqs, q_heads, kv_heads, head_dim)
+    if size == 0:
+        _check(1, "bitnet_attn_shared_workspace_bytes")
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    bitnet_workspace_init(ws[:ATTN_WORKSPACE_HEAD])
+    return ws
+
+
+def bitnet_attn_shared(cache, layer, q, table, kv_len, group_start, prefix_len, scale=None, window=0, sinks=0, out=None, workspace=None,
+                       dev_status=None, stream=None):
+    """bitnet_attn_decode for groups of sequences (group_start [groups + 1]) whose first prefix_len [groups] tokens are the same: read once
+    per group.  q [seqs][q_heads][head_dim] in the cache's type -> out, same shape and type."""
+    with _on(stream):
+        if workspace is None and q.dim() == 3 and q.shape[0] and q.shape[1] and q.shape[1] % cache.kv_heads == 0:
+            workspace = new_attn_shared_workspace(q.shape[0], q.shape[1], cache.kv_heads, cache.head_dim, cache.device)
+        return (_fast or _binding()).attn_shared(cache.ref, layer, q, table, kv_len, group_start, prefix_len, cache.scale if scale is None else scale,
+                                                 window, sinks, out, workspace, dev_status, None)
+
+
+# ---- rotary positions, norm, drawing of tokens
+ROPE_SCALING = {"none": 0, "linear": 1, "bands": 2}
+
+
+class RopeDesc(C.Structure):
+    """Mirror of bitnet_rope_t."""
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("reserved", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("context", C.c_double), ("magnitude", C.c_double),
+                ("freqs", C.POINTER(C.c_double)), ("ready", C.c_uint64), ("step", C.c_uint64 * 64)]
+
+
+class Rope:
+    """Rotation of the first `rot` elements of a head: pairs (i, i + rot/2) (layout "half") or (2i, 2i + 1) ("interleaved") turn by position *
+    base^(-2i/rot).  scaling "linear" divides the frequencies by factor, "bands" those of pairs that make fewer than `high` turns within `context`
+    positions (all of it below `low`).  freqs: rot/2 frequencies in radians per position, in place of all that; magnitude multiplies sines and cosines."""
+
+    def __init__(self, rot, base=10000.0, layout="half", scaling="none", factor=1.0, low=1.0, high=4.0, context=8192, freqs=None, magnitude=1.0):
+        if layout not in ("half", "interleaved") or scaling not in ROPE_SCALING:
+            raise BitnetError("Rope: layout is 'half' or 'interleaved', scaling 'none', 'linear' or 'bands'")
+        given = None
+        if freqs is not None:
+            freqs = [float(f) for f in freqs]
+            if len(freqs) != rot // 2:
+                raise BitnetError("Rope: freqs must be rot / 2 values")
+            given = (C.c_double * len(freqs))(*freqs)
+        self.rot, self.layout = rot, layout
+        self.desc = RopeDesc(rot_dim=rot, interleaved=int(layout == "interleaved"), scaling=ROPE_SCALING[scaling], base=base, factor=factor, low=low,
+                             high=high, context=context, magnitude=magnitude, freqs=given)
+        _check(lib().bitnet_rope_init(C.byref(self.desc)), "bitnet_rope_init")
+        self.desc.freqs = None                # (read by bitnet_rope_init only)
+        self.ref = C.addressof(self.desc)
+
+
+def bitnet_kv_append_rope(cache, layer, rope, q, k, v, table, kv_len, q_start=None, q_out=None, q_dtype=None, dev_status=None, stream=None):
+    """bitnet_kv_append with the rows of q [tokens][q_heads][head_dim] and k rotated by their tokens' positions; returns q's (q_out, or a new tensor of
+    q_dtype, by default q's type).  q = None: keys and values only."""
+    with _on(stream):
+        return (_fast or _binding()).kv_append_rope(cache.ref, layer, rope.ref, q, k, v, table, kv_len, q_start, q_out,
+                                                    -1 if q_dtype is None else KV_DTYPE.get(q_dtype, -1), dev_status, None)
+
+
+def bitnet_add_rmsnorm_quant(x, weight=None, eps=1e-5, residual=None, residual_out=None, y=None, q=None, act_scale=None, act_sum=None, stream=None):
+    """h = residual + x (written to residual_out; by default residual itself is updated), y = h / rms(h) * weight (written to y, if that is given), and the int8
+    codes that bitnet_quant_act gives for y: returns (q, act_scale)."""
+    with _on(stream):
+        return (_fast or _binding()).add_rmsnorm_quant(x, weight, eps, residual, residual if residual_out is None else residual_out, y, q, act_scale,
+                                                       act_sum, None)
+
+
+def bitnet_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, prob=None, stream=None):
+    """One token per row of logits [rows][vocab] from the random numbers u [rows]; the settings are CUDA vectors of one value per row, or None.
+    Returns (tokens int32, prob fp32: the tokens' shares of what was kept)."""
+    with _on(stream):
+        return (_fast or _binding()).sample(logits, u, temperature, top_k, top_p, min_p, tokens, prob, None)

@@ -73,6 +73,12 @@ struct PromptArgs {
   float4* part_o;                                     // [units][8 warps][32 pieces of 4 columns][32 rows]
   int* dev_status;
   uint32_t give_up;                                   // (test hook) the block before which a CTA gives up
+  // SHARED: q_start and seqs are those of the groups; see the kernel
+  const int32_t* prefix;                              // [groups]
+  float4* base_ml;                                    // [tokens][q_heads]: maximum, sum, and the CTAs that the item lies on
+  float* base_o;                                      // [tokens][q_heads][padded head_dim]
+  float2* spill_ml;                                   // [CTAs][2 tiles][128 rows]
+  float* spill_o;                                     // [CTAs][2 tiles][128 rows][padded head_dim]
 };
 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t saddr) {      // rows of 128 bytes, 128-byte swizzle
@@ -237,6 +243,8 @@ struct Item {
   int n0, t1;                       // blocks: 0 .. n0-1 (sinks), then t1 ..
   int b0, nb;                       // the part's first block, and its blocks; nb = -1: no more items
   int two;                          // the second tile has rows
+  int prefix;                       // SHARED: of the group, within the table
+  int c0, c1;                       // SHARED: the first and the last CTA that the item lies on
   int parts;                        // of the item, which join if there are several
   int part;
   int64_t unit0, id;                // the first part's place in the workspace, the item's number among those cut
@@ -267,7 +275,13 @@ __device__ __forceinline__ bool has_unseen(const PromptArgs& a, const Item& x, i
 }
 
 // KT: element type of q, the pools and out; HALVES: 64-column halves of a padded row.
-template <typename KT, int HALVES>
+//
+// SHARED: the part of single tokens' attention that groups of sequences have in common (attn_shared).  Rows are (sequence, query head) pairs of
+// one group and kv head, the columns the group's prefix, read through the pages of its first sequence; no order between rows and columns, but a row sees
+// no more than its sequence has, and what its window leaves.  All groups' items form one list of (item, block) that is cut into equal
+// contiguous parts, one per CTA; an item's first part goes to its rows' places in the workspace, a later one (a CTA has one at most, at its beginning) to
+// the CTA's, both as maximum, sum and unscaled O.  The kernel that follows takes each sequence's own tokens and joins (attn_decode.cu).
+template <typename KT, int HALVES, bool SHARED>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const PromptArgs a) {
   using L = Layout<HALVES>;
@@ -339,6 +353,176 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const bool mine = half < HALVES;
       const uint32_t box_bytes = (uint32_t)box_rows * 128;
       uint32_t kb = 0, kb_v = 0;                             // fills of K, of V so far
+      // The blocks of an item; false: somebody has given up.
+      auto copy_blocks = [&](const Item& x) -> bool {
+        auto look_up = [&](int j, int& y) -> int {
+          const int tok = block_start(x, j) + box * box_rows;
+          y = tok & ((1 << a.page_shift) - 1);
+          if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
+          return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
+        };
+        int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
+        const int n_stop = (int)min((int64_t)x.nb, (int64_t)(a.give_up - kb));
+        bool stop = false;
+        for (int j = 0; j < n_stop; ++j) {
+          const int cur = page, cur_y = y;
+          if (j + 1 < x.nb) page = look_up(j + 1, y);
+          const bool issue = cur != -2;
+          const bool bad = issue && (cur < 0 || cur >= a.num_pages);
+          if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+          const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
+          const int st = kb_v % STAGES;
+          const uint32_t par = ((kb_v / STAGES) & 1u) ^ 1u;
+#pragma unroll
+          for (int pool = 0; pool < 2; ++pool) {
+            uint64_t* full = pool ? &s.v_full[st] : &s.k_full[st];
+            stop = !kv_mbar_wait_warp(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
+            if (stop) break;
+            if (lane == 0) kv_mbar_expect(full, bytes);
+            __syncwarp();
+            if (issue)
+              kv_box_copy(smem_u32(smem + (pool ? L::V_OFF : L::K_OFF) + st * L::TILE_BYTES + half * HALF + box * box_bytes),
+                          pool ? &vmap : &kmap, half * 64, cur_y, x.head_kv, bad ? -1 : cur, a.layer, full);
+            ++(pool ? kb_v : kb);
+          }
+          if (stop) break;
+        }
+        if (n_stop < x.nb) {
+          kv_give_up(abort_flag, &g_prompt_error);
+          stop = true;
+        }
+        return !stop;
+      };
+      if constexpr (SHARED) {
+        // A lane's group among 32 from g0 on: its rows, its visible blocks, its items.
+        struct Group {
+          int q0, n, prefix, lo, n0, t1, nb;
+          int64_t items, before;       // before: (item, block) pairs of earlier groups of the 32
+        };
+        const int span = 2 * a.tile_tokens, heads = a.kv_heads * a.blocks;
+        int64_t chunk = 0;             // (item, block) pairs of the 32 groups
+        auto groups_at = [&](int g0) -> Group {
+          Group t = {0, 0, 0, 0, 0, 0, 1, 0, 0};
+          if (g0 + lane < a.seqs) {
+            t.q0 = __ldg(a.q_start + g0 + lane);
+            t.n = max(0, __ldg(a.q_start + g0 + lane + 1) - t.q0);
+            if (t.q0 < 0 || t.q0 >= a.tokens) t.n = 0;
+            else t.n = min(t.n, a.tokens - t.q0);
+            t.prefix = max(0, min(__ldg(a.prefix + g0 + lane), a.max_len));
+          }
+          if (a.window > 0) {
+            // what the window of the group's shortest sequence reaches back to
+            for (int k = 0; k < 32 && g0 + k < a.seqs; ++k) {
+              const int q0 = __shfl_sync(0xffffffffu, t.q0, k), n = __shfl_sync(0xffffffffu, t.n, k);
+              int least = 0x7fffffff;
+              for (int i = lane; i < n; i += 32) least = min(least, __ldg(a.kv_len + q0 + i));
+              least = __reduce_min_sync(0xffffffffu, least);
+              if (lane == k) t.lo = max(0, min(least - a.window, a.max_len));
+            }
+          }
+          const int end = (t.prefix + KB - 1) / KB;
+          t.t1 = t.lo / KB;
+          t.n0 = min(min((min(a.sinks, t.lo) + KB - 1) / KB, t.t1), end);
+          t.nb = max(1, t.n0 + max(0, end - t.t1));            // (a group without a prefix has a block with nothing visible)
+          t.items = (int64_t)((t.n + span - 1) / span) * heads;
+          int64_t sum = t.items * t.nb;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+          }
+          t.before = sum - t.items * t.nb;
+          chunk = __shfl_sync(0xffffffffu, sum, 31);
+          return t;
+        };
+        // the whole list, and this CTA's part [at, end)
+        Group mine_g = groups_at(0);
+        int64_t total = chunk, items = 0;
+        int longest = 0;
+        {
+          int64_t n = mine_g.items;
+          int most = mine_g.items > 0 ? mine_g.nb : 0;
+          for (int g0 = 32; g0 < a.seqs; g0 += 32) {
+            const Group t = groups_at(g0);
+            total += chunk;
+            n += t.items;
+            most = max(most, t.items > 0 ? t.nb : 0);
+          }
+#pragma unroll
+          for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
+          items = n;
+          longest = __reduce_max_sync(0xffffffffu, most);
+          if (a.seqs > 32) mine_g = groups_at(0);
+        }
+        // as many parts as CTAs; where all items are alike and fewer than CTAs, as many to each as fit, so that no CTA has parts of two
+        int64_t parts = min((int64_t)gridDim.x, total);
+        if (items > 0 && items <= gridDim.x && total == items * longest) parts = items * min((int64_t)gridDim.x / items, (int64_t)longest);
+        int64_t at = (int64_t)blockIdx.x < parts ? total * blockIdx.x / parts : total;
+        const int64_t end = (int64_t)blockIdx.x < parts ? total * (blockIdx.x + 1) / parts : total;
+        int g0 = 0;
+        int64_t base = 0;                                      // pairs before group g0
+        int it = 0;
+        for (bool stop = false; !stop;) {
+          if (!kv_mbar_wait_warp(&s.item_empty[it & 1], ((it >> 1) & 1u) ^ 1u, abort_flag, &g_prompt_error)) break;
+          if (at >= end) {
+            if (lane == 0) {
+              s.item[it & 1].nb = -1;
+              kv_mbar_arrive(&s.item_full[it & 1]);
+            }
+            break;
+          }
+          while (at >= base + chunk) {                         // (at < total: the groups that hold it are there)
+            base += chunk;
+            g0 += 32;
+            mine_g = groups_at(g0);
+          }
+          const int64_t local = at - base;
+          const unsigned here = __ballot_sync(0xffffffffu, mine_g.items > 0 && local >= mine_g.before && local < mine_g.before + mine_g.items * mine_g.nb);
+          const int who = __ffs(here) - 1;
+          const int q0 = __shfl_sync(0xffffffffu, mine_g.q0, who), n = __shfl_sync(0xffffffffu, mine_g.n, who), nb = __shfl_sync(0xffffffffu, mine_g.nb, who);
+          const int64_t in_group = local - __shfl_sync(0xffffffffu, mine_g.before, who), id = in_group / nb;
+          Item t;
+          t.seq = q0;
+          t.q0 = q0;
+          t.n_new = n;
+          const int hb = (int)(id % heads), b0 = hb % a.blocks * a.per_block;
+          t.head_kv = hb / a.blocks;
+          t.head0 = t.head_kv * a.group + b0;
+          t.heads = min(a.per_block, a.group - b0);
+          t.tok0 = (int)(id / heads) * span;
+          t.two = t.tok0 + a.tile_tokens < n;
+          t.prefix = __shfl_sync(0xffffffffu, mine_g.prefix, who);
+          t.n0 = __shfl_sync(0xffffffffu, mine_g.n0, who);
+          t.t1 = __shfl_sync(0xffffffffu, mine_g.t1, who);
+          t.b0 = (int)(in_group - id * nb);
+          t.nb = (int)min((int64_t)(nb - t.b0), end - at);
+          const int64_t first = at - t.b0;
+          t.c0 = (int)(((first + 1) * parts - 1) / total);
+          t.c1 = (int)(((first + nb) * parts - 1) / total);
+          t.pos0 = 0;
+          t.parts = 1;
+          t.part = 0;
+          t.unit0 = t.id = 0;
+          // the tokens that some row of the item sees: from its shortest sequence's window to its longest sequence's end
+          int least = 0x7fffffff, most = 0;
+          for (int i = t.tok0 + lane; i < min(n, t.tok0 + span); i += 32) {
+            const int len = __ldg(a.kv_len + q0 + i);
+            least = min(least, len);
+            most = max(most, len);
+          }
+          least = __reduce_min_sync(0xffffffffu, least);
+          most = __reduce_max_sync(0xffffffffu, most);
+          t.p_last = min(most, t.prefix) - 1;
+          t.lo = a.window > 0 ? max(0, min(least - a.window, a.max_len)) : 0;
+          if (lane == 0) {
+            s.item[it & 1] = t;
+            kv_mbar_arrive(&s.item_full[it & 1]);
+          }
+          ++it;
+          at += t.nb;
+          stop = !copy_blocks(t);
+        }
+      } else {
       // The items that are left when every SM has had as many as all can have (all items, if there are fewer than SMs) are cut
       // into parts of their blocks: as many as make one part per SM at most.  (8 tokens over 32768, 32/8 heads of 128: 474 us uncut, 72 in one part per
       // SM; with more parts than SMs the joins cost more than the SMs give.)
@@ -450,47 +634,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (!found) break;
         if (a.window > 0 && lane == 0 && a.dev_status && (int64_t)x.pos0 + min(x.n_new, x.tok0 + span) > a.max_len)
           atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-        auto look_up = [&](int j, int& y) -> int {
-          const int tok = block_start(x, j) + box * box_rows;
-          y = tok & ((1 << a.page_shift) - 1);
-          if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
-          return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
-        };
-        int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
-        const int n_stop = (int)min((int64_t)x.nb, (int64_t)(a.give_up - kb));
-        bool stop = false;
-        for (int j = 0; j < n_stop; ++j) {
-          const int cur = page, cur_y = y;
-          if (j + 1 < x.nb) page = look_up(j + 1, y);
-          const bool issue = cur != -2;
-          const bool bad = issue && (cur < 0 || cur >= a.num_pages);
-          if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-          const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
-          const int st = kb_v % STAGES;
-          const uint32_t par = ((kb_v / STAGES) & 1u) ^ 1u;
-#pragma unroll
-          for (int pool = 0; pool < 2; ++pool) {
-            uint64_t* full = pool ? &s.v_full[st] : &s.k_full[st];
-            stop = !kv_mbar_wait_warp(pool ? &s.v_empty[st] : &s.k_empty[st], par, abort_flag, &g_prompt_error);
-            if (stop) break;
-            if (lane == 0) kv_mbar_expect(full, bytes);
-            __syncwarp();
-            if (issue)
-              kv_box_copy(smem_u32(smem + (pool ? L::V_OFF : L::K_OFF) + st * L::TILE_BYTES + half * HALF + box * box_bytes),
-                          pool ? &vmap : &kmap, half * 64, cur_y, x.head_kv, bad ? -1 : cur, a.layer, full);
-            ++(pool ? kb_v : kb);
-          }
-          if (stop) break;
-        }
-        if (n_stop < x.nb) {
-          kv_give_up(abort_flag, &g_prompt_error);
-          stop = true;
-        }
-        if (stop) break;
+        if (!copy_blocks(x)) break;
       }
       if (a.room && lane == 0) {                              // the workspace is left as it was
         __threadfence();
         if (atomicAdd(a.drawn + 1, 1ull) == gridDim.x - 1) a.drawn[0] = a.drawn[1] = 0;
+      }
       }
       __syncwarp();
       // leave only when the copies have landed, which matters where those that wait for them have given up
@@ -660,8 +809,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int tok = x.tok0 + u * a.tile_tokens + row_tok;
       const bool valid = row < a.tile_tokens * a.per_block && hd < x.heads && tok < x.n_new && x.q0 >= 0 && (int64_t)x.q0 + tok < a.tokens;
       if (u == 1 && !x.two) continue;
-      const int64_t pos = valid ? (int64_t)x.pos0 + tok : -1;
-      const int p = (int)min(pos, (int64_t)a.max_len - 1);    // last token that the row may see; < 0: sees nothing
+      int64_t pos = valid ? (int64_t)x.pos0 + tok : -1;
+      if constexpr (SHARED) pos = valid ? (int64_t)__ldg(a.kv_len + x.q0 + tok) - 1 : -1;
+      int p = (int)min(pos, (int64_t)a.max_len - 1);          // last token that the row may see; < 0: sees nothing
+      if constexpr (SHARED) p = min(p, x.prefix - 1);
       // first token of its window
       const int wlo = a.window > 0 ? (int)max((int64_t)0, min(pos - a.window + 1, (int64_t)a.max_len)) : 0;
       float m = -INFINITY;
@@ -741,6 +892,49 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         if (lane == 0) kv_mbar_arrive(&s.p_full[u]);
       }
 
+      if constexpr (SHARED) {
+        // ---- maximum, sum and unscaled O, 16 columns at a time, through this warp's staging rows and out as pieces of 64 bytes
+        const float2 l = unpair(l2);
+        const float sum = l.x + l.y;
+        kv_mbar_wait(&s.o_full[u], items & 1u, abort_flag, &g_prompt_error);
+        fence_after();
+        ++items;
+        const bool first = x.b0 == 0;
+        const int64_t of_row = ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd), of_cta = ((int64_t)blockIdx.x * 2 + u) * ROWS + row;
+        if (valid) {
+          if (first) a.base_ml[of_row] = make_float4(m, sum, __int_as_float(x.c0), __int_as_float(x.c1));
+          else a.spill_ml[of_cta] = make_float2(m, sum);
+        }
+        const int64_t at = valid ? (first ? of_row : of_cta) * (steps * 16) : -1;
+        float* const dst = first ? a.base_o : a.spill_o;
+        const int piece = lane & 3;
+        int64_t to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          to[k] = __shfl_sync(0xffffffffu, at, 8 * k + (lane >> 2));
+          if (to[k] >= 0) to[k] += 4 * piece;
+        }
+        uint4* const stage = s.stage[warp];
+#pragma unroll 1
+        for (int i = 0; i < steps * 16; i += 16) {
+          tm_ld16(o_addr + i, v);
+          wait_ld<16>(v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) stage[lane * 4 + (k ^ ((lane >> 1) & 3))] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          __syncwarp();
+          uint4 y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = stage[(8 * k + (lane >> 2)) * 4 + (piece ^ ((lane >> 3) & 3))];
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (to[k] >= 0) *reinterpret_cast<uint4*>(dst + to[k] + i) = y[k];
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) kv_mbar_arrive(&s.o_empty[u]);         // O has been read
+        continue;
+      }
       float inv = 0.0f;
       float top_all = m;                                      // maximum of all parts
       bool mine_to_write = true;
@@ -877,9 +1071,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   if (warp == SOFT_WARPS + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-template <typename KT, int HALVES>
+template <typename KT, int HALVES, bool SHARED>
 int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const PromptArgs& a, int64_t grid, cudaStream_t st) {
-  auto kernel = attn_prompt_kernel<KT, HALVES>;
+  auto kernel = attn_prompt_kernel<KT, HALVES, SHARED>;
   constexpr size_t smem = Layout<HALVES>::TAIL + sizeof(Tail) + 1024;
   static_assert(smem <= 232448, "shared memory of one CTA");
   static std::atomic<uint64_t> have{0};                  // devices on which the kernel may take that much shared memory
@@ -911,11 +1105,8 @@ size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads) {
   return tokens > 0 && 2 * least <= sms ? (size_t)sms * PART_BYTES : 0;
 }
 
-int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, size_t ws_bytes, cudaStream_t st) {
-  CUtensorMap km, vm;
-  memcpy(&km, c->maps[0], sizeof km);
-  memcpy(&vm, c->maps[1], sizeof vm);
-  PromptArgs a;
+static PromptArgs args_of(const bitnet_kv_cache_t* c, const AttnArgs& x) {
+  PromptArgs a = {};
   a.q = static_cast<const uint8_t*>(x.q);
   a.out = static_cast<uint8_t*>(x.out);
   a.q_stride_token = x.q_stride_token;
@@ -945,6 +1136,22 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   a.c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-30f);
   a.dev_status = x.dev_status;
   a.give_up = x.give_up;
+  return a;
+}
+
+template <bool SHARED>
+static int launch_types(const bitnet_kv_cache_t* c, const PromptArgs& a, int dtype, int64_t grid, cudaStream_t st) {
+  CUtensorMap km, vm;
+  memcpy(&km, c->maps[0], sizeof km);
+  memcpy(&vm, c->maps[1], sizeof vm);
+  const bool two = a.head_dim > 64;
+  if (dtype == BITNET_KV_BF16)
+    return two ? launch_one<__nv_bfloat16, 2, SHARED>(km, vm, a, grid, st) : launch_one<__nv_bfloat16, 1, SHARED>(km, vm, a, grid, st);
+  return two ? launch_one<__half, 2, SHARED>(km, vm, a, grid, st) : launch_one<__half, 1, SHARED>(km, vm, a, grid, st);
+}
+
+int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, size_t ws_bytes, cudaStream_t st) {
+  PromptArgs a = args_of(c, x);
   // a sequence has at most one pair of tiles that is not full; which CTA has which, in how many parts, is found on the device
   const int64_t pairs = x.tokens / (2 * a.tile_tokens) + (x.seqs < x.tokens ? x.seqs : x.tokens);
   const int64_t sms = dev_info().sm_count, items = pairs * a.kv_heads * a.blocks;
@@ -956,9 +1163,39 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   const int64_t grid = a.room || items > sms ? sms : items;
   log_launch("attn_prompt_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%lld", a.tokens, a.q_heads, a.kv_heads,
              a.head_dim, a.window, (long long)grid);
-  const bool two = a.head_dim > 64;
-  if (x.dtype == BITNET_KV_BF16) return two ? launch_one<__nv_bfloat16, 2>(km, vm, a, grid, st) : launch_one<__nv_bfloat16, 1>(km, vm, a, grid, st);
-  return two ? launch_one<__half, 2>(km, vm, a, grid, st) : launch_one<__half, 1>(km, vm, a, grid, st);
+  return launch_types<false>(c, a, x.dtype, grid, st);
+}
+
+// The workspace of attn_shared: that of decode calls, then the rows' places, then the CTAs'.
+size_t attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int head_dim) {
+  const size_t row = (size_t)ceil_div(head_dim, 16) * 64;
+  return attn_decode_workspace_bytes() + (size_t)(seqs * q_heads) * (16 + row) + (size_t)dev_info().sm_count * 2 * ROWS * (8 + row);
+}
+
+SharedParts attn_shared_parts(void* ws, int64_t seqs, int64_t q_heads, int head_dim) {
+  const int64_t padded = ceil_div(head_dim, 16) * 16, rows = seqs * q_heads, spill = (int64_t)dev_info().sm_count * 2 * ROWS;
+  SharedParts p;
+  p.base_ml = reinterpret_cast<float4*>(attn_prompt_parts(ws));
+  p.base_o = reinterpret_cast<float*>(p.base_ml + rows);
+  p.spill_o = p.base_o + rows * padded;
+  p.spill_ml = reinterpret_cast<float2*>(p.spill_o + spill * padded);
+  p.padded = (int)padded;
+  return p;
+}
+
+// x.q_start, x.groups: the first sequence of each group, and how many there are; x.prefix: the prefixes.
+int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& x, const SharedParts& p, cudaStream_t st) {
+  PromptArgs a = args_of(c, x);
+  a.q_start = x.group_start;
+  a.seqs = (int)x.groups;
+  a.prefix = x.prefix_len;
+  a.base_ml = p.base_ml;
+  a.base_o = p.base_o;
+  a.spill_ml = p.spill_ml;
+  a.spill_o = p.spill_o;
+  log_launch("attn_prompt_kernel (shared prefixes) sequences=%d groups=%d q_heads=%d kv_heads=%d head_dim=%d window=%d", a.tokens, a.seqs, a.q_heads,
+             a.kv_heads, a.head_dim, a.window);
+  return launch_types<true>(c, a, x.dtype, dev_info().sm_count, st);
 }
 
 int attn_prompt_status(int* out) {

@@ -1,4 +1,4 @@
-// Python side of the cache and attention entry points: argument marshalling only, as the ctypes binding of the other calls, but
+// Python side of the entry points that a decode step calls around its linears: argument marshalling only, as the ctypes binding of the other calls, but
 // compiled, because a decode step makes many of these calls on small tensors (a call through ctypes took 12 us on the host,
 // of which the launch itself is 4).  Takes torch tensors, checks what the C ABI cannot see (types, shapes, strides,
 // devices), and calls the library's functions at the addresses given to bind().
@@ -28,6 +28,10 @@ struct {
   decltype(&bitnet_kv_copy_pages) copy_pages;
   decltype(&bitnet_attn_decode) decode;
   decltype(&bitnet_attn_prompt) prompt;
+  decltype(&bitnet_attn_shared) shared;
+  decltype(&bitnet_kv_append_rope) append_rope;
+  decltype(&bitnet_add_rmsnorm_quant) norm;
+  decltype(&bitnet_sample) sample;
 } g_fn;
 
 struct Refused {};                 // a Python exception is set
@@ -107,6 +111,29 @@ PyObject* done(int rc, const char* name) {
     return nullptr;
   }
   Py_RETURN_NONE;
+}
+
+// [rows][columns], columns contiguous, of fp32, bf16 or fp16.
+const at::Tensor& matrix(PyObject* o, const char* name, int64_t rows = -1, int64_t columns = -1) {
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda() || t.dim() != 2 || type_code(t) < 0 || (t.stride(1) != 1 && t.size(1) > 1))
+    refuse(name, "expected a CUDA matrix of fp32, bf16 or fp16 with contiguous rows");
+  if ((rows >= 0 && t.size(0) != rows) || (columns >= 0 && t.size(1) != columns)) refuse(name, "not of the expected shape");
+  return t;
+}
+// The caller's contiguous tensor of that type and shape, or a new one.
+at::Tensor made(PyObject* o, const char* name, at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
+  if (o == Py_None) return at::empty(shape, like.options().dtype(type));
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda() || t.sizes() != shape || t.scalar_type() != type || !t.is_contiguous()) refuse(name, "expected a contiguous CUDA tensor of its shape and type");
+  return t;
+}
+// A contiguous vector of n values of that type; null where it is None.
+const void* vector(PyObject* o, const char* name, int64_t n, at::ScalarType type) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda() || t.dim() != 1 || t.size(0) != n || t.scalar_type() != type || !t.is_contiguous()) refuse(name, "expected a contiguous CUDA vector of its length and type");
+  return t.data_ptr();
 }
 
 // Every entry: a fixed number of positional arguments (the Python functions supply the defaults).
@@ -248,6 +275,96 @@ PyObject* prompt(PyObject* const* a) {
   return rc ? done(rc, "bitnet_attn_prompt") : THPVariable_Wrap(out);
 }
 
+// cache, layer, q, table, kv_len, group_start, prefix_len, scale, window, sinks, out, workspace, dev_status, stream
+PyObject* shared(PyObject* const* a) {
+  const bitnet_kv_cache_t* c = cache(a[0]);
+  const at::Tensor& q = rows(a[2], "q", 0, c->head_dim);
+  const int64_t n = q.size(0);
+  const int32_t *table = book(a[3], "table", 2, n), *len = book(a[4], "kv_len", 1, n);
+  const int32_t* start = book(a[5], "group_start", 1);
+  const int64_t groups = tensor(a[5], "group_start").size(0) - 1;
+  const int32_t* prefix = book(a[6], "prefix_len", 1, groups);
+  const at::Tensor out = output(a[10], q, "bitnet_attn_shared");
+  const Space ws = space(a[11]);
+  const int rc = g_fn.shared(c, integer(a[1]), q.data_ptr(), type_code(q), q.size(1), step(q, 0), step(q, 1), table, tensor(a[3], "table").size(1),
+                             len, n, start, prefix, groups, (float)real(a[7]), integer(a[8]), integer(a[9]), out.data_ptr(), ws.p, ws.n,
+                             book_or_none(a[12], "dev_status"), stream(a[13], q));
+  return rc ? done(rc, "bitnet_attn_shared") : THPVariable_Wrap(out);
+}
+
+// cache, layer, rope, q, k, v, table, kv_len, q_start, q_out, q_type (a code; used without q_out), dev_status, stream
+PyObject* append_rope(PyObject* const* a) {
+  const bitnet_kv_cache_t* c = cache(a[0]);
+  const at::Tensor &k = rows(a[4], "k", c->kv_heads, c->head_dim), &v = rows(a[5], "v", c->kv_heads, c->head_dim);
+  if (k.scalar_type() != v.scalar_type() || k.size(0) != v.size(0) || step(k, 0) != step(v, 0) || step(k, 1) != step(v, 1))
+    refuse("bitnet_kv_append_rope", "k and v must have one type, shape and strides");
+  const bool with_q = a[3] != Py_None;
+  const at::Tensor& q = with_q ? rows(a[3], "q", 0, c->head_dim) : k;
+  if (with_q && (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0))) refuse("q", "must have k's type and number of tokens");
+  const int32_t* q_start = book_or_none(a[8], "q_start");
+  const int64_t seqs = q_start ? tensor(a[8], "q_start").size(0) - 1 : tensor(a[6], "table").size(0);
+  const int32_t* table = book(a[6], "table", 2, seqs);
+  at::Tensor out;
+  if (with_q) {
+    const int64_t code = integer(a[10]);
+    const at::ScalarType type = a[9] != Py_None ? tensor(a[9], "q_out").scalar_type()
+                                : code < 0      ? q.scalar_type()
+                                : code == BITNET_KV_F32 ? at::kFloat : code == BITNET_KV_F16 ? at::kHalf : at::kBFloat16;
+    out = made(a[9], "q_out", q.sizes(), type, q);
+  }
+  const int rc = g_fn.append_rope(c, integer(a[1]), static_cast<const bitnet_rope_t*>(PyLong_AsVoidPtr(a[2])), with_q ? q.data_ptr() : nullptr,
+                                  with_q ? q.size(1) : 0, step(q, 0), step(q, 1), k.data_ptr(), v.data_ptr(), type_code(k), step(k, 0), step(k, 1),
+                                  k.size(0), table, tensor(a[6], "table").size(1), book(a[7], "kv_len", 1, seqs), q_start, seqs,
+                                  with_q ? out.data_ptr() : nullptr, with_q ? type_code(out) : 0, book_or_none(a[11], "dev_status"), stream(a[12], k));
+  if (rc) return done(rc, "bitnet_kv_append_rope");
+  if (!with_q) Py_RETURN_NONE;
+  return THPVariable_Wrap(out);
+}
+
+// x, weight, eps, residual, residual_out, y, q, act_scale, act_sum, stream -> (q, act_scale)
+PyObject* norm(PyObject* const* a) {
+  const at::Tensor& x = matrix(a[0], "x");
+  const int64_t T = x.size(0), K = x.size(1);
+  const at::Tensor *res = nullptr, *res_out = nullptr, *w = nullptr, *y = nullptr;
+  if (a[1] != Py_None) {
+    w = &tensor(a[1], "weight");
+    if (!w->is_cuda() || w->dim() != 1 || w->size(0) != K || type_code(*w) < 0 || !w->is_contiguous()) refuse("weight", "expected a contiguous CUDA vector of x's width");
+  }
+  if (a[3] != Py_None) {
+    res = &matrix(a[3], "residual", T, K);
+    res_out = &matrix(a[4], "residual_out", T, K);
+    if (res->scalar_type() != res_out->scalar_type()) refuse("residual_out", "must have residual's type");
+  } else if (a[4] != Py_None) {
+    refuse("residual_out", "without a residual");
+  }
+  if (a[5] != Py_None) {
+    y = &matrix(a[5], "y", T, K);
+    if (!y->is_contiguous()) refuse("y", "must be contiguous");
+  }
+  const at::Tensor q = made(a[6], "q", {T, K}, at::kChar, x), scale = made(a[7], "act_scale", {T}, at::kFloat, x);
+  const void* sum = vector(a[8], "act_sum", T, at::kInt);
+  const int rc = g_fn.norm(x.data_ptr(), type_code(x), step(x, 0), res ? res->data_ptr() : nullptr, res ? type_code(*res) : 0, res ? step(*res, 0) : 0,
+                           res ? res_out->data_ptr() : nullptr, res ? step(*res_out, 0) : 0, w ? w->data_ptr() : nullptr, w ? type_code(*w) : 0,
+                           (float)real(a[2]), T, K, y ? y->data_ptr() : nullptr, y ? type_code(*y) : 0, q.data_ptr<int8_t>(),
+                           scale.data_ptr<float>(), static_cast<int32_t*>(const_cast<void*>(sum)), stream(a[9], x));
+  if (rc) return done(rc, "bitnet_add_rmsnorm_quant");
+  return Py_BuildValue("(NN)", THPVariable_Wrap(q), THPVariable_Wrap(scale));
+}
+
+// logits, u, temperature, top_k, top_p, min_p, tokens, prob, stream -> (tokens, prob)
+PyObject* sample(PyObject* const* a) {
+  const at::Tensor& x = matrix(a[0], "logits");
+  const int64_t n = x.size(0);
+  if (a[1] == Py_None) refuse("u", "expected a random number per row");
+  const at::Tensor tokens = made(a[6], "tokens", {n}, at::kInt, x), prob = made(a[7], "prob", {n}, at::kFloat, x);
+  auto f = [&](int i, const char* name) { return static_cast<const float*>(vector(a[i], name, n, at::kFloat)); };
+  const int rc = g_fn.sample(x.data_ptr(), type_code(x), step(x, 0), n, x.size(1), f(1, "u"), f(2, "temperature"),
+                             static_cast<const int32_t*>(vector(a[3], "top_k", n, at::kInt)), f(4, "top_p"), f(5, "min_p"),
+                             tokens.data_ptr<int32_t>(), prob.data_ptr<float>(), stream(a[8], x));
+  if (rc) return done(rc, "bitnet_sample");
+  return Py_BuildValue("(NN)", THPVariable_Wrap(tokens), THPVariable_Wrap(prob));
+}
+
 // BitnetError, the function that raises for a status, and the addresses of the library's functions in the order of g_fn.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *error, *status, *addresses;
@@ -284,6 +401,10 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          ENTRY("kv_copy_pages", 5, copy_pages),
                          ENTRY("attn_decode", 12, decode),
                          ENTRY("attn_prompt", 14, prompt),
+                         ENTRY("attn_shared", 14, shared),
+                         ENTRY("kv_append_rope", 13, append_rope),
+                         ENTRY("add_rmsnorm_quant", 10, norm),
+                         ENTRY("sample", 9, sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
 

@@ -213,6 +213,30 @@ int launch_gemm_i2s_prefill(const uint8_t* packed, float w_scale, int64_t M, int
                             const float* act_scale, int64_t T, float* y, int32_t* acc_out, void* ws, size_t ws_bytes,
                             cudaStream_t st);
 
+// Residual addition, root-mean-square norm, int8 quantiser (add_rmsnorm.cu).  Types are BITNET_KV_*; residual, weight, y, act_sum nullable.
+struct NormArgs {
+  const void *x, *residual, *weight;
+  void *residual_out, *y;
+  int8_t* q;
+  float* act_scale;
+  int32_t* act_sum;
+  int64_t stride_x, stride_residual, stride_residual_out, T, K;
+  double eps;
+  int x_type, residual_type, weight_type, y_type;
+};
+int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st);
+// One token per row of logits (sample.cu); temperature, top_k, top_p, min_p, prob nullable.
+struct SampleArgs {
+  const void* logits;
+  int64_t stride, rows;
+  int type, vocab, slice;    // slice: of a row per CTA (set by the launcher)
+  const float *u, *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* tokens;
+  float* prob;
+};
+int launch_sample(SampleArgs a, cudaStream_t st);
+
 int gemm_prefill_status(int* out);
 int gemv_tl_status(int* out);
 int gemm_prefill_status_clear();

@@ -71,6 +71,8 @@ int attn_args(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_d
   a->dtype = c->dtype;
   a->dev_status = dev_status;
   a->give_up = g_give_up.load(std::memory_order_relaxed);
+  a->group_start = a->prefix_len = nullptr;
+  a->groups = 0;
   return BITNET_OK;
 }
 
@@ -117,6 +119,43 @@ int bitnet_kv_append(const bitnet_kv_cache_t* c, int64_t layer, const void* k, c
   if (!k || !v || !aligned(k, al) || !aligned(v, al)) return BITNET_ERR_INVALID_ARG;
   return launch_kv_append(kv_view(c), (int)layer, k, v, in_dtype, stride_token, stride_head, tokens, seqs, table, table_width, kv_len,
                           q_start, c->dtype, dev_status, (cudaStream_t)stream);
+}
+
+int bitnet_kv_append_rope(const bitnet_kv_cache_t* c, int64_t layer, const bitnet_rope_t* rope, const void* q, int64_t q_heads,
+                          int64_t q_stride_token, int64_t q_stride_head, const void* k, const void* v, int in_type, int64_t stride_token,
+                          int64_t stride_head, int64_t tokens, const int32_t* table, int64_t table_width, const int32_t* kv_len,
+                          const int32_t* q_start, int64_t seqs, void* q_out, int out_type, int* dev_status, void* stream) {
+  int rc = check_cache(c);
+  if (rc) return rc;
+  rc = check_tokens(table, table_width, kv_len, q_start, tokens, seqs, dev_status);
+  if (rc) return rc;
+  if (!rope_ready(rope) || layer < 0 || layer >= c->layers || (in_type != BITNET_KV_F32 && in_type != c->dtype)) return BITNET_ERR_INVALID_ARG;
+  if (rope->rot_dim > c->head_dim) return BITNET_ERR_UNSUPPORTED_SHAPE;
+  if (q_heads < 0 || q_heads > 65536 || (q_heads && out_type != BITNET_KV_F32 && out_type != c->dtype)) return BITNET_ERR_INVALID_ARG;
+  if (tokens == 0) return BITNET_OK;
+  const uintptr_t size = in_type == BITNET_KV_F32 ? 4 : 2;
+  if (!k || !v || !aligned(k, size) || !aligned(v, size)) return BITNET_ERR_INVALID_ARG;
+  if (q_heads && (!q || !aligned(q, size) || !q_out || !aligned16(q_out))) return BITNET_ERR_INVALID_ARG;
+  RopeArgs a;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.in_type = in_type;
+  a.out_type = q_heads ? out_type : c->dtype;
+  a.q_heads = q_heads;
+  a.q_stride_token = q_heads ? q_stride_token : 0;
+  a.q_stride_head = q_heads ? q_stride_head : 0;
+  a.stride_token = stride_token;
+  a.stride_head = stride_head;
+  a.tokens = tokens;
+  a.seqs = seqs;
+  a.width = table_width;
+  a.table = table;
+  a.kv_len = kv_len;
+  a.q_start = q_start;
+  a.dev_status = dev_status;
+  return launch_kv_rope(kv_view(c), (int)layer, rope, a, c->dtype, (cudaStream_t)stream);
 }
 
 int bitnet_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t table_width, const int32_t* from_len,
@@ -232,6 +271,32 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
   // 70/149, 73/149, 143/150; 16/16 heads of 96, one sequence over 4096, 1 and 4 tokens: 16/29, 36/28.
   if (max_new <= 2) return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
   return launch_attn_prompt(c, a, workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+size_t bitnet_attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int64_t kv_heads, int64_t head_dim) {
+  if (seqs < 0 || seqs > COUNT || kv_heads < 1 || q_heads < kv_heads || q_heads > 65536 || q_heads % kv_heads || head_dim < 4 || head_dim > 128)
+    return 0;
+  return attn_shared_workspace_bytes(seqs, q_heads, (int)head_dim);
+}
+
+int bitnet_attn_shared(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_dtype, int64_t q_heads, int64_t stride_token,
+                       int64_t stride_head, const int32_t* table, int64_t table_width, const int32_t* kv_len, int64_t seqs,
+                       const int32_t* group_start, const int32_t* prefix_len, int64_t groups, float scale, int64_t window, int64_t sinks,
+                       void* out, void* workspace, size_t workspace_bytes, int* dev_status, void* stream) {
+  AttnArgs a;
+  const int rc = attn_args(c, layer, q, io_dtype, q_heads, stride_token, stride_head, seqs, table, table_width, kv_len, nullptr, seqs,
+                           scale, window, sinks, out, workspace, dev_status, &a);
+  if (rc) return rc;
+  if (io_dtype != c->dtype || groups < 0 || groups > COUNT) return BITNET_ERR_INVALID_ARG;
+  if (seqs == 0) return BITNET_OK;
+  if (groups < 1 || !ints(group_start) || !ints(prefix_len)) return BITNET_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < attn_shared_workspace_bytes(seqs, q_heads, c->head_dim)) return BITNET_ERR_WORKSPACE;
+  a.group_start = group_start;
+  a.prefix_len = prefix_len;
+  a.groups = groups;
+  const SharedParts p = attn_shared_parts(workspace, seqs, q_heads, c->head_dim);
+  const int first = launch_attn_shared_prefix(c, a, p, (cudaStream_t)stream);
+  return first ? first : launch_attn_shared_own(c, a, p, workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"

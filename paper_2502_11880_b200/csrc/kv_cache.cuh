@@ -58,7 +58,22 @@ struct AttnArgs {
   uint32_t give_up;         // the tile before which a CTA gives up (test hook; usually one that never comes)
   int dtype;
   int* dev_status;
+  // of attn_shared; null otherwise
+  const int32_t* group_start;   // [groups + 1]
+  const int32_t* prefix_len;    // [groups]
+  int64_t groups;
 };
+// Where attn_shared keeps what rows have of their group's prefix between its two kernels: maximum, sum and unscaled O of an item's first part
+// at the rows' places, of a later part at the places of the CTA that has it (attn_prompt.cu).
+struct SharedParts {
+  float4* base_ml;              // [seqs][q_heads]: maximum, sum, first and last CTA of the row's item
+  float* base_o;                // [seqs][q_heads][padded]
+  float2* spill_ml;             // [CTAs][2][128]
+  float* spill_o;               // [CTAs][2][128][padded]
+  int padded;                   // head_dim rounded up to 16
+};
+size_t attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int head_dim);
+SharedParts attn_shared_parts(void* ws, int64_t seqs, int64_t q_heads, int head_dim);
 // The workspace: counters that are zero between calls (of fixed number, so that no call's parts ever lie where another call's
 // counters are; the last 16 bytes deal out prompt items), the parts of decode rows, the parts of prompt items (where the caller
 // gave the room for them).
@@ -71,10 +86,24 @@ inline size_t attn_decode_workspace_bytes() { return attn_counters_bytes() + att
 size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads);
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
 int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, size_t ws_bytes, cudaStream_t st);
+int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, cudaStream_t st);
+int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, void* ws, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
                      int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
                      int dtype, int* dev_status, cudaStream_t st);
+// The same with rotation; q to q_out.
+struct RopeArgs {
+  const void *q, *k, *v;
+  void* q_out;
+  int in_type, out_type;
+  int64_t q_heads, q_stride_token, q_stride_head, stride_token, stride_head;
+  int64_t tokens, seqs, width;
+  const int32_t *table, *kv_len, *q_start;
+  int* dev_status;
+};
+bool rope_ready(const bitnet_rope_t* r);        // completed by bitnet_rope_init
+int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const RopeArgs& a, int dtype, cudaStream_t st);
 int launch_kv_reserve(int32_t* refs, int64_t num_pages, int32_t* table, int64_t seqs, int64_t width, const int32_t* from_len,
                       const int32_t* to_len, int page_size, int* dev_status, cudaStream_t st);
 int launch_kv_fork(const KvView& kv, int32_t* refs, int32_t* table, int64_t seqs, int64_t width, int32_t* len, const int32_t* parents,

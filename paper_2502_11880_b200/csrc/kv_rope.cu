@@ -1,0 +1,285 @@
+// New tokens' queries and keys rotated by their positions, keys and values written into the pages of the cache, in one pass over the
+// output of the Q/K/V linear.
+//
+//   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position * frequency of the pair
+//
+// where pair i of a row is (x[i], x[i + rot/2]) or (x[2i], x[2i + 1]); elements from rot on move as they are.
+//
+// Angles: a frequency is held as the fraction of a turn per position in 64-bit fixed point, so that position * frequency modulo a turn is
+// one integer product that wraps around by itself, exact to 2^-33 of a turn at any position; the top 32 bits go to sincospi as half turns.
+// (binary32 products would be off by 0.008 radians at position 131072, and a table of all positions is 67 MB that has to be read.)
+// The products and sums are binary32, rounded once to the type written.
+//
+// Bound by HBM for prompts and by latency for single tokens.  A row's pairs are cut into slots of two vectors of VEC elements; a thread
+// keeps its slot, and so its VEC sines and cosines, over all heads of a token that it visits.
+#include <cstring>
+#include <type_traits>
+
+#include "kv_cache.cuh"
+
+namespace bitnet {
+namespace {
+
+constexpr int THREADS = 128;
+
+struct RopeDev {
+  KvView kv;
+  const uint8_t *q, *k, *v;
+  uint8_t* q_out;
+  int64_t q_stride_token, q_stride_head, stride_token, stride_head;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int64_t width;
+  int tokens, seqs, layer, q_heads, rot, interleaved;
+  int page_shift;
+  int rotated, slots;        // slots of a row of q or k that hold pairs, and all of them
+  int at_once, split;        // rows that a CTA takes at a time, CTAs per token
+  int* dev_status;
+  float magnitude;
+  uint64_t step[64];         // turns per position, in 2^-64
+};
+
+// N elements of 4 or 2 bytes; aligned to N elements (16 bytes at most).
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const uint8_t* p, float (&x)[N]) {
+  if constexpr (std::is_same<T, float>::value) {
+    const float* f = reinterpret_cast<const float*>(p);
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(f + i));
+        x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+      }
+    } else if constexpr (N == 2) {
+      const float2 v = __ldcg(reinterpret_cast<const float2*>(f));
+      x[0] = v.x, x[1] = v.y;
+    } else {
+      x[0] = __ldcg(f);
+    }
+  } else {
+    T t[N];
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(t) = __ldcg(reinterpret_cast<const uint4*>(p));
+    else if constexpr (N == 4) *reinterpret_cast<uint2*>(t) = __ldcg(reinterpret_cast<const uint2*>(p));
+    else if constexpr (N == 2) *reinterpret_cast<uint32_t*>(t) = __ldcg(reinterpret_cast<const unsigned int*>(p));
+    else *reinterpret_cast<uint16_t*>(t) = __ldcg(reinterpret_cast<const unsigned short*>(p));
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = static_cast<float>(t[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ T to(float v) {
+  if constexpr (std::is_same<T, float>::value) return v;
+  else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(v);
+  else return __float2bfloat16_rn(v);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(uint8_t* p, const float (&x)[N]) {
+  struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec {
+    T t[N];
+  } v;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v.t[i] = to<T>(x[i]);
+  *reinterpret_cast<Vec*>(p) = v;
+}
+
+// KT: the cache's type; IN, OUT: of q, k, v and of q_out; VEC: elements of a vector.
+template <typename KT, typename IN, typename OUT, int VEC>
+__global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant__ RopeDev a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int n = blockIdx.x / a.split, part = blockIdx.x - n * a.split, lane = threadIdx.x & 31;
+  const int mine = threadIdx.x / a.slots, slot = threadIdx.x - mine * a.slots;
+  const int hq = a.q_heads, hkv = a.kv.kv_heads, dim = a.kv.head_dim, rows = hq + 2 * hkv, step = a.split * a.at_once;
+
+  // ---- a row's slot: its first row is loaded before the look-ups, which do not depend on it
+  const bool pairs = slot < a.rotated;
+  const int row0 = part * a.at_once + mine;
+  auto place = [&](bool rotate, int& d0, int& d1) {
+    if (rotate && !a.interleaved) {
+      d0 = slot * VEC;
+      d1 = d0 + a.rot / 2;
+    } else {
+      // (rows of v, and the rest of a row after its pairs, are cut without regard to pairs)
+      d0 = rotate || a.interleaved || !a.rotated ? 2 * VEC * slot : a.rot + 2 * VEC * (slot - a.rotated);
+      d1 = d0 + VEC;
+    }
+  };
+  int qd0, qd1;
+  place(pairs, qd0, qd1);
+  const int vd0 = 2 * VEC * slot, vd1 = vd0 + VEC;
+  float x0[VEC], x1[VEC];
+  auto load = [&](int row) {
+    const bool is_v = row >= hq + hkv;
+    const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
+    const uint8_t* src = row < hq ? a.q + ((int64_t)n * a.q_stride_token + row * a.q_stride_head) * (int)sizeof(IN)
+                                  : (is_v ? a.v : a.k) + ((int64_t)n * a.stride_token + (row - hq - (is_v ? hkv : 0)) * a.stride_head) * (int)sizeof(IN);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x0[i] = x1[i] = 0.0f;
+    if (d0 < dim) load_vec<IN, VEC>(src + d0 * (int)sizeof(IN), x0);
+    if (d1 < dim) load_vec<IN, VEC>(src + d1 * (int)sizeof(IN), x1);
+  };
+  const bool active = mine < a.at_once && row0 < rows;
+  if (active) load(row0);
+
+  // ---- the token's sequence, position and page
+  int seq = n;
+  int64_t pos;
+  if (a.q_start) {
+    // the number of sequences that begin after the first and not beyond token n, 32 at a time
+    seq = 0;
+    for (int s0 = 1; s0 < a.seqs; s0 += 32) {
+      const int s = s0 + lane;
+      const int in = __popc(__ballot_sync(0xffffffffu, s < a.seqs && __ldg(a.q_start + s) <= n));
+      seq += in;
+      if (in < 32) break;
+    }
+    pos = (int64_t)__ldg(a.kv_len + seq) - __ldg(a.q_start + seq + 1) + n;
+  } else {
+    pos = (int64_t)__ldg(a.kv_len + seq) - 1;
+  }
+  if (pos < 0 || !active) return;
+  const int64_t entry = pos >> a.page_shift;
+  const int page = entry < a.width ? __ldg(a.table + (int64_t)seq * a.width + entry) : -1;
+  const bool bad = page < 0 || page >= a.kv.num_pages;
+  if (bad && threadIdx.x == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+
+  float sn[VEC], cs[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int pair = slot * VEC + i;
+    if (pairs && 2 * pair < a.rot) {
+      const uint64_t turns = (uint64_t)pos * a.step[pair];
+      sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);       // 2^-31: half turns
+      sn[i] *= a.magnitude;
+      cs[i] *= a.magnitude;
+    } else {
+      sn[i] = 0.0f;
+      cs[i] = 1.0f;
+    }
+  }
+  const int64_t in_pool = 2 * (a.layer * a.kv.stride_layer + (bad ? 0 : page) * a.kv.stride_page + (pos & (a.kv.page_size - 1)) * a.kv.stride_row);
+  for (int row = row0;;) {
+    const bool is_v = row >= hq + hkv;
+    if (pairs && !is_v) {
+      if (a.interleaved) {
+        // x0, x1 hold 2 VEC elements one after the other: VEC pairs
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          if (2 * (slot * VEC + i) >= a.rot) continue;     // (the end of the last slot: moves as it is, infinities too)
+          if constexpr (VEC == 1) {
+            const float p = x0[0], q = x1[0];
+            x0[0] = p * cs[0] - q * sn[0];
+            x1[0] = q * cs[0] + p * sn[0];
+          } else {
+            float* const e = i < VEC / 2 ? &x0[2 * i] : &x1[2 * i - VEC];
+            const float p = e[0], q = e[1];
+            e[0] = p * cs[i] - q * sn[i];
+            e[1] = q * cs[i] + p * sn[i];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float p = x0[i], q = x1[i];
+          x0[i] = p * cs[i] - q * sn[i];
+          x1[i] = q * cs[i] + p * sn[i];
+        }
+      }
+    }
+    const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
+    if (row < hq) {
+      uint8_t* const dst = a.q_out + ((int64_t)n * hq + row) * dim * (int)sizeof(OUT);
+      if (d0 < dim) store_vec<OUT, VEC>(dst + d0 * (int)sizeof(OUT), x0);
+      if (d1 < dim) store_vec<OUT, VEC>(dst + d1 * (int)sizeof(OUT), x1);
+    } else if (!bad) {
+      uint8_t* const dst = (is_v ? a.kv.v : a.kv.k) + in_pool + 2 * ((row - hq - (is_v ? hkv : 0)) * a.kv.stride_head);
+      if (d0 < dim) store_vec<KT, VEC>(dst + 2 * d0, x0);
+      if (d1 < dim) store_vec<KT, VEC>(dst + 2 * d1, x1);
+      // the row's padding (head_dim is a multiple of 4, rows of 8) is cleared, as by appends
+      if (slot == 0 && (dim & 7)) *reinterpret_cast<uint2*>(dst + 2 * dim) = make_uint2(0u, 0u);
+    }
+    row += step;
+    if (row >= rows) break;
+    load(row);
+  }
+}
+
+template <typename KT, typename IN, typename OUT>
+cudaError_t launch_vec(const RopeDev& d, int vec, const cudaLaunchConfig_t& cfg) {
+  switch (vec) {
+    case 8: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 8>, d);
+    case 4: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 4>, d);
+    case 2: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 2>, d);
+    default: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 1>, d);
+  }
+}
+template <typename KT>
+cudaError_t launch_types(const RopeDev& d, bool in_f32, bool out_f32, int vec, const cudaLaunchConfig_t& cfg) {
+  if (in_f32) return out_f32 ? launch_vec<KT, float, float>(d, vec, cfg) : launch_vec<KT, float, KT>(d, vec, cfg);
+  return out_f32 ? launch_vec<KT, KT, float>(d, vec, cfg) : launch_vec<KT, KT, KT>(d, vec, cfg);
+}
+
+}  // namespace
+
+int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const RopeArgs& x, int dtype, cudaStream_t st) {
+  RopeDev d;
+  d.kv = kv;
+  d.q = static_cast<const uint8_t*>(x.q);
+  d.k = static_cast<const uint8_t*>(x.k);
+  d.v = static_cast<const uint8_t*>(x.v);
+  d.q_out = static_cast<uint8_t*>(x.q_out);
+  d.q_stride_token = x.q_stride_token;
+  d.q_stride_head = x.q_stride_head;
+  d.stride_token = x.stride_token;
+  d.stride_head = x.stride_head;
+  d.table = x.table;
+  d.kv_len = x.kv_len;
+  d.q_start = x.q_start;
+  d.width = x.width;
+  d.tokens = (int)x.tokens;
+  d.seqs = (int)x.seqs;
+  d.layer = layer;
+  d.q_heads = (int)x.q_heads;
+  d.rot = rope->rot_dim;
+  d.interleaved = rope->interleaved != 0;
+  d.page_shift = __builtin_ctz((unsigned)kv.page_size);
+  d.dev_status = x.dev_status;
+  d.magnitude = (float)rope->magnitude;
+  memcpy(d.step, rope->step, sizeof d.step);
+  const int dim = kv.head_dim;
+  // elements of a vector: as many as half a row's pairs, the head, strides and addresses allow
+  const bool in_f32 = x.in_type == BITNET_KV_F32, out_f32 = x.out_type == BITNET_KV_F32;
+  int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 8;
+  if (!d.interleaved) odd |= d.rot / 2;
+  int vec = (int)(odd & -odd);
+  if (vec > 8) vec = 8;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(x.k) | reinterpret_cast<uintptr_t>(x.v) | (x.q_heads ? reinterpret_cast<uintptr_t>(x.q) : 0);
+  const int size = in_f32 ? 4 : 2;
+  while (vec > 1 && at % (size * vec < 16 ? size * vec : 16)) vec /= 2;
+  d.rotated = d.interleaved ? (d.rot + 2 * vec - 1) / (2 * vec) : d.rot / (2 * vec);
+  const int rest = dim - (d.interleaved ? d.rotated * 2 * vec : d.rot), all = (dim + 2 * vec - 1) / (2 * vec);
+  d.slots = d.rotated + (rest > 0 ? (rest + 2 * vec - 1) / (2 * vec) : 0);
+  if (d.slots < all) d.slots = all;
+  d.at_once = THREADS / d.slots;
+  // CTAs per token: a row per thread while CTAs are few, all of a token's rows in one when there are enough tokens to fill the SMs
+  const int64_t rows = x.q_heads + 2 * kv.kv_heads, most = ceil_div(rows, d.at_once), sms = dev_info().sm_count;
+  int64_t split = 8 * sms / x.tokens;
+  split = split < 1 ? 1 : split > most ? most : split;
+  d.split = (int)ceil_div(most, ceil_div(most, split));           // (no CTA without rows, and even shares)
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(x.tokens * d.split));
+  cfg.blockDim = dim3(THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early_start_enabled(st) ? 1 : 0;
+  log_launch("kv_rope_kernel tokens=%d q_heads=%d kv_heads=%d vec=%d split=%d", d.tokens, d.q_heads, kv.kv_heads, vec, d.split);
+  const cudaError_t e = dtype == BITNET_KV_BF16 ? launch_types<__nv_bfloat16>(d, in_f32, out_f32, vec, cfg)
+                                                : launch_types<__half>(d, in_f32, out_f32, vec, cfg);
+  return e == cudaSuccess ? check_launch() : note_cuda_error(e);
+}
+
+}  // namespace bitnet
