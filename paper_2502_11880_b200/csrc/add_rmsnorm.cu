@@ -105,85 +105,121 @@ __device__ __forceinline__ float inverse_root(double v) {
 }
 __device__ __forceinline__ float scaled(float h, float r, float w) { return __fmul_rn(__fmul_rn(h, r), w); }
 
-// VPT: pieces of 4 elements per thread.  (Up to 4 the weights are loaded with the row, ahead of the reductions.)
-template <int VPT>
+// Four elements as they lie in memory: 16 bytes of binary32, or 8.
+template <int BYTES>
+struct Raw {
+  uint4 v;
+};
+template <>
+struct Raw<2> {
+  uint2 v;
+};
+template <int BYTES>
+__device__ __forceinline__ Raw<BYTES> load_raw(const void* p, int64_t i) {
+  Raw<BYTES> r;
+  if constexpr (BYTES == 4) r.v = __ldcg(reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i));
+  else r.v = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i));
+  return r;
+}
+__device__ __forceinline__ float4 widen(const Raw<4>& r, int) {
+  return make_float4(__uint_as_float(r.v.x), __uint_as_float(r.v.y), __uint_as_float(r.v.z), __uint_as_float(r.v.w));
+}
+__device__ __forceinline__ float4 widen(const Raw<2>& r, int type) {
+  const uint2 w = r.v;
+  if (type == BITNET_KV_BF16)
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+  const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), hi = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+  return make_float4(lo.x, lo.y, hi.x, hi.y);
+}
+
+// VPT: pieces of 4 elements per thread; XB, RB: bytes of an element of x and of the residual (0: none).  A CTA takes every gridDim.x-th row, and
+// has the next one's loads on their way while it reduces and writes the present one.
+template <int VPT, int XB, int RB>
 __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant__ NormDev d) {
   const NormArgs& a = d.a;
   __shared__ Red red;
-  const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, nt = blockDim.x, n4 = (int)(a.K / 4);
   if (tid == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr bool EARLY = VPT <= 4;
-  float4 h[VPT], w[EARLY ? VPT : 1];
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f), one = make_float4(1.f, 1.f, 1.f, 1.f);
-#pragma unroll
-  for (int k = 0; k < VPT; ++k) {
-    const int i = tid + k * nt;
-    h[k] = i < n4 ? load4(a.x, t * a.stride_x + 4 * (int64_t)i, a.x_type) : zero;
-  }
-  if (a.residual) {
-    float4 e[VPT];
+  Raw<XB> x[VPT];
+  Raw<RB> e[VPT];
+  auto fetch = [&](int64_t t) {
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       const int i = tid + k * nt;
-      e[k] = i < n4 ? load4(a.residual, t * a.stride_residual + 4 * (int64_t)i, a.residual_type) : zero;
+      if (i < n4) x[k] = load_raw<XB>(a.x, t * a.stride_x + 4 * (int64_t)i);
     }
+    if constexpr (RB > 0) {
 #pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-      h[k].x = rounded(h[k].x + e[k].x, a.residual_type);
-      h[k].y = rounded(h[k].y + e[k].y, a.residual_type);
-      h[k].z = rounded(h[k].z + e[k].z, a.residual_type);
-      h[k].w = rounded(h[k].w + e[k].w, a.residual_type);
+      for (int k = 0; k < VPT; ++k) {
+        const int i = tid + k * nt;
+        if (i < n4) e[k] = load_raw<RB>(a.residual, t * a.stride_residual + 4 * (int64_t)i);
+      }
     }
-  }
-  if (EARLY) {
-#pragma unroll
-    for (int k = 0; k < (EARLY ? VPT : 0); ++k) {
-      const int i = tid + k * nt;
-      w[k] = a.weight && i < n4 ? load4(a.weight, 4 * (int64_t)i, a.weight_type) : one;
-    }
-  }
-  double sum = 0.0;
-#pragma unroll
-  for (int k = 0; k < VPT; ++k) {
-    const double x = h[k].x, y = h[k].y, z = h[k].z, v = h[k].w;
-    sum = fma(x, x, sum);
-    sum = fma(y, y, sum);
-    sum = fma(z, z, sum);
-    sum = fma(v, v, sum);
-  }
-  if (a.residual_out) {
+  };
+  constexpr bool AHEAD = VPT <= 4;               // (eight pieces and the next eight would not fit the registers)
+  int64_t t = blockIdx.x;
+  if (AHEAD) fetch(t);
+  for (;;) {
+    if (!AHEAD) fetch(t);
+    float4 h[VPT];
+    double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       const int i = tid + k * nt;
-      if (i < n4) store4(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, a.residual_type, h[k]);
+      h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i >= n4) continue;
+      h[k] = widen(x[k], a.x_type);
+      if constexpr (RB > 0) {
+        const float4 r = widen(e[k], a.residual_type);
+        h[k].x = rounded(h[k].x + r.x, RB == 4 ? BITNET_KV_F32 : a.residual_type);
+        h[k].y = rounded(h[k].y + r.y, RB == 4 ? BITNET_KV_F32 : a.residual_type);
+        h[k].z = rounded(h[k].z + r.z, RB == 4 ? BITNET_KV_F32 : a.residual_type);
+        h[k].w = rounded(h[k].w + r.w, RB == 4 ? BITNET_KV_F32 : a.residual_type);
+        store4(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, a.residual_type, h[k]);
+      }
+      sum = fma((double)h[k].x, (double)h[k].x, sum);
+      sum = fma((double)h[k].y, (double)h[k].y, sum);
+      sum = fma((double)h[k].z, (double)h[k].z, sum);
+      sum = fma((double)h[k].w, (double)h[k].w, sum);
     }
-  }
-  const float r = inverse_root(block_sum(sum, red.sum) * d.inv_k + a.eps);
-  float top = 0.0f;
+    const int64_t next = t + gridDim.x;
+    if (AHEAD && next < a.T) fetch(next);
+    float4 w[VPT <= 2 ? VPT : 1];                // (few pieces: the weights come with the row, ahead of the reductions)
+    if constexpr (VPT <= 2) {
 #pragma unroll
-  for (int k = 0; k < VPT; ++k) {
-    const int i = tid + k * nt;
-    float4 v = one;
-    if (EARLY) v = w[EARLY ? k : 0];
-    else if (a.weight && i < n4) v = load4(a.weight, 4 * (int64_t)i, a.weight_type);
-    h[k] = make_float4(scaled(h[k].x, r, v.x), scaled(h[k].y, r, v.y), scaled(h[k].z, r, v.z), scaled(h[k].w, r, v.w));
-    if (i < n4) top = fmaxf(top, absmax4(h[k]));
-  }
-  const float amax = fmaxf(block_max(top, red.top), 1e-5f), s = __fdiv_rn(127.0f, amax);
-  int codes = 0;
+      for (int k = 0; k < VPT; ++k) {
+        const int i = tid + k * nt;
+        w[k] = a.weight && i < n4 ? load4(a.weight, 4 * (int64_t)i, a.weight_type) : make_float4(1.f, 1.f, 1.f, 1.f);
+      }
+    }
+    const float r = inverse_root(block_sum(sum, red.sum) * d.inv_k + a.eps);
+    float top = 0.0f;
 #pragma unroll
-  for (int k = 0; k < VPT; ++k) {
-    const int i = tid + k * nt;
-    if (i >= n4) continue;
-    const int c = quant4_packed(h[k], s);
-    codes = __dp4a(c, 0x01010101, codes);
-    reinterpret_cast<int*>(a.q + t * a.K)[i] = c;
-    if (a.y) store4(a.y, t * a.K + 4 * (int64_t)i, a.y_type, h[k]);
+    for (int k = 0; k < VPT; ++k) {
+      const int i = tid + k * nt;
+      float4 v = make_float4(1.f, 1.f, 1.f, 1.f);
+      if constexpr (VPT <= 2) v = w[k];
+      else if (a.weight && i < n4) v = load4(a.weight, 4 * (int64_t)i, a.weight_type);
+      h[k] = make_float4(scaled(h[k].x, r, v.x), scaled(h[k].y, r, v.y), scaled(h[k].z, r, v.z), scaled(h[k].w, r, v.w));
+      if (i < n4) top = fmaxf(top, absmax4(h[k]));
+    }
+    const float amax = fmaxf(block_max(top, red.top), 1e-5f), s = __fdiv_rn(127.0f, amax);
+    int codes = 0;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int i = tid + k * nt;
+      if (i >= n4) continue;
+      const int c = quant4_packed(h[k], s);
+      codes = __dp4a(c, 0x01010101, codes);
+      reinterpret_cast<int*>(a.q + t * a.K)[i] = c;
+      if (a.y) store4(a.y, t * a.K + 4 * (int64_t)i, a.y_type, h[k]);
+    }
+    if (tid == 0) a.act_scale[t] = __fdiv_rn(amax, 127.0f);
+    if (a.act_sum) store_sum(codes, red.codes, a.act_sum + t);
+    if (next >= a.T) break;
+    t = next;
   }
-  if (tid == 0) a.act_scale[t] = __fdiv_rn(amax, 127.0f);
-  if (a.act_sum) store_sum(codes, red.codes, a.act_sum + t);
 }
 
 // Rows of any length, stride and alignment: three walks over the row (h is read back where it was written, by the same thread).
@@ -231,6 +267,17 @@ int threads_for(int64_t pieces) {               // whole warps
   return (int)(n < 64 ? 64 : n > 1024 ? 1024 : n);
 }
 
+template <int VPT, int XB>
+cudaError_t launch_residual(const NormDev& d, const cudaLaunchConfig_t& cfg) {
+  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 0>, d);
+  return d.a.residual_type == BITNET_KV_F32 ? cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 4>, d)
+                                            : cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 2>, d);
+}
+template <int VPT>
+cudaError_t launch_x(const NormDev& d, const cudaLaunchConfig_t& cfg) {
+  return d.a.x_type == BITNET_KV_F32 ? launch_residual<VPT, 4>(d, cfg) : launch_residual<VPT, 2>(d, cfg);
+}
+
 }  // namespace
 
 int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
@@ -245,8 +292,10 @@ int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
   int vpt = a.T > 2 * (int64_t)dev_info().sm_count ? 4 : 1;
   while (vpt < 8 && ceil_div(n4, vpt) > 1024) vpt *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.T);
-  cfg.blockDim = dim3((unsigned)threads_for(vec ? ceil_div(n4, vpt) : ceil_div(a.K, 4)));
+  const int threads = threads_for(vec ? ceil_div(n4, vpt) : ceil_div(a.K, 4));
+  const int64_t resident = (int64_t)dev_info().sm_count * (1024 / threads);          // CTAs of 64 registers a thread
+  cfg.gridDim = dim3((unsigned)(vec && a.T > resident ? resident : a.T));
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -256,10 +305,10 @@ int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
   if (log_enabled()) log_launch("add_rmsnorm T=%lld K=%lld vec=%d vpt=%d", (long long)a.T, (long long)a.K, (int)vec, vpt);
   cudaError_t e;
   if (!vec) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_any_kernel, d);
-  else if (vpt == 1) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<1>, d);
-  else if (vpt == 2) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<2>, d);
-  else if (vpt == 4) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<4>, d);
-  else e = cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<8>, d);
+  else if (vpt == 1) e = launch_x<1>(d, cfg);
+  else if (vpt == 2) e = launch_x<2>(d, cfg);
+  else if (vpt == 4) e = launch_x<4>(d, cfg);
+  else e = launch_x<8>(d, cfg);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
 
