@@ -28,7 +28,6 @@ constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int BINS = THREADS;                // one per thread
 constexpr int LIST = 256;                    // items that are ranked by counting
 constexpr int MOST_CTAS = 8;                 // of a cluster
-constexpr float BINS_PER_E = BINS / 23.0f;   // weights that count lie within 33 ln 2 = 22.9 of the largest
 constexpr float ONE = 4294967296.0f;         // weight 1
 
 struct Hist {
@@ -41,7 +40,7 @@ struct Item {
 struct Say {                                 // what a CTA tells the others at a step
   float top;
   uint32_t index;
-  uint64_t lo, hi, mass;
+  uint64_t mass;
   uint32_t n;
 };
 struct Share {
@@ -54,7 +53,6 @@ struct Share {
   uint64_t warp_mass[WARPS];
   uint32_t warp_count[WARPS];
   float warp_top[WARPS];
-  uint64_t warp_lo[WARPS], warp_hi[WARPS];
   Item all[LIST];
   uint32_t listed;
   // found by one thread
@@ -100,24 +98,39 @@ __device__ __forceinline__ uint64_t place(float x, uint32_t index) {
   return (uint64_t)~up << 32 | index;
 }
 
+// Back to the value.
+__device__ __forceinline__ float value_at(uint64_t at) {
+  const uint32_t up = ~(uint32_t)(at >> 32);
+  return __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
+}
+
+constexpr float REACH = 33.0f;               // weights below 2^-33 of the largest count as 0
+constexpr float PER_T = (BINS - 1) / REACH;  // bins of the first histogram per log2
+
 struct Weigh {
-  float top, c, c_lo;                        // log2(e) / T in two pieces
-  // The weight in units of 2^-32, and (max - x) log2(e) / T.
-  __device__ __forceinline__ float operator()(float x, float& t) const {
-    if (x == top) {
-      t = 0.0f;
-      return ONE;
+  float top, c, c_lo;                        // the largest, finite; log2(e) / T in two pieces
+  // (max - x) log2(e) / T, which rises as x falls.
+  __device__ __forceinline__ float distance(float x, float& d) const {
+    d = top - x;
+    return d * c;
+  }
+  // The weight in units of 2^-32.  `exact`: max - x has no rounding error that matters (16-bit logits).
+  template <bool EXACT>
+  __device__ __forceinline__ float weight(float x, float d, float t) const {
+    float low = fmaf(d, c, -t);
+    low = fmaf(d, c_lo, low);
+    if (!EXACT) {
+      const float b = d - top;
+      low = fmaf((top - (d - b)) - (x + b), c, low);
     }
-    const float d = top - x, b = d - top, e = (top - (d - b)) - (x + b);            // d + e = top - x
-    t = d * c;
-    if (!(t < 33.0f)) return 0.0f;                                                  // (infinities, and 0 * infinity, too)
-    const float low = fmaf(d, c, -t) + fmaf(d, c_lo, e * c);
-    const float n = rintf(t);
+    const float m = t + 12582912.0f, n = m - 12582912.0f;                           // 1.5 * 2^23: n = round(t), also in m's low bits
     float f;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"((n - t) - low));
-    return f * __uint_as_float((uint32_t)(32 - (int)n + 127) << 23);
+    return f * __uint_as_float(((32u + 127u) << 23) - (__float_as_uint(m) << 23));
   }
 };
+// The bin of a distance below REACH.
+__device__ __forceinline__ int bin_of(float t) { return (int)(__float_as_uint(fmaf(t, PER_T, 8388608.0f)) & (BINS - 1)); }
 __device__ __forceinline__ uint32_t fixed(float w) { return __float2uint_rn(w); }   // (1 becomes 2^32 - 1)
 
 template <typename T, bool STAGED>
@@ -126,6 +139,13 @@ struct Slice {
   T* kept;             // STAGED: the slice in shared memory
   int first;           // index of local element 0 (which may lie before the slice, so that pieces of 16 bytes agree)
   int begin, end;      // local elements that belong to the slice
+  bool infinite;       // the row's largest is infinite: those count as 0, all others as -infinity
+  __device__ __forceinline__ float only_infinite(float v) const { return v == INFINITY ? 0.0f : -INFINITY; }
+  // (not STAGED)
+  __device__ __forceinline__ float at(int i) const {
+    const float v = i >= begin && i < end ? drawable(value(row[(int64_t)first + i])) : -INFINITY;
+    return infinite ? only_infinite(v) : v;
+  }
   // All elements of this CTA's slice, four at a time, each warp's one after the other; f(value, local index).
   template <typename F>
   __device__ __forceinline__ void each(int w0, int w1, F f) const {
@@ -137,7 +157,7 @@ struct Slice {
         for (int k = 0; k < 4; ++k) x[k] = value(v.t[k]);
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = i + k >= begin && i + k < end ? drawable(value(row[(int64_t)first + i + k])) : -INFINITY;
+        for (int k = 0; k < 4; ++k) x[k] = at(i + k);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) f(x[k], i + k);
@@ -181,6 +201,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
   x.first = i0 - off;
   x.begin = off;
   x.end = off + i1 - i0;
+  x.infinite = false;
   const int length = (x.end + 127) / 128 * 128;              // of the slice with what pads it
   float top = -INFINITY;
   if (STAGED) {
@@ -234,26 +255,37 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
     return;
   }
 
+  if (top == INFINITY) {
+    x.infinite = true;
+    top = 0.0f;
+    if (STAGED) {
+      for (int i = tid; i < length; i += THREADS) x.kept[i] = T(x.only_infinite(value(x.kept[i])));
+      __syncthreads();
+    }
+  }
+
+  constexpr bool EXACT = sizeof(T) == 2;
   Weigh weigh;
   weigh.top = top;
-  const double c = fmin(1.4426950408889634 / (double)temperature, 3e38);
-  weigh.c = greedy ? INFINITY : (float)c;                     // (then all but the largest weigh 0)
-  weigh.c_lo = greedy ? 0.0f : (float)(c - (double)weigh.c);
+  const double c = greedy ? 1.0 : fmin(1.4426950408889634 / (double)temperature, 3e38);
+  weigh.c = (float)c;
+  weigh.c_lo = (float)(c - (double)weigh.c);
   const float least = min_p > 0.0f && !greedy ? fminf(min_p, 1.0f) * ONE : 0.0f;
 
-  // ---- the last item that is kept, as a place in the order
-  uint64_t last = ~0ull;
+  // ---- the last item that is kept: its value, and its index among equal ones
+  float last = greedy ? top : -INFINITY;
+  uint32_t last_index = greedy ? 0xffffffffu : 0u;
   const bool by_k = !greedy && top_k > 0 && top_k < a.vocab, by_p = !greedy && top_p < 1.0f;
   if (by_k || by_p) {
     // all items by their distance from the largest
-    const float per_t = BINS_PER_E * 0.6931471805599453f;
     {
       Hist& h = s.hist;
       x.each(w0, w1, [&](float v, int) {
-        float t;
-        const uint32_t w = fixed(weigh(v, t));
-        if (w == 0) return;
-        const int b = min(BINS - 1, (int)(t * per_t));
+        float d;
+        const float t = weigh.distance(v, d);
+        if (!(t < REACH)) return;
+        const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
+        const int b = bin_of(t);
         atomicAdd(&h.count[b], 1u);
         if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
       });
@@ -312,60 +344,32 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       find(counts, limit, s.bin_count[tid], s.bin_mass[tid], 0, 0);
       const int b0 = s.bin;
       if (b0 < 0) return false;
-      uint64_t lo = 0, hi = ~0ull;                            // the range of the order that holds it
-      auto in_play = [&](float v, int i, uint64_t& at, uint32_t& w) {
-        float t;
-        w = fixed(weigh(v, t));
-        if (w == 0 || min(BINS - 1, (int)(t * per_t)) != b0) return false;
+      // the range of the order that holds it: at first that of the bin, with something to spare
+      uint64_t lo, hi;
+      {
+        const float margin = 1e-5f * (fabsf(top) + REACH / weigh.c);
+        lo = place(top - (b0 - 0.51f) / PER_T / weigh.c + margin, 0u);
+        hi = place(top - (b0 + 0.51f) / PER_T / weigh.c - margin, 0xffffffffu);
+        if (!(margin < 1e30f)) lo = 0, hi = ~(uint64_t)0;
+      }
+      auto in_play = [&](float v, int i, uint64_t& at, float& d, float& t) {
+        t = weigh.distance(v, d);
+        if (!(t < REACH) || bin_of(t) != b0) return false;
         at = place(v, (uint32_t)(x.first + i));
         return at >= lo && at <= hi;
       };
       // (every level takes 9 of 64 bits)
       for (int level = 0; level < 8 && s.bin >= 0 && s.bin_n > LIST; ++level) {
-        // ends of the range in use, then its histogram
-        uint64_t first = ~0ull, final = 0;
-        x.each(w0, w1, [&](float v, int i) {
-          uint64_t at;
-          uint32_t w;
-          if (in_play(v, i, at, w)) {
-            first = min(first, at);
-            final = max(final, at);
-          }
-        });
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-          first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
-          final = max(final, __shfl_xor_sync(0xffffffffu, final, o));
-        }
-        if (lane == 0) {
-          s.warp_lo[warp] = first;
-          s.warp_hi[warp] = final;
-        }
-        __syncthreads();
-        if (tid == 0) {
-          for (int w = 1; w < WARPS; ++w) {
-            first = min(first, s.warp_lo[w]);
-            final = max(final, s.warp_hi[w]);
-          }
-          s.say[step & 1].lo = first;
-          s.say[step & 1].hi = final;
-        }
-        cluster_barrier();
-        lo = ~0ull;
-        hi = 0;
-        for (int p = 0; p < ctas; ++p) {
-          lo = min(lo, peer_u64(&s.say[step & 1].lo, p));
-          hi = max(hi, peer_u64(&s.say[step & 1].hi, p));
-        }
-        ++step;
-        Hist& h = s.hist;                                     // (the others have read it: they have passed the barrier)
+        cluster_barrier();                                    // (the others have read the last histogram)
+        Hist& h = s.hist;
         h.count[tid] = h.lo[tid] = h.hi[tid] = 0;
         __syncthreads();
         const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 9);        // (hi - lo) >> shift < BINS
         x.each(w0, w1, [&](float v, int i) {
           uint64_t at;
-          uint32_t w;
-          if (!in_play(v, i, at, w)) return;
+          float d, t;
+          if (!in_play(v, i, at, d, t)) return;
+          const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
           const int b = (int)((at - lo) >> shift);
           atomicAdd(&h.count[b], 1u);
           if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
@@ -383,10 +387,10 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       __syncthreads();
       x.each(w0, w1, [&](float v, int i) {
         uint64_t at;
-        uint32_t w;
-        if (in_play(v, i, at, w)) {
+        float d, t;
+        if (in_play(v, i, at, d, t)) {
           const uint32_t k = atomicAdd(&s.listed, 1u);
-          if (k < LIST) s.list[step & 1][k] = Item{at, w};
+          if (k < LIST) s.list[step & 1][k] = Item{at, fixed(weigh.weight<EXACT>(v, d, t))};
         }
       });
       __syncthreads();
@@ -436,23 +440,29 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       __syncthreads();
       for (int w = 0; w < WARPS; ++w) all += s.warp_mass[w];
     }
+    auto cut = [&] {
+      last = value_at(s.found_at);
+      last_index = (uint32_t)s.found_at;
+    };
     if (by_k && resolve(true, (uint64_t)top_k)) {
-      last = s.found_at;
+      cut();
       all = s.found_mass;
     }
     if (by_p) {
       const double want = top_p > 0.0f ? ceil((double)top_p * (double)all) : 0.0;
-      if (resolve(false, want < 1.0 ? (uint64_t)1 : want < (double)all ? (uint64_t)want : all)) last = s.found_at;
+      if (resolve(false, want < 1.0 ? (uint64_t)1 : want < (double)all ? (uint64_t)want : all)) cut();
     }
   }
 
   // ---- the sum of what is kept, by stretches
   auto kept = [&](float v, int i, float& w) -> uint32_t {
-    float t;
-    w = weigh(v, t);
-    if (w < least || w == 0.0f) return 0u;
-    if (last != ~0ull && place(v, (uint32_t)(x.first + i)) > last) return 0u;
-    return fixed(w);
+    w = 0.0f;
+    if (v < last || (v == last && (uint32_t)(x.first + i) > last_index)) return 0u;
+    float d;
+    const float t = weigh.distance(v, d);
+    if (!(t < REACH)) return 0u;
+    w = weigh.weight<EXACT>(v, d, t);
+    return w < least ? 0u : fixed(w);
   };
   __syncthreads();
   uint64_t mine = 0;
@@ -490,7 +500,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (STAGED) v[k] = value(x.kept[i + k]);
-      else v[k] = i + k >= x.begin && i + k < x.end ? drawable(value(x.row[(int64_t)x.first + i + k])) : -INFINITY;
+      else v[k] = x.at(i + k);
       q[k] = kept(v[k], i + k, w[k]);
       four += q[k];
     }
