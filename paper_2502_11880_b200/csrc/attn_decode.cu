@@ -63,20 +63,9 @@ struct DecodeArgs {
   // SHARED
   const int32_t* group_start;                 // [groups + 1]
   const int32_t* prefix_len;                  // [groups]
-  int groups, per_block, tile_tokens, ctas;   // as the kernel before has cut its rows
+  int groups;
   SharedParts shared;
 };
-
-// The group of sequence n, its first sequence and its prefix within the table; first < 0: the sequence is in no group.
-struct Group {
-  int first, prefix;
-};
-__device__ __forceinline__ Group group_of(const DecodeArgs& a, int n) {
-  const int g = kv_seq_of(a.group_start, a.groups, n);
-  const int q0 = __ldg(a.group_start + g), q1 = __ldg(a.group_start + g + 1);
-  if (q0 < 0 || n < q0 || n >= q1) return Group{-1, 0};
-  return Group{q0, max(0, min(__ldg(a.prefix_len + g), a.max_len))};
-}
 
 // The visible tokens of one row: [s_lo, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
 // tokens there are not there; without a window such a position means all of the table).
@@ -103,7 +92,7 @@ __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
   if (r.beyond && r.lo == r.len) r.lo = r.len = 0;             // the window lies beyond the table: the sinks alone
   r.s_lo = 0;
   if constexpr (SHARED) {                                      // the group's prefix has been taken
-    const int prefix = group_of(a, n).prefix;
+    const int prefix = kv_group_of(a.group_start, a.prefix_len, a.groups, n, a.max_len).prefix;
     r.s_lo = min(prefix, r.s_end);
     r.lo = min(max(r.lo, prefix), r.len);
     r.n0 = r.s_lo < r.s_end ? (r.s_end + TILE - 1) / TILE - r.s_lo / TILE : 0;
@@ -207,7 +196,8 @@ struct Layout {
 // plain bulk copy, and ldmatrix meets distinct banks without a swizzle; tensor copies, whose 128-byte box rows begin at odd
 // multiples of 16 bytes there, took 114 instead of 85 us for 9 windows of 4096 tokens, 32 heads of 100.  (Rows of one 64-column half take
 // tensor copies whatever their length: not measured there.)
-// SHARED: the sequences' own tokens, after the kernel that took what groups of them have in common (attn_prompt.cu), whose sums join here.
+// SHARED: the sequences' own tokens, beyond what groups of them have in common (attn_shared.cu); rows go to the workspace as maximum, sum and
+// unscaled O.
 template <typename KT, bool F32, int DT, bool DENSE, bool SHARED>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const DecodeArgs a) {
@@ -429,7 +419,16 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     int n, head0, heads, c0, c1, first_slot;
   } pending[2];
   pending[0].n = pending[1].n = -1;
-  auto write_row = [&](int tok, int h0, int heads, int hh, int d0, const float4& acc, float sum) {
+  auto write_row = [&](int tok, int h0, int heads, int hh, int d0, const float4& acc, float big, float sum) {
+    if constexpr (SHARED) {                                // (l and O of fp16 without their scale)
+      if (hh >= heads) return;
+      const int64_t at = (int64_t)tok * a.q_heads + h0 + hh;
+      const float down = exp2_approx(-P_SHIFT);
+      if (lane == 0) a.shared.own_ml[at] = make_float2(big, sum * down);
+      if (d0 < a.shared.padded)
+        *reinterpret_cast<float4*>(a.shared.own_o + at * a.shared.padded + d0) = make_float4(acc.x * down, acc.y * down, acc.z * down, acc.w * down);
+      return;
+    }
     if (hh >= heads || d0 >= a.head_dim) return;
     const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);   // nothing visible: 0; NaN stays NaN
     const int64_t at = ((int64_t)tok * a.q_heads + h0 + hh) * a.head_dim + d0;
@@ -438,44 +437,6 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     } else {
       *reinterpret_cast<uint2*>(static_cast<KT*>(a.out) + at) =
           make_uint2(P2::pack(acc.x * inv, acc.y * inv), P2::pack(acc.z * inv, acc.w * inv));
-    }
-  };
-
-  // What the row's group has in common, on top of the sums over its own tokens (which HALF_T has scaled by 2^P_SHIFT).
-  auto with_prefix = [&](int tok, int h0, int heads, int hh, int d0, float4& acc, float& big, float& sum) {
-    if (hh >= heads) return;
-    const Group gr = group_of(a, tok);
-    if (gr.first < 0) return;
-    const int head = h0 + hh, in_group = head % a.group % a.per_block, at = (tok - gr.first) % (2 * a.tile_tokens);
-    const int64_t of_row = (int64_t)tok * a.q_heads + head;
-    const int in_cta = at / a.tile_tokens * 128 + at % a.tile_tokens * a.per_block + in_group;     // the row's place in a CTA's
-    const float4 ml = __ldcg(a.shared.base_ml + of_row);
-    const int c0 = max(__float_as_int(ml.z), 0), c1 = min(__float_as_int(ml.w), a.ctas - 1);        // (any, if that kernel gave up)
-    float top = fmaxf(big, ml.x);
-#pragma unroll 4
-    for (int c = c0 + 1; c <= c1; ++c) top = fmaxf(top, __ldcg(a.shared.spill_ml + (int64_t)c * 256 + in_cta).x);
-    const float f = big == -INFINITY ? 0.0f : exp2_approx(big - top);
-    acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-    sum *= f;
-    big = top;
-    const bool mine = d0 < a.shared.padded;
-    auto add = [&](float m, float l, const float* o) {
-      const float f = m == -INFINITY ? 0.0f : exp2_approx(m - top + P_SHIFT);
-      sum += f * l;
-      if (mine && f != 0.0f) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + d0));
-        acc.x += f * v.x;
-        acc.y += f * v.y;
-        acc.z += f * v.z;
-        acc.w += f * v.w;
-      }
-    };
-    add(ml.x, ml.y, a.shared.base_o + of_row * a.shared.padded);
-#pragma unroll 4
-    for (int c = c0 + 1; c <= c1; ++c) {
-      const int64_t at = (int64_t)c * 256 + in_cta;
-      const float2 y = __ldcg(a.shared.spill_ml + at);
-      add(y.x, y.y, a.shared.spill_o + at * a.shared.padded);
     }
   };
 
@@ -728,8 +689,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     }
 
     if (t_end - t0 == r.tiles) {
-      if constexpr (SHARED) with_prefix(n, head0, heads, hh, d0, acc, big, sum);
-      write_row(n, head0, heads, hh, d0, acc, sum);
+      write_row(n, head0, heads, hh, d0, acc, big, sum);
     } else {
       // ---- the row lies on several CTAs: this part goes to the workspace; the last to arrive joins them, at its end
       const int slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
@@ -789,8 +749,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         acc.w += f * v.w;
       }
     }
-    if constexpr (SHARED) with_prefix(p.n, p.head0, p.heads, hh, d0, acc, big, sum);
-    write_row(p.n, p.head0, p.heads, hh, d0, acc, sum);
+    write_row(p.n, p.head0, p.heads, hh, d0, acc, big, sum);
   }
 }
 
@@ -901,7 +860,7 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   return x.io_f32 ? launch_dt<__half, true>(km, vm, d, grid, st) : launch_dt<__half, false>(km, vm, d, grid, st);
 }
 
-// The sequences' own tokens, and the join with what launch_attn_shared_prefix has left in `p`.
+// The sequences' own tokens, to p.own_ml and p.own_o.
 int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& x, const SharedParts& p, void* ws, cudaStream_t st) {
   CUtensorMap km, vm;
   maps_of(c, &km, &vm);
@@ -910,10 +869,6 @@ int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& x, const 
   d.group_start = x.group_start;
   d.prefix_len = x.prefix_len;
   d.groups = (int)x.groups;
-  const int blocks = (int)ceil_div(d.group, 128);
-  d.per_block = (int)ceil_div(d.group, blocks);
-  d.tile_tokens = 128 / d.per_block;
-  d.ctas = grid;
   d.shared = p;
   log_launch("attn_decode_kernel (own tokens) sequences=%d groups=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.groups,
              d.q_heads, d.kv_heads, d.head_dim, d.window, grid);

@@ -280,7 +280,7 @@ __device__ __forceinline__ bool has_unseen(const PromptArgs& a, const Item& x, i
 // one group and kv head, the columns the group's prefix, read through the pages of its first sequence; no order between rows and columns, but a row sees
 // no more than its sequence has, and what its window leaves.  All groups' items form one list of (item, block) that is cut into equal
 // contiguous parts, one per CTA; an item's first part goes to its rows' places in the workspace, a later one (a CTA has one at most, at its beginning) to
-// the CTA's, both as maximum, sum and unscaled O.  The kernel that follows takes each sequence's own tokens and joins (attn_decode.cu).
+// the CTA's, both as maximum, sum and unscaled O.  Two kernels that follow take each sequence's own tokens and join (attn_shared.cu).
 template <typename KT, int HALVES, bool SHARED>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const PromptArgs a) {
@@ -1166,24 +1166,7 @@ int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   return launch_types<false>(c, a, x.dtype, grid, st);
 }
 
-// The workspace of attn_shared: that of decode calls, then the rows' places, then the CTAs'.
-size_t attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int head_dim) {
-  const size_t row = (size_t)ceil_div(head_dim, 16) * 64;
-  return attn_decode_workspace_bytes() + (size_t)(seqs * q_heads) * (16 + row) + (size_t)dev_info().sm_count * 2 * ROWS * (8 + row);
-}
-
-SharedParts attn_shared_parts(void* ws, int64_t seqs, int64_t q_heads, int head_dim) {
-  const int64_t padded = ceil_div(head_dim, 16) * 16, rows = seqs * q_heads, spill = (int64_t)dev_info().sm_count * 2 * ROWS;
-  SharedParts p;
-  p.base_ml = reinterpret_cast<float4*>(attn_prompt_parts(ws));
-  p.base_o = reinterpret_cast<float*>(p.base_ml + rows);
-  p.spill_o = p.base_o + rows * padded;
-  p.spill_ml = reinterpret_cast<float2*>(p.spill_o + spill * padded);
-  p.padded = (int)padded;
-  return p;
-}
-
-// x.q_start, x.groups: the first sequence of each group, and how many there are; x.prefix: the prefixes.
+// What groups of sequences have in common (attn_shared.cu).
 int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& x, const SharedParts& p, cudaStream_t st) {
   PromptArgs a = args_of(c, x);
   a.q_start = x.group_start;

@@ -294,9 +294,7 @@ int bitnet_attn_shared(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
   a.group_start = group_start;
   a.prefix_len = prefix_len;
   a.groups = groups;
-  const SharedParts p = attn_shared_parts(workspace, seqs, q_heads, c->head_dim);
-  const int first = launch_attn_shared_prefix(c, a, p, (cudaStream_t)stream);
-  return first ? first : launch_attn_shared_own(c, a, p, workspace, (cudaStream_t)stream);
+  return launch_attn_shared(c, a, workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"

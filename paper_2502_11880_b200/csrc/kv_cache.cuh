@@ -63,17 +63,18 @@ struct AttnArgs {
   const int32_t* prefix_len;    // [groups]
   int64_t groups;
 };
-// Where attn_shared keeps what rows have of their group's prefix between its two kernels: maximum, sum and unscaled O of an item's first part
+// Where attn_shared keeps what rows have of their group's prefix and of their own tokens between its kernels: maximum, sum and unscaled O of an item's first part
 // at the rows' places, of a later part at the places of the CTA that has it (attn_prompt.cu).
 struct SharedParts {
   float4* base_ml;              // [seqs][q_heads]: maximum, sum, first and last CTA of the row's item
   float* base_o;                // [seqs][q_heads][padded]
+  float2* own_ml;               // [seqs][q_heads], of the sequences' own tokens
+  float* own_o;                 // [seqs][q_heads][padded]
   float2* spill_ml;             // [CTAs][2][128]
   float* spill_o;               // [CTAs][2][128][padded]
   int padded;                   // head_dim rounded up to 16
 };
 size_t attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int head_dim);
-SharedParts attn_shared_parts(void* ws, int64_t seqs, int64_t q_heads, int head_dim);
 // The workspace: counters that are zero between calls (of fixed number, so that no call's parts ever lie where another call's
 // counters are; the last 16 bytes deal out prompt items), the parts of decode rows, the parts of prompt items (where the caller
 // gave the room for them).
@@ -88,6 +89,7 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, 
 int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, size_t ws_bytes, cudaStream_t st);
 int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, cudaStream_t st);
 int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, void* ws, cudaStream_t st);
+int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
                      int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
@@ -213,6 +215,17 @@ __device__ __forceinline__ int kv_seq_of(const int32_t* q_start, int seqs, int n
     else hi = mid;
   }
   return lo;
+}
+
+// The group of sequence n among groups that begin at start[..]: its first sequence (below 0: it is in none) and its prefix, of the table's `most` tokens.
+struct KvGroup {
+  int first, prefix;
+};
+__device__ __forceinline__ KvGroup kv_group_of(const int32_t* start, const int32_t* prefix, int groups, int n, int most) {
+  const int g = kv_seq_of(start, groups, n);
+  const int q0 = __ldg(start + g), q1 = __ldg(start + g + 1);
+  if (q0 < 0 || n < q0 || n >= q1) return KvGroup{-1, 0};
+  return KvGroup{q0, max(0, min(__ldg(prefix + g), most))};
 }
 #endif
 
