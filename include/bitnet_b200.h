@@ -605,7 +605,7 @@ int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const b
  * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
  * and that the probabilities of the prefix are rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
  * A sequence in no group (an array that is not as above) is taken by itself.  Reads at most the first 2^30 - 256 tokens of a prefix.
- * workspace: bitnet_attn_shared_workspace_bytes bytes (21 MB, and 1048 bytes per sequence and query head of 128); its first 64 KB as for the other attention
+ * workspace: bitnet_attn_shared_workspace_bytes bytes (26 MB, and 1056 bytes per sequence and query head of 128); its first 64 KB as for the other attention
  * calls, whose workspace it may be too.
  */
 size_t bitnet_attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int64_t kv_heads, int64_t head_dim);

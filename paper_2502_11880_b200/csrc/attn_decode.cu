@@ -60,20 +60,14 @@ struct DecodeArgs {
   float* part_o;                              // [2 * grid][8][D]
   int* dev_status;
   uint32_t give_up;                           // (test hook) the tile before which a CTA gives up
-  // SHARED
-  const int32_t* group_start;                 // [groups + 1]
-  const int32_t* prefix_len;                  // [groups]
-  int groups;
-  SharedParts shared;
 };
 
-// The visible tokens of one row: [s_lo, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
+// The visible tokens of one row: [0, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
 // tokens there are not there; without a window such a position means all of the table).
 struct Range {
-  int len, s_lo, s_end, lo, n0, t1, tiles, seq;
+  int len, s_end, lo, n0, t1, tiles, seq;
   bool beyond;
 };
-template <bool SHARED>
 __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
   Range r;
   r.seq = n;
@@ -90,15 +84,7 @@ __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
   r.s_end = min(a.sinks, r.lo);
   if (r.lo <= a.sinks) r.lo = r.s_end = 0;
   if (r.beyond && r.lo == r.len) r.lo = r.len = 0;             // the window lies beyond the table: the sinks alone
-  r.s_lo = 0;
-  if constexpr (SHARED) {                                      // the group's prefix has been taken
-    const int prefix = kv_group_of(a.group_start, a.prefix_len, a.groups, n, a.max_len).prefix;
-    r.s_lo = min(prefix, r.s_end);
-    r.lo = min(max(r.lo, prefix), r.len);
-    r.n0 = r.s_lo < r.s_end ? (r.s_end + TILE - 1) / TILE - r.s_lo / TILE : 0;
-  } else {
-    r.n0 = (r.s_end + TILE - 1) / TILE;
-  }
+  r.n0 = (r.s_end + TILE - 1) / TILE;
   r.t1 = r.lo / TILE;
   r.tiles = max(1, r.n0 + (r.len + TILE - 1) / TILE - r.t1);   // an empty row has one tile with nothing visible
   return r;
@@ -106,8 +92,8 @@ __device__ __forceinline__ Range range_of(const DecodeArgs& a, int n) {
 // First token of tile t, and the visible part [lo, hi) of the range it belongs to.
 __device__ __forceinline__ void tile_of(const Range& r, int t, int& first, int& lo, int& hi) {
   if (t < r.n0) {
-    first = (r.s_lo / TILE + t) * TILE;
-    lo = r.s_lo;
+    first = t * TILE;
+    lo = 0;
     hi = r.s_end;
   } else {
     first = (r.t1 + t - r.n0) * TILE;
@@ -196,9 +182,7 @@ struct Layout {
 // plain bulk copy, and ldmatrix meets distinct banks without a swizzle; tensor copies, whose 128-byte box rows begin at odd
 // multiples of 16 bytes there, took 114 instead of 85 us for 9 windows of 4096 tokens, 32 heads of 100.  (Rows of one 64-column half take
 // tensor copies whatever their length: not measured there.)
-// SHARED: the sequences' own tokens, beyond what groups of them have in common (attn_shared.cu); rows go to the workspace as maximum, sum and
-// unscaled O.
-template <typename KT, bool F32, int DT, bool DENSE, bool SHARED>
+template <typename KT, bool F32, int DT, bool DENSE>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const DecodeArgs a) {
   using L = Layout<DT>;
@@ -234,7 +218,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   int my_tiles = 0, my_row = 0;
   auto scan_chunk = [&](int n0, int64_t base) {            // tiles before token n0 + tid; returns the chunk's total
     const int n = n0 + tid;
-    my_row = n < a.tokens ? range_of<SHARED>(a, n).tiles : 0;
+    my_row = n < a.tokens ? range_of(a, n).tiles : 0;
     my_tiles = my_row * rows_per_token;
     int64_t x = my_tiles;
 #pragma unroll
@@ -299,7 +283,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
   int n = s.first_token;
   int64_t base = s.first_base;                             // tiles before token n
-  Range r = range_of<SHARED>(a, n);
+  Range r = range_of(a, n);
   int64_t item = begin;
   uint32_t it = 0;                                         // tiles of this CTA so far
 
@@ -388,7 +372,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       item += t_end - t0;
       if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
         base += (int64_t)r.tiles * rows_per_token;
-        r = range_of<SHARED>(a, ++n);
+        r = range_of(a, ++n);
       }
     }
     // leaves only when its copies have landed, which matters where the warps that wait for them have given up
@@ -419,16 +403,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     int n, head0, heads, c0, c1, first_slot;
   } pending[2];
   pending[0].n = pending[1].n = -1;
-  auto write_row = [&](int tok, int h0, int heads, int hh, int d0, const float4& acc, float big, float sum) {
-    if constexpr (SHARED) {                                // (l and O of fp16 without their scale)
-      if (hh >= heads) return;
-      const int64_t at = (int64_t)tok * a.q_heads + h0 + hh;
-      const float down = exp2_approx(-P_SHIFT);
-      if (lane == 0) a.shared.own_ml[at] = make_float2(big, sum * down);
-      if (d0 < a.shared.padded)
-        *reinterpret_cast<float4*>(a.shared.own_o + at * a.shared.padded + d0) = make_float4(acc.x * down, acc.y * down, acc.z * down, acc.w * down);
-      return;
-    }
+  auto write_row = [&](int tok, int h0, int heads, int hh, int d0, const float4& acc, float sum) {
     if (hh >= heads || d0 >= a.head_dim) return;
     const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);   // nothing visible: 0; NaN stays NaN
     const int64_t at = ((int64_t)tok * a.q_heads + h0 + hh) * a.head_dim + d0;
@@ -689,7 +664,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     }
 
     if (t_end - t0 == r.tiles) {
-      write_row(n, head0, heads, hh, d0, acc, big, sum);
+      write_row(n, head0, heads, hh, d0, acc, sum);
     } else {
       // ---- the row lies on several CTAs: this part goes to the workspace; the last to arrive joins them, at its end
       const int slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
@@ -718,7 +693,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     item += t_end - t0;
     if (row + 1 == rows_per_token && t_end == r.tiles && item < end) {
       base += (int64_t)r.tiles * rows_per_token;
-      r = range_of<SHARED>(a, ++n);
+      r = range_of(a, ++n);
     }
   }
 
@@ -749,7 +724,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         acc.w += f * v.w;
       }
     }
-    write_row(p.n, p.head0, p.heads, hh, d0, acc, big, sum);
+    write_row(p.n, p.head0, p.heads, hh, d0, acc, sum);
   }
 }
 
@@ -758,9 +733,9 @@ int padded_steps(int head_dim) {
   return dt <= 4 ? 4 : dt <= 6 ? 6 : dt;
 }
 
-template <typename KT, bool F32, int DT, bool DENSE, bool SHARED>
+template <typename KT, bool F32, int DT, bool DENSE = false>
 int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
-  auto kernel = attn_decode_kernel<KT, F32, DT, DENSE, SHARED>;
+  auto kernel = attn_decode_kernel<KT, F32, DT, DENSE>;
   constexpr size_t smem = Layout<DT>::SMEM;
   static_assert(smem <= 232448, "shared memory of one CTA");
   static std::atomic<uint64_t> have{0};                  // devices on which the kernel may take that much shared memory
@@ -779,20 +754,20 @@ int launch_one(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d
   cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, km, vm, d);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
-template <typename KT, bool F32, bool SHARED = false>
+template <typename KT, bool F32>
 int launch_dt(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d, int grid, cudaStream_t st) {
   if (d.row_bytes) {
     switch (padded_steps(d.head_dim)) {
-      case 6: return launch_one<KT, F32, 6, true, SHARED>(km, vm, d, grid, st);
-      case 7: return launch_one<KT, F32, 7, true, SHARED>(km, vm, d, grid, st);
-      default: return launch_one<KT, F32, 8, true, SHARED>(km, vm, d, grid, st);
+      case 6: return launch_one<KT, F32, 6, true>(km, vm, d, grid, st);
+      case 7: return launch_one<KT, F32, 7, true>(km, vm, d, grid, st);
+      default: return launch_one<KT, F32, 8, true>(km, vm, d, grid, st);
     }
   }
   switch (padded_steps(d.head_dim)) {
-    case 4: return launch_one<KT, F32, 4, false, SHARED>(km, vm, d, grid, st);
-    case 6: return launch_one<KT, F32, 6, false, SHARED>(km, vm, d, grid, st);
-    case 7: return launch_one<KT, F32, 7, false, SHARED>(km, vm, d, grid, st);
-    default: return launch_one<KT, F32, 8, false, SHARED>(km, vm, d, grid, st);
+    case 4: return launch_one<KT, F32, 4>(km, vm, d, grid, st);
+    case 6: return launch_one<KT, F32, 6>(km, vm, d, grid, st);
+    case 7: return launch_one<KT, F32, 7>(km, vm, d, grid, st);
+    default: return launch_one<KT, F32, 8>(km, vm, d, grid, st);
   }
 }
 
@@ -801,8 +776,12 @@ int launch_dt(const CUtensorMap& km, const CUtensorMap& vm, const DecodeArgs& d,
 // The parts of one call: two per CTA, whatever the call.
 size_t attn_decode_parts_bytes() { return 2 * (size_t)dev_info().sm_count * HEADS * (8 + 128 * 4); }
 
-static DecodeArgs args_of(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws) {
-  DecodeArgs d = {};
+int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
+  CUtensorMap km, vm;
+  const int first = c->layer_pages > 0 ? 2 : 0;
+  memcpy(&km, c->maps[first], sizeof km);
+  memcpy(&vm, c->maps[first + 1], sizeof vm);
+  DecodeArgs d;
   d.layer_pages = (int)c->layer_pages;
   d.k = static_cast<const uint8_t*>(c->k) + x.layer * c->stride_layer * 2;
   d.v = static_cast<const uint8_t*>(c->v) + x.layer * c->stride_layer * 2;
@@ -833,46 +812,19 @@ static DecodeArgs args_of(const bitnet_kv_cache_t* c, const AttnArgs& x, void* w
   const int64_t most = x.table_width * c->page_size;
   d.max_len = most > 0x7fffff00 ? 0x7fffff00 : (int)most;
   d.c = x.scale * 1.4426950408889634f;
-  const size_t slots = 2 * (size_t)dev_info().sm_count * HEADS;
+  const int grid = dev_info().sm_count;
+  const size_t slots = 2 * (size_t)grid * HEADS;
   d.counters = attn_counters(ws);
   uint8_t* const w = attn_decode_parts(ws);
   d.part_ml = reinterpret_cast<float2*>(w);
   d.part_o = reinterpret_cast<float*>(w + slots * 8);
   d.dev_status = x.dev_status;
   d.give_up = x.give_up;
-  return d;
-}
-static void maps_of(const bitnet_kv_cache_t* c, CUtensorMap* km, CUtensorMap* vm) {
-  const int first = c->layer_pages > 0 ? 2 : 0;
-  memcpy(km, c->maps[first], sizeof *km);
-  memcpy(vm, c->maps[first + 1], sizeof *vm);
-}
-
-int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
-  CUtensorMap km, vm;
-  maps_of(c, &km, &vm);
-  const DecodeArgs d = args_of(c, x, ws);
-  const int grid = dev_info().sm_count;
   log_launch("attn_decode_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.q_heads, d.kv_heads, d.head_dim,
              d.window, grid);
   if (x.dtype == BITNET_KV_BF16)
     return x.io_f32 ? launch_dt<__nv_bfloat16, true>(km, vm, d, grid, st) : launch_dt<__nv_bfloat16, false>(km, vm, d, grid, st);
   return x.io_f32 ? launch_dt<__half, true>(km, vm, d, grid, st) : launch_dt<__half, false>(km, vm, d, grid, st);
-}
-
-// The sequences' own tokens, to p.own_ml and p.own_o.
-int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& x, const SharedParts& p, void* ws, cudaStream_t st) {
-  CUtensorMap km, vm;
-  maps_of(c, &km, &vm);
-  DecodeArgs d = args_of(c, x, ws);
-  const int grid = dev_info().sm_count;
-  d.group_start = x.group_start;
-  d.prefix_len = x.prefix_len;
-  d.groups = (int)x.groups;
-  d.shared = p;
-  log_launch("attn_decode_kernel (own tokens) sequences=%d groups=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.groups,
-             d.q_heads, d.kv_heads, d.head_dim, d.window, grid);
-  return x.dtype == BITNET_KV_BF16 ? launch_dt<__nv_bfloat16, false, true>(km, vm, d, grid, st) : launch_dt<__half, false, true>(km, vm, d, grid, st);
 }
 
 int attn_status(int* out) {

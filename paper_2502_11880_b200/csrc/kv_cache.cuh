@@ -63,13 +63,11 @@ struct AttnArgs {
   const int32_t* prefix_len;    // [groups]
   int64_t groups;
 };
-// Where attn_shared keeps what rows have of their group's prefix and of their own tokens between its kernels: maximum, sum and unscaled O of an item's first part
-// at the rows' places, of a later part at the places of the CTA that has it (attn_prompt.cu).
+// Where attn_shared keeps what rows (a sequence and a query head) have of their group's prefix between its kernels: of an item's first part at the rows'
+// places, of a later part at the places of the CTA that has it (attn_prompt.cu).
 struct SharedParts {
   float4* base_ml;              // [seqs][q_heads]: maximum, sum, first and last CTA of the row's item
-  float* base_o;                // [seqs][q_heads][padded]
-  float2* own_ml;               // [seqs][q_heads], of the sequences' own tokens
-  float* own_o;                 // [seqs][q_heads][padded]
+  float* base_o;                // [seqs][q_heads][padded], unscaled
   float2* spill_ml;             // [CTAs][2][128]
   float* spill_o;               // [CTAs][2][128][padded]
   int padded;                   // head_dim rounded up to 16
@@ -88,7 +86,6 @@ size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads);
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
 int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, size_t ws_bytes, cudaStream_t st);
 int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, cudaStream_t st);
-int launch_attn_shared_own(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, void* ws, cudaStream_t st);
 int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,

@@ -92,5 +92,5 @@ def test_calls_refuse_what_was_not_initialised(L):
 def test_shared_workspace_sizes(L):
     f = bn.bitnet_attn_shared_workspace_bytes
     assert f(0, 32, 8, 128) > bn.bitnet_attn_workspace_bytes(0, 32, 8, 128)
-    assert f(64, 64, 8, 128) - f(0, 64, 8, 128) == 64 * 64 * 1048
+    assert f(64, 64, 8, 128) - f(0, 64, 8, 128) == 64 * 64 * 1056
     assert f(1, 30, 8, 128) == 0 and f(-1, 32, 8, 128) == 0 and f(1, 32, 8, 132) == 0 and f(1, 0, 1, 64) == 0
