@@ -122,6 +122,7 @@ struct OwnLayout {
   struct Tail {
     int64_t scan[OWN_WARPS];
     int most[OWN_WARPS];
+    int64_t cut[OWN_WARPS][2];                // of the list: where a warp's part begins, and the next one's
     int64_t begin[OWN_WARPS], end[OWN_WARPS], base[OWN_WARPS];
     int first[OWN_WARPS];
   };
@@ -178,24 +179,26 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   const bool whole = rows >= 2 * warps || longest <= 6;
   const int64_t parts = min(warps, whole ? rows : total);
   // (warps of different CTAs take neighbouring parts: the SMs have equally many)
-  const int64_t id0 = blockIdx.x;
-  auto cut = [&](int64_t part) { return total * part / parts; };
+  const int64_t id = blockIdx.x + (int64_t)warp * gridDim.x;
+  if (lane < 2) {
+    s.cut[warp][lane] = id < parts ? total * (id + lane) / parts : -1;
+    if (lane == 0) s.begin[warp] = s.end[warp] = id < parts ? total : 0;
+  }
+  __syncthreads();
   auto find_cuts = [&](int n0) {
-#pragma unroll
-    for (int w = 0; w < OWN_WARPS; ++w) {
-      const int64_t id = id0 + (int64_t)w * gridDim.x;
-      if (id >= parts) {
-        if (tid == 0) s.begin[w] = s.end[w] = 0;
-        continue;
+    const int64_t mine = my_excl + my_tiles;
+#pragma unroll 1
+    for (int k = 0; k < 2 * OWN_WARPS; ++k) {
+      const int64_t c = s.cut[k >> 1][k & 1];
+      if (c < my_excl || c >= mine) continue;
+      const int64_t at = whole ? my_excl + (c - my_excl) / my_row * my_row : c;
+      if (k & 1) {
+        s.end[k >> 1] = at;
+      } else {
+        s.begin[k >> 1] = at;
+        s.first[k >> 1] = n0 + tid;
+        s.base[k >> 1] = my_excl;
       }
-      const int64_t c0 = cut(id), c1 = cut(id + 1), mine = my_excl + my_tiles;
-      if (c0 >= my_excl && c0 < mine) {
-        s.first[w] = n0 + tid;
-        s.base[w] = my_excl;
-        s.begin[w] = whole ? my_excl + (c0 - my_excl) / my_row * my_row : c0;
-      }
-      if (c1 == total && tid == 0) s.end[w] = total;
-      if (c1 >= my_excl && c1 < mine) s.end[w] = whole ? my_excl + (c1 - my_excl) / my_row * my_row : c1;
     }
   };
   if (a.seqs <= OWN_THREADS) {
@@ -208,95 +211,88 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     }
   }
   __syncthreads();
-  const int64_t id = id0 + (int64_t)warp * gridDim.x, end = s.end[warp];
-  int64_t item = s.begin[warp], base = s.base[warp];
-  if (id >= parts || item >= end) return;
-  int n = s.first[warp];
-  Own r = own_of(a, n);
+  if (id >= parts || s.begin[warp] >= s.end[warp]) return;
 
-  // ---- filling: a second place in the list, STAGES - 1 tiles ahead
+  // A place in the list, and a second one STAGES - 1 tiles ahead, where the ring is filled.
+  struct Place {
+    int64_t left;                             // tiles of the part from here on
+    int n, t, kv, block;                      // sequence, tile of the row, the row's kv head and block of query heads
+    Own r;
+  } p, f;
+  auto next_row = [&](Place& p) {
+    p.t = 0;
+    if (++p.block < a.head_blocks) return;
+    p.block = 0;
+    if (++p.kv < a.kv_heads) return;
+    p.kv = 0;
+    if (p.left > 0) p.r = own_of(a, ++p.n);
+  };
+  {
+    const int64_t item = s.begin[warp], in_seq = item - s.base[warp];
+    p.left = s.end[warp] - item;
+    p.n = s.first[warp];
+    p.r = own_of(a, p.n);
+    const int row = (int)(in_seq / p.r.tiles);
+    p.t = (int)(in_seq - (int64_t)row * p.r.tiles);
+    p.kv = row / a.head_blocks;
+    p.block = row - p.kv * a.head_blocks;
+    f = p;
+  }
+  auto tile_of = [&](const Own& r, int t, int& first, int& lo, int& hi) {
+    const bool sink = t < r.n0;
+    lo = sink ? r.s_lo : r.lo;
+    hi = sink ? r.s_hi : r.hi;
+    first = (lo / TILE + (sink ? t : t - r.n0)) * TILE;
+  };
   const uint32_t ring = smem_u32(smem) + warp * L::STAGES * L::STAGE;
   constexpr int PIECES = L::ROW / 16, AT_ONCE = 32 / PIECES;          // 16-byte pieces of a row, rows per step
   const int piece = lane % PIECES, sub = lane / PIECES;
-  const int pieces = (a.head_dim + 7) / 8;
-  struct Place {
-    int64_t item, base;
-    int n, t, row;                            // tile of the row, row of the sequence
-    Own r;
-  } f;
-  f.item = item;
-  f.base = base;
-  f.n = n;
-  f.r = r;
-  f.row = (int)((item - base) / r.tiles);
-  f.t = (int)((item - base) - (int64_t)f.row * r.tiles);
-  auto tile_of = [&](const Own& r, int t, int& first, int& lo, int& hi) {
-    if (t < r.n0) {
-      first = (r.s_lo / TILE + t) * TILE;
-      lo = r.s_lo;
-      hi = r.s_hi;
-    } else {
-      first = (r.lo / TILE + t - r.n0) * TILE;
-      lo = r.lo;
-      hi = r.hi;
-    }
+  const int bytes = max(0, min(16, 2 * a.head_dim - 16 * piece));    // (the rest is filled with zeros: padding may be anything)
+  // the page of the lane's token in f's tile; -2: not read
+  auto look_up = [&]() -> int {
+    int first, lo, hi;
+    tile_of(f.r, f.t, first, lo, hi);
+    const int tok = first + (lane & (TILE - 1));
+    return f.left > 0 && tok >= lo && tok < hi ? __ldg(a.table + (int64_t)f.n * a.table_width + (tok >> a.page_shift)) : -2;
   };
-  auto step = [&](Place& p) {                 // to the next tile
-    ++p.item;
-    if (++p.t < p.r.tiles) return;
-    p.t = 0;
-    if (++p.row < rows_per_seq) return;
-    p.row = 0;
-    p.base += (int64_t)p.r.tiles * rows_per_seq;
-    if (p.item < end) p.r = own_of(a, ++p.n);
-  };
+  int page = look_up();                       // (a tile ahead of the copies)
   uint32_t filled = 0;
   auto fill = [&] {
-    if (f.item < end) {
+    if (f.left > 0) {
       int first, lo, hi;
       tile_of(f.r, f.t, first, lo, hi);
-      // lane's token of the tile: its page, or -1 where nothing is to be read
+      const bool there = page >= 0 && page < a.num_pages;
+      if (((page != -2 && !there) || (f.r.beyond && lane == 0)) && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
       const int tok = first + (lane & (TILE - 1));
-      int page = -1;
-      if (tok >= lo && tok < hi) {
-        page = __ldg(a.table + (int64_t)f.n * a.table_width + (tok >> a.page_shift));
-        if (page < 0 || page >= a.num_pages) {
-          page = -1;
-          if (a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-        }
-      }
-      if (f.r.beyond && lane == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-      const int64_t head = (int64_t)(f.row / a.head_blocks) * a.head_bytes;
-      const uint32_t to = ring + (filled % L::STAGES) * L::STAGE;
+      const int64_t of_lane = there ? page * a.page_bytes + (int64_t)(tok & ((1 << a.page_shift) - 1)) * a.row_bytes + f.kv * a.head_bytes : -1;
+      --f.left;
+      if (++f.t == f.r.tiles) next_row(f);
+      page = look_up();
+      const uint32_t to = ring + (filled % L::STAGES) * L::STAGE + sub * L::ROW;
 #pragma unroll
       for (int i = 0; i < TILE; i += AT_ONCE) {
-        const int row = i + sub;
-        const int pg = __shfl_sync(0xffffffffu, page, row);
-        const bool there = pg >= 0 && piece < pieces;
-        const int64_t at = there ? pg * a.page_bytes + head + (int64_t)((first + row) & ((1 << a.page_shift) - 1)) * a.row_bytes + piece * 16 : 0;
-        const uint32_t dst = to + row * L::ROW + ((piece & ~7) | ((piece ^ row) & 7)) * 16;
-        const int bytes = there ? min(16, 2 * a.head_dim - 16 * piece) : 0;     // (the rest is filled with zeros: padding may be anything)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(a.k + at), "r"(bytes) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + TILE * L::ROW), "l"(a.v + at), "r"(bytes) : "memory");
+        const int64_t of_row = __shfl_sync(0xffffffffu, of_lane, i + sub);
+        const int64_t at = max(of_row, (int64_t)0) + piece * 16;
+        const uint32_t dst = to + i * L::ROW + ((piece & ~7) | ((piece ^ (i + sub)) & 7)) * 16;
+        const int n = of_row < 0 ? 0 : bytes;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(a.k + (n ? at : 0)), "r"(n) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + TILE * L::ROW), "l"(a.v + (n ? at : 0)), "r"(n) : "memory");
       }
       ++filled;
-      step(f);
     }
     cp_commit();
   };
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < L::STAGES - 1; ++i) fill();
 
   const int g = lane >> 2, t4 = lane & 3;                  // accumulator row (head) and column pair
   const int k_row = (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;
   const int v_row = lane & 15, v_piece = lane >> 4;
   uint32_t used = 0;
-  while (item < end) {
-    const int row = (int)((item - base) / r.tiles);
-    const int t0 = (int)((item - base) - (int64_t)row * r.tiles);
-    const int t_end = (int)min((int64_t)r.tiles, t0 + end - item);
-    const int block = row % a.head_blocks, heads = min(HEADS, a.group - block * HEADS);
-    const int head0 = row / a.head_blocks * a.group + block * HEADS;
+  while (p.left > 0) {
+    const Own r = p.r;
+    const int n = p.n, t0 = p.t, t_end = (int)min((int64_t)r.tiles, t0 + p.left);
+    const int heads = min(HEADS, a.group - p.block * HEADS), head0 = p.kv * a.group + p.block * HEADS;
     uint32_t qa[DT][2];
     {
       const bool have = g < heads;
@@ -324,9 +320,9 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
       float sc[2][2][4] = {};
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
-        const int p = 2 * i + k_piece;
+        const int at = 2 * i + k_piece;
         uint32_t b[4];
-        ldsm4(kbase + k_row * L::ROW + ((p & ~7) | ((p ^ k_row) & 7)) * 16, b);
+        ldsm4(kbase + k_row * L::ROW + ((at & ~7) | ((at ^ k_row) & 7)) * 16, b);
         P2::mma(sc[i & 1][0], qa[i][0], 0u, qa[i][1], 0u, b[0], b[1]);
         P2::mma(sc[i & 1][1], qa[i][0], 0u, qa[i][1], 0u, b[2], b[3]);
       }
@@ -355,22 +351,22 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
         m = m_new;
       }
       const float ref = (m == -INFINITY ? 0.0f : m) - P_SHIFT;
-      float p[4];
+      float e[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = exp2_approx(x[j] - ref);
-      l += (p[0] + p[1]) + (p[2] + p[3]);
+      for (int j = 0; j < 4; ++j) e[j] = exp2_approx(x[j] - ref);
+      l += (e[0] + e[1]) + (e[2] + e[3]);
       uint32_t ph[2], pm[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        ph[j] = P2::pack(p[2 * j], p[2 * j + 1]);
+        ph[j] = P2::pack(e[2 * j], e[2 * j + 1]);
         const float2 hf = P2::unpack(ph[j]);
-        pm[j] = P2::pack(p[2 * j] - hf.x, p[2 * j + 1] - hf.y);
+        pm[j] = P2::pack(e[2 * j] - hf.x, e[2 * j + 1] - hf.y);
       }
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
-        const int p = 2 * i + v_piece;
+        const int at = 2 * i + v_piece;
         uint32_t b[4];
-        ldsm4_t(vbase + v_row * L::ROW + ((p & ~7) | ((p ^ v_row) & 7)) * 16, b);
+        ldsm4_t(vbase + v_row * L::ROW + ((at & ~7) | ((at ^ v_row) & 7)) * 16, b);
         P2::mma(o[2 * i], ph[0], pm[0], ph[1], pm[1], b[0], b[1]);
         P2::mma(o[2 * i + 1], ph[0], pm[0], ph[1], pm[1], b[2], b[3]);
       }
@@ -387,7 +383,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
       if (t4 == 0) {
         if (t0 == 0) {
           // the last warp that has a part of this row
-          const int w1 = whole ? (int)id : (int)(((item + r.tiles) * parts - 1) / total);
+          const int w1 = whole || t_end == r.tiles ? (int)id : (int)(((s.end[warp] - p.left + r.tiles) * parts - 1) / total);
           a.own_ml[at] = make_float4(m, l * down, __int_as_float((int)id), __int_as_float(w1));
         } else {
           a.late_ml[late] = make_float2(m, l * down);
@@ -398,11 +394,8 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
         if (8 * j < a.padded)
           *reinterpret_cast<float2*>(dst + 8 * j) = make_float2((o[j][0] + o[j][2]) * down, (o[j][1] + o[j][3]) * down);
     }
-    item += t_end - t0;
-    if (row + 1 == rows_per_seq && t_end == r.tiles && item < end) {
-      base += (int64_t)r.tiles * rows_per_seq;
-      r = own_of(a, ++n);
-    }
+    p.left -= t_end - t0;
+    if (t_end == r.tiles) next_row(p);
   }
 }
 
