@@ -794,6 +794,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ------------------------------------------------------------ one thread per row
+    // (SHARED, whose parts are joined by maxima: fp16 probabilities relative to 2^-7 of the maximum, clear of that type's smallest steps and, with LAZY,
+    // of its largest; the part's maximum is given out less that)
+    constexpr float SHIFT = SHARED && std::is_same<KT, __half>::value ? 7.0f : 0.0f;
     const int u = warp >> 2, quarter = warp & 3, row = tid & 127;
     const int row_tok = row / a.per_block, hd = row % a.per_block;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
@@ -863,7 +866,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             }
           }
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
+        const float ref = (m == -INFINITY ? 0.0f : m) - SHIFT;
         const uint64_t r2 = pair(-ref, -ref);
         // ---- exponentials of 64 columns, which become 32 of P
         auto exps = [&](uint32_t* x) {
@@ -902,8 +905,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         const bool first = x.b0 == 0;
         const int64_t of_row = ((int64_t)(x.q0 + tok) * a.q_heads + x.head0 + hd), of_cta = ((int64_t)blockIdx.x * 2 + u) * ROWS + row;
         if (valid) {
-          if (first) a.base_ml[of_row] = make_float4(m, sum, __int_as_float(x.c0), __int_as_float(x.c1));
-          else a.spill_ml[of_cta] = make_float2(m, sum);
+          if (first) a.base_ml[of_row] = make_float4(m - SHIFT, sum, __int_as_float(x.c0), __int_as_float(x.c1));
+          else a.spill_ml[of_cta] = make_float2(m - SHIFT, sum);
         }
         const int64_t at = valid ? (first ? of_row : of_cta) * (steps * 16) : -1;
         float* const dst = first ? a.base_o : a.spill_o;

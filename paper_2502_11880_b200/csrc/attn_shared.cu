@@ -60,11 +60,16 @@ __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
                : "memory");
 }
 
+// 16 bytes to shared memory, the first `n` from `src`, the rest zeros.
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, int n, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(n), "l"(policy) : "memory");
+}
+
 // ------------------------------------------------------------------------------------------------ own tokens
 // Rows here are (sequence, kv head, block of up to 8 query heads), their tokens cut into tiles of 16.  All rows' tiles form one list that is dealt to the
 // warps in equal contiguous parts; a warp works by itself, with a ring of tiles of its own that plain asynchronous copies fill, so that
 // some 1200 short rows are under way at a time and none waits for another.  (The decode kernel, whose eight warps meet at every
-// row's end, took 55 us for 64 sequences of up to 400 own tokens, 64/8 heads of 128, and 36 for 40 of up to 300, 16/16 heads of 96; HBM needs 8 and 7.)  A row's
+// row's end, took 55 us for 64 sequences of up to 400 own tokens, 64/8 heads of 128, and 36 for 40 of up to 300, 16/16 heads of 96; HBM needs 8 and 7, this kernel takes 22 and 16.)  A row's
 // first part goes to its place in the workspace, a later one (a warp has one at most, at its beginning) to the warp's.
 // S = Q K^T and O += P V on mma.sync m16n8k16, the heads as rows 0..7; rows 8..15 of P hold what rounding took from rows 0..7, so that probabilities
 // have 16 (bf16) or 22 bits.
@@ -181,7 +186,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   // (warps of different CTAs take neighbouring parts: the SMs have equally many)
   const int64_t id = blockIdx.x + (int64_t)warp * gridDim.x;
   if (lane < 2) {
-    s.cut[warp][lane] = id < parts ? total * (id + lane) / parts : -1;
+    s.cut[warp][lane] = id < parts ? kv_quotient(total * (id + lane), parts) : -1;
     if (lane == 0) s.begin[warp] = s.end[warp] = id < parts ? total : 0;
   }
   __syncthreads();
@@ -191,7 +196,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     for (int k = 0; k < 2 * OWN_WARPS; ++k) {
       const int64_t c = s.cut[k >> 1][k & 1];
       if (c < my_excl || c >= mine) continue;
-      const int64_t at = whole ? my_excl + (c - my_excl) / my_row * my_row : c;
+      const int64_t at = whole ? my_excl + kv_quotient(c - my_excl, my_row) * my_row : c;
       if (k & 1) {
         s.end[k >> 1] = at;
       } else {
@@ -232,7 +237,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     p.left = s.end[warp] - item;
     p.n = s.first[warp];
     p.r = own_of(a, p.n);
-    const int row = (int)(in_seq / p.r.tiles);
+    const int row = (int)kv_quotient(in_seq, p.r.tiles);
     p.t = (int)(in_seq - (int64_t)row * p.r.tiles);
     p.kv = row / a.head_blocks;
     p.block = row - p.kv * a.head_blocks;
@@ -248,6 +253,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   constexpr int PIECES = L::ROW / 16, AT_ONCE = 32 / PIECES;          // 16-byte pieces of a row, rows per step
   const int piece = lane % PIECES, sub = lane / PIECES;
   const int bytes = max(0, min(16, 2 * a.head_dim - 16 * piece));    // (the rest is filled with zeros: padding may be anything)
+  const uint64_t policy = policy_evict_first();            // (tokens are read once: what else is in L2, the kernels' instructions too, stays)
   // the page of the lane's token in f's tile; -2: not read
   auto look_up = [&]() -> int {
     int first, lo, hi;
@@ -275,8 +281,8 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
         const int64_t at = max(of_row, (int64_t)0) + piece * 16;
         const uint32_t dst = to + i * L::ROW + ((piece & ~7) | ((piece ^ (i + sub)) & 7)) * 16;
         const int n = of_row < 0 ? 0 : bytes;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(a.k + (n ? at : 0)), "r"(n) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + TILE * L::ROW), "l"(a.v + (n ? at : 0)), "r"(n) : "memory");
+        copy16(dst, a.k + (n ? at : 0), n, policy);
+        copy16(dst + TILE * L::ROW, a.v + (n ? at : 0), n, policy);
       }
       ++filled;
     }
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
       if (t4 == 0) {
         if (t0 == 0) {
           // the last warp that has a part of this row
-          const int w1 = whole || t_end == r.tiles ? (int)id : (int)(((s.end[warp] - p.left + r.tiles) * parts - 1) / total);
+          const int w1 = whole || t_end == r.tiles ? (int)id : (int)kv_quotient((s.end[warp] - p.left + r.tiles) * parts - 1, total);
           a.own_ml[at] = make_float4(m, l * down, __int_as_float((int)id), __int_as_float(w1));
         } else {
           a.late_ml[late] = make_float2(m, l * down);
@@ -421,7 +427,7 @@ template <typename KT>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const __grid_constant__ JoinArgs a) {
   const int lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
-  const int tok = (int)(row / a.q_heads), head = (int)(row - (int64_t)tok * a.q_heads);
+  const int tok = (int)kv_quotient(row, a.q_heads), head = (int)(row - (int64_t)tok * a.q_heads);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (row >= a.rows) return;

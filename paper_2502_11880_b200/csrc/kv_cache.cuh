@@ -197,6 +197,11 @@ __device__ __forceinline__ void kv_bulk_copy(uint32_t dst, const void* src, uint
                : "memory");
 }
 
+// a / b for a >= 0, b >= 1.  (Most fit 32 bits, in which a division is a quarter as long.)
+__device__ __forceinline__ int64_t kv_quotient(int64_t a, int64_t b) {
+  return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -52,7 +52,7 @@ class Groups:
                         p = int(order[r[e]])
                         if j and (e + 1) * page <= prefix and bool(torch.isfinite(t[1, p, :, :c]).all()):
                             continue             # shared, and there
-                        if j and e * page < prefix < (e + 1) * page:
+                        if j and e * page < prefix:
                             keep = min(prefix - e * page, c, of_first - e * page)
                             if keep > 0:
                                 x[:, :keep] = t[1, int(order[first_row[e]]), :, :keep]
@@ -128,6 +128,25 @@ def test_long_prefix_over_all_ctas():
 def test_more_items_than_ctas():
     s = Groups([(130 + i, [200 + i, 300]) for i in range(70)], 8, 32, 16, HF, seed=3)
     s.check(s.queries(8))
+
+
+def test_more_groups_and_sequences_than_threads():
+    """More than are looked at at a time, some groups without sequences, or shorter than their prefix; with and without a window."""
+    s = Groups([(37 * (i % 3), [40 + i % 90] * (i % 3)) for i in range(400)], 2, 16, 8, BF, seed=4)
+    q = s.queries(4)
+    for window, sinks in ((0, 0), (30, 2)):
+        s.check(q, window=window, sinks=sinks)
+
+
+def test_many_small_probabilities():
+    """One token far ahead of many: each of those has a probability below fp16's normal numbers, together they have most of the weight."""
+    s = Groups([(20032, [20040, 40000])], 1, 64, 64, HF, seed=16)
+    s.k[1, :, :, :, 1:] = 0
+    s.k[1, :, :, :, 0] = 0
+    s.k[1, s.table[0, 0].long(), 0, 5, 0] = 9.5 * 8
+    q = torch.zeros_like(s.queries(2))
+    q[..., 0] = 1
+    s.check(q)
 
 
 def test_scales_and_rising_maxima():
