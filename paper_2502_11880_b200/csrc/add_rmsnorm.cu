@@ -106,54 +106,56 @@ __device__ __forceinline__ float inverse_root(double v) {
 __device__ __forceinline__ float scaled(float h, float r, float w) { return __fmul_rn(__fmul_rn(h, r), w); }
 
 // Four elements as they lie in memory: 16 bytes of binary32, or 8.
-template <int BYTES>
+constexpr int NONE = -1;
+template <int TYPE>
 struct Raw {
-  uint4 v;
-};
-template <>
-struct Raw<2> {
   uint2 v;
 };
-template <int BYTES>
-__device__ __forceinline__ Raw<BYTES> load_raw(const void* p, int64_t i) {
-  Raw<BYTES> r;
-  if constexpr (BYTES == 4) r.v = __ldcg(reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i));
+template <>
+struct Raw<BITNET_KV_F32> {
+  uint4 v;
+};
+template <int TYPE>
+__device__ __forceinline__ Raw<TYPE> load_raw(const void* p, int64_t i) {
+  Raw<TYPE> r;
+  if constexpr (TYPE == BITNET_KV_F32) r.v = __ldcg(reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i));
   else r.v = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i));
   return r;
 }
-__device__ __forceinline__ float4 widen(const Raw<4>& r, int) {
+__device__ __forceinline__ float4 widen(const Raw<BITNET_KV_F32>& r) {
   return make_float4(__uint_as_float(r.v.x), __uint_as_float(r.v.y), __uint_as_float(r.v.z), __uint_as_float(r.v.w));
 }
-__device__ __forceinline__ float4 widen(const Raw<2>& r, int type) {
+template <int TYPE>
+__device__ __forceinline__ float4 widen(const Raw<TYPE>& r) {
   const uint2 w = r.v;
-  if (type == BITNET_KV_BF16)
+  if (TYPE == BITNET_KV_BF16)
     return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
   const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), hi = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
   return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 
-// VPT: pieces of 4 elements per thread; XB, RB: bytes of an element of x and of the residual (0: none).  A CTA takes every gridDim.x-th row, and
+// VPT: pieces of 4 elements per thread; XT, RT: types of x and of the residual (or NONE).  A CTA takes every gridDim.x-th row, and
 // has the next one's loads on their way while it reduces and writes the present one.
-template <int VPT, int XB, int RB>
+template <int VPT, int XT, int RT>
 __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant__ NormDev d) {
   const NormArgs& a = d.a;
   __shared__ Red red;
   const int tid = threadIdx.x, nt = blockDim.x, n4 = (int)(a.K / 4);
   if (tid == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  Raw<XB> x[VPT];
-  Raw<RB> e[VPT];
+  Raw<XT> x[VPT];
+  Raw<RT> e[VPT];
   auto fetch = [&](int64_t t) {
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       const int i = tid + k * nt;
-      if (i < n4) x[k] = load_raw<XB>(a.x, t * a.stride_x + 4 * (int64_t)i);
+      if (i < n4) x[k] = load_raw<XT>(a.x, t * a.stride_x + 4 * (int64_t)i);
     }
-    if constexpr (RB > 0) {
+    if constexpr (RT != NONE) {
 #pragma unroll
       for (int k = 0; k < VPT; ++k) {
         const int i = tid + k * nt;
-        if (i < n4) e[k] = load_raw<RB>(a.residual, t * a.stride_residual + 4 * (int64_t)i);
+        if (i < n4) e[k] = load_raw<RT>(a.residual, t * a.stride_residual + 4 * (int64_t)i);
       }
     }
   };
@@ -161,22 +163,28 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
   int64_t t = blockIdx.x;
   if (AHEAD) fetch(t);
   for (;;) {
-    if (!AHEAD) fetch(t);
     float4 h[VPT];
     double sum = 0.0;
+    if (!AHEAD) {
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int i = tid + k * nt;
+        if (i < n4) h[k] = widen(load_raw<XT>(a.x, t * a.stride_x + 4 * (int64_t)i));
+      }
+    }
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       const int i = tid + k * nt;
-      h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (AHEAD || i >= n4) h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i >= n4) continue;
-      h[k] = widen(x[k], a.x_type);
-      if constexpr (RB > 0) {
-        const float4 r = widen(e[k], a.residual_type);
-        h[k].x = rounded(h[k].x + r.x, RB == 4 ? BITNET_KV_F32 : a.residual_type);
-        h[k].y = rounded(h[k].y + r.y, RB == 4 ? BITNET_KV_F32 : a.residual_type);
-        h[k].z = rounded(h[k].z + r.z, RB == 4 ? BITNET_KV_F32 : a.residual_type);
-        h[k].w = rounded(h[k].w + r.w, RB == 4 ? BITNET_KV_F32 : a.residual_type);
-        store4(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, a.residual_type, h[k]);
+      if (AHEAD) h[k] = widen(x[k]);
+      if constexpr (RT != NONE) {
+        const float4 r = widen(AHEAD ? e[k] : load_raw<RT>(a.residual, t * a.stride_residual + 4 * (int64_t)i));
+        h[k].x = rounded(h[k].x + r.x, RT);
+        h[k].y = rounded(h[k].y + r.y, RT);
+        h[k].z = rounded(h[k].z + r.z, RT);
+        h[k].w = rounded(h[k].w + r.w, RT);
+        store4(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, RT, h[k]);
       }
       sum = fma((double)h[k].x, (double)h[k].x, sum);
       sum = fma((double)h[k].y, (double)h[k].y, sum);
@@ -267,15 +275,22 @@ int threads_for(int64_t pieces) {               // whole warps
   return (int)(n < 64 ? 64 : n > 1024 ? 1024 : n);
 }
 
-template <int VPT, int XB>
+template <int VPT, int XT>
 cudaError_t launch_residual(const NormDev& d, const cudaLaunchConfig_t& cfg) {
-  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 0>, d);
-  return d.a.residual_type == BITNET_KV_F32 ? cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 4>, d)
-                                            : cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XB, 2>, d);
+  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, NONE>, d);
+  switch (d.a.residual_type) {
+    case BITNET_KV_F32: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F32>, d);
+    case BITNET_KV_BF16: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_BF16>, d);
+    default: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F16>, d);
+  }
 }
 template <int VPT>
 cudaError_t launch_x(const NormDev& d, const cudaLaunchConfig_t& cfg) {
-  return d.a.x_type == BITNET_KV_F32 ? launch_residual<VPT, 4>(d, cfg) : launch_residual<VPT, 2>(d, cfg);
+  switch (d.a.x_type) {
+    case BITNET_KV_F32: return launch_residual<VPT, BITNET_KV_F32>(d, cfg);
+    case BITNET_KV_BF16: return launch_residual<VPT, BITNET_KV_BF16>(d, cfg);
+    default: return launch_residual<VPT, BITNET_KV_F16>(d, cfg);
+  }
 }
 
 }  // namespace

@@ -40,32 +40,32 @@ struct RopeDev {
   uint64_t step[64];         // turns per position, in 2^-64
 };
 
-// N elements of 4 or 2 bytes; aligned to N elements (16 bytes at most).
+// N elements of 4 or 2 bytes as they lie in memory, aligned to N elements (16 bytes at most).
 template <typename T, int N>
-__device__ __forceinline__ void load_vec(const uint8_t* p, float (&x)[N]) {
-  if constexpr (std::is_same<T, float>::value) {
-    const float* f = reinterpret_cast<const float*>(p);
-    if constexpr (N >= 4) {
+struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec {
+  T t[N];
+};
+template <typename T, int N>
+__device__ __forceinline__ Vec<T, N> load_vec(const uint8_t* p) {
+  constexpr int BYTES = sizeof(T) * N;
+  union {
+    Vec<T, N> v;
+    uint4 a[(BYTES + 15) / 16];
+    uint2 b;
+    unsigned int c;
+    unsigned short d;
+  } x;
+  if constexpr (BYTES >= 16) {
 #pragma unroll
-      for (int i = 0; i < N; i += 4) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(f + i));
-        x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
-      }
-    } else if constexpr (N == 2) {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(f));
-      x[0] = v.x, x[1] = v.y;
-    } else {
-      x[0] = __ldcg(f);
-    }
+    for (int i = 0; i < BYTES / 16; ++i) x.a[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  } else if constexpr (BYTES == 8) {
+    x.b = __ldg(reinterpret_cast<const uint2*>(p));
+  } else if constexpr (BYTES == 4) {
+    x.c = __ldg(reinterpret_cast<const unsigned int*>(p));
   } else {
-    T t[N];
-    if constexpr (N == 8) *reinterpret_cast<uint4*>(t) = __ldcg(reinterpret_cast<const uint4*>(p));
-    else if constexpr (N == 4) *reinterpret_cast<uint2*>(t) = __ldcg(reinterpret_cast<const uint2*>(p));
-    else if constexpr (N == 2) *reinterpret_cast<uint32_t*>(t) = __ldcg(reinterpret_cast<const unsigned int*>(p));
-    else *reinterpret_cast<uint16_t*>(t) = __ldcg(reinterpret_cast<const unsigned short*>(p));
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = static_cast<float>(t[i]);
+    x.d = __ldg(reinterpret_cast<const unsigned short*>(p));
   }
+  return x.v;
 }
 template <typename T>
 __device__ __forceinline__ T to(float v) {
@@ -75,12 +75,10 @@ __device__ __forceinline__ T to(float v) {
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_vec(uint8_t* p, const float (&x)[N]) {
-  struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec {
-    T t[N];
-  } v;
+  Vec<T, N> v;
 #pragma unroll
   for (int i = 0; i < N; ++i) v.t[i] = to<T>(x[i]);
-  *reinterpret_cast<Vec*>(p) = v;
+  *reinterpret_cast<Vec<T, N>*>(p) = v;
 }
 
 // KT: the cache's type; IN, OUT: of q, k, v and of q_out; VEC: elements of a vector.
@@ -92,32 +90,44 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
   const int mine = threadIdx.x / a.slots, slot = threadIdx.x - mine * a.slots;
   const int hq = a.q_heads, hkv = a.kv.kv_heads, dim = a.kv.head_dim, rows = hq + 2 * hkv, step = a.split * a.at_once;
 
-  // ---- a row's slot: its first row is loaded before the look-ups, which do not depend on it
+  // ---- a row's slot: two vectors, neighbouring threads' vectors side by side.  Pairs of the half layout: a vector of first elements and that of
+  // the second ones; elsewhere vectors slot and slot + half of those that there are.
   const bool pairs = slot < a.rotated;
   const int row0 = part * a.at_once + mine;
-  auto place = [&](bool rotate, int& d0, int& d1) {
-    if (rotate && !a.interleaved) {
-      d0 = slot * VEC;
-      d1 = d0 + a.rot / 2;
-    } else {
-      // (rows of v, and the rest of a row after its pairs, are cut without regard to pairs)
-      d0 = rotate || a.interleaved || !a.rotated ? 2 * VEC * slot : a.rot + 2 * VEC * (slot - a.rotated);
-      d1 = d0 + VEC;
-    }
+  auto place = [&](int start, int s, int& d0, int& d1) {   // of the vectors from element `start` on
+    const int n = (dim - start) / VEC, half = (n + 1) / 2;
+    d0 = s < half ? start + s * VEC : dim;
+    d1 = s + half < n && s < half ? start + (s + half) * VEC : dim;
   };
-  int qd0, qd1;
-  place(pairs, qd0, qd1);
-  const int vd0 = 2 * VEC * slot, vd1 = vd0 + VEC;
-  float x0[VEC], x1[VEC];
-  auto load = [&](int row) {
-    const bool is_v = row >= hq + hkv;
-    const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
-    const uint8_t* src = row < hq ? a.q + ((int64_t)n * a.q_stride_token + row * a.q_stride_head) * (int)sizeof(IN)
-                                  : (is_v ? a.v : a.k) + ((int64_t)n * a.stride_token + (row - hq - (is_v ? hkv : 0)) * a.stride_head) * (int)sizeof(IN);
+  int qd0, qd1, vd0, vd1;
+  place(0, slot, vd0, vd1);
+  if (a.interleaved) {
+    qd0 = vd0;
+    qd1 = vd1;
+    if (VEC == 1) {                                        // (a pair is two vectors)
+      qd0 = 2 * slot;
+      qd1 = qd0 + 1;
+    }
+  } else if (pairs) {
+    qd0 = slot * VEC;
+    qd1 = qd0 + a.rot / 2;
+  } else {
+    place(a.rot, slot - a.rotated, qd0, qd1);
+  }
+  // (several rows' loads on their way together)
+  constexpr int AT_A_TIME = 4;
+  Vec<IN, VEC> in0[AT_A_TIME], in1[AT_A_TIME];
+  auto load = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x0[i] = x1[i] = 0.0f;
-    if (d0 < dim) load_vec<IN, VEC>(src + d0 * (int)sizeof(IN), x0);
-    if (d1 < dim) load_vec<IN, VEC>(src + d1 * (int)sizeof(IN), x1);
+    for (int k = 0; k < AT_A_TIME; ++k) {
+      const int row = first + k * step;
+      const bool is_v = row >= hq + hkv;
+      const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
+      const uint8_t* src = row < hq ? a.q + ((int64_t)n * a.q_stride_token + row * a.q_stride_head) * (int)sizeof(IN)
+                                    : (is_v ? a.v : a.k) + ((int64_t)n * a.stride_token + (row - hq - (is_v ? hkv : 0)) * a.stride_head) * (int)sizeof(IN);
+      if (row < rows && d0 < dim) in0[k] = load_vec<IN, VEC>(src + d0 * (int)sizeof(IN));
+      if (row < rows && d1 < dim) in1[k] = load_vec<IN, VEC>(src + d1 * (int)sizeof(IN));
+    }
   };
   const bool active = mine < a.at_once && row0 < rows;
   if (active) load(row0);
@@ -144,34 +154,46 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
   const bool bad = page < 0 || page >= a.kv.num_pages;
   if (bad && threadIdx.x == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
 
+  // sines and cosines of the slot's pairs: of VEC pairs, or of VEC / 2 in each of the two vectors
   float sn[VEC], cs[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
-    const int pair = slot * VEC + i;
+    int pair = slot * VEC + i;
+    if (VEC > 1 && a.interleaved) pair = i < VEC / 2 ? qd0 / 2 + i : qd1 / 2 + i - VEC / 2;
+    sn[i] = 0.0f;
+    cs[i] = 1.0f;
     if (pairs && 2 * pair < a.rot) {
       const uint64_t turns = (uint64_t)pos * a.step[pair];
       sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);       // 2^-31: half turns
       sn[i] *= a.magnitude;
       cs[i] *= a.magnitude;
-    } else {
-      sn[i] = 0.0f;
-      cs[i] = 1.0f;
     }
   }
   const int64_t in_pool = 2 * (a.layer * a.kv.stride_layer + (bad ? 0 : page) * a.kv.stride_page + (pos & (a.kv.page_size - 1)) * a.kv.stride_row);
-  for (int row = row0;;) {
+  for (int first = row0;;) {
+#pragma unroll
+    for (int k = 0; k < AT_A_TIME; ++k) {
+    const int row = first + k * step;
+    if (row >= rows) break;
     const bool is_v = row >= hq + hkv;
+    float x0[VEC], x1[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      x0[i] = static_cast<float>(in0[k].t[i]);
+      x1[i] = static_cast<float>(in1[k].t[i]);
+    }
     if (pairs && !is_v) {
       if (a.interleaved) {
-        // x0, x1 hold 2 VEC elements one after the other: VEC pairs
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          if (2 * (slot * VEC + i) >= a.rot) continue;     // (the end of the last slot: moves as it is, infinities too)
+          // (elements beyond rot move as they are, infinities too)
           if constexpr (VEC == 1) {
+            if (2 * slot >= a.rot) continue;
             const float p = x0[0], q = x1[0];
             x0[0] = p * cs[0] - q * sn[0];
             x1[0] = q * cs[0] + p * sn[0];
           } else {
+            if ((i < VEC / 2 ? qd0 + 2 * i : qd1 + 2 * i - VEC) >= a.rot) continue;
             float* const e = i < VEC / 2 ? &x0[2 * i] : &x1[2 * i - VEC];
             const float p = e[0], q = e[1];
             e[0] = p * cs[i] - q * sn[i];
@@ -199,16 +221,18 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
       // the row's padding (head_dim is a multiple of 4, rows of 8) is cleared, as by appends
       if (slot == 0 && (dim & 7)) *reinterpret_cast<uint2*>(dst + 2 * dim) = make_uint2(0u, 0u);
     }
-    row += step;
-    if (row >= rows) break;
-    load(row);
+    }
+    first += AT_A_TIME * step;
+    if (first >= rows) break;
+    load(first);
   }
 }
 
 template <typename KT, typename IN, typename OUT>
 cudaError_t launch_vec(const RopeDev& d, int vec, const cudaLaunchConfig_t& cfg) {
+  if constexpr (sizeof(IN) == 2 && sizeof(OUT) == 2)
+    if (vec == 8) return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 8>, d);
   switch (vec) {
-    case 8: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 8>, d);
     case 4: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 4>, d);
     case 2: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 2>, d);
     default: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 1>, d);
@@ -253,14 +277,16 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 8;
   if (!d.interleaved) odd |= d.rot / 2;
   int vec = (int)(odd & -odd);
-  if (vec > 8) vec = 8;
+  // (16 bytes of the wider type: with 32 a warp's access would touch every sector twice; 4 x 2048 tokens, fp32 in, bf16 out: 42 us against XX)
+  const int widest = in_f32 || (out_f32 && x.q_heads) ? 4 : 8;
+  if (vec > widest) vec = widest;
   const uintptr_t at = reinterpret_cast<uintptr_t>(x.k) | reinterpret_cast<uintptr_t>(x.v) | (x.q_heads ? reinterpret_cast<uintptr_t>(x.q) : 0);
   const int size = in_f32 ? 4 : 2;
   while (vec > 1 && at % (size * vec < 16 ? size * vec : 16)) vec /= 2;
-  d.rotated = d.interleaved ? (d.rot + 2 * vec - 1) / (2 * vec) : d.rot / (2 * vec);
-  const int rest = dim - (d.interleaved ? d.rotated * 2 * vec : d.rot), all = (dim + 2 * vec - 1) / (2 * vec);
-  d.slots = d.rotated + (rest > 0 ? (rest + 2 * vec - 1) / (2 * vec) : 0);
-  if (d.slots < all) d.slots = all;
+  auto slots = [&](int elements) { return (elements / vec + 1) / 2; };
+  d.slots = slots(dim);
+  d.rotated = d.interleaved ? d.slots : d.rot / (2 * vec);
+  if (!d.interleaved && d.rotated + slots(dim - d.rot) > d.slots) d.slots = d.rotated + slots(dim - d.rot);
   d.at_once = THREADS / d.slots;
   // CTAs per token: a row per thread while CTAs are few, all of a token's rows in one when there are enough tokens to fill the SMs
   const int64_t rows = x.q_heads + 2 * kv.kv_heads, most = ceil_div(rows, d.at_once), sms = dev_info().sm_count;
