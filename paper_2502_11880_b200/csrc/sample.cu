@@ -26,35 +26,40 @@ namespace {
 
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int BINS = THREADS;                // one per thread
-constexpr int LIST = 256;                    // items that are ranked by counting
+constexpr int LIST = 128;                    // items that are ranked by counting
+constexpr int POOL = 1024;                   // items of a bin that are set aside, so that what follows need not look at the whole row
 constexpr int MOST_CTAS = 8;                 // of a cluster
 constexpr float ONE = 4294967296.0f;         // weight 1
 
 struct Hist {
   uint32_t count[BINS], lo[BINS], hi[BINS];
 };
-struct Item {
-  uint64_t at;                               // place in the order
-  uint32_t w;
-};
-struct Say {                                 // what a CTA tells the others at a step
-  float top;
+struct Logit {
+  float x;
   uint32_t index;
-  uint64_t mass;
-  uint32_t n;
+};
+struct Sums {
+  uint64_t mass[BINS];
+  uint32_t count[BINS];
 };
 struct Share {
-  Hist hist;
-  Item list[2][LIST];                        // of every second step, so that a CTA may go on while another one still reads
-  Say say[2];
+  // written by the others, read after a barrier of the cluster
+  float top[MOST_CTAS][WARPS];
+  uint64_t part_mass[BINS];                  // of a cluster of C CTAs, BINS / C bins are this CTA's to add up: C parts of each
+  uint32_t part_count[BINS];
+  Sums row, level;                           // sums over the cluster: of the first histogram, of a later one
+  uint64_t item_at[MOST_CTAS][LIST];         // items to be ranked: their places in the order, and weights
+  uint32_t item_w[MOST_CTAS][LIST];
+  uint32_t items[MOST_CTAS];
+  uint64_t cta_mass[MOST_CTAS];
   // this CTA's own
-  uint32_t bin_count[BINS];                  // the first histogram, of the whole row
-  uint64_t bin_mass[BINS];
+  Hist hist;
   uint64_t warp_mass[WARPS];
   uint32_t warp_count[WARPS];
-  float warp_top[WARPS];
-  Item all[LIST];
-  uint32_t listed;
+  uint64_t all_at[LIST];
+  uint32_t all_w[LIST];
+  Logit pool[POOL];
+  uint32_t listed, pooled;
   // found by one thread
   int bin;
   uint32_t before_n, bin_n;
@@ -66,21 +71,15 @@ __device__ __forceinline__ uint32_t peer(const void* p, int rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
   return r;
 }
-__device__ __forceinline__ uint32_t peer_u32(const void* p, int rank) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
-  return v;
+__device__ __forceinline__ void tell(const void* p, int rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
 }
-__device__ __forceinline__ uint64_t peer_u64(const void* p, int rank) {
-  uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer(p, rank)) : "memory");
-  return v;
+__device__ __forceinline__ void tell(const void* p, int rank, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer(p, rank)), "l"(v) : "memory");
 }
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
+// A barrier of the cluster in two halves: what was written before `arrive`, the others' memory too, is there after `await`.
+__device__ __forceinline__ void arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void await() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float value(__half v) { return __half2float(v); }
@@ -98,6 +97,12 @@ __device__ __forceinline__ uint64_t place(float x, uint32_t index) {
   return (uint64_t)~up << 32 | index;
 }
 
+// The value of that rank among all, ascending (those that are no numbers lie at both ends).
+__device__ __forceinline__ float value_of_rank(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+__device__ __forceinline__ uint32_t rank_of_value(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
 // Back to the value.
 __device__ __forceinline__ float value_at(uint64_t at) {
   const uint32_t up = ~(uint32_t)(at >> 32);
@@ -180,6 +185,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
   const int64_t r = blockIdx.x / ctas;
+  arrive();                                                   // (the others may write here: this CTA runs; awaited before the first such write)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -232,16 +238,23 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
   s.hist.count[tid] = s.hist.lo[tid] = s.hist.hi[tid] = 0;
 #pragma unroll
   for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) s.warp_top[warp] = top;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < WARPS; ++w) top = fmaxf(top, s.warp_top[w]);
-    s.say[0].top = top;
-  }
-  uint32_t step = 0;                                          // the buffers of this step: [step & 1]
-  cluster_barrier();
-  for (int p = 0; p < ctas; ++p) top = p ? fmaxf(top, __uint_as_float(peer_u32(&s.say[0].top, p))) : __uint_as_float(peer_u32(&s.say[0].top, 0));
-  ++step;
+  bool pending = true;                                        // an arrival that has not been awaited (the same in all CTAs)
+  auto settle = [&] {
+    if (pending) await();
+    pending = false;
+  };
+  auto meet = [&] {
+    settle();
+    arrive();
+    await();
+  };
+  settle();
+  if (lane < ctas) tell(&s.top[rank][warp], lane, __float_as_uint(top));
+  meet();
+  top = -INFINITY;
+  for (int i = lane; i < ctas * WARPS; i += 32) top = fmaxf(top, (&s.top[0][0])[i]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 
   // a warp's stretch of the slice
   const int stretch = (length / 128 + WARPS - 1) / WARPS * 128;
@@ -251,7 +264,6 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       a.tokens[r] = -1;
       if (a.prob) a.prob[r] = 0.0f;
     }
-    cluster_barrier();                                        // (nobody leaves while the others read)
     return;
   }
 
@@ -290,22 +302,31 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
         if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
       });
     }
-    cluster_barrier();
-    uint32_t count = 0;
-    uint64_t mass = 0;
-    // this thread's bin over all CTAs
-    auto gather = [&] {
-      Hist& h = s.hist;
-      count = 0;
-      mass = 0;
-      for (int p = 0; p < ctas; ++p) {
-        count += peer_u32(&h.count[tid], p);
-        mass += (uint64_t)peer_u32(&h.hi[tid], p) << 32 | peer_u32(&h.lo[tid], p);
-      }
-      ++step;
+    // The histogram's bins summed over the cluster, to every CTA's `to`: each CTA adds up its share of the bins, and tells the others.
+    auto gather = [&](Sums& to) {
+      const int share = BINS / ctas, p = tid / share, of = tid - p * share;
+      __syncthreads();
+      tell(&s.part_mass[rank * share + of], p, (uint64_t)s.hist.hi[tid] << 32 | s.hist.lo[tid]);
+      tell(&s.part_count[rank * share + of], p, s.hist.count[tid]);
+      meet();
+      // (every bin of the share by as many threads as there are CTAs, each of which tells one)
+      const int bin = rank * share + of;
+      uint64_t mass = 0;
+      uint32_t count = 0;
+#pragma unroll
+      for (int k = 0; k < MOST_CTAS; ++k)
+        if (k < ctas) {
+          mass += s.part_mass[k * share + of];
+          count += s.part_count[k * share + of];
+        }
+      tell(&to.mass[bin], p, mass);
+      tell(&to.count[bin], p, count);
+      meet();
     };
     // the bin where the inclusive count or sum, on top of what comes before the bins, reaches `limit`
-    auto find = [&](bool counts, uint64_t limit, uint32_t count, uint64_t mass, uint32_t before_n, uint64_t before_mass) {
+    auto find = [&](bool counts, uint64_t limit, const Sums& sums, uint32_t before_n, uint64_t before_mass) {
+      const uint32_t count = sums.count[tid];
+      const uint64_t mass = sums.mass[tid];
       uint32_t n = count;
       uint64_t m = mass;
 #pragma unroll
@@ -341,87 +362,119 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
     };
     // the last item kept: the first in the order with which the count or sum reaches `limit`; false: all together do not
     auto resolve = [&](bool counts, uint64_t limit) -> bool {
-      find(counts, limit, s.bin_count[tid], s.bin_mass[tid], 0, 0);
+      find(counts, limit, s.row, 0, 0);
       const int b0 = s.bin;
       if (b0 < 0) return false;
-      // the range of the order that holds it: at first that of the bin, with something to spare
-      uint64_t lo, hi;
+      // the bin's values: [from, to).  The bin falls as the value rises: of all values, by rank, those whose bin lies beyond b are counted digit by digit, 32
+      // at a time.
+      float from, to;
       {
-        const float margin = 1e-5f * (fabsf(top) + REACH / weigh.c);
-        lo = place(top - (b0 - 0.51f) / PER_T / weigh.c + margin, 0u);
-        hi = place(top - (b0 + 0.51f) / PER_T / weigh.c - margin, 0xffffffffu);
-        if (!(margin < 1e30f)) lo = 0, hi = ~(uint64_t)0;
+        uint32_t beyond[2] = {0, 0};
+        const uint32_t of_top = rank_of_value(top);
+#pragma unroll 1
+        for (int shift = 30; shift >= 0; shift -= 5) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t u = beyond[k] + ((uint32_t)lane << shift) + ((1u << shift) - 1u);     // the last of the lane's block
+            float d;
+            const float t = weigh.distance(value_of_rank(u), d);
+            const bool no = u < of_top && !(t < REACH && bin_of(t) <= b0 - k) && (shift < 30 || lane < 4);
+            beyond[k] += (uint32_t)__popc(__ballot_sync(0xffffffffu, no)) << shift;
+          }
+        }
+        from = value_of_rank(beyond[0]);
+        to = b0 > 0 ? value_of_rank(beyond[1]) : INFINITY;
       }
-      auto in_play = [&](float v, int i, uint64_t& at, float& d, float& t) {
-        t = weigh.distance(v, d);
-        if (!(t < REACH) || bin_of(t) != b0) return false;
-        at = place(v, (uint32_t)(x.first + i));
-        return at >= lo && at <= hi;
+      // the range of the order that holds it: at first the bin's
+      uint64_t lo = place(b0 > 0 ? value_of_rank(rank_of_value(to) - 1) : top, 0u), hi = place(from, 0xffffffffu);
+      const bool pool = s.bin_n <= POOL;
+      if (pool) {
+        if (tid == 0) s.pooled = 0;
+        __syncthreads();
+        x.each(w0, w1, [&](float v, int i) {
+          if (v >= from && v < to) {
+            const uint32_t k = atomicAdd(&s.pooled, 1u);
+            if (k < POOL) s.pool[k] = Logit{v, (uint32_t)(x.first + i)};
+          }
+        });
+        __syncthreads();
+      }
+      // all of the bin's items that lie in the range
+      auto in_play = [&](auto f) {
+        auto look = [&](float v, uint32_t index) {
+          const uint64_t at = place(v, index);
+          if (at < lo || at > hi) return;
+          float d;
+          const float t = weigh.distance(v, d);
+          f(at, fixed(weigh.weight<EXACT>(v, d, t)));
+        };
+        if (pool) {
+          for (uint32_t i = tid; i < min(s.pooled, (uint32_t)POOL); i += THREADS) look(s.pool[i].x, s.pool[i].index);
+        } else {
+          x.each(w0, w1, [&](float v, int i) {
+            if (v >= from && v < to) look(v, (uint32_t)(x.first + i));
+          });
+        }
       };
       // (every level takes 9 of 64 bits)
       for (int level = 0; level < 8 && s.bin >= 0 && s.bin_n > LIST; ++level) {
-        cluster_barrier();                                    // (the others have read the last histogram)
         Hist& h = s.hist;
         h.count[tid] = h.lo[tid] = h.hi[tid] = 0;
         __syncthreads();
         const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 9);        // (hi - lo) >> shift < BINS
-        x.each(w0, w1, [&](float v, int i) {
-          uint64_t at;
-          float d, t;
-          if (!in_play(v, i, at, d, t)) return;
-          const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
+        in_play([&](uint64_t at, uint32_t w) {
           const int b = (int)((at - lo) >> shift);
           atomicAdd(&h.count[b], 1u);
           if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
         });
         const uint32_t before_n = s.before_n;
         const uint64_t before_mass = s.before_mass;
-        cluster_barrier();
-        gather();
-        find(counts, limit, count, mass, before_n, before_mass);
+        gather(s.level);
+        find(counts, limit, s.level, before_n, before_mass);
         lo += (uint64_t)s.bin << shift;
         hi = min(hi, lo + (((uint64_t)1 << shift) - 1));
       }
       // the bin's items, of all CTAs, ranked
       if (tid == 0) s.listed = 0;
       __syncthreads();
-      x.each(w0, w1, [&](float v, int i) {
-        uint64_t at;
-        float d, t;
-        if (in_play(v, i, at, d, t)) {
-          const uint32_t k = atomicAdd(&s.listed, 1u);
-          if (k < LIST) s.list[step & 1][k] = Item{at, fixed(weigh.weight<EXACT>(v, d, t))};
+      settle();                                               // (the others are done with the items before these)
+      in_play([&](uint64_t at, uint32_t w) {
+        const uint32_t k = atomicAdd(&s.listed, 1u);
+        if (k >= LIST) return;
+        for (int p = 0; p < ctas; ++p) {
+          tell(&s.item_at[rank][k], p, at);
+          tell(&s.item_w[rank][k], p, w);
         }
       });
       __syncthreads();
-      if (tid == 0) s.say[step & 1].n = s.listed;
-      cluster_barrier();
+      if (tid < ctas) tell(&s.items[rank], tid, min(s.listed, (uint32_t)LIST));
+      meet();
       uint32_t n = 0;
       for (int p = 0; p < ctas; ++p) {
-        const uint32_t m = peer_u32(&s.say[step & 1].n, p);
+        const uint32_t m = s.items[p];
         if (tid < m && n + tid < LIST) {
-          s.all[n + tid].at = peer_u64(&s.list[step & 1][tid].at, p);
-          s.all[n + tid].w = peer_u32(&s.list[step & 1][tid].w, p);
+          s.all_at[n + tid] = s.item_at[p][tid];
+          s.all_w[n + tid] = s.item_w[p][tid];
         }
         n += m;
       }
       n = min(n, (uint32_t)LIST);
-      ++step;
       __syncthreads();
+      arrive();                                               // (awaited ahead of the next items, or the next barrier)
+      pending = true;
       if (tid < n) {
-        const Item me = s.all[tid];
+        const uint64_t me = s.all_at[tid];
+        const uint32_t my_w = s.all_w[tid];
         uint32_t k = s.before_n;
         uint64_t m = s.before_mass;
-        for (uint32_t j = 0; j < n; ++j) {
-          const Item o = s.all[j];
-          if (o.at <= me.at) {
+        for (uint32_t j = 0; j < n; ++j)
+          if (s.all_at[j] <= me) {
             ++k;
-            m += o.w;
+            m += s.all_w[j];
           }
-        }
-        const uint64_t incl = counts ? k : m, excl = counts ? k - 1 : m - me.w;
+        const uint64_t incl = counts ? k : m, excl = counts ? k - 1 : m - my_w;
         if (excl < limit && incl >= limit) {
-          s.found_at = me.at;
+          s.found_at = me;
           s.found_mass = m;
         }
       }
@@ -429,12 +482,10 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       return true;
     };
 
-    gather();
-    s.bin_count[tid] = count;
-    s.bin_mass[tid] = mass;
+    gather(s.row);
     uint64_t all = 0;
     {
-      const uint64_t m = warp_sum_u64(mass);
+      const uint64_t m = warp_sum_u64(s.row.mass[tid]);
       __syncthreads();
       if (lane == 0) s.warp_mass[warp] = m;
       __syncthreads();
@@ -478,15 +529,15 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
     if (w < warp) before += s.warp_mass[w];
     of_cta += s.warp_mass[w];
   }
-  if (tid == 0) s.say[step & 1].mass = of_cta;
-  cluster_barrier();
+  settle();
+  if (tid < ctas) tell(&s.cta_mass[rank], tid, of_cta);
+  meet();                                                     // (the last one: nothing of another CTA is written or read after it)
   uint64_t total = 0;
   for (int p = 0; p < ctas; ++p) {
-    const uint64_t m = peer_u64(&s.say[step & 1].mass, p);
+    const uint64_t m = s.cta_mass[p];
     if (p < rank) before += m;
     total += m;
   }
-  cluster_barrier();                                          // (nobody leaves while the others read)
 
   // ---- the item at which the sum exceeds u * total (greedy rows: the first of the largest)
   uint64_t target = greedy ? 0 : __umul64hi(total, __float2ull_rz(u * 18446744073709551616.0f));
