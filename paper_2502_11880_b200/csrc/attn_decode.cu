@@ -312,7 +312,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         tile_of(r, t, first, lo, hi);
         const int tok = first + box * box_rows;
         if (t >= t_end || !mine || tok >= hi || tok + box_rows <= lo) return -2;
-        return __ldg(a.table + (int64_t)r.seq * a.table_width + (tok >> a.page_shift));
+        return max(__ldg(a.table + (int64_t)r.seq * a.table_width + (tok >> a.page_shift)), -1);
       };
       // (four tiles' pages are looked up while the four before are copied: one at a time the look-up's latency, 0.7 us, was
       // every tile's time)

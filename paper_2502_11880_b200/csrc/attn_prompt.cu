@@ -359,7 +359,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           const int tok = block_start(x, j) + box * box_rows;
           y = tok & ((1 << a.page_shift) - 1);
           if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
-          return __ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift));
+          return max(__ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift)), -1);
         };
         int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
         const int n_stop = (int)min((int64_t)x.nb, (int64_t)(a.give_up - kb));

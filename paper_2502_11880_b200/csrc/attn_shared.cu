@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     int first, lo, hi;
     tile_of(f.r, f.t, first, lo, hi);
     const int tok = first + (lane & (TILE - 1));
-    return f.left > 0 && tok >= lo && tok < hi ? __ldg(a.table + (int64_t)f.n * a.table_width + (tok >> a.page_shift)) : -2;
+    return f.left > 0 && tok >= lo && tok < hi ? max(__ldg(a.table + (int64_t)f.n * a.table_width + (tok >> a.page_shift)), -1) : -2;
   };
   int page = look_up();                       // (a tile ahead of the copies)
   uint32_t filled = 0;
