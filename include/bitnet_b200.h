@@ -545,8 +545,8 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* cache, int64_t layer, const void
  *   h = residual + x (without residual: x);  r = 1 / sqrt(mean_k(h^2) + eps);  y = (h r) weight;  q, act_scale, act_sum as
  *   bitnet_quant_act(y) gives them.
  *   x[T][K], residual[T][K], residual_out[T][K], y[T][K]: each of its own element type; strides between rows in elements.
- *   residual, weight[K] (NULL: 1), y and act_sum are nullable; residual_out goes with residual, has its type, and may be residual or x itself (then
- *   with its stride).  No other buffers may overlap.
+ *   residual, weight[K] (NULL: 1), y and act_sum are nullable; residual_out goes with residual, has its type, and may be residual itself, or x where
+ *   that has the same type (then with its stride).  No other buffers, and no two rows of residual_out, may overlap.
  * The sum is binary32 rounded to residual's type, and that value is what is normed.  The squares are summed in 64 bits and r is rounded once; from
  * there every step is one binary32 operation: q does not depend on T, on strides or on which kernel ran.  eps >= 0.  q and y are contiguous.
  * Rows of up to 32768 elements (a multiple of 4, at strides of 4 elements, x and the others at 16-byte (16-bit types: 8-byte) addresses)
@@ -589,8 +589,8 @@ int bitnet_rope_init(bitnet_rope_t* rope);
  * q_start as for bitnet_kv_append; positions are those of the tokens.
  *   q, k, v: of `in_type` (fp32 or the cache's type), head_dim contiguous, any strides (multiples of 8 elements, and 16-byte addresses, are fastest); k and v
  *   have one pair of strides.  q_heads = 0: q and q_out are not looked at.  q_out may be q itself where q is contiguous and of q_out's type.
- * rot_dim may not exceed head_dim.  A token before the start (an idle row) is passed over, its row of q_out left as it was; one without a page is
- * reported, its row of q_out is written.
+ * rot_dim may not exceed head_dim.  A token before the start (an idle row), or behind q_start[seqs] (a padded batch), is passed over, its row of q_out left as
+ * it was; one without a page is reported, its row of q_out is written.
  */
 int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const bitnet_rope_t* rope, const void* q, int64_t q_heads,
                           int64_t q_stride_token, int64_t q_stride_head, const void* k, const void* v, int in_type, int64_t stride_token,

@@ -417,7 +417,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
               int least = 0x7fffffff;
               for (int i = lane; i < n; i += 32) least = min(least, __ldg(a.kv_len + q0 + i));
               least = __reduce_min_sync(0xffffffffu, least);
-              if (lane == k) t.lo = max(0, min(least - a.window, a.max_len));
+              if (lane == k) t.lo = (int)max((int64_t)0, min((int64_t)least - a.window, (int64_t)a.max_len));
             }
           }
           const int end = (t.prefix + KB - 1) / KB;
@@ -513,7 +513,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           least = __reduce_min_sync(0xffffffffu, least);
           most = __reduce_max_sync(0xffffffffu, most);
           t.p_last = min(most, t.prefix) - 1;
-          t.lo = a.window > 0 ? max(0, min(least - a.window, a.max_len)) : 0;
+          t.lo = a.window > 0 ? (int)max((int64_t)0, min((int64_t)least - a.window, (int64_t)a.max_len)) : 0;
           if (lane == 0) {
             s.item[it & 1] = t;
             kv_mbar_arrive(&s.item_full[it & 1]);
@@ -813,7 +813,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const bool valid = row < a.tile_tokens * a.per_block && hd < x.heads && tok < x.n_new && x.q0 >= 0 && (int64_t)x.q0 + tok < a.tokens;
       if (u == 1 && !x.two) continue;
       int64_t pos = valid ? (int64_t)x.pos0 + tok : -1;
-      if constexpr (SHARED) pos = valid ? (int64_t)__ldg(a.kv_len + x.q0 + tok) - 1 : -1;
+      if constexpr (SHARED) pos = valid ? max((int64_t)__ldg(a.kv_len + x.q0 + tok), (int64_t)0) - 1 : -1;
       int p = (int)min(pos, (int64_t)a.max_len - 1);          // last token that the row may see; < 0: sees nothing
       if constexpr (SHARED) p = min(p, x.prefix - 1);
       // first token of its window

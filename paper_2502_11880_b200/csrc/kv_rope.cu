@@ -40,7 +40,7 @@ struct RopeDev {
   uint64_t step[64];         // turns per position, in 2^-64
 };
 
-// N elements of 4 or 2 bytes as they lie in memory, aligned to N elements (16 bytes at most).
+// N elements of 4 or 2 bytes as they lie in memory, aligned to N elements (16 bytes at most).  (q may be overwritten by this call: no read-only path.)
 template <typename T, int N>
 struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec {
   T t[N];
@@ -57,13 +57,13 @@ __device__ __forceinline__ Vec<T, N> load_vec(const uint8_t* p) {
   } x;
   if constexpr (BYTES >= 16) {
 #pragma unroll
-    for (int i = 0; i < BYTES / 16; ++i) x.a[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < BYTES / 16; ++i) x.a[i] = __ldca(reinterpret_cast<const uint4*>(p) + i);
   } else if constexpr (BYTES == 8) {
-    x.b = __ldg(reinterpret_cast<const uint2*>(p));
+    x.b = __ldca(reinterpret_cast<const uint2*>(p));
   } else if constexpr (BYTES == 4) {
-    x.c = __ldg(reinterpret_cast<const unsigned int*>(p));
+    x.c = __ldca(reinterpret_cast<const unsigned int*>(p));
   } else {
-    x.d = __ldg(reinterpret_cast<const unsigned short*>(p));
+    x.d = __ldca(reinterpret_cast<const unsigned short*>(p));
   }
   return x.v;
 }
@@ -144,7 +144,9 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
       seq += in;
       if (in < 32) break;
     }
-    pos = (int64_t)__ldg(a.kv_len + seq) - __ldg(a.q_start + seq + 1) + n;
+    const int end = __ldg(a.q_start + seq + 1);
+    // (a token behind the last sequence, or ahead of the first, is nobody's)
+    pos = n < end && n >= __ldg(a.q_start + seq) ? (int64_t)__ldg(a.kv_len + seq) - end + n : -1;
   } else {
     pos = (int64_t)__ldg(a.kv_len + seq) - 1;
   }

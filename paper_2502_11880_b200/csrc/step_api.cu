@@ -34,6 +34,9 @@ int bitnet_add_rmsnorm_quant(const void* x, int x_type, int64_t stride_x, const 
   if (!aligned16(q) || (y && !aligned16(y))) return BITNET_ERR_INVALID_ARG;
   if (residual && (!of_type(residual, residual_type) || !of_type(residual_out, residual_type))) return BITNET_ERR_INVALID_ARG;
   if (weight && !of_type(weight, weight_type)) return BITNET_ERR_INVALID_ARG;
+  // rows that lie on one another would be written by several CTAs, and x in another type be read after it was overwritten
+  if (residual && T > 1 && (stride_residual_out < 0 ? -stride_residual_out : stride_residual_out) < K) return BITNET_ERR_INVALID_ARG;
+  if (residual && residual_out == x && residual_type != x_type) return BITNET_ERR_INVALID_ARG;
   NormArgs a;
   a.x = x;
   a.residual = residual;

@@ -245,6 +245,19 @@ def test_length_beyond_the_table():
     assert torch.equal(s.run(q), want)
 
 
+def test_lengths_below_zero():
+    """Idle rows, however far below: they see nothing, and the others of their group what they see without them."""
+    s = Groups([(200, [210, 260, 333])], 2, 64, 16, BF, seed=17)
+    q = s.queries(8)
+    for window in (0, 150):
+        want = s.run(q, window=window)
+        for n in (0, -1, -2 ** 31):
+            s.len[1] = n
+            out = s.run(q, window=window)
+            assert bool((out[1] == 0).all()) and all(torch.allclose(out[i].float(), want[i].float(), rtol=2 ** -7, atol=2 ** -7) for i in (0, 2))
+        s.len[1] = 260
+
+
 def test_graph():
     s = Groups([(200, [210, 260, 333]), (0, [40])], 4, 128, 16, BF, seed=13)
     q = s.queries(16)

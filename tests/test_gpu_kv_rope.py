@@ -236,6 +236,26 @@ def test_idle_rows_and_bad_pages():
     assert int(status) == 7
 
 
+def test_tokens_behind_the_last_sequence():
+    """A padded batch: rows that belong to no sequence are left as they were, and write nothing."""
+    c = Case([(5, 3), (40, 2), (7, 4)], 4, 2, 64, 16, BF, F32)
+    good = c.run(bn.Rope(64), F32).clone()
+    k, v = c.k.clone(), c.v.clone()
+    c.k.fill_(7.0), c.v.fill_(7.0)
+    pad = lambda t: torch.cat([t, torch.full((6, *t.shape[1:]), 3.0, device="cuda")])
+    out, status = torch.full((15, 4, 64), 9.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bn.bitnet_kv_append_rope(c.cache, 1, bn.Rope(64), pad(c.q), pad(c.k_new), pad(c.v_new), c.table, c.len, c.start, q_out=out, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(out[:9], good) and bool((out[9:] == 9.0).all())
+    assert torch.equal(c.k, k) and torch.equal(c.v, v)
+    c.k.fill_(7.0)
+    start = torch.tensor([2, 3, 5, 9], dtype=torch.int32, device="cuda")       # two ahead of the first
+    out.fill_(9.0)
+    bn.bitnet_kv_append_rope(c.cache, 1, bn.Rope(64), c.q, c.k_new, c.v_new, c.table, c.len, start, q_out=out[:9], dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and bool((out[:2] == 9.0).all()) and torch.equal(out[2:9], good[2:9])
+
+
 def test_graph():
     c = Case([(5, 1), (40, 1)], 4, 2, 64, 16, BF, F32)
     rope, out = bn.Rope(64), torch.empty(2, 4, 64, device="cuda")

@@ -21,7 +21,7 @@ def norm(L, x=FAKE, xt=2, sx=64, r=FAKE, rt=2, sr=64, ro=FAKE, so=64, w=FAKE, wt
     return L.bitnet_add_rmsnorm_quant(x, xt, sx, r, rt, sr, ro, so, w, wt, eps, T, K, y, yt, q, sc, sm, NULL)
 
 
-@pytest.mark.parametrize("bad", [dict(x=NULL), dict(x=ODD), dict(xt=3), dict(xt=-1), dict(rt=7), dict(wt=4), dict(yt=3), dict(ro=NULL), dict(r=NULL), dict(r=ODD), dict(ro=ODD),
+@pytest.mark.parametrize("bad", [dict(x=NULL), dict(x=ODD), dict(xt=3), dict(xt=-1), dict(rt=7), dict(wt=4), dict(yt=3), dict(ro=NULL), dict(r=NULL), dict(r=ODD), dict(ro=ODD), dict(T=2, so=0), dict(T=2, so=63), dict(T=2, so=-63), dict(xt=0),
                                  dict(w=ODD), dict(eps=-1.0), dict(eps=INF), dict(eps=NAN), dict(T=-1), dict(K=0), dict(T=1 << 31), dict(K=1 << 31), dict(q=NULL),
                                  dict(q=C.c_void_p(4104)), dict(y=C.c_void_p(4104)), dict(sc=NULL), dict(sc=C.c_void_p(4098)), dict(sm=C.c_void_p(4098))])
 def test_norm_is_checked(L, bad):
