@@ -549,7 +549,7 @@ int bitnet_attn_prompt(const bitnet_kv_cache_t* cache, int64_t layer, const void
  *   that has the same type (then with its stride).  No other buffers, and no two rows of residual_out, may overlap.
  * The sum is binary32 rounded to residual's type, and that value is what is normed.  The squares are summed in 64 bits and r is rounded once; from
  * there every step is one binary32 operation: q does not depend on T, on strides or on which kernel ran.  eps >= 0.  q and y are contiguous.
- * Rows of up to 32768 elements (a multiple of 4, at strides of 4 elements, x and the others at 16-byte (16-bit types: 8-byte) addresses)
+ * Rows of up to 131072 elements (a multiple of 4, at strides of 4 elements, x and the others at 16-byte (16-bit types: 8-byte) addresses)
  * are read once; any other row is walked three times.
  */
 int bitnet_add_rmsnorm_quant(const void* x, int x_type, int64_t stride_x, const void* residual, int residual_type, int64_t stride_residual,

@@ -16,6 +16,8 @@
 namespace bitnet {
 namespace {
 
+constexpr int64_t MOST_K = 8 * 16384;     // a cluster of 8 CTAs of 1024 threads with four pieces each
+
 struct NormDev {
   NormArgs a;
   double inv_k;
@@ -60,6 +62,10 @@ struct Red {
   double sum[32];
   float top[32];
   int codes[32];
+  // of a cluster's CTAs
+  double cta_sum[8];
+  float cta_top[8];
+  int cta_codes[8];
 };
 __device__ __forceinline__ double block_sum(double v, double* red) {
   const int lane = threadIdx.x & 31;
@@ -83,17 +89,34 @@ __device__ __forceinline__ float block_max(float v, float* red) {
   for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-__device__ __forceinline__ void store_sum(int v, int* red, int32_t* to) {
+// In thread 0.
+__device__ __forceinline__ int sum_of_codes(int v, int* red) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int total = 0;
+  int total = 0;
+  if (threadIdx.x == 0)
     for (int w = 0; w < (int)(blockDim.x >> 5); ++w) total += red[w];
-    *to = total;
-  }
+  return total;
 }
+// Into the shared memory of CTA `rank` of the cluster, at the place that p has here.
+__device__ __forceinline__ uint32_t peer(const void* p, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void tell(const double* p, int rank, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer(p, rank)), "d"(v) : "memory");
+}
+__device__ __forceinline__ void tell(const float* p, int rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer(p, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void tell(const int* p, int rank, int v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void await() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // 1 / sqrt(v), rounded once to binary32: two Newton steps in 64 bits from the 32-bit estimate, where that has a range to stand on.
 __device__ __forceinline__ float inverse_root(double v) {
   if (!(v > 1e-30 && v < 1e30)) return (float)(1.0 / sqrt(v));
@@ -135,12 +158,22 @@ __device__ __forceinline__ float4 widen(const Raw<TYPE>& r) {
 }
 
 // VPT: pieces of 4 elements per thread; XT, RT: types of x and of the residual (or NONE).  A CTA takes every gridDim.x-th row, and
-// has the next one's loads on their way while it reduces and writes the present one.
-template <int VPT, int XT, int RT>
+// has the next one's loads on their way while it reduces and writes the present one.  WIDE: the CTAs of a cluster share a row; their sums and
+// maxima meet in every CTA's shared memory (a barrier of the cluster lies between any two uses of a place there).
+template <int VPT, int XT, int RT, bool WIDE>
 __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant__ NormDev d) {
   const NormArgs& a = d.a;
   __shared__ Red red;
-  const int tid = threadIdx.x, nt = blockDim.x, n4 = (int)(a.K / 4);
+  int ctas = 1, rank = 0;
+  if constexpr (WIDE) {
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    arrive();                                    // (the others may write here: awaited before the first such write)
+  }
+  // this CTA's pieces of a row: [from, n4)
+  const int tid = threadIdx.x, nt = blockDim.x, all4 = (int)(a.K / 4), share = (all4 + ctas - 1) / ctas;
+  const int from = min(all4, rank * share), n4 = min(all4, from + share);
+  const int64_t rows_at_once = gridDim.x / ctas;
   if (tid == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   Raw<XT> x[VPT];
@@ -148,38 +181,31 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
   auto fetch = [&](int64_t t) {
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-      const int i = tid + k * nt;
+      const int i = from + tid + k * nt;
       if (i < n4) x[k] = load_raw<XT>(a.x, t * a.stride_x + 4 * (int64_t)i);
     }
     if constexpr (RT != NONE) {
 #pragma unroll
       for (int k = 0; k < VPT; ++k) {
-        const int i = tid + k * nt;
+        const int i = from + tid + k * nt;
         if (i < n4) e[k] = load_raw<RT>(a.residual, t * a.stride_residual + 4 * (int64_t)i);
       }
     }
   };
-  constexpr bool AHEAD = VPT <= 4;               // (eight pieces and the next eight would not fit the registers)
-  int64_t t = blockIdx.x;
-  if (AHEAD) fetch(t);
+  int64_t t = blockIdx.x / ctas;
+  bool met = !WIDE;
+  fetch(t);
   for (;;) {
     float4 h[VPT];
     double sum = 0.0;
-    if (!AHEAD) {
-#pragma unroll
-      for (int k = 0; k < VPT; ++k) {
-        const int i = tid + k * nt;
-        if (i < n4) h[k] = widen(load_raw<XT>(a.x, t * a.stride_x + 4 * (int64_t)i));
-      }
-    }
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-      const int i = tid + k * nt;
-      if (AHEAD || i >= n4) h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int i = from + tid + k * nt;
+      h[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i >= n4) continue;
-      if (AHEAD) h[k] = widen(x[k]);
+      h[k] = widen(x[k]);
       if constexpr (RT != NONE) {
-        const float4 r = widen(AHEAD ? e[k] : load_raw<RT>(a.residual, t * a.stride_residual + 4 * (int64_t)i));
+        const float4 r = widen(e[k]);
         h[k].x = rounded(h[k].x + r.x, RT);
         h[k].y = rounded(h[k].y + r.y, RT);
         h[k].z = rounded(h[k].z + r.z, RT);
@@ -191,40 +217,67 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
       sum = fma((double)h[k].z, (double)h[k].z, sum);
       sum = fma((double)h[k].w, (double)h[k].w, sum);
     }
-    const int64_t next = t + gridDim.x;
-    if (AHEAD && next < a.T) fetch(next);
+    const int64_t next = t + rows_at_once;
+    if (next < a.T) fetch(next);
     float4 w[VPT <= 2 ? VPT : 1];                // (few pieces: the weights come with the row, ahead of the reductions)
     if constexpr (VPT <= 2) {
 #pragma unroll
       for (int k = 0; k < VPT; ++k) {
-        const int i = tid + k * nt;
+        const int i = from + tid + k * nt;
         w[k] = a.weight && i < n4 ? load4(a.weight, 4 * (int64_t)i, a.weight_type) : make_float4(1.f, 1.f, 1.f, 1.f);
       }
     }
-    const float r = inverse_root(block_sum(sum, red.sum) * d.inv_k + a.eps);
+    sum = block_sum(sum, red.sum);
+    if constexpr (WIDE) {
+      if (!met) await();
+      met = true;
+      if (tid < ctas) tell(&red.cta_sum[rank], tid, sum);
+      arrive();
+      await();
+      sum = 0.0;
+      for (int p = 0; p < ctas; ++p) sum += red.cta_sum[p];
+    }
+    const float r = inverse_root(sum * d.inv_k + a.eps);
     float top = 0.0f;
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-      const int i = tid + k * nt;
+      const int i = from + tid + k * nt;
       float4 v = make_float4(1.f, 1.f, 1.f, 1.f);
       if constexpr (VPT <= 2) v = w[k];
       else if (a.weight && i < n4) v = load4(a.weight, 4 * (int64_t)i, a.weight_type);
       h[k] = make_float4(scaled(h[k].x, r, v.x), scaled(h[k].y, r, v.y), scaled(h[k].z, r, v.z), scaled(h[k].w, r, v.w));
       if (i < n4) top = fmaxf(top, absmax4(h[k]));
     }
-    const float amax = fmaxf(block_max(top, red.top), 1e-5f), s = __fdiv_rn(127.0f, amax);
+    top = block_max(top, red.top);
+    if constexpr (WIDE) {
+      if (tid < ctas) tell(&red.cta_top[rank], tid, top);
+      arrive();
+      await();
+      for (int p = 0; p < ctas; ++p) top = fmaxf(top, red.cta_top[p]);
+    }
+    const float amax = fmaxf(top, 1e-5f), s = __fdiv_rn(127.0f, amax);
     int codes = 0;
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-      const int i = tid + k * nt;
+      const int i = from + tid + k * nt;
       if (i >= n4) continue;
       const int c = quant4_packed(h[k], s);
       codes = __dp4a(c, 0x01010101, codes);
       reinterpret_cast<int*>(a.q + t * a.K)[i] = c;
       if (a.y) store4(a.y, t * a.K + 4 * (int64_t)i, a.y_type, h[k]);
     }
-    if (tid == 0) a.act_scale[t] = __fdiv_rn(amax, 127.0f);
-    if (a.act_sum) store_sum(codes, red.codes, a.act_sum + t);
+    if (tid == 0 && rank == 0) a.act_scale[t] = __fdiv_rn(amax, 127.0f);
+    if (a.act_sum) {
+      codes = sum_of_codes(codes, red.codes);
+      if constexpr (WIDE) {
+        if (tid == 0) tell(&red.cta_codes[rank], 0, codes);
+        arrive();
+        await();
+        codes = 0;
+        for (int p = 0; p < ctas; ++p) codes += red.cta_codes[p];
+      }
+      if (tid == 0 && rank == 0) a.act_sum[t] = codes;
+    }
     if (next >= a.T) break;
     t = next;
   }
@@ -264,7 +317,10 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_any_kernel(const __grid_cons
     if (a.y) store1(a.y, t * a.K + i, a.y_type, y);
   }
   if (tid == 0) a.act_scale[t] = __fdiv_rn(amax, 127.0f);
-  if (a.act_sum) store_sum(codes, red.codes, a.act_sum + t);
+  if (a.act_sum) {
+    codes = sum_of_codes(codes, red.codes);
+    if (tid == 0) a.act_sum[t] = codes;
+  }
 }
 
 bool pieces_of_4(const void* p, int64_t stride, int type) {
@@ -275,21 +331,21 @@ int threads_for(int64_t pieces) {               // whole warps
   return (int)(n < 64 ? 64 : n > 1024 ? 1024 : n);
 }
 
-template <int VPT, int XT>
+template <int VPT, int XT, bool WIDE>
 cudaError_t launch_residual(const NormDev& d, const cudaLaunchConfig_t& cfg) {
-  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, NONE>, d);
+  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, NONE, WIDE>, d);
   switch (d.a.residual_type) {
-    case BITNET_KV_F32: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F32>, d);
-    case BITNET_KV_BF16: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_BF16>, d);
-    default: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F16>, d);
+    case BITNET_KV_F32: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F32, WIDE>, d);
+    case BITNET_KV_BF16: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_BF16, WIDE>, d);
+    default: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F16, WIDE>, d);
   }
 }
-template <int VPT>
+template <int VPT, bool WIDE>
 cudaError_t launch_x(const NormDev& d, const cudaLaunchConfig_t& cfg) {
   switch (d.a.x_type) {
-    case BITNET_KV_F32: return launch_residual<VPT, BITNET_KV_F32>(d, cfg);
-    case BITNET_KV_BF16: return launch_residual<VPT, BITNET_KV_BF16>(d, cfg);
-    default: return launch_residual<VPT, BITNET_KV_F16>(d, cfg);
+    case BITNET_KV_F32: return launch_residual<VPT, BITNET_KV_F32, WIDE>(d, cfg);
+    case BITNET_KV_BF16: return launch_residual<VPT, BITNET_KV_BF16, WIDE>(d, cfg);
+    default: return launch_residual<VPT, BITNET_KV_F16, WIDE>(d, cfg);
   }
 }
 
@@ -299,31 +355,46 @@ int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
   NormDev d;
   d.a = a;
   d.inv_k = 1.0 / (double)a.K;
-  const bool vec = a.K % 4 == 0 && a.K <= 32768 && pieces_of_4(a.x, a.stride_x, a.x_type) && pieces_of_4(a.residual, a.stride_residual, a.residual_type) &&
+  const bool vec = a.K % 4 == 0 && a.K <= MOST_K && pieces_of_4(a.x, a.stride_x, a.x_type) && pieces_of_4(a.residual, a.stride_residual, a.residual_type) &&
                    pieces_of_4(a.residual_out, a.stride_residual_out, a.residual_type) && pieces_of_4(a.weight, 0, a.weight_type) &&
                    pieces_of_4(a.y, 0, a.y_type) && pieces_of_4(a.q, 0, BITNET_KV_BF16);
-  const int64_t n4 = ceil_div(a.K, 4);
-  // pieces per thread: as many threads as a row has pieces where rows are few (latency), four pieces where they fill the SMs
-  int vpt = a.T > 2 * (int64_t)dev_info().sm_count ? 4 : 1;
-  while (vpt < 8 && ceil_div(n4, vpt) > 1024) vpt *= 2;
+  const int64_t sms = dev_info().sm_count;
+  // A cluster of CTAs for a row that four pieces of 1024 threads do not hold, and for long rows that are few (16 x 28672: 7.0 us by one CTA with eight pieces a
+  // thread, 4.5 by four).
+  int ctas = 1;
+  while (vec && ctas < 8 && (a.K > 16384 * (int64_t)ctas || (a.K >= 16384 && a.T * ctas * 4 <= sms && ctas < 4))) ctas *= 2;
+  const int64_t n4 = ceil_div(ceil_div(a.K, 4), ctas);
+  // pieces per thread: as many threads as there are pieces where rows are few (latency), four pieces where they fill the SMs
+  int vpt = a.T * ctas > 2 * sms ? 4 : 1;
+  while (vpt < 4 && ceil_div(n4, vpt) > 1024) vpt *= 2;
+  if (ctas > 1 && vpt < 2) vpt = 2;
+  const int threads = threads_for(vec ? ceil_div(n4, vpt) : n4);
+  const int64_t resident = sms * (1024 / threads) / ctas;          // rows that CTAs of 64 registers a thread hold at a time
   cudaLaunchConfig_t cfg = {};
-  const int threads = threads_for(vec ? ceil_div(n4, vpt) : ceil_div(a.K, 4));
-  const int64_t resident = (int64_t)dev_info().sm_count * (1024 / threads);          // CTAs of 64 registers a thread
-  cfg.gridDim = dim3((unsigned)(vec && a.T > resident ? resident : a.T));
+  cfg.gridDim = dim3((unsigned)((vec && a.T > resident ? resident : a.T) * ctas));
   cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
+  int attrs = 0;
+  if (ctas > 1) {
+    attr[attrs].id = cudaLaunchAttributeClusterDimension;
+    attr[attrs].val.clusterDim.x = ctas;
+    attr[attrs].val.clusterDim.y = 1;
+    attr[attrs++].val.clusterDim.z = 1;
+  }
+  if (early_start_enabled(st)) {
+    attr[attrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[attrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = early_start_enabled(st) ? 1 : 0;
-  if (log_enabled()) log_launch("add_rmsnorm T=%lld K=%lld vec=%d vpt=%d", (long long)a.T, (long long)a.K, (int)vec, vpt);
+  cfg.numAttrs = attrs;
+  if (log_enabled()) log_launch("add_rmsnorm T=%lld K=%lld vec=%d vpt=%d ctas=%d", (long long)a.T, (long long)a.K, (int)vec, vpt, ctas);
   cudaError_t e;
   if (!vec) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_any_kernel, d);
-  else if (vpt == 1) e = launch_x<1>(d, cfg);
-  else if (vpt == 2) e = launch_x<2>(d, cfg);
-  else if (vpt == 4) e = launch_x<4>(d, cfg);
-  else e = launch_x<8>(d, cfg);
+  else if (ctas > 1) e = vpt == 2 ? launch_x<2, true>(d, cfg) : launch_x<4, true>(d, cfg);
+  else if (vpt == 1) e = launch_x<1, false>(d, cfg);
+  else if (vpt == 2) e = launch_x<2, false>(d, cfg);
+  else e = launch_x<4, false>(d, cfg);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
 

@@ -48,7 +48,7 @@ def check(x, residual=None, weight=None, eps=1e-5, y_type=F32, residual_out=None
 
 
 @pytest.mark.parametrize("T,K", [(1, 1), (2, 3), (1, 4), (5, 7), (3, 64), (2, 100), (1, 1536), (7, 4096), (2, 4098), (300, 3200), (400, 1028), (3, 8192),
-                                 (1, 16384), (2, 16388), (1, 28672), (2, 32768), (1, 32772), (1, 40001)])
+                                 (1, 16384), (2, 16388), (1, 28672), (2, 32768), (1, 32772), (1, 40001), (2, 40000), (300, 20000), (40, 16384), (5, 70000), (1, 131072), (1, 131076)])
 def test_sizes(T, K):
     check(rows((T, K), F32, K), rows((T, K), F32, K + 1, 3), rows((K,), F32, K + 2))
 
@@ -57,7 +57,7 @@ def test_sizes(T, K):
 @pytest.mark.parametrize("residual", [None, F32, BF, HF])
 @pytest.mark.parametrize("weight,y", [(None, F32), (F32, BF), (BF, HF), (HF, F32)])
 def test_types(x, residual, weight, y):
-    for T, K in ((5, 520), (320, 260), (2, 33)):
+    for T, K in ((5, 520), (320, 260), (2, 33), (3, 16400)):
         check(rows((T, K), x, 1, 2), None if residual is None else rows((T, K), residual, 2), None if weight is None else rows((K,), weight, 3), y_type=y)
 
 
