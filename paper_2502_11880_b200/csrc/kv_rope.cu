@@ -279,7 +279,7 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 8;
   if (!d.interleaved) odd |= d.rot / 2;
   int vec = (int)(odd & -odd);
-  // (16 bytes of the wider type: with 32 a warp's access would touch every sector twice; 4 x 2048 tokens, fp32 in, bf16 out: 42 us against XX)
+  // (16 bytes of the wider type: with 32 a warp's access would touch every sector twice; 4 x 2048 tokens, fp32 in, bf16 out: 42 us against 49)
   const int widest = in_f32 || (out_f32 && x.q_heads) ? 4 : 8;
   if (vec > widest) vec = widest;
   const uintptr_t at = reinterpret_cast<uintptr_t>(x.k) | reinterpret_cast<uintptr_t>(x.v) | (x.q_heads ? reinterpret_cast<uintptr_t>(x.q) : 0);

@@ -365,10 +365,10 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       find(counts, limit, s.row, 0, 0);
       const int b0 = s.bin;
       if (b0 < 0) return false;
-      // the bin's values: [from, to).  The bin falls as the value rises: of all values, by rank, those whose bin lies beyond b are counted digit by digit, 32
-      // at a time.
-      float from, to;
-      {
+      // the range of the order that holds it: the bin's, and where that is to be divided its values, [from, to).  The bin falls as the value rises: of all
+      // values, by rank, those whose bin lies beyond b are counted digit by digit, 32 at a time.
+      uint64_t lo = 0, hi = ~(uint64_t)0;
+      if (s.bin_n > LIST) {
         uint32_t beyond[2] = {0, 0};
         const uint32_t of_top = rank_of_value(top);
 #pragma unroll 1
@@ -382,17 +382,21 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
             beyond[k] += (uint32_t)__popc(__ballot_sync(0xffffffffu, no)) << shift;
           }
         }
-        from = value_of_rank(beyond[0]);
-        to = b0 > 0 ? value_of_rank(beyond[1]) : INFINITY;
+        lo = place(b0 > 0 ? value_of_rank(beyond[1] - 1) : top, 0u);
+        hi = place(value_of_rank(beyond[0]), 0xffffffffu);
       }
-      // the range of the order that holds it: at first the bin's
-      uint64_t lo = place(b0 > 0 ? value_of_rank(rank_of_value(to) - 1) : top, 0u), hi = place(from, 0xffffffffu);
+      auto in_bin = [&](float v) {
+        float d;
+        const float t = weigh.distance(v, d);
+        return t < REACH && bin_of(t) == b0;
+      };
+      // its items set aside, where there are not too many
       const bool pool = s.bin_n <= POOL;
       if (pool) {
         if (tid == 0) s.pooled = 0;
         __syncthreads();
         x.each(w0, w1, [&](float v, int i) {
-          if (v >= from && v < to) {
+          if (in_bin(v)) {
             const uint32_t k = atomicAdd(&s.pooled, 1u);
             if (k < POOL) s.pool[k] = Logit{v, (uint32_t)(x.first + i)};
           }
@@ -412,7 +416,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
           for (uint32_t i = tid; i < min(s.pooled, (uint32_t)POOL); i += THREADS) look(s.pool[i].x, s.pool[i].index);
         } else {
           x.each(w0, w1, [&](float v, int i) {
-            if (v >= from && v < to) look(v, (uint32_t)(x.first + i));
+            if (in_bin(v)) look(v, (uint32_t)(x.first + i));
           });
         }
       };
@@ -462,20 +466,31 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       __syncthreads();
       arrive();                                               // (awaited ahead of the next items, or the next barrier)
       pending = true;
-      if (tid < n) {
-        const uint64_t me = s.all_at[tid];
-        const uint32_t my_w = s.all_w[tid];
-        uint32_t k = s.before_n;
-        uint64_t m = s.before_mass;
-        for (uint32_t j = 0; j < n; ++j)
+      // (four threads to an item)
+      static_assert(4 * LIST <= THREADS, "");
+      {
+        const uint32_t i = tid >> 2;
+        const uint64_t me = i < n ? s.all_at[i] : 0;
+        uint32_t k = 0;
+        uint64_t m = 0;
+        for (uint32_t j = tid & 3; j < n; j += 4)
           if (s.all_at[j] <= me) {
             ++k;
             m += s.all_w[j];
           }
-        const uint64_t incl = counts ? k : m, excl = counts ? k - 1 : m - my_w;
-        if (excl < limit && incl >= limit) {
-          s.found_at = me;
-          s.found_mass = m;
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          k += __shfl_xor_sync(0xffffffffu, k, o);
+          m += __shfl_xor_sync(0xffffffffu, m, o);
+        }
+        k += s.before_n;
+        m += s.before_mass;
+        if (i < n && (tid & 3) == 0) {
+          const uint64_t incl = counts ? k : m, excl = counts ? k - 1 : m - s.all_w[i];
+          if (excl < limit && incl >= limit) {
+            s.found_at = me;
+            s.found_mass = m;
+          }
         }
       }
       __syncthreads();
