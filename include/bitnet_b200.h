@@ -393,6 +393,8 @@ int bitnet_debug_wait_timeout_probe(void* stream);
  * before it for one that has run out, and goes the way of a call that gives up: the output is not to be used, and bitnet_device_status
  * reports BITNET_ERR_TIMEOUT until bitnet_device_status_clear. */
 void bitnet_debug_attn_give_up(int64_t tile);
+/* always = 1: bitnet_attn_shared hands no call to the decode kernel; 0: as described there. */
+void bitnet_debug_attn_shared(int always);
 /* Inverse of the packers: packed -> w[M][K] int8.  dev_status set if an invalid code is met. */
 int bitnet_unpack_i2s(const void* packed, int64_t M, int64_t K, int8_t* w, int* dev_status,
                       void* stream);
@@ -600,10 +602,11 @@ int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const b
 /*
  * bitnet_attn_decode for sequences that share beginnings: forked samples of one prompt, requests over one document.  Sequences
  * group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1], ascending, group_start[0] = 0, group_start[groups] = seqs) have their first prefix_len[g] tokens
- * (int32 [groups]; 0: none) in common: those are read through the row of the table of the group's first sequence (which has to hold their pages), once for the whole group, on the tensor cores;
- * every sequence's own tokens after them through its own row.  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
+ * (int32 [groups]; 0: none) in common: those are read through the row of the table of the group's first sequence, once for the whole group, on the tensor cores;
+ * every sequence's own tokens after them through its own row.  (Where there is little to be saved the decode kernel takes the call and every sequence's tokens
+ * are read through its own row: all rows of a group have to hold the prefix's pages.)  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
  * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
- * and that the probabilities of the prefix are rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
+ * and that the probabilities of the prefix may be rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
  * A sequence in no group (an array that is not as above) is taken by itself.  Reads at most the first 2^30 - 256 tokens of a prefix.
  * workspace: bitnet_attn_shared_workspace_bytes bytes (26 MB, and 1056 bytes per sequence and query head of 128); its first 64 KB as for the other attention
  * calls, whose workspace it may be too.

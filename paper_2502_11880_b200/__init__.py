@@ -33,7 +33,7 @@ SYMBOLS = [
     "bitnet_kv_cache_init", "bitnet_kv_append", "bitnet_kv_reserve", "bitnet_kv_workspace_bytes", "bitnet_kv_fork", "bitnet_kv_free",
     "bitnet_kv_trim", "bitnet_kv_compact", "bitnet_kv_copy_pages", "bitnet_attn_workspace_bytes", "bitnet_attn_decode", "bitnet_attn_prompt",
     "bitnet_debug_attn_give_up", "bitnet_attn_shared", "bitnet_attn_shared_workspace_bytes", "bitnet_rope_init", "bitnet_kv_append_rope",
-    "bitnet_add_rmsnorm_quant", "bitnet_sample",
+    "bitnet_add_rmsnorm_quant", "bitnet_sample", "bitnet_debug_attn_shared",
 ]
 
 _lib = None
@@ -59,6 +59,8 @@ def lib():
         L.bitnet_debug_wait_timeout_probe.argtypes = [vp]
         L.bitnet_debug_attn_give_up.argtypes = [i64]
         L.bitnet_debug_attn_give_up.restype = None
+        L.bitnet_debug_attn_shared.argtypes = [ci]
+        L.bitnet_debug_attn_shared.restype = None
         L.bitnet_set_early_start.argtypes = [ci]
         L.bitnet_set_early_start.restype = None
         L.bitnet_set_tl2_lookup.argtypes = [ci]
@@ -140,6 +142,11 @@ def bitnet_debug_wait_timeout_probe(stream=None):
 def bitnet_debug_attn_give_up(tile):
     """Test hook: CTAs of the attention kernels give up before their tile-th tile of cached tokens (-1: off)."""
     lib().bitnet_debug_attn_give_up(tile)
+
+
+def bitnet_debug_attn_shared(always: bool):
+    """Test hook: bitnet_attn_shared hands no call to the decode kernel."""
+    lib().bitnet_debug_attn_shared(int(bool(always)))
 
 
 def bitnet_set_early_start(enable: bool):

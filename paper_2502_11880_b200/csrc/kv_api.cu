@@ -1,4 +1,5 @@
 // C ABI of the paged key-value cache and the attention over it: argument checks and dispatch.
+#include <algorithm>
 #include <cmath>
 
 #include "kv_cache.cuh"
@@ -17,6 +18,19 @@ bool ints_or_null(const void* p) { return aligned(p, 4); }
 bool page_size_ok(int64_t n) { return n >= 8 && n <= (1 << 20) && (n & (n - 1)) == 0; }
 int64_t clamp_int(int64_t x) { return x < MOST ? x : MOST; }
 std::atomic<uint32_t> g_give_up{0xffffffffu};       // bitnet_debug_attn_give_up
+std::atomic<int> g_shared_always{0};                // bitnet_debug_attn_shared
+
+// Whether a shared call is one for the decode kernel, which reads a prefix once for every sequence, from L2 all but the first time, but in one launch: at
+// most 16 tiles (64 tokens of a kv head) per SM beyond twice the groups' share, going by what rows of the table, or their windows, may hold.
+// Measured, decode / shared (us), sequences x prefix: 32/8 heads of 128: 8 x 2048: 19/28, 8 x 4096: 29/31, 16 x 4096: 47/32, 2 x 16384: 29/44; 16/16 heads of
+// 96: 8 x 1024: 20/26, 8 x 2048: 33/28; 12/4 heads of 64: 8 x 4096: 17/25, 32 x 4096: 40/25.
+bool light(const AttnArgs& a, const bitnet_kv_cache_t* c) {
+  if (g_shared_always.load(std::memory_order_relaxed)) return false;
+  int64_t tokens = a.table_width * c->page_size;
+  if (a.window > 0) tokens = std::min(tokens, (int64_t)a.window + a.sinks + 64);
+  const double rows = (double)c->kv_heads * ceil_div(a.q_heads / c->kv_heads, 8);
+  return rows * ceil_div(tokens, 64) * (double)(a.tokens - 2 * a.groups) <= 16.0 * dev_info().sm_count;
+}
 
 // The books: table[seqs][width] and refs[num_pages].
 int check_books(const int32_t* refs, int64_t num_pages, const int32_t* table, int64_t seqs, int64_t width) {
@@ -239,6 +253,8 @@ size_t bitnet_attn_workspace_bytes(int64_t tokens, int64_t q_heads, int64_t kv_h
   return attn_decode_workspace_bytes() + attn_prompt_parts_bytes(tokens, (int)q_heads, (int)kv_heads);
 }
 
+void bitnet_debug_attn_shared(int always) { g_shared_always = always; }
+
 void bitnet_debug_attn_give_up(int64_t tile) { g_give_up = tile < 0 || tile >= 0xffffffffll ? 0xffffffffu : (uint32_t)tile; }
 
 int bitnet_attn_decode(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_dtype, int64_t q_heads, int64_t stride_token,
@@ -294,6 +310,7 @@ int bitnet_attn_shared(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
   a.group_start = group_start;
   a.prefix_len = prefix_len;
   a.groups = groups;
+  if (light(a, c)) return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
   return launch_attn_shared(c, a, workspace, (cudaStream_t)stream);
 }
 

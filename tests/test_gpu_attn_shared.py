@@ -9,6 +9,14 @@ from kv_ref import attn_ref, check_attn
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True, params=["as it goes", "always shared"])
+def path(request):
+    """Calls of these sizes are mostly ones that the decode kernel takes: every test runs a second time without it."""
+    bn.bitnet_debug_attn_shared(request.param == "always shared")
+    yield request.param
+    bn.bitnet_debug_attn_shared(False)
+
 BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
 PROMPT_P = {BF: 2.0 ** -8, HF: 2.0 ** -11}       # relative rounding of the prefix's probabilities
 
@@ -168,13 +176,25 @@ def test_agrees_with_decode():
     assert torch.allclose(a.float(), b.float(), rtol=2 ** -7, atol=2 ** -7)
 
 
-def test_the_first_sequences_pages_are_read():
-    """A prefix is read through the first sequence's row: other rows need no pages there."""
+def test_the_first_sequences_pages_are_read(path):
+    """A prefix is read through the first sequence's row: where the decode kernel does not take the call, other rows' pages there are not looked at."""
     s = Groups([(320, [330, 400, 350])], 2, 64, 16, BF, seed=7)
     q = s.queries(8)
     want = s.run(q)
-    s.table[1:, :320 // 16] = -1
-    assert torch.equal(s.run(q), want)
+    if path == "always shared":
+        s.table[1:, :320 // 16] = -1
+        assert torch.equal(s.run(q), want)
+
+
+def test_calls_go_by_what_there_is_to_save():
+    """Few tokens, or groups of one or two: the decode kernel's results, bit for bit; many: not."""
+    for groups, alike in (([(500, [510] * 4)], True), ([(4000, [4010, 4100])] * 3, True), ([(4096, [4100] * 24)], False)):
+        s = Groups(groups, 8, 128, 16, BF, seed=18)
+        q = s.queries(16)
+        bn.bitnet_debug_attn_shared(False)
+        a, b = s.run(q), bn.bitnet_attn_decode(s.cache, 1, q, s.table, s.len)
+        assert torch.equal(a, b) == alike
+        assert torch.allclose(a.float(), b.float(), rtol=2 ** -7, atol=2 ** -7)
 
 
 def test_strides_other_pool_order_stream_and_one_workspace():
@@ -212,14 +232,14 @@ def test_bad_pages_are_reported():
             assert int(status) == 7 and torch.equal(out[2], good[2]) and torch.isfinite(out).all()
 
 
-def test_a_first_sequence_without_the_prefixs_pages_is_reported():
+def test_a_first_sequence_without_the_prefixs_pages_is_reported(path):
     """The first sequence has 300 of the 500 tokens that the others have: their tokens from 300 on have no page to be read from."""
     s = Groups([(500, [300, 0, 500, 700, 20])], 2, 128, 16, BF, seed=129)
     s.table[0, -(-300 // 16):] = -1
     status = ints([0])
     out = bn.bitnet_attn_shared(s.cache, 1, s.queries(8), s.table, s.len, s.start, s.prefix, dev_status=status)
     torch.cuda.synchronize()
-    assert int(status) == 7 and torch.isfinite(out).all() and bool((out[1] == 0).all())
+    assert (int(status) == 7 or path != "always shared") and torch.isfinite(out).all() and bool((out[1] == 0).all())
 
 
 def test_arrays_of_groups_that_are_not_as_they_should():
