@@ -23,9 +23,10 @@ struct NormDev {
   double inv_k;
 };
 
-__device__ __forceinline__ float4 load4(const void* p, int64_t i, int type) {     // i: a multiple of 4 elements
-  if (type == BITNET_KV_F32) return __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + i));
-  const uint2 w = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i));
+// Four weights, which every row takes again: through the first-level cache.
+__device__ __forceinline__ float4 load_weights(const void* p, int i, int type) {
+  if (type == BITNET_KV_F32) return __ldg(static_cast<const float4*>(p) + i);
+  const uint2 w = __ldg(static_cast<const uint2*>(p) + i);
   if (type == BITNET_KV_BF16)
     return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
   const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), hi = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
 #pragma unroll
       for (int k = 0; k < VPT; ++k) {
         const int i = from + tid + k * nt;
-        w[k] = a.weight && i < n4 ? load4(a.weight, 4 * (int64_t)i, a.weight_type) : make_float4(1.f, 1.f, 1.f, 1.f);
+        w[k] = a.weight && i < n4 ? load_weights(a.weight, i, a.weight_type) : make_float4(1.f, 1.f, 1.f, 1.f);
       }
     }
     sum = block_sum(sum, red.sum);
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
       const int i = from + tid + k * nt;
       float4 v = make_float4(1.f, 1.f, 1.f, 1.f);
       if constexpr (VPT <= 2) v = w[k];
-      else if (a.weight && i < n4) v = load4(a.weight, 4 * (int64_t)i, a.weight_type);
+      else if (a.weight && i < n4) v = load_weights(a.weight, i, a.weight_type);
       h[k] = make_float4(scaled(h[k].x, r, v.x), scaled(h[k].y, r, v.y), scaled(h[k].z, r, v.z), scaled(h[k].w, r, v.w));
       if (i < n4) top = fmaxf(top, absmax4(h[k]));
     }
