@@ -158,6 +158,26 @@ __device__ __forceinline__ float4 widen(const Raw<TYPE>& r) {
   return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 
+template <int TYPE>
+__device__ __forceinline__ Raw<TYPE> narrow(const float4& v) {
+  Raw<TYPE> r;
+  if constexpr (TYPE == BITNET_KV_F32) {
+    r.v = make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w));
+  } else if constexpr (TYPE == BITNET_KV_BF16) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    r.v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    const __half2 lo = __floats2half2_rn(v.x, v.y), hi = __floats2half2_rn(v.z, v.w);
+    r.v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  }
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ void store_raw(void* p, int64_t i, const Raw<TYPE>& r) {
+  if constexpr (TYPE == BITNET_KV_F32) *reinterpret_cast<uint4*>(static_cast<float*>(p) + i) = r.v;
+  else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = r.v;
+}
+
 // VPT: pieces of 4 elements per thread; XT, RT: types of x and of the residual (or NONE).  A CTA takes every gridDim.x-th row, and
 // has the next one's loads on their way while it reduces and writes the present one.  WIDE: the CTAs of a cluster share a row; their sums and
 // maxima meet in every CTA's shared memory (a barrier of the cluster lies between any two uses of a place there).
@@ -207,11 +227,9 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
       h[k] = widen(x[k]);
       if constexpr (RT != NONE) {
         const float4 r = widen(e[k]);
-        h[k].x = rounded(h[k].x + r.x, RT);
-        h[k].y = rounded(h[k].y + r.y, RT);
-        h[k].z = rounded(h[k].z + r.z, RT);
-        h[k].w = rounded(h[k].w + r.w, RT);
-        store4(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, RT, h[k]);
+        const Raw<RT> stored = narrow<RT>(make_float4(h[k].x + r.x, h[k].y + r.y, h[k].z + r.z, h[k].w + r.w));
+        store_raw<RT>(a.residual_out, t * a.stride_residual_out + 4 * (int64_t)i, stored);
+        h[k] = widen(stored);
       }
       sum = fma((double)h[k].x, (double)h[k].x, sum);
       sum = fma((double)h[k].y, (double)h[k].y, sum);
