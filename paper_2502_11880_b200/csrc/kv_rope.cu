@@ -6,12 +6,17 @@
 // where pair i of a row is (x[i], x[i + rot/2]) or (x[2i], x[2i + 1]); elements from rot on move as they are.
 //
 // Angles: a frequency is held as the fraction of a turn per position in 64-bit fixed point, so that position * frequency modulo a turn is
-// one integer product that wraps around by itself, exact to 2^-33 of a turn at any position; the top 32 bits go to sincospi as half turns.
+// one integer product that wraps around by itself, right to 2^-33 of a turn at any position; its top 32 bits go to sincospi as half turns in
+// binary32, right to 2^-26 of a turn.
 // (binary32 products would be off by 0.008 radians at position 131072, and a table of all positions is 67 MB that has to be read.)
 // The products and sums are binary32, rounded once to the type written.
 //
-// Bound by HBM for prompts and by latency for single tokens.  A row's pairs are cut into slots of two vectors of VEC elements; a thread
-// keeps its slot, and so its VEC sines and cosines, over all heads of a token that it visits.
+// Bound by HBM for prompts (rows of odd sizes: by instructions, a vector is what the sizes allow) and by latency for single tokens.  A CTA has a token, or some
+// of its heads where tokens are few; its threads compute a sine and a cosine each and share them.  A row's pairs are cut into slots of two vectors of
+// VEC elements; a thread keeps its slot, and so its VEC pairs' sines and cosines, over all heads that it visits.
+//
+// Measured (us, a B200): 32 tokens, 64/8 heads of 128: 3.0; 4 x 2048 tokens, 32/8 heads of 128, fp32 in, bf16 out: 39 (6.1 TB/s); bf16 in and out,
+// 4096 tokens: 24 (3.3 TB/s).  With every thread computing its own sines: 3.8, 43, 34.
 #include <cstring>
 #include <type_traits>
 
@@ -84,16 +89,20 @@ __device__ __forceinline__ void store_vec(uint8_t* p, const float (&x)[N]) {
 // KT: the cache's type; IN, OUT: of q, k, v and of q_out; VEC: elements of a vector.
 template <typename KT, typename IN, typename OUT, int VEC>
 __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant__ RopeDev a) {
+  __shared__ float2 turn[64];                // cosine and sine of each pair
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int n = blockIdx.x / a.split, part = blockIdx.x - n * a.split, lane = threadIdx.x & 31;
+  // A thread's rows on their way at a time.  4 x 2048 tokens, 32/8 heads of 128, fp32 in, bf16 out: 43, 39, 38, 48 us with 1, 2, 3, 4; 3 x 517, 32/32 of
+  // 100, interleaved, fp16: 19.5, 16.3, 17.0, 24.8.  By single elements a row in four pieces (74, 81 with two).
+  constexpr int AT_A_TIME = VEC == 1 ? 4 : 2;
+  constexpr int IN_BYTES = sizeof(IN), OUT_BYTES = sizeof(OUT);
+  const int lane = threadIdx.x & 31;
   const int mine = threadIdx.x / a.slots, slot = threadIdx.x - mine * a.slots;
   const int hq = a.q_heads, hkv = a.kv.kv_heads, dim = a.kv.head_dim, rows = hq + 2 * hkv, step = a.split * a.at_once;
 
   // ---- a row's slot: two vectors, neighbouring threads' vectors side by side.  Pairs of the half layout: a vector of first elements and that of
   // the second ones; elsewhere vectors slot and slot + half of those that there are.
   const bool pairs = slot < a.rotated;
-  const int row0 = part * a.at_once + mine;
   auto place = [&](int start, int s, int& d0, int& d1) {   // of the vectors from element `start` on
     const int n = (dim - start) / VEC, half = (n + 1) / 2;
     d0 = s < half ? start + s * VEC : dim;
@@ -114,19 +123,25 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
   } else {
     place(a.rot, slot - a.rotated, qd0, qd1);
   }
-  // (several rows' loads on their way together)
-  constexpr int AT_A_TIME = 4;
+  // the first pair of the slot's first vector, and of its second one (of the half layout both have the same)
+  const int pair0 = VEC > 1 && a.interleaved ? qd0 / 2 : slot * VEC, pair1 = VEC > 1 && a.interleaved ? qd1 / 2 - VEC / 2 : pair0;
+
+  const int n = a.split == 1 ? blockIdx.x : blockIdx.x / a.split, row0 = (blockIdx.x - n * a.split) * a.at_once + mine;
+  const uint8_t* const q_in = a.q + (int64_t)n * a.q_stride_token * IN_BYTES;
+  const uint8_t* const k_in = a.k + (int64_t)n * a.stride_token * IN_BYTES;
+  const uint8_t* const v_in = a.v + (int64_t)n * a.stride_token * IN_BYTES;
+  // (several rows' loads on their way together, the first ones before the look-ups, which they do not depend on)
   Vec<IN, VEC> in0[AT_A_TIME], in1[AT_A_TIME];
   auto load = [&](int first) {
 #pragma unroll
     for (int k = 0; k < AT_A_TIME; ++k) {
       const int row = first + k * step;
-      const bool is_v = row >= hq + hkv;
+      const bool is_q = row < hq, is_v = row >= hq + hkv;
       const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
-      const uint8_t* src = row < hq ? a.q + ((int64_t)n * a.q_stride_token + row * a.q_stride_head) * (int)sizeof(IN)
-                                    : (is_v ? a.v : a.k) + ((int64_t)n * a.stride_token + (row - hq - (is_v ? hkv : 0)) * a.stride_head) * (int)sizeof(IN);
-      if (row < rows && d0 < dim) in0[k] = load_vec<IN, VEC>(src + d0 * (int)sizeof(IN));
-      if (row < rows && d1 < dim) in1[k] = load_vec<IN, VEC>(src + d1 * (int)sizeof(IN));
+      const uint8_t* const src = (is_q ? q_in : is_v ? v_in : k_in) +
+                                 (int64_t)(row - (is_q ? 0 : is_v ? hq + hkv : hq)) * (is_q ? a.q_stride_head : a.stride_head) * IN_BYTES;
+      if (row < rows && d0 < dim) in0[k] = load_vec<IN, VEC>(src + d0 * IN_BYTES);
+      if (row < rows && d1 < dim) in1[k] = load_vec<IN, VEC>(src + d1 * IN_BYTES);
     }
   };
   const bool active = mine < a.at_once && row0 < rows;
@@ -150,79 +165,79 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
   } else {
     pos = (int64_t)__ldg(a.kv_len + seq) - 1;
   }
-  if (pos < 0 || !active) return;
+  if (pos < 0) return;                                   // (so for all threads)
+  // sines and cosines, a pair per thread
+  if (2 * (int)threadIdx.x < a.rot) {
+    const uint64_t turns = (uint64_t)pos * a.step[threadIdx.x];
+    float sn, cs;
+    sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &sn, &cs);             // 2^-31: half turns
+    turn[threadIdx.x] = make_float2(cs * a.magnitude, sn * a.magnitude);
+  }
   const int64_t entry = pos >> a.page_shift;
   const int page = entry < a.width ? __ldg(a.table + (int64_t)seq * a.width + entry) : -1;
   const bool bad = page < 0 || page >= a.kv.num_pages;
   if (bad && threadIdx.x == 0 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
-
-  // sines and cosines of the slot's pairs: of VEC pairs, or of VEC / 2 in each of the two vectors
-  float sn[VEC], cs[VEC];
+  __syncthreads();
+  if (!active) return;
+  float2 cs[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
-    int pair = slot * VEC + i;
-    if (VEC > 1 && a.interleaved) pair = i < VEC / 2 ? qd0 / 2 + i : qd1 / 2 + i - VEC / 2;
-    sn[i] = 0.0f;
-    cs[i] = 1.0f;
-    if (pairs && 2 * pair < a.rot) {
-      const uint64_t turns = (uint64_t)pos * a.step[pair];
-      sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &sn[i], &cs[i]);       // 2^-31: half turns
-      sn[i] *= a.magnitude;
-      cs[i] *= a.magnitude;
-    }
+    const int pair = (i < VEC / 2 ? pair0 : pair1) + i;
+    cs[i] = pairs && 2 * pair < a.rot ? turn[pair] : make_float2(1.0f, 0.0f);
   }
   const int64_t in_pool = 2 * (a.layer * a.kv.stride_layer + (bad ? 0 : page) * a.kv.stride_page + (pos & (a.kv.page_size - 1)) * a.kv.stride_row);
+  uint8_t* const q_out = a.q_out + (int64_t)n * hq * dim * OUT_BYTES;
   for (int first = row0;;) {
 #pragma unroll
     for (int k = 0; k < AT_A_TIME; ++k) {
-    const int row = first + k * step;
-    if (row >= rows) break;
-    const bool is_v = row >= hq + hkv;
-    float x0[VEC], x1[VEC];
+      const int row = first + k * step;
+      if (row >= rows) break;
+      const bool is_q = row < hq, is_v = row >= hq + hkv;
+      float x0[VEC], x1[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      x0[i] = static_cast<float>(in0[k].t[i]);
-      x1[i] = static_cast<float>(in1[k].t[i]);
-    }
-    if (pairs && !is_v) {
-      if (a.interleaved) {
+      for (int i = 0; i < VEC; ++i) {
+        x0[i] = static_cast<float>(in0[k].t[i]);
+        x1[i] = static_cast<float>(in1[k].t[i]);
+      }
+      if (pairs && !is_v) {
+        if (a.interleaved) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          // (elements beyond rot move as they are, infinities too)
-          if constexpr (VEC == 1) {
-            if (2 * slot >= a.rot) continue;
-            const float p = x0[0], q = x1[0];
-            x0[0] = p * cs[0] - q * sn[0];
-            x1[0] = q * cs[0] + p * sn[0];
-          } else {
-            if ((i < VEC / 2 ? qd0 + 2 * i : qd1 + 2 * i - VEC) >= a.rot) continue;
-            float* const e = i < VEC / 2 ? &x0[2 * i] : &x1[2 * i - VEC];
-            const float p = e[0], q = e[1];
-            e[0] = p * cs[i] - q * sn[i];
-            e[1] = q * cs[i] + p * sn[i];
+          for (int i = 0; i < VEC; ++i) {
+            // (elements beyond rot move as they are, infinities too)
+            if constexpr (VEC == 1) {
+              if (2 * slot >= a.rot) continue;
+              const float p = x0[0], q = x1[0];
+              x0[0] = p * cs[0].x - q * cs[0].y;
+              x1[0] = q * cs[0].x + p * cs[0].y;
+            } else {
+              if ((i < VEC / 2 ? qd0 + 2 * i : qd1 + 2 * i - VEC) >= a.rot) continue;
+              float* const e = i < VEC / 2 ? &x0[2 * i] : &x1[2 * i - VEC];
+              const float p = e[0], q = e[1];
+              e[0] = p * cs[i].x - q * cs[i].y;
+              e[1] = q * cs[i].x + p * cs[i].y;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float p = x0[i], q = x1[i];
+            x0[i] = p * cs[i].x - q * cs[i].y;
+            x1[i] = q * cs[i].x + p * cs[i].y;
           }
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float p = x0[i], q = x1[i];
-          x0[i] = p * cs[i] - q * sn[i];
-          x1[i] = q * cs[i] + p * sn[i];
-        }
       }
-    }
-    const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
-    if (row < hq) {
-      uint8_t* const dst = a.q_out + ((int64_t)n * hq + row) * dim * (int)sizeof(OUT);
-      if (d0 < dim) store_vec<OUT, VEC>(dst + d0 * (int)sizeof(OUT), x0);
-      if (d1 < dim) store_vec<OUT, VEC>(dst + d1 * (int)sizeof(OUT), x1);
-    } else if (!bad) {
-      uint8_t* const dst = (is_v ? a.kv.v : a.kv.k) + in_pool + 2 * ((row - hq - (is_v ? hkv : 0)) * a.kv.stride_head);
-      if (d0 < dim) store_vec<KT, VEC>(dst + 2 * d0, x0);
-      if (d1 < dim) store_vec<KT, VEC>(dst + 2 * d1, x1);
-      // the row's padding (head_dim is a multiple of 4, rows of 8) is cleared, as by appends
-      if (slot == 0 && (dim & 7)) *reinterpret_cast<uint2*>(dst + 2 * dim) = make_uint2(0u, 0u);
-    }
+      const int d0 = is_v ? vd0 : qd0, d1 = is_v ? vd1 : qd1;
+      if (is_q) {
+        uint8_t* const dst = q_out + row * dim * OUT_BYTES;
+        if (d0 < dim) store_vec<OUT, VEC>(dst + d0 * OUT_BYTES, x0);
+        if (d1 < dim) store_vec<OUT, VEC>(dst + d1 * OUT_BYTES, x1);
+      } else if (!bad) {
+        uint8_t* const dst = (is_v ? a.kv.v : a.kv.k) + in_pool + 2 * ((row - (is_v ? hq + hkv : hq)) * a.kv.stride_head);
+        if (d0 < dim) store_vec<KT, VEC>(dst + 2 * d0, x0);
+        if (d1 < dim) store_vec<KT, VEC>(dst + 2 * d1, x1);
+        // the row's padding (head_dim is a multiple of 4, rows of 8) is cleared, as by appends
+        if (slot == 0 && (dim & 7)) *reinterpret_cast<uint2*>(dst + 2 * dim) = make_uint2(0u, 0u);
+      }
     }
     first += AT_A_TIME * step;
     if (first >= rows) break;
@@ -232,8 +247,6 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
 
 template <typename KT, typename IN, typename OUT>
 cudaError_t launch_vec(const RopeDev& d, int vec, const cudaLaunchConfig_t& cfg) {
-  if constexpr (sizeof(IN) == 2 && sizeof(OUT) == 2)
-    if (vec == 8) return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 8>, d);
   switch (vec) {
     case 4: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 4>, d);
     case 2: return cudaLaunchKernelEx(&cfg, kv_rope_kernel<KT, IN, OUT, 2>, d);
@@ -256,6 +269,7 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   d.v = static_cast<const uint8_t*>(x.v);
   d.q_out = static_cast<uint8_t*>(x.q_out);
   d.q_stride_token = x.q_stride_token;
+  const int size = x.in_type == BITNET_KV_F32 ? 4 : 2;
   d.q_stride_head = x.q_stride_head;
   d.stride_token = x.stride_token;
   d.stride_head = x.stride_head;
@@ -276,14 +290,12 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   const int dim = kv.head_dim;
   // elements of a vector: as many as half a row's pairs, the head, strides and addresses allow
   const bool in_f32 = x.in_type == BITNET_KV_F32, out_f32 = x.out_type == BITNET_KV_F32;
-  int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 8;
+  // (four at most: 4 x 2048 tokens, fp32 in, bf16 out: 42 us against 49 with 32-byte vectors, a warp's access would touch every sector twice; 16-bit in
+  // and out: 24 us with four as with eight)
+  int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 4;
   if (!d.interleaved) odd |= d.rot / 2;
   int vec = (int)(odd & -odd);
-  // (16 bytes of the wider type: with 32 a warp's access would touch every sector twice; 4 x 2048 tokens, fp32 in, bf16 out: 42 us against 49)
-  const int widest = in_f32 || (out_f32 && x.q_heads) ? 4 : 8;
-  if (vec > widest) vec = widest;
   const uintptr_t at = reinterpret_cast<uintptr_t>(x.k) | reinterpret_cast<uintptr_t>(x.v) | (x.q_heads ? reinterpret_cast<uintptr_t>(x.q) : 0);
-  const int size = in_f32 ? 4 : 2;
   while (vec > 1 && at % (size * vec < 16 ? size * vec : 16)) vec /= 2;
   auto slots = [&](int elements) { return (elements / vec + 1) / 2; };
   d.slots = slots(dim);
