@@ -37,6 +37,9 @@ int bitnet_add_rmsnorm_quant(const void* x, int x_type, int64_t stride_x, const 
   // rows that lie on one another would be written by several CTAs, and x in another type be read after it was overwritten
   if (residual && T > 1 && (stride_residual_out < 0 ? -stride_residual_out : stride_residual_out) < K) return BITNET_ERR_INVALID_ARG;
   if (residual && residual_out == x && residual_type != x_type) return BITNET_ERR_INVALID_ARG;
+  // (in place, each row in its own place)
+  if (residual && T > 1 && ((residual_out == x && stride_residual_out != stride_x) || (residual_out == residual && stride_residual_out != stride_residual)))
+    return BITNET_ERR_INVALID_ARG;
   NormArgs a;
   a.x = x;
   a.residual = residual;

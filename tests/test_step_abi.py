@@ -28,6 +28,11 @@ def test_norm_is_checked(L, bad):
     assert norm(L, **bad) == 1
 
 
+@pytest.mark.parametrize("where", [dict(r=C.c_void_p(8192), sx=128), dict(x=C.c_void_p(8192), sr=128)])       # in place over x, over the residual
+def test_norm_in_place_keeps_its_stride(L, where):
+    assert norm(L, T=2, **where) == 1
+
+
 def test_calls_with_nothing_to_do(L):
     assert norm(L, T=0, x=NULL, q=NULL, sc=NULL) == 0
     assert L.bitnet_sample(NULL, 2, 64, 0, 64, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL) == 0
