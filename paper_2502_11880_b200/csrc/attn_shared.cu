@@ -4,6 +4,10 @@
 //   2. the sequences' own tokens (attn_own_kernel), in parts over the warps;
 //   3. the join (attn_join_kernel).
 // A part of a row is its maximum m, its sum l = sum 2^(s - m) and O = sum 2^(s - m) V, s in units of log2.
+//
+// Measured (us, a B200, the three in turn), bf16: 64 sequences over 16384 tokens with up to 400 of their own, 64/8 heads of 128: 80, of which 45, 22 and 8
+// (35 GFLOP of products need 21; the decode kernel, which reads the prefix for every sequence: 382); 40 in three groups over 4000, 704 and 0, 16/16 heads
+// of 96, fp16, window 2048: 43 (93).
 #include <cstring>
 #include <type_traits>
 
@@ -149,11 +153,12 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   // ---- the list of tiles: total, and where the warps' parts begin
   const int rows_per_seq = a.kv_heads * a.head_blocks;
   int64_t total = 0, my_excl = 0;
-  int longest = 0, my_tiles = 0, my_row = 1;
+  int64_t my_tiles = 0;
+  int longest = 0, my_row = 1;
   auto scan_chunk = [&](int n0, int64_t base) {            // tiles before sequence n0 + tid; returns the chunk's total
     const int n = n0 + tid;
     my_row = n < a.seqs ? own_of(a, n).tiles : 0;
-    my_tiles = my_row * rows_per_seq;
+    my_tiles = (int64_t)my_row * rows_per_seq;
     int64_t x = my_tiles;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -407,7 +412,8 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------------------------ join
 // With a row's parts, m = max m_k, out = sum_k 2^(m_k - m) O_k / sum_k 2^(m_k - m) l_k in the order of the parts, in fp32, rounded once.  A warp per row
-// (sequence and query head); maxima and sums are read by its lanes side by side, the parts of O eight at a time.
+// (sequence and query head); maxima and sums are read by its lanes side by side, the parts of O eight at a time.  Bound by latency: 26 MB of parts, all in
+// L2, in 8 us for 64 sequences with 64 query heads of 128.
 constexpr int JOIN_WARPS = 4;
 
 struct JoinArgs {
