@@ -5,9 +5,8 @@
 //   3. the join (attn_join_kernel).
 // A part of a row is its maximum m, its sum l = sum 2^(s - m) and O = sum 2^(s - m) V, s in units of log2.
 //
-// Measured (us, a B200, the three in turn), bf16: 64 sequences over 16384 tokens with up to 400 of their own, 64/8 heads of 128: 80, of which 45, 22 and 8
-// (35 GFLOP of products need 21; the decode kernel, which reads the prefix for every sequence: 382); 40 in three groups over 4000, 704 and 0, 16/16 heads
-// of 96, fp16, window 2048: 43 (93).
+// Measured (us, a B200), bf16: 64 sequences over 16384 tokens with up to 400 of their own, 64/8 heads of 128: 76, by themselves 45, 22 and 8 (35 GFLOP
+// of products need 21; the decode kernel, which reads the prefix for every sequence: 382); 40 in three groups over 4000, 704 and 0, 16/16 heads of 96, fp16, window 2048: 38 (93).
 #include <cstring>
 #include <type_traits>
 
@@ -147,8 +146,10 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   extern __shared__ __align__(128) uint8_t smem[];
   typename L::Tail& s = *reinterpret_cast<typename L::Tail*>(smem + OWN_WARPS * L::STAGES * L::STAGE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // This grid starts where SMs are done with kernel 1, which let it go when all before it was complete, and of whose results nothing is read here.  It
+  // ends after kernel 1, so that the join follows both.  (The three in turn: 80.7 and 42.6 us against 76.2 and 38.1.)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto others_done = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
 
   // ---- the list of tiles: total, and where the warps' parts begin
   const int rows_per_seq = a.kv_heads * a.head_blocks;
@@ -221,7 +222,10 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     }
   }
   __syncthreads();
-  if (id >= parts || s.begin[warp] >= s.end[warp]) return;
+  if (id >= parts || s.begin[warp] >= s.end[warp]) {
+    others_done();
+    return;
+  }
 
   // A place in the list, and a second one STAGES - 1 tiles ahead, where the ring is filled.
   struct Place {
@@ -408,6 +412,7 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
     p.left -= t_end - t0;
     if (t_end == r.tiles) next_row(p);
   }
+  others_done();
 }
 
 // ------------------------------------------------------------------------------------------------ join

@@ -122,3 +122,14 @@ def test_two_services_on_two_streams():
                 s.run()
     torch.cuda.synchronize()
     assert all(torch.equal(s.tokens, t) and torch.equal(s.logits, x) for s, (t, x) in zip(pair, want))
+
+
+def test_steps_through_prefix_own_tokens_and_join():
+    """The same with the shared attention in its own three kernels, small as the calls are."""
+    bn.bitnet_debug_attn_shared(1)
+    try:
+        for n, prompt in ((4, 333), (40, 64), (150, 600)):
+            test_steps_back_to_back_and_in_a_graph(n, prompt)
+        test_two_services_on_two_streams()
+    finally:
+        bn.bitnet_debug_attn_shared(0)
