@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(THREADS) kv_rope_kernel(const __grid_constant_
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // A thread's rows on their way at a time.  4 x 2048 tokens, 32/8 heads of 128, fp32 in, bf16 out: 43, 39, 38, 48 us with 1, 2, 3, 4; 3 x 517, 32/32 of
-  // 100, interleaved, fp16: 19.5, 16.3, 17.0, 24.8.  By single elements a row in four pieces (74, 81 with two).
+  // 100, interleaved, fp16: 19.5, 16.3, 17.0, 24.8 (two with the next ones on their way: 38.9 and 15.7, but 3.3 instead of 3.0 for 32 tokens, and
+  // single elements 15 % slower).  By single elements a row in four pieces (74, 81 with two).
   constexpr int AT_A_TIME = VEC == 1 ? 4 : 2;
   constexpr int IN_BYTES = sizeof(IN), OUT_BYTES = sizeof(OUT);
   const int lane = threadIdx.x & 31;
@@ -303,8 +304,9 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   if (!d.interleaved && d.rotated + slots(dim - d.rot) > d.slots) d.slots = d.rotated + slots(dim - d.rot);
   d.at_once = THREADS / d.slots;
   // CTAs per token: a row per thread while CTAs are few, all of a token's rows in one when there are enough tokens to fill the SMs
+  // (up to 8, 16, 32 and 64 CTAs per SM: 16.3, 15.4, 16.5 and 17.9 us for 3 x 517 tokens, 32/32 heads of 100; 24.1, 24.2, 24.2 and 26.3 for 4096, 32/8 of 128)
   const int64_t rows = x.q_heads + 2 * kv.kv_heads, most = ceil_div(rows, d.at_once), sms = dev_info().sm_count;
-  int64_t split = 8 * sms / x.tokens;
+  int64_t split = 16 * sms / x.tokens;
   split = split < 1 ? 1 : split > most ? most : split;
   d.split = (int)ceil_div(most, ceil_div(most, split));           // (no CTA without rows, and even shares)
   cudaLaunchConfig_t cfg = {};
