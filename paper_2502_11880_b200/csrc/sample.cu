@@ -180,7 +180,7 @@ __device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
 }
 
 template <typename T, bool STAGED>
-__global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Share& s = *reinterpret_cast<Share*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -292,19 +292,27 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
   uint32_t last_index = greedy ? 0xffffffffu : 0u;
   const bool by_k = !greedy && top_k > 0 && top_k < a.vocab, by_p = !greedy && top_p < 1.0f;
   if (by_k || by_p) {
-    // all items by their distance from the largest
-    {
+    // all items by their distance from the largest: counts, and sums of weights where those are asked for
+    auto histogram = [&](bool sums) {
       Hist& h = s.hist;
-      x.each(w0, w1, [&](float v, int) {
-        float d;
-        const float t = weigh.distance(v, d);
-        if (!(t < REACH)) return;
-        const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
-        const int b = bin_of(t);
-        atomicAdd(&h.count[b], 1u);
-        if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
-      });
-    }
+      if (sums) {
+        x.each(w0, w1, [&](float v, int) {
+          float d;
+          const float t = weigh.distance(v, d);
+          if (!(t < REACH)) return;
+          const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
+          const int b = bin_of(t);
+          atomicAdd(&h.count[b], 1u);
+          if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
+        });
+      } else {
+        x.each(w0, w1, [&](float v, int) {
+          float d;
+          const float t = weigh.distance(v, d);
+          if (t < REACH) atomicAdd(&h.count[bin_of(t)], 1u);
+        });
+      }
+    };
     // The histogram's bins summed over the cluster, to every CTA's `to`: each CTA adds up its share of the bins, and tells the others.
     auto gather = [&](Sums& to) {
       const int share = BINS / ctas, p = tid / share, of = tid - p * share;
@@ -363,11 +371,9 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       }
       __syncthreads();
     };
-    // the last item kept: the first in the order with which the count or sum reaches `limit`; false: all together do not
-    auto resolve = [&](bool counts, uint64_t limit) -> bool {
-      find(counts, limit, s.row, 0, 0);
+    // the last item kept, of the bin that was found: the first in the order with which the count or sum reaches `limit`
+    auto resolve = [&](bool counts, uint64_t limit) {
       const int b0 = s.bin;
-      if (b0 < 0) return false;
       // the range of the order that holds it: the bin's, and where that is to be divided its values, [from, to).  The bin falls as the value rises: of all
       // values, by rank, those whose bin lies beyond b are counted digit by digit, 32 at a time.
       uint64_t lo = 0, hi = ~(uint64_t)0;
@@ -393,7 +399,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
         const float t = weigh.distance(v, d);
         return t < REACH && bin_of(t) == b0;
       };
-      // its items set aside, where there are not too many
+      // the bin's items set aside, where there are not too many
       const bool pool = s.bin_n <= POOL;
       if (pool) {
         if (tid == 0) s.pooled = 0;
@@ -497,12 +503,104 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
         }
       }
       __syncthreads();
-      return true;
+    };
+    // what top_p of `all` asks for
+    auto share_of = [&](uint64_t all) -> uint64_t {
+      const double want = top_p > 0.0f ? ceil((double)top_p * (double)all) : 0.0;
+      return want < 1.0 ? (uint64_t)1 : want < (double)all ? (uint64_t)want : all;
+    };
+    // The bin that was found and those before it have LIST items at most: all that may be kept.  They are brought to the cluster's first CTA, which ranks
+    // them, applies the rules (the first one if `count_here`) and draws.
+    auto few = [&] { return s.bin >= 0 && s.before_n + s.bin_n <= LIST; };
+    auto draw_of_few = [&](bool count_here, uint64_t all) {
+      const int b0 = s.bin;
+      if (tid == 0) s.listed = 0;
+      __syncthreads();
+      settle();
+      x.each(w0, w1, [&](float v, int i) {
+        float d;
+        const float t = weigh.distance(v, d);
+        if (!(t < REACH) || bin_of(t) > b0) return;
+        const uint32_t k = atomicAdd(&s.listed, 1u);
+        if (k >= LIST) return;
+        tell(&s.item_at[rank][k], 0, place(v, (uint32_t)(x.first + i)));
+        tell(&s.item_w[rank][k], 0, fixed(weigh.weight<EXACT>(v, d, t)));
+      });
+      __syncthreads();
+      if (tid == 0) tell(&s.items[rank], 0, min(s.listed, (uint32_t)LIST));
+      meet();                                                 // (the last one)
+      if (rank != 0) return;
+      uint32_t n = 0;
+      for (int p = 0; p < ctas; ++p) {
+        const uint32_t m = s.items[p];
+        if (tid < m && n + tid < LIST) {
+          s.all_at[n + tid] = s.item_at[p][tid];
+          s.all_w[n + tid] = s.item_w[p][tid];
+        }
+        n += m;
+      }
+      n = min(n, (uint32_t)LIST);
+      __syncthreads();
+      // an item's rank, from 1, and the sum up to it; four threads to an item
+      const uint32_t i = tid >> 2;
+      const uint64_t me = i < n ? s.all_at[i] : 0;
+      const uint32_t w = i < n ? s.all_w[i] : 0u;
+      uint32_t k = 0;
+      uint64_t m = 0;
+      for (uint32_t j = tid & 3; j < n; j += 4)
+        if (s.all_at[j] <= me) {
+          ++k;
+          m += s.all_w[j];
+        }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        k += __shfl_xor_sync(0xffffffffu, k, o);
+        m += __shfl_xor_sync(0xffffffffu, m, o);
+      }
+      if (count_here) {
+        if (i < n && (int)k == top_k) s.found_mass = m;
+        __syncthreads();
+        all = s.found_mass;
+      }
+      float d;
+      const float v = value_at(me), t = weigh.distance(v, d), exact_w = i < n ? weigh.weight<EXACT>(v, d, t) : 0.0f;
+      const bool keep = i < n && (!count_here || (int)k <= top_k) && (!by_p || m - w < share_of(all)) && !(exact_w < least);
+      __syncthreads();
+      if (i < n && (tid & 3) == 0) s.all_w[i] = keep ? w : 0u;
+      __syncthreads();
+      // those ahead of it in the vocabulary
+      uint64_t total = 0, before = 0;
+      for (uint32_t j = tid & 3; j < n; j += 4) {
+        const uint32_t of_j = s.all_w[j];
+        total += of_j;
+        if ((uint32_t)s.all_at[j] < (uint32_t)me) before += of_j;
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+      }
+      const uint64_t target = __umul64hi(total, __float2ull_rz(u * 18446744073709551616.0f));
+      if (keep && (tid & 3) == 0 && before <= target && before + w > target) {
+        a.tokens[r] = (int)(uint32_t)me;
+        if (a.prob) a.prob[r] = (float)((double)exact_w / (double)total);
+      }
     };
 
-    gather(s.row);
+    // (no sums where top_k says that few are kept; seldom wrong: many equal values)
+    bool short_k = false;
+#pragma unroll 1
+    for (bool sums = !(by_k && top_k <= LIST);; sums = true) {
+      histogram(sums);
+      gather(s.row);
+      if (by_k) find(true, (uint64_t)top_k, s.row, 0, 0);
+      short_k = by_k && few();
+      if (sums || short_k) break;
+      s.hist.count[tid] = 0;
+      __syncthreads();
+    }
     uint64_t all = 0;
-    {
+    if (!short_k) {
       const uint64_t m = warp_sum_u64(s.row.mass[tid]);
       __syncthreads();
       if (lane == 0) s.warp_mass[warp] = m;
@@ -513,13 +611,24 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__
       last = value_at(s.found_at);
       last_index = (uint32_t)s.found_at;
     };
-    if (by_k && resolve(true, (uint64_t)top_k)) {
+    if (by_k && !short_k && s.bin >= 0) {
+      resolve(true, (uint64_t)top_k);
       cut();
       all = s.found_mass;
     }
-    if (by_p) {
-      const double want = top_p > 0.0f ? ceil((double)top_p * (double)all) : 0.0;
-      if (resolve(false, want < 1.0 ? (uint64_t)1 : want < (double)all ? (uint64_t)want : all)) cut();
+    bool short_p = false;
+    if (by_p && !short_k) {
+      const uint64_t limit = share_of(all);
+      find(false, limit, s.row, 0, 0);
+      short_p = few();
+      if (!short_p && s.bin >= 0) {
+        resolve(false, limit);
+        cut();
+      }
+    }
+    if (short_k || short_p) {
+      draw_of_few(short_k, all);
+      return;
     }
   }
 
