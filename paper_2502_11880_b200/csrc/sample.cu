@@ -9,6 +9,8 @@
 // over shared memory, and what the CTAs tell each other goes through distributed shared memory:
 //   * the maximum;
 //   * a histogram over (max - x) / T, linear, so that broad and peaked rows both spread over it;
+//   * where the bins up to the one that holds the last kept item have FEW items at most: these, in the first CTA, which ranks them by counting, applies the
+//     rules and draws; otherwise
 //   * while the bin that holds the last kept item has more than LIST items: another histogram over that bin's range of the order
 //     (64 bits: the value's bits, then the index, so that any number of equal values is taken apart too);
 //   * the bin's items, ranked by counting: the last item kept, as a place in the order;
@@ -18,7 +20,7 @@
 // max - x and of the product carried along, so that a weight is off by the exponential's own 2^-22 only.
 //
 // Bound by barriers for few rows and by instructions for many: some 35 an item for its weight and its bin.  Measured (us, a B200): 1 x 32000, fp32, top-k 50,
-// top-p 0.9: 14; 64 x 128256, fp32, settings per row: 62 (HBM needs 5); 256 x 50021, bf16, top-p 0.92: 76 (HBM needs 4).
+// top-p 0.9: 8.4 (14 without the short list); 64 x 128256, fp32, settings per row: 59 (HBM needs 5); 256 x 50021, bf16, top-p 0.92: 79 (HBM needs 4).
 #include <cstring>
 #include <type_traits>
 
@@ -30,6 +32,7 @@ namespace {
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int BINS = THREADS;                // one per thread
 constexpr int LIST = 128;                    // items that are ranked by counting
+constexpr int FEW = 256;                     // items of a row that are left to one CTA
 constexpr int POOL = 1024;                   // items of a bin that are set aside, so that what follows need not look at the whole row
 constexpr int MOST_CTAS = 8;                 // of a cluster
 constexpr float ONE = 4294967296.0f;         // weight 1
@@ -45,23 +48,41 @@ struct Sums {
   uint64_t mass[BINS];
   uint32_t count[BINS];
 };
+// What a division of a bin needs, and what the end of a row with few items needs.
+struct Division {
+  Sums level;                                // sums over the cluster of a later histogram
+  uint64_t item_at[MOST_CTAS][LIST];         // items to be ranked: their places in the order, and weights
+  uint32_t item_w[MOST_CTAS][LIST];
+  Logit pool[POOL];                          // (this CTA's own)
+};
+struct End {
+  uint64_t at[MOST_CTAS][FEW];
+  uint32_t w[MOST_CTAS][FEW];
+};
 struct Share {
   // written by the others, read after a barrier of the cluster
   float top[MOST_CTAS][WARPS];
   uint64_t part_mass[BINS];                  // of a cluster of C CTAs, BINS / C bins are this CTA's to add up: C parts of each
   uint32_t part_count[BINS];
-  Sums row, level;                           // sums over the cluster: of the first histogram, of a later one
-  uint64_t item_at[MOST_CTAS][LIST];         // items to be ranked: their places in the order, and weights
-  uint32_t item_w[MOST_CTAS][LIST];
+  Sums row;                                  // sums over the cluster, of the first histogram
+  union {
+    Division div;
+    End few;
+  };
   uint32_t items[MOST_CTAS];
   uint64_t cta_mass[MOST_CTAS];
   // this CTA's own
-  Hist hist;
+  union {
+    Hist hist;
+    struct {
+      uint64_t few_at[FEW];
+      uint32_t few_w[FEW];
+    };
+  };
   uint64_t warp_mass[WARPS];
   uint32_t warp_count[WARPS];
   uint64_t all_at[LIST];
   uint32_t all_w[LIST];
-  Logit pool[POOL];
   uint32_t listed, pooled;
   // found by one thread
   int bin;
@@ -407,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         x.each(w0, w1, [&](float v, int i) {
           if (in_bin(v)) {
             const uint32_t k = atomicAdd(&s.pooled, 1u);
-            if (k < POOL) s.pool[k] = Logit{v, (uint32_t)(x.first + i)};
+            if (k < POOL) s.div.pool[k] = Logit{v, (uint32_t)(x.first + i)};
           }
         });
         __syncthreads();
@@ -422,7 +443,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
           f(at, fixed(weigh.weight<EXACT>(v, d, t)));
         };
         if (pool) {
-          for (uint32_t i = tid; i < min(s.pooled, (uint32_t)POOL); i += THREADS) look(s.pool[i].x, s.pool[i].index);
+          for (uint32_t i = tid; i < min(s.pooled, (uint32_t)POOL); i += THREADS) look(s.div.pool[i].x, s.div.pool[i].index);
         } else {
           x.each(w0, w1, [&](float v, int i) {
             if (in_bin(v)) look(v, (uint32_t)(x.first + i));
@@ -442,8 +463,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         });
         const uint32_t before_n = s.before_n;
         const uint64_t before_mass = s.before_mass;
-        gather(s.level);
-        find(counts, limit, s.level, before_n, before_mass);
+        gather(s.div.level);
+        find(counts, limit, s.div.level, before_n, before_mass);
         lo += (uint64_t)s.bin << shift;
         hi = min(hi, lo + (((uint64_t)1 << shift) - 1));
       }
@@ -455,8 +476,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         const uint32_t k = atomicAdd(&s.listed, 1u);
         if (k >= LIST) return;
         for (int p = 0; p < ctas; ++p) {
-          tell(&s.item_at[rank][k], p, at);
-          tell(&s.item_w[rank][k], p, w);
+          tell(&s.div.item_at[rank][k], p, at);
+          tell(&s.div.item_w[rank][k], p, w);
         }
       });
       __syncthreads();
@@ -466,8 +487,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       for (int p = 0; p < ctas; ++p) {
         const uint32_t m = s.items[p];
         if (tid < m && n + tid < LIST) {
-          s.all_at[n + tid] = s.item_at[p][tid];
-          s.all_w[n + tid] = s.item_w[p][tid];
+          s.all_at[n + tid] = s.div.item_at[p][tid];
+          s.all_w[n + tid] = s.div.item_w[p][tid];
         }
         n += m;
       }
@@ -509,9 +530,9 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       const double want = top_p > 0.0f ? ceil((double)top_p * (double)all) : 0.0;
       return want < 1.0 ? (uint64_t)1 : want < (double)all ? (uint64_t)want : all;
     };
-    // The bin that was found and those before it have LIST items at most: all that may be kept.  They are brought to the cluster's first CTA, which ranks
+    // The bin that was found and those before it have FEW items at most: all that may be kept.  They are brought to the cluster's first CTA, which ranks
     // them, applies the rules (the first one if `count_here`) and draws.
-    auto few = [&] { return s.bin >= 0 && s.before_n + s.bin_n <= LIST; };
+    auto few = [&] { return s.bin >= 0 && s.before_n + s.bin_n <= FEW; };
     auto draw_of_few = [&](bool count_here, uint64_t all) {
       const int b0 = s.bin;
       if (tid == 0) s.listed = 0;
@@ -522,38 +543,39 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         const float t = weigh.distance(v, d);
         if (!(t < REACH) || bin_of(t) > b0) return;
         const uint32_t k = atomicAdd(&s.listed, 1u);
-        if (k >= LIST) return;
-        tell(&s.item_at[rank][k], 0, place(v, (uint32_t)(x.first + i)));
-        tell(&s.item_w[rank][k], 0, fixed(weigh.weight<EXACT>(v, d, t)));
+        if (k >= FEW) return;
+        tell(&s.few.at[rank][k], 0, place(v, (uint32_t)(x.first + i)));
+        tell(&s.few.w[rank][k], 0, fixed(weigh.weight<EXACT>(v, d, t)));
       });
       __syncthreads();
-      if (tid == 0) tell(&s.items[rank], 0, min(s.listed, (uint32_t)LIST));
+      if (tid == 0) tell(&s.items[rank], 0, min(s.listed, (uint32_t)FEW));
       meet();                                                 // (the last one)
       if (rank != 0) return;
       uint32_t n = 0;
       for (int p = 0; p < ctas; ++p) {
         const uint32_t m = s.items[p];
-        if (tid < m && n + tid < LIST) {
-          s.all_at[n + tid] = s.item_at[p][tid];
-          s.all_w[n + tid] = s.item_w[p][tid];
+        if (tid < m && n + tid < FEW) {
+          s.few_at[n + tid] = s.few.at[p][tid];
+          s.few_w[n + tid] = s.few.w[p][tid];
         }
         n += m;
       }
-      n = min(n, (uint32_t)LIST);
+      n = min(n, (uint32_t)FEW);
       __syncthreads();
-      // an item's rank, from 1, and the sum up to it; four threads to an item
-      const uint32_t i = tid >> 2;
-      const uint64_t me = i < n ? s.all_at[i] : 0;
-      const uint32_t w = i < n ? s.all_w[i] : 0u;
+      // an item's rank, from 1, and the sum up to it; as many threads to an item as there are, up to 32
+      static_assert(THREADS == 512 && FEW <= THREADS, "");
+      const int log2_per = min(5, __clz((int)max(n, 1u) - 1) - 23), per = 1 << log2_per;
+      const uint32_t i = tid >> log2_per, part = tid & (per - 1);
+      const uint64_t me = i < n ? s.few_at[i] : 0;
+      const uint32_t w = i < n ? s.few_w[i] : 0u;
       uint32_t k = 0;
       uint64_t m = 0;
-      for (uint32_t j = tid & 3; j < n; j += 4)
-        if (s.all_at[j] <= me) {
+      for (uint32_t j = part; j < n; j += per)
+        if (s.few_at[j] <= me) {
           ++k;
-          m += s.all_w[j];
+          m += s.few_w[j];
         }
-#pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
+      for (int o = 1; o < per; o <<= 1) {
         k += __shfl_xor_sync(0xffffffffu, k, o);
         m += __shfl_xor_sync(0xffffffffu, m, o);
       }
@@ -566,22 +588,21 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       const float v = value_at(me), t = weigh.distance(v, d), exact_w = i < n ? weigh.weight<EXACT>(v, d, t) : 0.0f;
       const bool keep = i < n && (!count_here || (int)k <= top_k) && (!by_p || m - w < share_of(all)) && !(exact_w < least);
       __syncthreads();
-      if (i < n && (tid & 3) == 0) s.all_w[i] = keep ? w : 0u;
+      if (i < n && part == 0) s.few_w[i] = keep ? w : 0u;
       __syncthreads();
       // those ahead of it in the vocabulary
       uint64_t total = 0, before = 0;
-      for (uint32_t j = tid & 3; j < n; j += 4) {
-        const uint32_t of_j = s.all_w[j];
+      for (uint32_t j = part; j < n; j += per) {
+        const uint32_t of_j = s.few_w[j];
         total += of_j;
-        if ((uint32_t)s.all_at[j] < (uint32_t)me) before += of_j;
+        if ((uint32_t)s.few_at[j] < (uint32_t)me) before += of_j;
       }
-#pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
+      for (int o = 1; o < per; o <<= 1) {
         total += __shfl_xor_sync(0xffffffffu, total, o);
         before += __shfl_xor_sync(0xffffffffu, before, o);
       }
       const uint64_t target = __umul64hi(total, __float2ull_rz(u * 18446744073709551616.0f));
-      if (keep && (tid & 3) == 0 && before <= target && before + w > target) {
+      if (keep && part == 0 && before <= target && before + w > target) {
         a.tokens[r] = (int)(uint32_t)me;
         if (a.prob) a.prob[r] = (float)((double)exact_w / (double)total);
       }
@@ -590,7 +611,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     // (no sums where top_k says that few are kept; seldom wrong: many equal values)
     bool short_k = false;
 #pragma unroll 1
-    for (bool sums = !(by_k && top_k <= LIST);; sums = true) {
+    for (bool sums = !(by_k && top_k <= FEW - FEW / 8);; sums = true) {
       histogram(sums);
       gather(s.row);
       if (by_k) find(true, (uint64_t)top_k, s.row, 0, 0);

@@ -126,6 +126,28 @@ def test_many_ties_at_the_border():
     assert tokens.tolist() == (torch.tensor(u).double() * 10).int().tolist()       # (binary32 has 0.9 just below 9 tenths)
 
 
+@pytest.mark.parametrize("vocab,dtype", [(600, F32), (9000, BF), (30011, F32), (400001, F32)])
+def test_short_and_long_lists(vocab, dtype):
+    """Some 256 items that may be kept: on both sides of it, by either rule, by both, with ties across the cut, and with fewer items in reach."""
+    ks = [1, 31, 32, 33, 127, 128, 129, 223, 224, 225, 255, 256, 257, 300]
+    if vocab > 100000:
+        ks = [128, 256, 257]
+    u = [(i * 0.37 + 0.011) % 1 for i in range(len(ks))]
+    x = logits(len(ks), vocab, dtype, 11, 3.0)
+    check(x, u, k=ks)
+    check(x, u, k=ks, p=[0.95, 0.5, 1.0, 0.999, 0.9, 0.3, 0.99, 0.9, 0.01, 0.97, 0.8, 0.9999, 0.6, 0.9][:len(ks)], m=([0.0, 0.05] * 7)[:len(ks)],
+          t=([0.6, 1.0] * 7)[:len(ks)])
+    check(x, u, p=[0.02 * (i + 1) for i in range(len(ks))], t=[0.8] * len(ks))
+    check(x, u, k=[2000] * len(ks), p=[0.05 * (i + 1) for i in range(len(ks))])
+    coarse = (x * 2).round() / 2                  # equal ones lie at the cut, more than there is room for in some rows
+    check(coarse, u, k=ks)
+    check(coarse, u, k=ks, p=[0.9] * len(ks))
+    few = torch.full_like(x, -300.0)              # out of reach, but for a few
+    few[:, ::vocab // 30] = x[:, ::vocab // 30].clamp(-3, 3)
+    check(few, u, k=ks)
+    check(few, u, k=ks, p=[0.7] * len(ks))
+
+
 def test_close_values():
     """Neighbouring floats: the order goes by the last bit."""
     base = torch.arange(3000, dtype=torch.int32, device="cuda") + torch.tensor(5.0).view(torch.int32).item()
