@@ -8,19 +8,21 @@
 // (a few wrong bits of r would move codes that lie next to a border); from there every step is one binary32 operation, and the codes are
 // those that bitnet_quant_act gives for y.
 //
-// Bound by HBM for many rows, by the latency of loads and two reductions for few.  Measured (us, a B200): 1 x 4096: 2.5; 16 x 28672: 4.5; 4099 x 8192, fp32 x
-// and a bf16 residual: 62 (4.9 TB/s, 0.74 of a copy's rate; instructions take 60 % of the issue slots, and two CTAs of 512 threads per SM have no more on
-// its way).  There the next row's loads ahead of the reductions took it from 98 to 74, types as template parameters to 69, weights through the first-level
-// cache to 64, one rounding of the new residual for the store and the sum to 62.
+// Bound by HBM for many rows, by the latency of loads and two reductions for few.  Measured (us, a B200): 1 x 4096: 2.3; 16 x 28672: 4.2; 4099 x 8192, fp32 x
+// and a bf16 residual: 56 (5.4 TB/s, 0.82 of a copy's rate; what is left is the latency of the reductions between loads and codes).  There the next row's loads ahead of the
+// reductions took it from 98 to 74, types as template parameters to 69, weights through the first-level cache to 64, one rounding of the new residual for
+// the store and the sum to 62, maxima by one instruction a warp to 60, the next row through shared memory to 56.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "common.cuh"
 #include "device_utils.cuh"
+#include "kv_cache.cuh"
 
 namespace bitnet {
 namespace {
 
+constexpr int MOST_STAGED = 64 * 1024;    // bytes of a row in shared memory: 8192 elements of x and residual, or 16384 of x
 constexpr int64_t MOST_K = 8 * 16384;     // a cluster of 8 CTAs of 1024 threads with four pieces each
 
 struct NormDev {
@@ -79,21 +81,21 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   if (lane == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = lane < (int)(blockDim.x >> 5) ? red[lane] : 0.0;
+  const int slot = blockDim.x > 512 ? lane : lane & 15;
+  v = slot < (int)(blockDim.x >> 5) ? red[slot] : 0.0;
+  if (blockDim.x > 512) v += __shfl_xor_sync(0xffffffffu, v, 16);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 __device__ __forceinline__ float block_max(float v, float* red) {
+  // (numbers from 0 on: their bits are in the same order)
   const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
   if (lane == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
   v = lane < (int)(blockDim.x >> 5) ? red[lane] : 0.0f;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
 // In thread 0.
 __device__ __forceinline__ int sum_of_codes(int v, int* red) {
@@ -177,6 +179,14 @@ __device__ __forceinline__ Raw<TYPE> narrow(const float4& v) {
   }
   return r;
 }
+// A thread's piece on its way into shared memory, or from there.
+template <int TYPE>
+__device__ __forceinline__ void copy_raw(uint32_t dst, const void* p, int64_t i) {
+  if constexpr (TYPE == BITNET_KV_F32)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(static_cast<const float*>(p) + i) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(static_cast<const uint16_t*>(p) + i) : "memory");
+}
 template <int TYPE>
 __device__ __forceinline__ void store_raw(void* p, int64_t i, const Raw<TYPE>& r) {
   if constexpr (TYPE == BITNET_KV_F32) *reinterpret_cast<uint4*>(static_cast<float*>(p) + i) = r.v;
@@ -186,8 +196,10 @@ __device__ __forceinline__ void store_raw(void* p, int64_t i, const Raw<TYPE>& r
 // VPT: pieces of 4 elements per thread; XT, RT: types of x and of the residual (or NONE).  A CTA takes every gridDim.x-th row, and
 // has the next one's loads on their way while it reduces and writes the present one.  WIDE: the CTAs of a cluster share a row; their sums and
 // maxima meet in every CTA's shared memory (a barrier of the cluster lies between any two uses of a place there).
-template <int VPT, int XT, int RT, bool WIDE>
-__global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant__ NormDev d) {
+// STAGED: the next row comes through shared memory, every thread's pieces by and for itself (which leaves two CTAs of 512 threads per SM the registers
+// to have much of a row's work under way: 4099 x 8192: 56 us against 60 by registers, with two rows on their way 63, with three CTAs per SM 62).
+template <int VPT, int XT, int RT, bool WIDE, bool STAGED>
+__global__ void __launch_bounds__(STAGED ? 512 : 1024, STAGED ? 2 : 1) add_rmsnorm_kernel(const __grid_constant__ NormDev d) {
   const NormArgs& a = d.a;
   __shared__ Red red;
   int ctas = 1, rank = 0;
@@ -204,6 +216,25 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
   asm volatile("griddepcontrol.wait;" ::: "memory");
   Raw<XT> x[VPT];
   Raw<RT> e[VPT];
+  extern __shared__ __align__(16) uint8_t staged[];        // the pieces of x, then those of the residual
+  constexpr int XB = (int)sizeof(Raw<XT>), EB = RT == NONE ? 0 : (int)sizeof(Raw<RT>);
+  uint8_t* const x_at = staged + tid * XB;
+  uint8_t* const e_at = staged + VPT * nt * XB + tid * EB;
+  auto copy = [&](int64_t t) {
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int i = from + tid + k * nt;
+      if (i < n4) copy_raw<XT>(smem_u32(x_at) + k * nt * XB, a.x, t * a.stride_x + 4 * (int64_t)i);
+    }
+    if constexpr (RT != NONE) {
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int i = from + tid + k * nt;
+        if (i < n4) copy_raw<RT>(smem_u32(e_at) + k * nt * EB, a.residual, t * a.stride_residual + 4 * (int64_t)i);
+      }
+    }
+    cp_commit();
+  };
   auto fetch = [&](int64_t t) {
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
@@ -220,8 +251,17 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
   };
   int64_t t = blockIdx.x / ctas;
   bool met = !WIDE;
-  fetch(t);
+  if constexpr (STAGED) copy(t);
+  else fetch(t);
   for (;;) {
+    if constexpr (STAGED) {
+      cp_wait<0>();
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        x[k] = *reinterpret_cast<const Raw<XT>*>(x_at + k * nt * XB);
+        if constexpr (RT != NONE) e[k] = *reinterpret_cast<const Raw<RT>*>(e_at + k * nt * EB);
+      }
+    }
     float4 h[VPT];
     double sum = 0.0;
 #pragma unroll
@@ -242,7 +282,10 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const __grid_constant
       sum = fma((double)h[k].w, (double)h[k].w, sum);
     }
     const int64_t next = t + rows_at_once;
-    if (next < a.T) fetch(next);
+    if (next < a.T) {
+      if constexpr (STAGED) copy(next);          // (in the place of values that have been used above)
+      else fetch(next);
+    }
     float4 w[VPT <= 2 ? VPT : 1];                // (few pieces: the weights come with the row, ahead of the reductions)
     if constexpr (VPT <= 2) {
 #pragma unroll
@@ -355,21 +398,30 @@ int threads_for(int64_t pieces) {               // whole warps
   return (int)(n < 64 ? 64 : n > 1024 ? 1024 : n);
 }
 
-template <int VPT, int XT, bool WIDE>
+template <int VPT, int XT, int RT, bool WIDE, bool STAGED>
+cudaError_t launch_one(const NormDev& d, const cudaLaunchConfig_t& cfg) {
+  auto kernel = add_rmsnorm_kernel<VPT, XT, RT, WIDE, STAGED>;
+  if (STAGED) {
+    static std::atomic<uint64_t> have{0};
+    if (allow_smem(kernel, MOST_STAGED, &have) != BITNET_OK) return cudaErrorInvalidValue;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, d);
+}
+template <int VPT, int XT, bool WIDE, bool STAGED>
 cudaError_t launch_residual(const NormDev& d, const cudaLaunchConfig_t& cfg) {
-  if (!d.a.residual) return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, NONE, WIDE>, d);
-  switch (d.a.residual_type) {
-    case BITNET_KV_F32: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F32, WIDE>, d);
-    case BITNET_KV_BF16: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_BF16, WIDE>, d);
-    default: return cudaLaunchKernelEx(&cfg, add_rmsnorm_kernel<VPT, XT, BITNET_KV_F16, WIDE>, d);
+  if (VPT == 8 || !d.a.residual) return launch_one<VPT, XT, NONE, WIDE, STAGED>(d, cfg);
+  if constexpr (VPT < 8) switch (d.a.residual_type) {
+    case BITNET_KV_F32: return launch_one<VPT, XT, BITNET_KV_F32, WIDE, STAGED>(d, cfg);
+    case BITNET_KV_BF16: return launch_one<VPT, XT, BITNET_KV_BF16, WIDE, STAGED>(d, cfg);
+    default: return launch_one<VPT, XT, BITNET_KV_F16, WIDE, STAGED>(d, cfg);
   }
 }
-template <int VPT, bool WIDE>
+template <int VPT, bool WIDE, bool STAGED>
 cudaError_t launch_x(const NormDev& d, const cudaLaunchConfig_t& cfg) {
   switch (d.a.x_type) {
-    case BITNET_KV_F32: return launch_residual<VPT, BITNET_KV_F32, WIDE>(d, cfg);
-    case BITNET_KV_BF16: return launch_residual<VPT, BITNET_KV_BF16, WIDE>(d, cfg);
-    default: return launch_residual<VPT, BITNET_KV_F16, WIDE>(d, cfg);
+    case BITNET_KV_F32: return launch_residual<VPT, BITNET_KV_F32, WIDE, STAGED>(d, cfg);
+    case BITNET_KV_BF16: return launch_residual<VPT, BITNET_KV_BF16, WIDE, STAGED>(d, cfg);
+    default: return launch_residual<VPT, BITNET_KV_F16, WIDE, STAGED>(d, cfg);
   }
 }
 
@@ -392,11 +444,17 @@ int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
   int vpt = a.T * ctas > 2 * sms ? 4 : 1;
   while (vpt < 4 && ceil_div(n4, vpt) > 1024) vpt *= 2;
   if (ctas > 1 && vpt < 2) vpt = 2;
+  // Many rows come through shared memory, two CTAs or more to an SM, except longer ones with a residual, as eight pieces a thread would take more registers
+  // than there are (4096 x 14336, bf16: 114 us against 104; without a residual 65 against 73) or 64 KB a row (4096 x 8192, both fp32: 79 against 75).
+  const int64_t bytes4 = 4 * ((a.x_type == BITNET_KV_F32 ? 4 : 2) + (!a.residual ? 0 : a.residual_type == BITNET_KV_F32 ? 4 : 2));
+  const bool staged = vec && ctas == 1 && a.T > 2 * sms && (!a.residual || (n4 <= 2048 && n4 * bytes4 <= 48 * 1024));
+  if (staged && n4 > 2048) vpt = 8;
   const int threads = threads_for(vec ? ceil_div(n4, vpt) : n4);
   const int64_t resident = sms * (1024 / threads) / ctas;          // rows that CTAs of 64 registers a thread hold at a time
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((vec && a.T > resident ? resident : a.T) * ctas));
   cfg.blockDim = dim3((unsigned)threads);
+  if (staged) cfg.dynamicSmemBytes = (size_t)(threads * vpt * bytes4);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int attrs = 0;
@@ -415,10 +473,11 @@ int launch_add_rmsnorm(const NormArgs& a, cudaStream_t st) {
   if (log_enabled()) log_launch("add_rmsnorm T=%lld K=%lld vec=%d vpt=%d ctas=%d", (long long)a.T, (long long)a.K, (int)vec, vpt, ctas);
   cudaError_t e;
   if (!vec) e = cudaLaunchKernelEx(&cfg, add_rmsnorm_any_kernel, d);
-  else if (ctas > 1) e = vpt == 2 ? launch_x<2, true>(d, cfg) : launch_x<4, true>(d, cfg);
-  else if (vpt == 1) e = launch_x<1, false>(d, cfg);
-  else if (vpt == 2) e = launch_x<2, false>(d, cfg);
-  else e = launch_x<4, false>(d, cfg);
+  else if (ctas > 1) e = vpt == 2 ? launch_x<2, true, false>(d, cfg) : launch_x<4, true, false>(d, cfg);
+  else if (staged) e = vpt == 4 ? launch_x<4, false, true>(d, cfg) : launch_x<8, false, true>(d, cfg);
+  else if (vpt == 1) e = launch_x<1, false, false>(d, cfg);
+  else if (vpt == 2) e = launch_x<2, false, false>(d, cfg);
+  else e = launch_x<4, false, false>(d, cfg);
   return e == cudaSuccess ? check_launch() : note_cuda_error(e);
 }
 
