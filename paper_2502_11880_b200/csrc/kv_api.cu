@@ -22,8 +22,8 @@ std::atomic<int> g_shared_always{0};                // bitnet_debug_attn_shared
 
 // Whether a shared call is one for the decode kernel, which reads a prefix once for every sequence, from L2 all but the first time, but in one launch: at
 // most 16 tiles (64 tokens of a kv head) per SM beyond twice the groups' share, going by what rows of the table, or their windows, may hold.
-// Measured, decode / shared (us), sequences x prefix: 32/8 heads of 128: 8 x 2048: 19/28, 8 x 4096: 29/31, 16 x 4096: 47/32, 2 x 16384: 29/44; 16/16 heads of
-// 96: 8 x 1024: 20/26, 8 x 2048: 33/28; 12/4 heads of 64: 8 x 4096: 17/25, 32 x 4096: 40/25.
+// Measured, decode / shared (us), sequences x prefix: 32/8 heads of 128: 8 x 2048: 19/27, 8 x 4096: 29/29, 16 x 4096: 46/30, 3 x 32768: 63/67, 4 x 16384:
+// 50/41; 16/16 heads of 96: 2 x 16384: 65/58, 4 x 2048: 22/26, 8 x 2048: 33/26; 12/4 heads of 64: 8 x 4096: 17/24, 32 x 4096: 40/25.
 bool light(const AttnArgs& a, const bitnet_kv_cache_t* c) {
   if (g_shared_always.load(std::memory_order_relaxed)) return false;
   int64_t tokens = a.table_width * c->page_size;
