@@ -277,8 +277,8 @@ __device__ __forceinline__ bool has_unseen(const PromptArgs& a, const Item& x, i
 // KT: element type of q, the pools and out; HALVES: 64-column halves of a padded row.
 //
 // SHARED: the part of single tokens' attention that groups of sequences have in common (attn_shared).  Rows are (sequence, query head) pairs of
-// one group and kv head, the columns the group's prefix, read through the pages of its first sequence; no order between rows and columns, but a row sees
-// no more than its sequence has, and what its window leaves.  All groups' items form one list of (item, block) that is cut into equal
+// one group and kv head, the columns the group's prefix, read through the pages of its first sequence that has any; no order between rows and columns, but a
+// row sees no more than its sequence has, and what its window leaves.  All groups' items form one list of (item, block) that is cut into equal
 // contiguous parts, one per CTA; an item's first part goes to its rows' places in the workspace, a later one (a CTA has one at most, at its beginning) to
 // the CTA's, both as maximum, sum and unscaled O.  Two kernels that follow take each sequence's own tokens and join (attn_shared.cu).
 // Bound by the softmax's exponentials and, where CTAs have few blocks, by their start: 64 sequences over 16384 tokens, 64/8 heads of 128, bf16: 45 us, of
@@ -483,8 +483,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           const int who = __ffs(here) - 1;
           const int q0 = __shfl_sync(0xffffffffu, mine_g.q0, who), n = __shfl_sync(0xffffffffu, mine_g.n, who), nb = __shfl_sync(0xffffffffu, mine_g.nb, who);
           const int64_t in_group = local - __shfl_sync(0xffffffffu, mine_g.before, who), id = in_group / nb;
+          // the sequence through whose row the prefix is read: the group's first that has tokens (a finished sample's row is empty)
+          int reader = q0;
+          for (int i = 0; i < n; i += 32) {
+            const unsigned live = __ballot_sync(0xffffffffu, i + lane < n && __ldg(a.kv_len + q0 + i + lane) > 0);
+            if (!live) continue;
+            reader = q0 + i + __ffs(live) - 1;
+            break;
+          }
           Item t;
-          t.seq = q0;
+          t.seq = reader;
           t.q0 = q0;
           t.n_new = n;
           const int hb = (int)(id % heads), b0 = hb % a.blocks * a.per_block;

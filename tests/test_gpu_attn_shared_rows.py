@@ -1,0 +1,51 @@
+"""Which row of the table a shared prefix is read through, where rows of its group are empty or have given up pages."""
+import pytest
+import torch
+
+import paper_2502_11880_b200 as bn
+from kv_ref import attn_ref, check_attn
+from test_gpu_attn_shared import BF, HF, PROMPT_P, Groups, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, params=["as it goes", "always shared"])
+def path(request):
+    bn.bitnet_debug_attn_shared(request.param == "always shared")
+    yield request.param
+    bn.bitnet_debug_attn_shared(False)
+
+
+def check(s, q, window=0, sinks=0):
+    """Against 64 bits, through every sequence's own row; nothing is reported, rows without tokens are 0."""
+    status, scale = ints([0]), s.cache.head_dim ** -0.5
+    out = bn.bitnet_attn_shared(s.cache, 1, q, s.table, s.len, s.start, s.prefix, window=window, sinks=sinks, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and bn.bitnet_device_status() == 0
+    lens = s.len.tolist()
+    check_attn(out, attn_ref(s.k[1], s.v[1], q, s.table, [n - 1 for n in lens], range(len(lens)), scale, window, sinks), PROMPT_P[s.cache.dtype])
+    assert all(bool((out[i] == 0).all()) for i, n in enumerate(lens) if n == 0)
+
+
+def free(s, rows):
+    """As bitnet_kv_free leaves them."""
+    for i in rows:
+        s.len[i] = 0
+        s.table[i] = -1
+
+
+@pytest.mark.parametrize("gone", [[0], [0, 1, 2], [0, 3, 6], [1, 5]])
+def test_a_finished_sample_does_not_take_its_group_along(gone):
+    """Samples end one after the other, the first ones too; the others go on."""
+    for groups, hq, hkv, dim, page, dtype in (([(333, [340, 345, 401, 390]), (128, [129, 200, 150])], 8, 2, 128, 16, BF),
+                                              ([(300, [320, 333, 310, 301]), (77, [80, 99, 90])], 4, 4, 96, 32, HF)):
+        s = Groups(groups, hkv, dim, page, dtype, seed=31)
+        free(s, gone)
+        check(s, s.queries(hq))
+
+
+def test_the_first_of_many_that_has_tokens():
+    """More sequences than are looked at at a time, in several items; all of another group are gone."""
+    s = Groups([(200, [210 + i % 50 for i in range(90)]), (64, [70, 80])], 1, 64, 16, BF, seed=32)
+    free(s, [*range(70), 90, 91])
+    check(s, s.queries(8))
