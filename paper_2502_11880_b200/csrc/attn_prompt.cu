@@ -413,11 +413,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             t.prefix = max(0, min(__ldg(a.prefix + g0 + lane), a.max_len));
           }
           if (a.window > 0) {
-            // what the window of the group's shortest sequence reaches back to
+            // what the window of the group's shortest sequence that has tokens reaches back to
             for (int k = 0; k < 32 && g0 + k < a.seqs; ++k) {
               const int q0 = __shfl_sync(0xffffffffu, t.q0, k), n = __shfl_sync(0xffffffffu, t.n, k);
               int least = 0x7fffffff;
-              for (int i = lane; i < n; i += 32) least = min(least, __ldg(a.kv_len + q0 + i));
+              for (int i = lane; i < n; i += 32) {
+                const int len = __ldg(a.kv_len + q0 + i);
+                if (len > 0) least = min(least, len);
+              }
               least = __reduce_min_sync(0xffffffffu, least);
               if (lane == k) t.lo = (int)max((int64_t)0, min((int64_t)least - a.window, (int64_t)a.max_len));
             }
@@ -513,10 +516,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           t.parts = 1;
           t.part = 0;
           t.unit0 = t.id = 0;
-          // the tokens that some row of the item sees: from its shortest sequence's window to its longest sequence's end
+          // the tokens that some row of the item sees: from its shortest sequence's window to its longest sequence's end, empty ones left out
           int least = 0x7fffffff, most = 0;
           for (int i = t.tok0 + lane; i < min(n, t.tok0 + span); i += 32) {
             const int len = __ldg(a.kv_len + q0 + i);
+            if (len <= 0) continue;
             least = min(least, len);
             most = max(most, len);
           }

@@ -49,3 +49,28 @@ def test_the_first_of_many_that_has_tokens():
     s = Groups([(200, [210 + i % 50 for i in range(90)]), (64, [70, 80])], 1, 64, 16, BF, seed=32)
     free(s, [*range(70), 90, 91])
     check(s, s.queries(8))
+
+
+def trimmed(s, window, sinks):
+    """As bitnet_kv_trim leaves the table, each row by its own length; what is given up holds anything."""
+    page = s.cache.page_size
+    kept = set()
+    for i, n in enumerate(s.len.tolist()):
+        for e in range(-(-n // page)):
+            if e * page >= sinks and (e + 1) * page <= n - window:
+                s.table[i, e] = -1
+        kept |= set(s.table[i].tolist())
+    gone = [p for p in range(s.cache.num_pages) if p not in kept]
+    for t in (s.k, s.v):
+        t[1, gone] = float("nan")
+
+
+@pytest.mark.parametrize("sinks", [0, 5])
+def test_an_empty_row_does_not_undo_the_window(sinks):
+    """What left the windows was given up: a row without tokens in the group (a padded batch) does not ask for it."""
+    for idle in ([2], [0], [1, 3], [0, 1, 2, 3]):
+        s = Groups([(900, [1000, 1000, 1000, 1000]), (640, [700] * 3)], 2, 64, 16, BF, seed=33)
+        for i in idle:
+            s.len[i], s.table[i] = 0, -1
+        trimmed(s, 200, sinks)
+        check(s, s.queries(8), window=200, sinks=sinks)
