@@ -603,7 +603,8 @@ int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const b
  * bitnet_attn_decode for sequences that share beginnings: forked samples of one prompt, requests over one document.  Sequences
  * group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1], ascending, group_start[0] = 0, group_start[groups] = seqs) have their first prefix_len[g] tokens
  * (int32 [groups]; 0: none) in common: those are read through the row of the table of the group's first sequence that has tokens (kv_len above 0: the first may
- * be finished and freed), once for the whole group, on the tensor cores; every sequence's own tokens after them through its own row.  (Where there is little to be saved the decode kernel takes the call and every sequence's tokens
+ * be finished and freed), with a window behind the sinks through the row of one that sees them (others may have given them up), once for the whole group, on the
+ * tensor cores; every sequence's own tokens after them through its own row.  (Where there is little to be saved the decode kernel takes the call and every sequence's tokens
  * are read through its own row: all rows of a group have to hold the prefix's pages.)  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
  * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
  * and that the probabilities of the prefix may be rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.

@@ -357,11 +357,36 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       uint32_t kb = 0, kb_v = 0;                             // fills of K, of V so far
       // The blocks of an item; false: somebody has given up.
       auto copy_blocks = [&](const Item& x) -> bool {
+        // SHARED: with a window, the sequence that the lane's last box was read through, and its length
+        int reader = x.seq, reader_len = -1;
         auto look_up = [&](int j, int& y) -> int {
           const int tok = block_start(x, j) + box * box_rows;
           y = tok & ((1 << a.page_shift) - 1);
           if (!mine || tok > x.p_last || (tok >= a.sinks && tok + box_rows <= x.lo)) return -2;   // seen by no row
-          return max(__ldg(a.table + (int64_t)x.seq * a.table_width + (tok >> a.page_shift)), -1);
+          int seq = x.seq;
+          if constexpr (SHARED) {
+            if (a.window > 0 && tok >= a.sinks) {
+              // Rows may have given up what left their own windows: a sequence of the group whose window holds what is read of the box, or else
+              // the longest that sees some of it.  (Neighbouring boxes have the same one nearly always.)
+              const int upto = min(tok + box_rows, x.p_last + 1);
+              auto holds = [&](int len) { return len >= upto && (int64_t)len - a.window < upto; };
+              if (!holds(reader_len)) {
+                reader_len = -1;
+                for (int i = 0; i < x.n_new; ++i) {
+                  const int len = __ldg(a.kv_len + x.q0 + i);
+                  const bool all = holds(len);
+                  if (all || (len > tok && len > reader_len && (int64_t)len - a.window < upto)) {
+                    reader = x.q0 + i;
+                    reader_len = len;
+                  }
+                  if (all) break;
+                }
+              }
+              if (reader_len < 0) return -3;                       // between the windows: seen by no row, but not cleared either
+              seq = reader;
+            }
+          }
+          return max(__ldg(a.table + (int64_t)seq * a.table_width + (tok >> a.page_shift)), -1);
         };
         int y = 0, page = x.nb > 0 ? look_up(0, y) : 0;
         const int n_stop = (int)min((int64_t)x.nb, (int64_t)(a.give_up - kb));
@@ -370,8 +395,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           const int cur = page, cur_y = y;
           if (j + 1 < x.nb) page = look_up(j + 1, y);
           const bool issue = cur != -2;
-          const bool bad = issue && (cur < 0 || cur >= a.num_pages);
-          if (bad && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
+          const bool bad = issue && (cur < 0 || cur >= a.num_pages);   // (read as zeros)
+          if (bad && cur != -3 && a.dev_status) atomicExch(a.dev_status, BITNET_ERR_BAD_PAGE);
           const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, issue)) * box_bytes;
           const int st = kb_v % STAGES;
           const uint32_t par = ((kb_v / STAGES) & 1u) ^ 1u;

@@ -74,3 +74,16 @@ def test_an_empty_row_does_not_undo_the_window(sinks):
             s.len[i], s.table[i] = 0, -1
         trimmed(s, 200, sinks)
         check(s, s.queries(8), window=200, sinks=sinks)
+
+
+@pytest.mark.parametrize("window,sinks", [(200, 0), (200, 5), (64, 70), (333, 1)])
+def test_rows_that_have_given_up_different_pages(window, sinks):
+    """Sequences of very different lengths, each trimmed by its own: what one gave up another still sees."""
+    for groups, hq, hkv, dim, page, dtype in (([(900, [1400, 950, 1000, 930])], 8, 2, 64, 16, BF),
+                                              ([(900, [1400, 300, 1000, 600, 20]), (640, [700, 641])], 8, 8, 96, 32, HF),         # gaps between windows
+                                              ([(910, [2000, 905, 0, 1050, 911])], 8, 2, 128, 16, BF),                             # part of a page
+                                              ([(1200, [1900 - 12 * i for i in range(80)])], 4, 1, 64, 128, BF),                   # several items
+                                              ([(1200, [1900, 1700, 1210])], 4, 1, 64, 256, HF)):
+        s = Groups(groups, hkv, dim, page, dtype, seed=34)
+        trimmed(s, window, sinks)
+        check(s, s.queries(hq), window=window, sinks=sinks)
