@@ -1,4 +1,4 @@
-"""Which row of the table a shared prefix is read through, where rows of its group are empty or have given up pages."""
+"""Which row of the table a shared prefix is read through, where rows of its group are empty or have given up pages; one long sequence among many short ones."""
 import pytest
 import torch
 
@@ -87,3 +87,26 @@ def test_rows_that_have_given_up_different_pages(window, sinks):
         s = Groups(groups, hkv, dim, page, dtype, seed=34)
         trimmed(s, window, sinks)
         check(s, s.queries(hq), window=window, sinks=sinks)
+
+
+def test_one_long_sequence_among_many(path):
+    """More rows than warps, one of them with nearly all tokens: it is taken by all warps, not by one after the other."""
+    s = Groups([(64, [70 + i % 30 for i in range(600)]), (0, [9000])], 4, 64, 16, BF, seed=35)
+    q = s.queries(8)
+    check(s, q)
+    if path == "always shared":
+        ws, out = bn.new_attn_shared_workspace(601, 8, 4, 64), torch.empty_like(q)
+        # some 48 us where its 563 tiles of a head are shared out, 390 where a warp has them all; the decode kernel takes 46
+        times = []
+        for run in (lambda: bn.bitnet_attn_shared(s.cache, 1, q, s.table, s.len, s.start, s.prefix, out=out, workspace=ws),
+                    lambda: bn.bitnet_attn_decode(s.cache, 1, q, s.table, s.len, out=out, workspace=ws)):
+            best = float("inf")
+            for _ in range(20):
+                a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+                a.record()
+                run()
+                b.record()
+                torch.cuda.synchronize()
+                best = min(best, a.elapsed_time(b))
+            times.append(best)
+        assert times[0] < 2 * times[1], times
