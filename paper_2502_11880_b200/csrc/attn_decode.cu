@@ -60,6 +60,7 @@ struct DecodeArgs {
   float* part_o;                              // [2 * grid][8][D]
   int* dev_status;
   uint32_t give_up;                           // (test hook) the tile before which a CTA gives up
+  const int* route;                           // not 0 there: the kernels of shared prefixes take the call; null: they do not
 };
 
 // The visible tokens of one row: [0, s_end) and [lo, len), as tiles; whether a window is that of a position beyond the table (whose
@@ -209,6 +210,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (a.route && __ldcg(a.route)) return;
 
   // ---- the list of tiles: total, this CTA's part [item, end), and the token it begins in
   const int rows_per_token = a.kv_heads * a.head_blocks;
@@ -820,6 +822,7 @@ int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   d.part_o = reinterpret_cast<float*>(w + slots * 8);
   d.dev_status = x.dev_status;
   d.give_up = x.give_up;
+  d.route = x.route;
   log_launch("attn_decode_kernel tokens=%d q_heads=%d kv_heads=%d head_dim=%d window=%d grid=%d", d.tokens, d.q_heads, d.kv_heads, d.head_dim,
              d.window, grid);
   if (x.dtype == BITNET_KV_BF16)

@@ -79,6 +79,7 @@ struct PromptArgs {
   float* base_o;                                      // [tokens][q_heads][padded head_dim]
   float2* spill_ml;                                   // [CTAs][2 tiles][128 rows]
   float* spill_o;                                     // [CTAs][2 tiles][128 rows][padded head_dim]
+  const int* route;                                   // 0 there: the decode kernel takes the call; null: it does not
 };
 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t saddr) {      // rows of 128 bytes, 128-byte swizzle
@@ -293,6 +294,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   volatile int* abort_flag = &s.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
+  if constexpr (SHARED) {
+    if (a.route) {                                          // (looked at before there is anything to be given back)
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      if (!__ldcg(a.route)) return;
+    }
+  }
   if (tid == 0) {
     kv_mbar_init(&s.q_full, 2);
     kv_mbar_init(&s.q_empty, 1);
@@ -1218,6 +1225,7 @@ int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& x, con
   a.base_o = p.base_o;
   a.spill_ml = p.spill_ml;
   a.spill_o = p.spill_o;
+  a.route = x.route;
   log_launch("attn_prompt_kernel (shared prefixes) sequences=%d groups=%d q_heads=%d kv_heads=%d head_dim=%d window=%d", a.tokens, a.seqs, a.q_heads,
              a.kv_heads, a.head_dim, a.window);
   return launch_types<true>(c, a, x.dtype, dev_info().sm_count, st);

@@ -101,6 +101,7 @@ struct OwnArgs {
   float* late_o;                              // [warps][8][padded]
   int padded;
   int* dev_status;
+  const int* route;                           // 0 there: the decode kernel takes the call; null: it does not
 };
 
 // A sequence's own tokens that its last token sees: [s_lo, s_hi) of the sinks and [lo, hi), as tiles.
@@ -151,6 +152,10 @@ __global__ void __launch_bounds__(OWN_THREADS, 1) attn_own_kernel(const __grid_c
   // ends after kernel 1, so that the join follows both.  (The three in turn: 80.7 and 42.6 us against 76.2 and 38.1.)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   auto others_done = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+  if (a.route && !__ldcg(a.route)) {
+    others_done();
+    return;
+  }
 
   // ---- the list of tiles: total, and where the warps' parts begin
   const int rows_per_seq = a.kv_heads * a.head_blocks;
@@ -434,6 +439,7 @@ struct JoinArgs {
   const int32_t* prefix_len;
   int64_t rows;
   int q_heads, group, per_block, tile_tokens, groups, head_dim, ctas;
+  const int* route;
 };
 
 template <typename KT>
@@ -443,7 +449,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const __grid
   const int tok = (int)kv_quotient(row, a.q_heads), head = (int)(row - (int64_t)tok * a.q_heads);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (row >= a.rows) return;
+  if (row >= a.rows || (a.route && !__ldcg(a.route))) return;
   const int d = 4 * lane;
   const bool mine = d < a.p.padded;
   const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -515,6 +521,60 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const __grid
       make_uint2(Two<KT>::pack(acc.x * inv, acc.y * inv), Two<KT>::pack(acc.z * inv, acc.w * inv));
 }
 
+// ------------------------------------------------------------------------------------------------ which kernels
+// Whether the groups share enough for the three kernels, in tiles of 64 tokens of a kv head: 3 R - T > limit, where T tiles are seen by all sequences and R of
+// them, of a group's prefix, by another sequence too.  One CTA: a warp per group, a thread per sequence.
+constexpr int ROUTE_THREADS = 1024;
+
+struct RouteArgs {
+  const int32_t *kv_len, *group_start, *prefix_len;
+  int seqs, groups, window, sinks, max_len;
+  int64_t limit;
+  int* route;
+};
+
+__global__ void __launch_bounds__(ROUTE_THREADS) attn_route_kernel(const __grid_constant__ RouteArgs a) {
+  __shared__ unsigned long long seen, again;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (tid == 0) seen = again = 0;
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // tiles of the first `most` tokens that a sequence's last token sees
+  auto tiles = [&](int len, int most) {
+    const int end = min(len, most);
+    if (end <= 0) return 0;
+    const int lo = a.window > 0 ? max(0, len - a.window) : 0;
+    const int tokens = lo >= end ? min(a.sinks, end) : min(a.sinks, lo) + end - lo;
+    return (int)(((int64_t)tokens + 63) / 64);
+  };
+  auto add = [&](unsigned long long& to, int64_t v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0 && v) atomicAdd(&to, (unsigned long long)v);
+  };
+  int64_t mine = 0;
+  for (int64_t i = tid; i < a.seqs; i += ROUTE_THREADS) mine += tiles(__ldg(a.kv_len + i), a.max_len);
+  add(seen, mine);
+  mine = 0;
+  for (int64_t g = tid >> 5; g < a.groups; g += ROUTE_THREADS / 32) {
+    const int q0 = __ldg(a.group_start + g), q1 = min(__ldg(a.group_start + g + 1), a.seqs);
+    if (q0 < 0 || q1 - (int64_t)q0 < 2) continue;
+    const int prefix = min(__ldg(a.prefix_len + g), a.max_len);
+    int top = 0;
+    for (int64_t i = q0 + lane; i < q1; i += 32) {
+      const int t = tiles(__ldg(a.kv_len + i), prefix);
+      mine += t;
+      top = max(top, t);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) mine -= top;                            // (read once in any case)
+  }
+  add(again, mine);
+  __syncthreads();
+  if (tid == 0) *a.route = 3 * (int64_t)again - (int64_t)seen > a.limit;
+}
+
 // ------------------------------------------------------------------------------------------------ launches
 template <typename K, typename A>
 int launch(K kernel, unsigned grid, int threads, int smem, cudaStream_t st, const A& a) {
@@ -551,6 +611,7 @@ struct Places {
   float4* own_ml;
   float *own_o, *late_o;
   float2* late_ml;
+  int* route;
   size_t bytes;
 };
 // The workspace: that of decode calls, then the rows' places, the CTAs' and the warps'.
@@ -572,6 +633,7 @@ Places places(uint8_t* at, int64_t rows, int head_dim) {
   x.own_ml = reinterpret_cast<float4*>(take(rows, 16));
   x.p.spill_ml = reinterpret_cast<float2*>(take(sms * 2 * ROWS, 8));
   x.late_ml = reinterpret_cast<float2*>(take(sms * OWN_WARPS * HEADS, 8));
+  x.route = reinterpret_cast<int*>(take(1, 16));
   x.bytes = (size_t)(at - begin);
   return x;
 }
@@ -582,10 +644,31 @@ size_t attn_shared_workspace_bytes(int64_t seqs, int64_t q_heads, int head_dim) 
   return attn_decode_workspace_bytes() + places(nullptr, seqs * q_heads, head_dim).bytes;
 }
 
-int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, cudaStream_t st) {
+int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& args, int64_t ask, void* ws, cudaStream_t st) {
+  AttnArgs x = args;
   const int64_t rows = x.tokens * x.q_heads;
   const Places w = places(attn_prompt_parts(ws), rows, c->head_dim);
-  int rc = launch_attn_shared_prefix(c, x, w.p, st);
+  const int64_t most = x.table_width * c->page_size;
+  const int max_len = most > 0x3fffff00 ? 0x3fffff00 : (int)most;     // (as for the prefixes)
+  int rc;
+  if (ask >= 0) {
+    RouteArgs r = {};
+    r.kv_len = x.kv_len;
+    r.group_start = x.group_start;
+    r.prefix_len = x.prefix_len;
+    r.seqs = (int)x.tokens;
+    r.groups = (int)x.groups;
+    r.window = x.window;
+    r.sinks = x.sinks;
+    r.max_len = max_len;
+    r.limit = ask;
+    r.route = w.route;
+    log_launch("attn_route_kernel sequences=%d groups=%d", r.seqs, r.groups);
+    rc = launch(attn_route_kernel, 1, ROUTE_THREADS, 0, st, r);
+    if (rc != BITNET_OK) return rc;
+    x.route = w.route;
+  }
+  rc = launch_attn_shared_prefix(c, x, w.p, st);
   if (rc != BITNET_OK) return rc;
 
   OwnArgs a = {};
@@ -613,8 +696,7 @@ int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   a.num_pages = (int)c->num_pages;
   a.window = x.window;
   a.sinks = x.sinks;
-  const int64_t most = x.table_width * c->page_size;
-  a.max_len = most > 0x3fffff00 ? 0x3fffff00 : (int)most;     // (as for the prefixes)
+  a.max_len = max_len;
   a.c = x.scale * 1.4426950408889634f;
   a.own_ml = w.own_ml;
   a.own_o = w.own_o;
@@ -622,6 +704,7 @@ int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   a.late_o = w.late_o;
   a.padded = w.p.padded;
   a.dev_status = x.dev_status;
+  a.route = x.route;
   log_launch("attn_own_kernel sequences=%d groups=%d q_heads=%d kv_heads=%d head_dim=%d window=%d", a.seqs, a.groups, a.q_heads, a.kv_heads,
              a.head_dim, a.window);
   rc = x.dtype == BITNET_KV_BF16 ? launch_own<__nv_bfloat16>(a, st) : launch_own<__half>(a, st);
@@ -644,9 +727,12 @@ int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& x, void* ws, 
   j.tile_tokens = ROWS / j.per_block;
   j.head_dim = c->head_dim;
   j.ctas = dev_info().sm_count;
+  j.route = x.route;
   const unsigned grid = (unsigned)ceil_div(rows, JOIN_WARPS);
-  return x.dtype == BITNET_KV_BF16 ? launch(attn_join_kernel<__nv_bfloat16>, grid, JOIN_WARPS * 32, 0, st, j)
-                                   : launch(attn_join_kernel<__half>, grid, JOIN_WARPS * 32, 0, st, j);
+  rc = x.dtype == BITNET_KV_BF16 ? launch(attn_join_kernel<__nv_bfloat16>, grid, JOIN_WARPS * 32, 0, st, j)
+                                 : launch(attn_join_kernel<__half>, grid, JOIN_WARPS * 32, 0, st, j);
+  if (rc != BITNET_OK || ask < 0) return rc;
+  return launch_attn_decode(c, x, ws, st);
 }
 
 }  // namespace bitnet

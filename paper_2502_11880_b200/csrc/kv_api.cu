@@ -20,16 +20,25 @@ int64_t clamp_int(int64_t x) { return x < MOST ? x : MOST; }
 std::atomic<uint32_t> g_give_up{0xffffffffu};       // bitnet_debug_attn_give_up
 std::atomic<int> g_shared_always{0};                // bitnet_debug_attn_shared
 
-// Whether a shared call is one for the decode kernel, which reads a prefix once for every sequence, from L2 all but the first time, but in one launch: at
-// most 16 tiles (64 tokens of a kv head) per SM beyond twice the groups' share, going by what rows of the table, or their windows, may hold.
-// Measured, decode / shared (us), sequences x prefix: 32/8 heads of 128: 8 x 2048: 19/27, 8 x 4096: 29/29, 16 x 4096: 46/30, 3 x 32768: 63/67, 4 x 16384:
-// 50/41; 16/16 heads of 96: 2 x 16384: 65/58, 4 x 2048: 22/26, 8 x 2048: 33/26; 12/4 heads of 64: 8 x 4096: 17/24, 32 x 4096: 40/25.
-bool light(const AttnArgs& a, const bitnet_kv_cache_t* c) {
-  if (g_shared_always.load(std::memory_order_relaxed)) return false;
+// Which kernels take a shared call.  The decode kernel reads a prefix once for every sequence, from L2 all but the first time, but in one launch and, tile by
+// tile (64 tokens of a kv head), in some two thirds of the time.  With T tiles read by all sequences, R of them again for another sequence of a group, the
+// shared kernels are faster where 3 R - T > 2 X: X = 32 tiles per SM, 16 where every query head has a kv head of its own, for which the decode kernel takes
+// longer.  The host knows the numbers of sequences and groups, and bounds the tokens by the table's width or the window.  It can tell where the groups, if
+// they are alike, share enough, and where even all sequences in one group would save less than asking costs.  In between (most sequences alone, groups that are
+// empty) the device is asked, which knows lengths and prefixes: two more launches, and the kernels that do not take the call end at once, 4 to 7 us.
+// Measured, decode / shared (us): 32/8 heads of 128: 8 over 2048: 19/32, 8 over 4096: 29/33, 16 over 4096: 45/33, 64 over 2048: 82/35; 8 groups of 3 over 2048: 40/47,
+// 32 of them 125/95; groups of 2 over 16384: 4: 89/104, 8: 167/165, 32: 656/485; 64 over 16384 and 64 alone with up to 600: 774/108, asked 112; 64 alone over 2048:
+// 97/155, asked 104; 16/16 heads of 96: 4 over 2048: 22/26, 4 over 4096: 36/30, 8 over 2048: 33/29; 2 groups of 2 over 16384: 120/95, 64 of 2 over 2048: 406/264.
+enum class Route { DECODE, SHARED, ASK };
+Route route_of(const AttnArgs& a, const bitnet_kv_cache_t* c, int64_t* limit) {
+  const int64_t rows = c->kv_heads * ceil_div(a.q_heads / c->kv_heads, 8);
+  *limit = 2 * (a.q_heads == c->kv_heads ? 16 : 32) * (int64_t)dev_info().sm_count / rows;
+  if (g_shared_always.load(std::memory_order_relaxed)) return Route::SHARED;
   int64_t tokens = a.table_width * c->page_size;
   if (a.window > 0) tokens = std::min(tokens, (int64_t)a.window + a.sinks + 64);
-  const double rows = (double)c->kv_heads * ceil_div(a.q_heads / c->kv_heads, 8);
-  return rows * ceil_div(tokens, 64) * (double)(a.tokens - 2 * a.groups) <= 16.0 * dev_info().sm_count;
+  const double tiles = (double)ceil_div(tokens, 64);
+  if (tiles * (double)(2 * a.tokens - 3 * a.groups) > (double)*limit) return Route::SHARED;
+  return tiles * (double)(2 * a.tokens - 3) <= 2.0 * (double)*limit ? Route::DECODE : Route::ASK;
 }
 
 // The books: table[seqs][width] and refs[num_pages].
@@ -87,6 +96,7 @@ int attn_args(const bitnet_kv_cache_t* c, int64_t layer, const void* q, int io_d
   a->give_up = g_give_up.load(std::memory_order_relaxed);
   a->group_start = a->prefix_len = nullptr;
   a->groups = 0;
+  a->route = nullptr;
   return BITNET_OK;
 }
 
@@ -310,8 +320,10 @@ int bitnet_attn_shared(const bitnet_kv_cache_t* c, int64_t layer, const void* q,
   a.group_start = group_start;
   a.prefix_len = prefix_len;
   a.groups = groups;
-  if (light(a, c)) return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
-  return launch_attn_shared(c, a, workspace, (cudaStream_t)stream);
+  int64_t limit;
+  const Route route = route_of(a, c, &limit);
+  if (route == Route::DECODE) return launch_attn_decode(c, a, workspace, (cudaStream_t)stream);
+  return launch_attn_shared(c, a, route == Route::ASK ? limit : -1, workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -62,6 +62,7 @@ struct AttnArgs {
   const int32_t* group_start;   // [groups + 1]
   const int32_t* prefix_len;    // [groups]
   int64_t groups;
+  const int* route;             // set on the device (1: the kernels of shared prefixes take the call, 0: the decode kernel); null: one of them is meant
 };
 // Where attn_shared keeps what rows (a sequence and a query head) have of their group's prefix between its kernels: of an item's first part at the rows'
 // places, of a later part at the places of the CTA that has it (attn_prompt.cu).
@@ -86,7 +87,8 @@ size_t attn_prompt_parts_bytes(int64_t tokens, int q_heads, int kv_heads);
 int launch_attn_decode(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
 int launch_attn_prompt(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, size_t ws_bytes, cudaStream_t st);
 int launch_attn_shared_prefix(const bitnet_kv_cache_t* c, const AttnArgs& a, const SharedParts& p, cudaStream_t st);
-int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& a, void* ws, cudaStream_t st);
+// ask >= 0: the device weighs what the groups share against that many tiles, and one of this and the decode kernel takes the call.
+int launch_attn_shared(const bitnet_kv_cache_t* c, const AttnArgs& a, int64_t ask, void* ws, cudaStream_t st);
 
 int launch_kv_append(const KvView& kv, int layer, const void* k, const void* v, int in_dtype, int64_t stride_token, int64_t stride_head,
                      int64_t tokens, int64_t seqs, const int32_t* table, int64_t width, const int32_t* kv_len, const int32_t* q_start,
