@@ -567,7 +567,7 @@ int bitnet_add_rmsnorm_quant(const void* x, int x_type, int64_t stride_x, const 
  *                         between (1 - s) f / factor + s f with s = (n - low) / (high - low).
  *   freqs (HOST, rot_dim / 2 values, radians per position; read by bitnet_rope_init only) takes the place of all of that.
  *   magnitude multiplies the sines and cosines (0 means 1).
- * Angles are right to 2^-26 of a turn at every position.  The description is plain host data, completed by bitnet_rope_init; it may be copied
+ * Angles are right to 2^-26 of a turn at every position (given frequencies: of up to 64 turns a position).  The description is plain host data, completed by bitnet_rope_init; it may be copied
  * and is read during a call only.
  */
 enum { BITNET_ROPE_NONE = 0, BITNET_ROPE_LINEAR = 1, BITNET_ROPE_BANDS = 2 };

@@ -6,8 +6,8 @@
 // where pair i of a row is (x[i], x[i + rot/2]) or (x[2i], x[2i + 1]); elements from rot on move as they are.
 //
 // Angles: a frequency is held as the fraction of a turn per position in 64-bit fixed point, so that position * frequency modulo a turn is
-// one integer product that wraps around by itself, right to 2^-33 of a turn at any position; its top 32 bits go to sincospi as half turns in
-// binary32, right to 2^-26 of a turn.
+// one integer product that wraps around by itself, right to 2^-32 of a turn at any position (the steps are right to one unit of 2^-64); its top 32
+// bits go to sincospi as half turns in binary32, right to 2^-26 of a turn.
 // (binary32 products would be off by 0.008 radians at position 131072, and a table of all positions is 67 MB that has to be read.)
 // The products and sums are binary32, rounded once to the type written.
 //

@@ -1,5 +1,6 @@
 // C ABI of the norm, the rotation's description and the drawing of tokens: argument checks and dispatch.
 #include <cmath>
+#include <limits>
 
 #include "common.cuh"
 
@@ -74,26 +75,30 @@ int bitnet_rope_init(bitnet_rope_t* r) {
     if (r->scaling == BITNET_ROPE_BANDS && !(r->high > r->low && r->context > 0.0 && std::isfinite(r->high) && std::isfinite(r->low) && std::isfinite(r->context)))
       return BITNET_ERR_INVALID_ARG;
   }
-  constexpr double TAU = 6.283185307179586;
+  // In 64 bits of mantissa: a step is right to one unit of 2^-64 of a turn.  (53 bits were off by 2^-24 of a turn at positions near 2^31.)
+  using Wide = long double;
+  static_assert(std::numeric_limits<Wide>::digits >= 64, "");
+  constexpr Wide TAU = 6.283185307179586476925286766559005768L;
   for (int i = 0; i < 64; ++i) {
     r->step[i] = 0;
     if (i >= r->rot_dim / 2) continue;
-    double f;
+    Wide f;
     if (r->freqs) {
       f = r->freqs[i];
     } else {
-      f = std::pow(r->base, -2.0 * i / r->rot_dim);
+      f = std::pow((Wide)r->base, (Wide)(-2 * i) / r->rot_dim);
       if (r->scaling == BITNET_ROPE_LINEAR) f /= r->factor;
       if (r->scaling == BITNET_ROPE_BANDS) {
-        double s = (f * r->context / TAU - r->low) / (r->high - r->low);
-        s = s < 0.0 ? 0.0 : s > 1.0 ? 1.0 : s;
-        f = (1.0 - s) * f / r->factor + s * f;
+        Wide s = (f * r->context / TAU - r->low) / ((Wide)r->high - r->low);
+        s = s < 0 ? 0 : s > 1 ? 1 : s;
+        f = (1 - s) * f / r->factor + s * f;
       }
     }
-    if (!std::isfinite(f)) return BITNET_ERR_INVALID_ARG;
-    double turns = f / TAU;
+    if (!std::isfinite((double)f)) return BITNET_ERR_INVALID_ARG;
+    Wide turns = f / TAU;
     turns -= std::floor(turns);                            // [0, 1]; backwards is forwards by the rest of a turn
-    r->step[i] = turns >= 1.0 ? 0 : (uint64_t)std::ldexp(turns, 64);
+    turns = std::round(std::ldexp(turns, 64));
+    r->step[i] = turns >= std::ldexp((Wide)1, 64) ? 0 : (uint64_t)turns;
   }
   if (r->magnitude == 0.0) r->magnitude = 1.0;
   r->ready = READY;
