@@ -629,7 +629,8 @@ int bitnet_attn_shared(const bitnet_kv_cache_t* cache, int64_t layer, const void
  *   temperature <= 0 or not a number: the largest logit of lowest index, prob 1.  tokens[rows] int32; prob[rows] fp32, nullable.
  * A logit that is no number counts as -infinity, which is never drawn; infinite ones share all weight.  A row of nothing but those gives token -1, prob 0.
  * Weights are kept as 32-bit fixed point of the largest (those below 2^-33 of it count as 0), and added exactly: the token does not depend on rows, strides or
- * how the work is split.  vocab at most 2^30.
+ * how the work is split.  A weight is right to 2^-22 of itself, of 16-bit logits to 2^-22 + 2^-24 (max x - x) / temperature; a max x - x beyond binary32's range
+ * counts as infinite, whatever the temperature.  vocab at most 2^30.
  */
 int bitnet_sample(const void* logits, int type, int64_t stride, int64_t rows, int64_t vocab, const float* u, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* prob, void* stream);

@@ -17,7 +17,8 @@
 //   * the sum of what is kept per warp's stretch of the vocabulary; the warp whose stretch holds the token walks it.
 // Sums: weights as 32-bit fixed point of the largest (weights below 2^-33 of it count as 0, are never drawn), added as integers of
 // 64 bits: no sum depends on an order, a split or the size of the cluster.  The exponent is computed with the rounding errors of
-// max - x and of the product carried along, so that a weight is off by the exponential's own 2^-22 only.
+// the product and, for fp32 logits, of max - x carried along, so that a weight is off by the exponential's own 2^-22 only; of 16-bit logits by what max - x
+// loses as well, 2^-24 (max - x) / T, 2^-19.5 for the least weight that counts.  (To carry that too takes 256 x 50021 from 79 to 85 us.)
 //
 // Bound by barriers for few rows and by instructions for many: some 35 an item for its weight and its bin.  Measured (us, a B200): 1 x 32000, fp32, top-k 50,
 // top-p 0.9: 8.4 (14 without the short list); 64 x 128256, fp32, settings per row: 59 (HBM needs 5); 256 x 50021, bf16, top-p 0.92: 79 (HBM needs 4).
@@ -143,12 +144,12 @@ struct Weigh {
     d = top - x;
     return d * c;
   }
-  // The weight in units of 2^-32.  `exact`: max - x has no rounding error that matters (16-bit logits).
-  template <bool EXACT>
+  // The weight in units of 2^-32.  SHORT: max - x as it is rounded (16-bit logits).
+  template <bool SHORT>
   __device__ __forceinline__ float weight(float x, float d, float t) const {
     float low = fmaf(d, c, -t);
     low = fmaf(d, c_lo, low);
-    if (!EXACT) {
+    if (!SHORT) {
       const float b = d - top;
       low = fmaf((top - (d - b)) - (x + b), c, low);
     }
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     }
   }
 
-  constexpr bool EXACT = sizeof(T) == 2;
+  constexpr bool SHORT = sizeof(T) == 2;
   Weigh weigh;
   weigh.top = top;
   const double c = greedy ? 1.0 : fmin(1.4426950408889634 / (double)temperature, 3e38);
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
           float d;
           const float t = weigh.distance(v, d);
           if (!(t < REACH)) return;
-          const uint32_t w = fixed(weigh.weight<EXACT>(v, d, t));
+          const uint32_t w = fixed(weigh.weight<SHORT>(v, d, t));
           const int b = bin_of(t);
           atomicAdd(&h.count[b], 1u);
           if (atomicAdd(&h.lo[b], w) + w < w) atomicAdd(&h.hi[b], 1u);
@@ -440,7 +441,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
           if (at < lo || at > hi) return;
           float d;
           const float t = weigh.distance(v, d);
-          f(at, fixed(weigh.weight<EXACT>(v, d, t)));
+          f(at, fixed(weigh.weight<SHORT>(v, d, t)));
         };
         if (pool) {
           for (uint32_t i = tid; i < min(s.pooled, (uint32_t)POOL); i += THREADS) look(s.div.pool[i].x, s.div.pool[i].index);
@@ -545,7 +546,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         const uint32_t k = atomicAdd(&s.listed, 1u);
         if (k >= FEW) return;
         tell(&s.few.at[rank][k], 0, place(v, (uint32_t)(x.first + i)));
-        tell(&s.few.w[rank][k], 0, fixed(weigh.weight<EXACT>(v, d, t)));
+        tell(&s.few.w[rank][k], 0, fixed(weigh.weight<SHORT>(v, d, t)));
       });
       __syncthreads();
       if (tid == 0) tell(&s.items[rank], 0, min(s.listed, (uint32_t)FEW));
@@ -585,7 +586,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         all = s.found_mass;
       }
       float d;
-      const float v = value_at(me), t = weigh.distance(v, d), exact_w = i < n ? weigh.weight<EXACT>(v, d, t) : 0.0f;
+      const float v = value_at(me), t = weigh.distance(v, d), exact_w = i < n ? weigh.weight<SHORT>(v, d, t) : 0.0f;
       const bool keep = i < n && (!count_here || (int)k <= top_k) && (!by_p || m - w < share_of(all)) && !(exact_w < least);
       __syncthreads();
       if (i < n && part == 0) s.few_w[i] = keep ? w : 0u;
@@ -660,7 +661,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     float d;
     const float t = weigh.distance(v, d);
     if (!(t < REACH)) return 0u;
-    w = weigh.weight<EXACT>(v, d, t);
+    w = weigh.weight<SHORT>(v, d, t);
     return w < least ? 0u : fixed(w);
   };
   __syncthreads();
