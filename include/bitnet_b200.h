@@ -608,7 +608,8 @@ int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const b
  * are read through its own row: all rows of a group have to hold the prefix's pages.)  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
  * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
  * and that the probabilities of the prefix may be rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
- * A sequence in no group (an array that is not as above) is taken by itself.  Reads at most the first 2^30 - 256 tokens of a prefix.
+ * Groups may be empty or of one sequence.  A sequence in no group (starts that do not begin at 0, end at seqs or stay within them) is taken by itself; where starts
+ * descend, so that groups overlap, nothing outside the arrays is read or written, but the rows of those sequences are not to be used.  Reads at most the first 2^30 - 256 tokens of a prefix.
  * workspace: bitnet_attn_shared_workspace_bytes bytes (26 MB, and 1056 bytes per sequence and query head of 128); its first 64 KB as for the other attention
  * calls, whose workspace it may be too.
  */
