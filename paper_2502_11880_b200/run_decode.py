@@ -49,11 +49,11 @@ class Step(Layer):
 
     def __init__(self, hidden, heads, kv_heads, vocab, seed=0):
         super().__init__(hidden, heads, kv_heads, seed)
-        self.vocab = -(-vocab // 16) * 16
+        self.vocab, self.head_rows = vocab, -(-vocab // 16) * 16                     # (a linear has a multiple of 16 rows)
         self.embedding = synth.normal(seed, 100, self.vocab, hidden).cuda()
         self.norms = [1 + 0.1 * synth.normal(seed, 101 + i, 1, hidden)[0].cuda() for i in range(2)]
         self.rope = bn.Rope(self.dim, base=500000.0, scaling="bands", factor=8.0, context=8192)
-        self.head = bn.pack("i2s", synth.ternary(seed, 2, self.vocab, hidden, 1 / 3, 1 / 3, device="cuda"))
+        self.head = bn.pack("i2s", synth.ternary(seed, 2, self.head_rows, hidden, 1 / 3, 1 / 3, device="cuda"))
         self.head_scale = 2.0 * (hidden * 2 / 3) ** -0.5
 
     def _linear(self, blob, scale, rows, codes, act_scale):
@@ -69,7 +69,7 @@ class Step(Layer):
     def end(self, stream, attn):
         """Logits; the stream is updated in place."""
         o = self.linear(1, attn.float().reshape(attn.shape[0], -1))
-        return self._linear(self.head, self.head_scale, self.vocab, *bn.bitnet_add_rmsnorm_quant(o, self.norms[1], residual=stream))
+        return self._linear(self.head, self.head_scale, self.head_rows, *bn.bitnet_add_rmsnorm_quant(o, self.norms[1], residual=stream))[:, :self.vocab]
 
 
 def full(a):
