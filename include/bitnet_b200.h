@@ -605,7 +605,8 @@ int bitnet_kv_append_rope(const bitnet_kv_cache_t* cache, int64_t layer, const b
  * (int32 [groups]; 0: none) in common: those are read through the row of the table of the group's first sequence that has tokens (kv_len above 0: the first may
  * be finished and freed), with a window behind the sinks through the row of one that sees them (others may have given them up), once for the whole group, on the
  * tensor cores; every sequence's own tokens after them through its own row.  (Where there is little to be saved the decode kernel takes the call and every sequence's tokens
- * are read through its own row: all rows of a group have to hold the prefix's pages.)  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
+ * are read through its own row: all rows of a group have to hold the prefix's pages.  What there is to be saved is judged by table_width, or the window, where counts do
+ * not leave it to the device: a table much wider than its longest sequence costs short calls some 10 us.)  prefix_len need not end at a page's end (a fork copies the page filled in part), and a
  * sequence shorter than it sees its own kv_len of it.  Window, sinks, scale and the rest as for bitnet_attn_decode, except that q and out have the cache's type,
  * and that the probabilities of the prefix may be rounded to it, as in prompt calls.  There, too, a NaN or infinity in V that some sequence of a group sees may reach others of it.
  * Groups may be empty or of one sequence.  A sequence in no group (starts that do not begin at 0, end at seqs or stay within them) is taken by itself; where starts
