@@ -518,23 +518,28 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           const int who = __ffs(here) - 1;
           const int q0 = __shfl_sync(0xffffffffu, mine_g.q0, who), n = __shfl_sync(0xffffffffu, mine_g.n, who), nb = __shfl_sync(0xffffffffu, mine_g.nb, who);
           const int64_t in_group = local - __shfl_sync(0xffffffffu, mine_g.before, who), id = in_group / nb;
+          const int hb = (int)(id % heads), tok0 = (int)(id / heads) * span;
+          // lengths of the group's first sequences, and of the item's first (on their way together)
+          const int len_of_group = lane < n ? __ldg(a.kv_len + q0 + lane) : 0;
+          int len_of_item = tok0 + lane < n ? __ldg(a.kv_len + q0 + tok0 + lane) : 0;
           // the sequence through whose row the prefix is read: the group's first that has tokens (a finished sample's row is empty)
           int reader = q0;
-          for (int i = 0; i < n; i += 32) {
-            const unsigned live = __ballot_sync(0xffffffffu, i + lane < n && __ldg(a.kv_len + q0 + i + lane) > 0);
-            if (!live) continue;
-            reader = q0 + i + __ffs(live) - 1;
-            break;
+          for (int i = 0, len = len_of_group;;) {
+            const unsigned live = __ballot_sync(0xffffffffu, len > 0);
+            if (live) reader = q0 + i + __ffs(live) - 1;
+            i += 32;
+            if (live || i >= n) break;
+            len = i + lane < n ? __ldg(a.kv_len + q0 + i + lane) : 0;
           }
           Item t;
           t.seq = reader;
           t.q0 = q0;
           t.n_new = n;
-          const int hb = (int)(id % heads), b0 = hb % a.blocks * a.per_block;
+          const int b0 = hb % a.blocks * a.per_block;
           t.head_kv = hb / a.blocks;
           t.head0 = t.head_kv * a.group + b0;
           t.heads = min(a.per_block, a.group - b0);
-          t.tok0 = (int)(id / heads) * span;
+          t.tok0 = tok0;
           t.two = t.tok0 + a.tile_tokens < n;
           t.prefix = __shfl_sync(0xffffffffu, mine_g.prefix, who);
           t.n0 = __shfl_sync(0xffffffffu, mine_g.n0, who);
@@ -550,11 +555,13 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           t.unit0 = t.id = 0;
           // the tokens that some row of the item sees: from its shortest sequence's window to its longest sequence's end, empty ones left out
           int least = 0x7fffffff, most = 0;
-          for (int i = t.tok0 + lane; i < min(n, t.tok0 + span); i += 32) {
-            const int len = __ldg(a.kv_len + q0 + i);
-            if (len <= 0) continue;
-            least = min(least, len);
-            most = max(most, len);
+          const int stop_at = min(n, tok0 + span);
+          for (int i = tok0 + lane; i < stop_at; i += 32) {
+            if (len_of_item > 0) {
+              least = min(least, len_of_item);
+              most = max(most, len_of_item);
+            }
+            if (i + 32 < stop_at) len_of_item = __ldg(a.kv_len + q0 + i + 32);
           }
           least = __reduce_min_sync(0xffffffffu, least);
           most = __reduce_max_sync(0xffffffffu, most);
