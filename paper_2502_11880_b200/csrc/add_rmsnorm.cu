@@ -11,7 +11,9 @@
 // Bound by HBM for many rows, by the latency of loads and two reductions for few.  Measured (us, a B200): 1 x 4096: 2.3; 16 x 28672: 4.2; 4099 x 8192, fp32 x
 // and a bf16 residual: 56 (5.4 TB/s, 0.82 of a copy's rate; what is left is the latency of the reductions between loads and codes).  There the next row's loads ahead of the
 // reductions took it from 98 to 74, types as template parameters to 69, weights through the first-level cache to 64, one rounding of the new residual for
-// the store and the sum to 62, maxima by one instruction a warp to 60, the next row through shared memory to 56.
+// the store and the sum to 62, maxima by one instruction a warp to 60, the next row through shared memory to 56.  16-bit rows have the same instructions for half the
+// bytes: bf16, without / with a residual: 4096 x 8192: 41 / 53 (HBM needs 15 / 36), 4096 x 14336: 68 / 106 (27 / 63).  The general kernel, three walks over a row by
+// single elements: 4096 x 8191, fp32 both: 339 (67), bf16 both: 470 (36); 16 x 8191: 10; 1 x 4095: 7.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

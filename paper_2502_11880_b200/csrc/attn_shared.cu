@@ -3,9 +3,10 @@
 //      (attn_prompt.cu), in parts over the CTAs;
 //   2. the sequences' own tokens (attn_own_kernel), in parts over the warps;
 //   3. the join (attn_join_kernel).
+// Where the host cannot tell whether the groups share enough, attn_route_kernel finds out, and these three or the decode kernel end at once.
 // A part of a row is its maximum m, its sum l = sum 2^(s - m) and O = sum 2^(s - m) V, s in units of log2.
 //
-// Measured (us, a B200), bf16: 64 sequences over 16384 tokens with up to 400 of their own, 64/8 heads of 128: 76, by themselves 45, 22 and 8 (35 GFLOP
+// Measured (us, a B200), bf16: 64 sequences over 16384 tokens with up to 400 of their own, 64/8 heads of 128: 77, by themselves 45, 22 and 8 (35 GFLOP
 // of products need 21; the decode kernel, which reads the prefix for every sequence: 382); 40 in three groups over 4000, 704 and 0, 16/16 heads of 96,
 // fp16, window 2048: 38 (93).
 #include <cstring>

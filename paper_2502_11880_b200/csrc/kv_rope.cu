@@ -16,7 +16,8 @@
 // VEC elements; a thread keeps its slot, and so its VEC pairs' sines and cosines, over all heads that it visits.
 //
 // Measured (us, a B200): 32 tokens, 64/8 heads of 128: 3.0; 4 x 2048 tokens, 32/8 heads of 128, fp32 in, bf16 out: 39 (6.1 TB/s); bf16 in and out,
-// 4096 tokens: 24 (3.3 TB/s).  With every thread computing its own sines: 3.8, 43, 34.
+// 3222 tokens: 24 (3.3 TB/s, half of a copy's rate: 8 bytes a vector, two rows of a thread on their way), 4096 tokens: 30.  With every thread computing its
+// own sines the first, second and third: 3.8, 43, 34.
 #include <cstring>
 #include <type_traits>
 
@@ -292,7 +293,7 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   // elements of a vector: as many as half a row's pairs, the head, strides and addresses allow
   const bool in_f32 = x.in_type == BITNET_KV_F32, out_f32 = x.out_type == BITNET_KV_F32;
   // (four at most: 4 x 2048 tokens, fp32 in, bf16 out: 42 us against 49 with 32-byte vectors, a warp's access would touch every sector twice; 16-bit in
-  // and out: 24 us with four as with eight)
+  // and out, 3222 tokens: 24 us with four as with eight)
   int64_t odd = dim | x.q_stride_token | x.q_stride_head | x.stride_token | x.stride_head | 4;
   if (!d.interleaved) odd |= d.rot / 2;
   int vec = (int)(odd & -odd);
@@ -304,7 +305,7 @@ int launch_kv_rope(const KvView& kv, int layer, const bitnet_rope_t* rope, const
   if (!d.interleaved && d.rotated + slots(dim - d.rot) > d.slots) d.slots = d.rotated + slots(dim - d.rot);
   d.at_once = THREADS / d.slots;
   // CTAs per token: a row per thread while CTAs are few, all of a token's rows in one when there are enough tokens to fill the SMs
-  // (up to 8, 16, 32 and 64 CTAs per SM: 16.3, 15.4, 16.5 and 17.9 us for 3 x 517 tokens, 32/32 heads of 100; 24.1, 24.2, 24.2 and 26.3 for 4096, 32/8 of 128)
+  // (up to 8, 16, 32 and 64 CTAs per SM: 16.3, 15.4, 16.5 and 17.9 us for 3 x 517 tokens, 32/32 heads of 100; 24.1, 24.2, 24.2 and 26.3 for 3222, 32/8 of 128, 16-bit)
   const int64_t rows = x.q_heads + 2 * kv.kv_heads, most = ceil_div(rows, d.at_once), sms = dev_info().sm_count;
   int64_t split = 16 * sms / x.tokens;
   split = split < 1 ? 1 : split > most ? most : split;

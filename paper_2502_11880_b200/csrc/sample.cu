@@ -20,8 +20,10 @@
 // the product and, for fp32 logits, of max - x carried along, so that a weight is off by the exponential's own 2^-22 only; of 16-bit logits by what max - x
 // loses as well, 2^-24 (max - x) / T, 2^-19.5 for the least weight that counts.  (To carry that too takes 256 x 50021 from 79 to 85 us.)
 //
-// Bound by barriers for few rows and by instructions for many: some 35 an item for its weight and its bin.  Measured (us, a B200): 1 x 32000, fp32, top-k 50,
-// top-p 0.9: 8.4 (14 without the short list); 64 x 128256, fp32, settings per row: 59 (HBM needs 5); 256 x 50021, bf16, top-p 0.92: 79 (HBM needs 4).
+// Bound by barriers for few rows; for many by waits (results of shared atomics, barriers of the cluster) and instructions together: 83 an item at 45 % of the issue
+// slots for 64 x 128256, 118 at 61 % for 256 x 50021.  Measured (us, a B200): 1 x 32000, fp32, top-k 50, top-p 0.9: 8.4 (14 without the short list);
+// 64 x 128256, fp32, settings per row: 59 (HBM needs 5); 256 x 50021, bf16, top-p 0.92: 79 (HBM needs 4; 75 before there was the short list's code).  Rows that do
+// not fit shared memory, read at every pass, temperature alone / with top-p: 1 x 700001, fp32: 50 / 91; 64 x 400000, fp32: 94 / 193; 64 x 700001, bf16: 173 / 423.
 #include <cstring>
 #include <type_traits>
 
